@@ -63,6 +63,7 @@ enum {
 };
 
 enum { SOLO_GRAD_FP32 = 0, SOLO_GRAD_BF16 = 1 };
+enum { SOLO_FP32 = 0, SOLO_BF16 = 1 };     /* element types of the operators around the step */
 
 /* flags */
 #define SOLO_FLAG_STOCHASTIC 1u   /* xi ~ U(-0.5, 0.5); clear = xi = 0 */
@@ -234,6 +235,127 @@ int solo_multi_table_build(const solo_tensor *tensors, uint32_t count, const sol
 int solo_adamw_step_multi(const void *table_device, uint32_t count, uint64_t units,
                           uint32_t table_flags, const float *grad_scale, uint64_t step,
                           const solo_config *cfg, void *stream);
+
+/* ==== around the step ============================================================================
+ * The operators of a training loop that lie next to the optimizer step: the gradients' global norm
+ * and clipping, the embedding and its gradient, the log probabilities of given tokens and their
+ * gradient.  The conventions of the step hold: device pointers owned by the caller, a host struct
+ * read during the call, work enqueued on `stream`, no allocation, no synchronisation, SOLO_OK or a
+ * negative code with nothing enqueued.  A workspace needs no initialisation, holds nothing between
+ * calls and serves one call at a time (calls on one stream follow each other).  Tensors need the
+ * alignment of their elements only.  Every call gives the same bits for the same inputs: no sum is
+ * made by atomic additions.  All calls can be captured into a HIP graph. */
+
+/* ---- global norm and clipping ---------------------------------------------------------------
+ * Over the tensors g_k of a table, with u = *unscale (the reciprocal of a loss scale; NULL: 1):
+ *
+ *   N_k = |u| sqrt(sum g_k^2)     N = sqrt(sum N_k^2)     c = u * (N > max_norm ? max_norm / N : 1)
+ *
+ * *norm = N, *grad_scale = c (what solo_adamw_step_mp and _multi take as grad_scale), tensor_norm[k] =
+ * N_k.  Squares and sums are binary64, so N is that of the exact sum to about one rounding, for every
+ * finite gradient.  Where N is not finite (a gradient is not, or N exceeds binary32), c is 0.
+ * solo_grad_clip also writes clipped_k = c * g_k, rounded once; where c is 0, zeros, whatever the
+ * gradient holds.  The table is built like that of the multi-tensor step:
+ *
+ *   units = solo_norm_units(grads, count);
+ *   solo_norm_table_build(grads, count, host_buffer, solo_norm_table_bytes(count, units));
+ *   copy host_buffer to a 16-byte aligned device buffer `table`
+ *   solo_grad_norm(table, count, units, unscale, max_norm, norm, grad_scale, tensor_norm, workspace, stream);
+ */
+typedef struct solo_grad {
+    const void *grad;      /* fp32[n] or bf16[n], DEVICE                                        */
+    void *clipped;         /* the same type: where solo_grad_clip writes; may be grad itself, or
+                              NULL (not written); must not overlap another tensor               */
+    uint64_t n;            /* elements, up to 2^40; 0 is allowed                                */
+    uint32_t dtype;        /* SOLO_FP32 or SOLO_BF16                                            */
+    uint32_t reserved;     /* must be 0                                                         */
+} solo_grad;
+
+/* Work units of the table: 0 if grads is NULL, all tensors are empty or one is too long. */
+uint64_t solo_norm_units(const solo_grad *grads, uint32_t count);
+size_t solo_norm_table_bytes(uint32_t count, uint64_t units);
+size_t solo_norm_workspace_bytes(uint64_t units);
+int solo_norm_table_build(const solo_grad *grads, uint32_t count, void *table_host, size_t table_bytes);
+
+/* max_norm >= 0 (infinity: no clipping); workspace: solo_norm_workspace_bytes, 16-byte aligned;
+ * tensor_norm: float[count] or NULL.  norm, grad_scale: one float each. */
+int solo_grad_norm(const void *table_device, uint32_t count, uint64_t units, const float *unscale, float max_norm,
+                   float *norm, float *grad_scale, float *tensor_norm, void *workspace, void *stream);
+int solo_grad_clip(const void *table_device, uint32_t count, uint64_t units, const float *unscale, float max_norm,
+                   float *norm, float *grad_scale, float *tensor_norm, void *workspace, void *stream);
+
+/* ---- embedding --------------------------------------------------------------------------------
+ *   rows[i] = scale * table[t_i]            grad_table[v] = scale * sum over i with t_i = v of grad_rows[i]
+ *
+ * A token outside [0, vocab) (padding) gives a row of zeros and has no gradient.  Sums are binary32 in
+ * an order that the tokens alone determine; one rounding to bf16 at the end.  Every row of grad_table is
+ * written, those without a token with zeros; with SOLO_EMBEDDING_ACCUMULATE the sums are added to what
+ * is there (a table that is also the head of the model, a second micro-batch) and other rows are not
+ * touched. */
+#define SOLO_EMBEDDING_ACCUMULATE 1u
+typedef struct solo_embedding_shape {
+    uint64_t vocab, dim;        /* rows and columns of the table; below 2^31 and 2^24            */
+    uint64_t tokens;            /* below 2^28                                                    */
+    uint64_t table_stride;      /* elements from row to row, >= dim, below 2^31                  */
+    uint64_t rows_stride;       /* the same of rows / grad_rows                                  */
+    uint32_t table_dtype;       /* of table / grad_table                                         */
+    uint32_t rows_dtype;        /* of rows / grad_rows                                           */
+    uint32_t token_bits;        /* 32 or 64: signed whole numbers                                */
+    uint32_t flags;             /* 0 or SOLO_EMBEDDING_ACCUMULATE (gradient only)                */
+    float scale;                /* finite                                                        */
+    uint32_t reserved;          /* must be 0                                                     */
+} solo_embedding_shape;
+
+int solo_embedding(const void *table, const void *tokens, void *rows, const solo_embedding_shape *shape, void *stream);
+/* Bytes of workspace of solo_embedding_grad (16-byte aligned), no fewer for more tokens; 0 if the shape is invalid. */
+size_t solo_embedding_workspace_bytes(const solo_embedding_shape *shape);
+int solo_embedding_grad(const void *grad_rows, const void *tokens, void *grad_table, void *workspace, size_t workspace_bytes,
+                        const solo_embedding_shape *shape, void *stream);
+
+/* ---- log probabilities ------------------------------------------------------------------------
+ * For every row x of logits, with z = scale * x (scale: the reciprocal of a temperature), L = ln sum e^z
+ * and p = e^(z - L):
+ *
+ *   logprob = z_t - L             of the row's target t
+ *   entropy = -sum p ln p
+ *   rank = number of columns whose logit is larger than the target's
+ *   top_logprob, top_token [rows, top]: z - L of the `top` largest logits and their columns, larger ones
+ *            first, ties by the lower column; places behind the last column are -inf and -1
+ *   stats [rows, 2]: what solo_logprob_grad takes: a logit near the row's largest, and the sum of e^z relative to it
+ *
+ * and for a loss with d loss / d logprob = a, d loss / d entropy = b (one float per row each):
+ *
+ *   grad_logits_j = scale * (a (delta_jt - p_j) - b p_j (ln p_j + entropy))
+ *
+ * (the alternatives carry no gradient).  Logits of -inf have probability 0; in a row that has no other,
+ * logprob is -inf, entropy and gradient are 0.  A target outside [0, cols) means none (a padding
+ * position): the row is not read, logprob and entropy are 0, rank is -1, the alternatives are -inf and -1,
+ * the gradient is 0.  A NaN or +inf in a row makes its logprob, entropy and gradient NaN and its alternatives
+ * and rank unspecified.  solo_logprob_with_grad does both for weights that are known beforehand (a mean over
+ * tokens), reading the logits from HBM once. */
+#define SOLO_TOP_MAX 32
+typedef struct solo_logits {
+    uint64_t rows, cols;        /* cols below 2^31                                               */
+    uint64_t stride;            /* elements from row to row of logits, >= cols                   */
+    uint64_t grad_stride;       /* the same of grad_logits                                       */
+    uint32_t dtype;             /* of logits and grad_logits                                     */
+    uint32_t target_bits;       /* 32 or 64: signed whole numbers                                */
+    uint32_t top;               /* alternatives, 0 .. SOLO_TOP_MAX                               */
+    uint32_t reserved;          /* must be 0                                                     */
+    float scale;                /* > 0, finite                                                   */
+    uint32_t reserved2;         /* must be 0                                                     */
+} solo_logits;
+
+/* targets may be NULL (no logprob, no rank: both NULL then); every output may be NULL, the alternatives if top is 0. */
+int solo_logprob(const void *logits, const void *targets, float *logprob, float *entropy, int32_t *rank,
+                 float *top_logprob, int32_t *top_token, float *stats, const solo_logits *shape, void *stream);
+/* entropy, stats: of solo_logprob on the same logits, targets and scale.  grad_logprob or grad_entropy may be NULL (0).
+ * grad_logits may be the logits themselves (same stride); it must not overlap them in another way. */
+int solo_logprob_grad(const void *logits, const void *targets, const float *entropy, const float *stats,
+                      const float *grad_logprob, const float *grad_entropy, void *grad_logits,
+                      const solo_logits *shape, void *stream);
+int solo_logprob_with_grad(const void *logits, const void *targets, const float *grad_logprob, const float *grad_entropy,
+                           float *logprob, float *entropy, void *grad_logits, const solo_logits *shape, void *stream);
 
 /* Static, human-readable text for a return code. */
 const char *solo_strerror(int code);

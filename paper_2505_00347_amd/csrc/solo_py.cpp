@@ -1,4 +1,4 @@
-// The step calls of the Python binding, marshalled natively.
+// The step calls of the Python binding and those of the operators around the step, marshalled natively.
 //
 // A step of a small tensor takes the GPU 4-6 us; a ctypes call with eleven or thirteen arguments,
 // seven data_ptr() calls from Python and a torch.cuda.current_stream() object took the host 7.8 us
@@ -166,6 +166,107 @@ PyObject *multi(PyObject *, PyObject *const *a, Py_ssize_t count)
     return PyLong_FromLong(rc);
 }
 
+// ---- the operators around the step ----------------------------------------------------------
+// An entry point whose last argument is the stream, with its twin through ctypes.
+template <typename F>
+struct Entry {
+    F call = nullptr;
+    PyObject *by_ctypes = nullptr;
+};
+Entry<decltype(&solo_grad_norm)> g_grad_norm;
+Entry<decltype(&solo_grad_clip)> g_grad_clip;
+Entry<decltype(&solo_embedding)> g_embedding;
+Entry<decltype(&solo_embedding_grad)> g_embedding_grad;
+Entry<decltype(&solo_logprob)> g_logprob;
+Entry<decltype(&solo_logprob_grad)> g_logprob_grad;
+Entry<decltype(&solo_logprob_with_grad)> g_logprob_with_grad;
+
+template <typename T>
+bool argument(PyObject *o, T *&out) { return pointer(o, out); }
+bool argument(PyObject *o, float &out)
+{
+    if (!PyFloat_Check(o) && !PyLong_Check(o)) return false;        // (one for ctypes)
+    const double x = PyFloat_AsDouble(o);
+    out = (float)x;
+    return !(x == -1.0 && PyErr_Occurred());
+}
+template <typename T>
+bool argument(PyObject *o, T &out)
+{
+    uint64_t x;
+    if (!integer(o, x)) return false;
+    out = (T)x;
+    return true;
+}
+
+// The arguments in their C types, from the front; the last one is the stream.
+template <typename F, typename... Got>
+int convert(F fn, PyObject *const *a, int (*rest)(void *), Got... got)
+{
+    (void)rest;
+    void *stream = nullptr;
+    if (!stream_of(*a, stream)) return 1;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = fn(got..., stream);
+    Py_END_ALLOW_THREADS
+    return rc;
+}
+template <typename F, typename Next, typename... Rest, typename... Got>
+int convert(F fn, PyObject *const *a, int (*rest)(Next, Rest...), Got... got)
+{
+    (void)rest;
+    Next x;
+    if (!argument(*a, x)) return 1;
+    return convert(fn, a + 1, (int (*)(Rest...))nullptr, got..., x);
+}
+template <typename... A>
+constexpr Py_ssize_t arity(int (*)(A...)) { return (Py_ssize_t)sizeof...(A); }
+
+template <auto *entry>
+PyObject *operation(PyObject *, PyObject *const *a, Py_ssize_t count)
+{
+    const Py_ssize_t want = arity((decltype(entry->call))nullptr);
+    if (!entry->call || count != want) {
+        PyErr_Format(PyExc_TypeError, "%zd arguments expected, got %zd", want, count);
+        return nullptr;
+    }
+    const int rc = convert(entry->call, a, entry->call);
+    if (rc <= 0) return PyLong_FromLong(rc);
+    return by_ctypes(entry->by_ctypes, a, count);          // (1: not an argument that is taken here)
+}
+
+template <auto *entry>
+void keep(PyObject *address, PyObject *by_ctypes)
+{
+    Py_INCREF(by_ctypes);
+    Py_XSETREF(entry->by_ctypes, by_ctypes);
+    entry->call = reinterpret_cast<decltype(entry->call)>((uintptr_t)PyLong_AsUnsignedLongLong(address));
+}
+
+// bind_operations({name: (address, the call through ctypes)})
+PyObject *bind_operations(PyObject *, PyObject *calls)
+{
+    struct { const char *name; void (*keep)(PyObject *, PyObject *); } known[] = {
+        {"solo_grad_norm", keep<&g_grad_norm>}, {"solo_grad_clip", keep<&g_grad_clip>}, {"solo_embedding", keep<&g_embedding>},
+        {"solo_embedding_grad", keep<&g_embedding_grad>}, {"solo_logprob", keep<&g_logprob>},
+        {"solo_logprob_grad", keep<&g_logprob_grad>}, {"solo_logprob_with_grad", keep<&g_logprob_with_grad>}};
+    if (!PyDict_Check(calls)) {
+        PyErr_SetString(PyExc_TypeError, "a dict expected");
+        return nullptr;
+    }
+    for (auto &k : known) {
+        PyObject *pair = PyDict_GetItemString(calls, k.name), *address, *by_ctypes;
+        if (!pair) {
+            PyErr_Format(PyExc_KeyError, "%s", k.name);
+            return nullptr;
+        }
+        if (!PyArg_ParseTuple(pair, "O!O", &PyLong_Type, &address, &by_ctypes)) return nullptr;
+        k.keep(address, by_ctypes);
+    }
+    Py_RETURN_NONE;
+}
+
 // bind(address of solo_adamw_step_mp, of solo_adamw_step_multi, config type, its size, ArgumentError, ctypes' base
 //      class, the step through ctypes, the multi-tensor step through ctypes, slow stream, torch's current
 //      device, torch's raw stream of a device): the last two may be None
@@ -205,6 +306,11 @@ PyObject *forked(PyObject *, PyObject *)
 PyMethodDef methods[] = {
     {"step", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(step)), METH_FASTCALL, "solo_adamw_step_mp"},
     {"multi", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(multi)), METH_FASTCALL, "solo_adamw_step_multi"},
+#define SOLO_OPERATION(name) \
+    {"solo_" #name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(operation<&g_##name>)), METH_FASTCALL, "solo_" #name}
+    SOLO_OPERATION(grad_norm), SOLO_OPERATION(grad_clip), SOLO_OPERATION(embedding), SOLO_OPERATION(embedding_grad),
+    SOLO_OPERATION(logprob), SOLO_OPERATION(logprob_grad), SOLO_OPERATION(logprob_with_grad),
+    {"bind_operations", bind_operations, METH_O, "the entry points of the operators around the step"},
     {"bind", bind, METH_VARARGS, "the entry points and types of the binding"},
     {"forked", forked, METH_NOARGS, "called in a forked child"},
     {nullptr, nullptr, 0, nullptr}};

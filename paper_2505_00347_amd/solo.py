@@ -27,6 +27,9 @@ SOLO_FLAG_M_DYNAMIC_EXPONENT = 2
 SOLO_FLAG_ADABELIEF = 4
 SOLO_FLAG_COUPLED_DECAY = 8
 SOLO_TABLE_BF16_COPY, SOLO_TABLE_SHORT_BLOCK = 1, 2
+SOLO_FP32, SOLO_BF16 = 0, 1
+SOLO_EMBEDDING_ACCUMULATE = 1
+SOLO_TOP_MAX = 32
 
 
 class solo_config(C.Structure):
@@ -53,6 +56,22 @@ class solo_tensor(C.Structure):
                 ("v_scale", C.c_void_p), ("v_base", C.c_void_p), ("n", C.c_uint64)]
 
 
+class solo_grad(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("clipped", C.c_void_p), ("n", C.c_uint64), ("dtype", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class solo_embedding_shape(C.Structure):
+    _fields_ = [("vocab", C.c_uint64), ("dim", C.c_uint64), ("tokens", C.c_uint64), ("table_stride", C.c_uint64),
+                ("rows_stride", C.c_uint64), ("table_dtype", C.c_uint32), ("rows_dtype", C.c_uint32),
+                ("token_bits", C.c_uint32), ("flags", C.c_uint32), ("scale", C.c_float), ("reserved", C.c_uint32)]
+
+
+class solo_logits(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("cols", C.c_uint64), ("stride", C.c_uint64), ("grad_stride", C.c_uint64),
+                ("dtype", C.c_uint32), ("target_bits", C.c_uint32), ("top", C.c_uint32), ("reserved", C.c_uint32),
+                ("scale", C.c_float), ("reserved2", C.c_uint32)]
+
+
 class SoloError(RuntimeError):
     def __init__(self, code):
         self.code = code
@@ -61,12 +80,14 @@ class SoloError(RuntimeError):
 
 _lib = None
 _step = _multi = None            # the calls of a step: native, or through ctypes
+_calls = None                    # those of the operators around the step, by name
+_torch = None
 _loading = threading.RLock()
 
 
 def lib():
     """Load libsolo.so (built by ``python -m paper_2505_00347_amd.build``)."""
-    global _lib, _step, _multi
+    global _lib, _step, _multi, _calls, _torch
     if _lib is not None:
         return _lib
     with _loading:
@@ -78,13 +99,16 @@ def lib():
             # Loaded after it, libsolo binds to that runtime, the one the tensors and streams of the
             # callers belong to; loaded before it, libsolo would bind to the system's copy, and every
             # launch on a torch stream would fail.
-            import torch  # noqa: F401
+            import torch
             L = _declared(C.CDLL(LIB_PATH))
             step, multi = functools.partial(_step_by_ctypes, L), functools.partial(_multi_by_ctypes, L)
+            calls = {name: functools.partial(_by_ctypes, getattr(L, name)) for name in _OPERATIONS}
             if os.path.exists(NATIVE_PATH):
                 native = _native_calls(L, step, multi)
                 step, multi = native.step, native.multi
-            _step, _multi = step, multi
+                native.bind_operations({name: (C.cast(getattr(L, name), C.c_void_p).value, call) for name, call in calls.items()})
+                calls = {name: getattr(native, name) for name in _OPERATIONS}
+            _step, _multi, _calls, _torch = step, multi, calls, torch
             _lib = L                 # last: a thread that finds it set finds the others set
     return _lib
 
@@ -111,7 +135,43 @@ def _declared(L):
     L.solo_multi_table_build.argtypes = [tp, u32, cfgp, vp, C.c_size_t, C.POINTER(C.c_uint32)]
     L.solo_adamw_step_multi.restype = C.c_int
     L.solo_adamw_step_multi.argtypes = [vp, u32, u64, u32, vp, u64, cfgp, vp]
+    gp, size = C.POINTER(solo_grad), C.c_size_t
+    L.solo_norm_units.restype = u64; L.solo_norm_units.argtypes = [gp, u32]
+    L.solo_norm_table_bytes.restype = size; L.solo_norm_table_bytes.argtypes = [u32, u64]
+    L.solo_norm_workspace_bytes.restype = size; L.solo_norm_workspace_bytes.argtypes = [u64]
+    L.solo_norm_table_build.restype = C.c_int; L.solo_norm_table_build.argtypes = [gp, u32, vp, size]
+    L.solo_embedding_workspace_bytes.restype = size
+    L.solo_embedding_workspace_bytes.argtypes = [C.POINTER(solo_embedding_shape)]
+    norm = [vp, u32, u64, vp, C.c_float, vp, vp, vp, vp, vp]
+    for name, types in {"solo_grad_norm": norm, "solo_grad_clip": norm, "solo_embedding": [vp] * 5,
+                        "solo_embedding_grad": [vp, vp, vp, vp, size, vp, vp], "solo_logprob": [vp] * 10,
+                        "solo_logprob_grad": [vp] * 9, "solo_logprob_with_grad": [vp] * 9}.items():
+        getattr(L, name).restype, getattr(L, name).argtypes = C.c_int, types
     return L
+
+
+_OPERATIONS = ("solo_grad_norm", "solo_grad_clip", "solo_embedding", "solo_embedding_grad", "solo_logprob",
+               "solo_logprob_grad", "solo_logprob_with_grad")
+
+
+def _by_ctypes(function, *args):
+    return function(*[a.data_ptr() if hasattr(a, "data_ptr") else a for a in args[:-1]], _stream(args[-1]))
+
+
+def _operation(name, check, *args):
+    """Calls an operator around the step; the last argument is the stream."""
+    if _calls is None:
+        lib()
+    rc = _calls[name](*args)
+    if check and rc != SOLO_OK:
+        raise SoloError(rc)
+    return rc
+
+
+def _address(struct, kind):
+    if not isinstance(struct, kind):
+        raise C.ArgumentError(f"a {kind.__name__} expected, got {type(struct).__name__}")
+    return C.addressof(struct)
 
 
 def _native_calls(L, step, multi):
@@ -242,6 +302,240 @@ class SoloMultiTable:
     def step(self, step, grad_scale=None, stream=None):
         return solo_adamw_step_multi(self.table, self.count, self.units, self.flags, grad_scale, step,
                                      self.cfg, stream)
+
+
+# ---- around the step: norm and clipping, embedding, log probabilities (include/solo.h) ----------
+
+def solo_norm_units(grads, count): return lib().solo_norm_units(grads, count)
+def solo_norm_table_bytes(count, units): return lib().solo_norm_table_bytes(count, units)
+def solo_norm_workspace_bytes(units): return lib().solo_norm_workspace_bytes(units)
+
+
+def solo_norm_table_build(grads, count, table_host, table_bytes, check=True):
+    rc = lib().solo_norm_table_build(grads, count, table_host, table_bytes)
+    if check and rc != SOLO_OK:
+        raise SoloError(rc)
+    return rc
+
+
+def solo_grad_norm(table_device, count, units, unscale, max_norm, norm, grad_scale, tensor_norm, workspace, stream=None, check=True):
+    return _operation("solo_grad_norm", check, table_device, count, units, unscale, max_norm, norm, grad_scale, tensor_norm, workspace, stream)
+
+
+def solo_grad_clip(table_device, count, units, unscale, max_norm, norm, grad_scale, tensor_norm, workspace, stream=None, check=True):
+    return _operation("solo_grad_clip", check, table_device, count, units, unscale, max_norm, norm, grad_scale, tensor_norm, workspace, stream)
+
+
+def solo_embedding(table, tokens, rows, shape, stream=None, check=True):
+    return _operation("solo_embedding", check, table, tokens, rows, _address(shape, solo_embedding_shape), stream)
+
+
+def solo_embedding_workspace_bytes(shape): return lib().solo_embedding_workspace_bytes(C.byref(shape))
+
+
+def solo_embedding_grad(grad_rows, tokens, grad_table, workspace, workspace_bytes, shape, stream=None, check=True):
+    return _operation("solo_embedding_grad", check, grad_rows, tokens, grad_table, workspace, workspace_bytes,
+                      _address(shape, solo_embedding_shape), stream)
+
+
+def solo_logprob(logits, targets, logprob, entropy, rank, top_logprob, top_token, stats, shape, stream=None, check=True):
+    return _operation("solo_logprob", check, logits, targets, logprob, entropy, rank, top_logprob, top_token, stats,
+                      _address(shape, solo_logits), stream)
+
+
+def solo_logprob_grad(logits, targets, entropy, stats, grad_logprob, grad_entropy, grad_logits, shape, stream=None, check=True):
+    return _operation("solo_logprob_grad", check, logits, targets, entropy, stats, grad_logprob, grad_entropy, grad_logits,
+                      _address(shape, solo_logits), stream)
+
+
+def solo_logprob_with_grad(logits, targets, grad_logprob, grad_entropy, logprob, entropy, grad_logits, shape, stream=None, check=True):
+    return _operation("solo_logprob_with_grad", check, logits, targets, grad_logprob, grad_entropy, logprob, entropy, grad_logits,
+                      _address(shape, solo_logits), stream)
+
+
+def _dtype(tensor):
+    if tensor.dtype is _torch.float32:
+        return SOLO_FP32
+    if tensor.dtype is _torch.bfloat16:
+        return SOLO_BF16
+    raise TypeError(f"float32 or bfloat16 expected, got {tensor.dtype}")
+
+
+def _token_bits(tensor, n):
+    if tensor.dim() != 1 or tensor.numel() != n:
+        raise ValueError(f"{n} tokens in one dimension expected, got {tuple(tensor.shape)}")
+    if n > 1 and tensor.stride(0) != 1:
+        raise ValueError("tokens must be contiguous")
+    if tensor.dtype is _torch.int64:
+        return 64
+    if tensor.dtype is _torch.int32:
+        return 32
+    raise TypeError(f"int64 or int32 tokens expected, got {tensor.dtype}")
+
+
+def _row_stride(tensor, rows, cols, name):
+    """Elements from row to row of a matrix whose rows are contiguous."""
+    if tuple(tensor.shape) != (rows, cols):
+        raise ValueError(f"{name}: shape {(rows, cols)} expected, got {tuple(tensor.shape)}")
+    if cols > 1 and tensor.stride(1) != 1:
+        raise ValueError(f"{name}: rows must be contiguous")
+    stride = tensor.stride(0) if rows > 1 else cols
+    if stride < cols:
+        raise ValueError(f"{name}: rows must not overlap")
+    return stride
+
+
+def _row_weights(tensor, rows, name):
+    if tensor is not None and (tensor.dtype is not _torch.float32 or tuple(tensor.shape) != (rows,) or not tensor.is_contiguous()):
+        raise ValueError(f"{name}: {rows} contiguous float32 values expected")
+
+
+class SoloGradNorm:
+    """Global norm of a set of gradient tensors, and clipping: the device table of the tensors (of any shape, contiguous,
+    float32 or bfloat16) with its workspace and results.  `clipped`: tensors of the same shapes and types that clip()
+    writes; they may be the gradients themselves (clipping in place).
+
+    norm() and clip() return (norm [1], grad_scale [1], tensor_norm [count]): buffers of this object that the next
+    call overwrites.  grad_scale is what SoloState.step and SoloMultiTable.step take."""
+
+    def __init__(self, grads, clipped=None, device="cuda"):
+        lib()
+        self.count = len(grads)
+        if clipped is not None and len(clipped) != self.count:
+            raise ValueError(f"{self.count} clipped tensors expected, got {len(clipped)}")
+        arr = (solo_grad * self.count)()
+        for k, g in enumerate(grads):
+            c = clipped[k] if clipped is not None else None
+            if not g.is_contiguous() or (c is not None and (not c.is_contiguous() or c.dtype is not g.dtype or c.shape != g.shape)):
+                raise ValueError(f"tensor {k}: contiguous gradients, and clipped ones of the same shapes and types, expected")
+            arr[k] = solo_grad(_ptr(g), _ptr(c), g.numel(), _dtype(g), 0)
+        self.units = solo_norm_units(arr, self.count)
+        nbytes = solo_norm_table_bytes(self.count, self.units)
+        host = _torch.empty((nbytes + 15) // 16 * 16, dtype=_torch.uint8)
+        if self.count:
+            solo_norm_table_build(arr, self.count, host.data_ptr(), nbytes)
+        self.table = host.to(device)
+        self.workspace = _torch.empty(solo_norm_workspace_bytes(self.units), dtype=_torch.uint8, device=device)
+        self.results = _torch.zeros(1, device=device), _torch.ones(1, device=device), _torch.zeros(self.count, device=device)
+        self.writes = clipped is not None
+        self._keep = grads, clipped                # the buffers the table points to
+
+    def _run(self, name, max_norm, unscale, stream):
+        if unscale is not None and unscale.dtype is not _torch.float32:
+            raise TypeError(f"unscale: float32 expected, got {unscale.dtype}")
+        _operation(name, True, self.table, self.count, self.units, unscale, max_norm, *self.results, self.workspace, stream)
+        return self.results
+
+    def norm(self, max_norm=float("inf"), unscale=None, stream=None):
+        return self._run("solo_grad_norm", max_norm, unscale, stream)
+
+    def clip(self, max_norm, unscale=None, stream=None):
+        if not self.writes:
+            raise ValueError("no tensors to write the clipped gradients to")
+        return self._run("solo_grad_clip", max_norm, unscale, stream)
+
+
+class SoloEmbedding:
+    """Lookup in an embedding table [vocab, dim] and the table's gradient, for up to `tokens` tokens a call: the workspace
+    that the gradient needs.  Tables and rows may be float32 or bfloat16, each on its own; their rows contiguous, at any
+    distance; tokens int64 or int32, those outside the table are padding."""
+
+    def __init__(self, vocab, dim, tokens, scale=1.0, device="cuda"):
+        lib()
+        self.vocab, self.dim, self.tokens, self.scale, self.device = vocab, dim, tokens, scale, device
+        shape = solo_embedding_shape(vocab, dim, tokens, dim, dim, SOLO_FP32, SOLO_FP32, 64, 0, scale, 0)
+        self.workspace_bytes = solo_embedding_workspace_bytes(shape)
+        if not self.workspace_bytes:
+            raise SoloError(SOLO_E_INVALID)
+        self.workspace = None                      # of the first gradient
+
+    def _shape(self, table, rows, ids, flags):
+        n = ids.numel()
+        if n > self.tokens:
+            raise ValueError(f"at most {self.tokens} tokens expected, got {n}")
+        return solo_embedding_shape(self.vocab, self.dim, n, _row_stride(table, self.vocab, self.dim, "table"),
+                                    _row_stride(rows, n, self.dim, "rows"), _dtype(table), _dtype(rows), _token_bits(ids, n),
+                                    flags, self.scale, 0)
+
+    def lookup(self, table, ids, out, stream=None):
+        """out[i] = scale * table[ids[i]]"""
+        shape = self._shape(table, out, ids, 0)
+        _operation("solo_embedding", True, table, ids, out, C.addressof(shape), stream)
+        return out
+
+    def grad(self, grad_rows, ids, out, accumulate=False, stream=None):
+        """out[v] = scale * the sum of the rows whose token is v; added to `out` if `accumulate`."""
+        shape = self._shape(out, grad_rows, ids, SOLO_EMBEDDING_ACCUMULATE if accumulate else 0)
+        if self.workspace is None:
+            self.workspace = _torch.empty(self.workspace_bytes, dtype=_torch.uint8, device=self.device)
+        _operation("solo_embedding_grad", True, grad_rows, ids, out, self.workspace, self.workspace_bytes, C.addressof(shape), stream)
+        return out
+
+
+class SoloLogprob:
+    """Log probabilities, entropies, ranks and `top` alternatives of up to `rows` rows of `cols` logits (float32 or
+    bfloat16, rows contiguous, at any distance), and the gradient: the buffers of the results, which the next call overwrites.
+    Targets are int64 or int32; one outside the columns is a padding position."""
+
+    def __init__(self, rows, cols, top=0, rank=False, scale=1.0, device="cuda"):
+        lib()
+        if not 0 <= top <= SOLO_TOP_MAX:
+            raise ValueError(f"0 to {SOLO_TOP_MAX} alternatives expected, got {top}")
+        self.rows, self.cols, self.top, self.scale = rows, cols, top, scale
+        f32, i32 = dict(dtype=_torch.float32, device=device), dict(dtype=_torch.int32, device=device)
+        self.logprob, self.entropy = _torch.empty(rows, **f32), _torch.empty(rows, **f32)
+        self.stats = _torch.empty((rows, 2), **f32)
+        self.rank = _torch.empty(rows, **i32) if rank else None
+        self.top_logprob = _torch.empty((rows, top), **f32) if top else None
+        self.top_token = _torch.empty((rows, top), **i32) if top else None
+
+    def _shape(self, logits, targets, out=None):
+        r = logits.shape[0]
+        if r > self.rows:
+            raise ValueError(f"at most {self.rows} rows expected, got {r}")
+        stride = _row_stride(logits, r, self.cols, "logits")
+        grad_stride = stride
+        if out is not None:
+            grad_stride = _row_stride(out, r, self.cols, "gradient")
+            if out.dtype is not logits.dtype:
+                raise TypeError(f"gradient: {logits.dtype} expected, got {out.dtype}")
+        return solo_logits(r, self.cols, stride, grad_stride, _dtype(logits), 64 if targets is None else _token_bits(targets, r),
+                           self.top, 0, self.scale, 0)
+
+    def forward(self, logits, targets, stream=None):
+        """(logprob, entropy[, rank][, top_logprob, top_token]); without targets, logprob and rank are None."""
+        shape = self._shape(logits, targets)
+        none = targets is None
+        logprob, rank = (None, None) if none else (self.logprob, self.rank)
+        _operation("solo_logprob", True, logits, targets, logprob, self.entropy, rank, self.top_logprob, self.top_token, self.stats,
+                   C.addressof(shape), stream)
+        results = [logprob, self.entropy]
+        if self.rank is not None:
+            results.append(rank)
+        if self.top:
+            results += [self.top_logprob, self.top_token]
+        return tuple(results) if shape.rows == self.rows else tuple(t if t is None else t[:shape.rows] for t in results)
+
+    def grad(self, logits, targets, grad_logprob, grad_entropy, out, stream=None):
+        """Gradient of the logits behind forward() on the same ones, for the gradients of logprob and entropy (or None)."""
+        shape = self._shape(logits, targets, out)
+        _row_weights(grad_logprob, shape.rows, "grad_logprob")
+        _row_weights(grad_entropy, shape.rows, "grad_entropy")
+        _operation("solo_logprob_grad", True, logits, targets, self.entropy, self.stats, grad_logprob, grad_entropy, out,
+                   C.addressof(shape), stream)
+        return out
+
+    def forward_grad(self, logits, targets, grad_logprob, grad_entropy, out, stream=None):
+        """(logprob, entropy, gradient) in one pass, for row weights that are known beforehand."""
+        shape = self._shape(logits, targets, out)
+        _row_weights(grad_logprob, shape.rows, "grad_logprob")
+        _row_weights(grad_entropy, shape.rows, "grad_entropy")
+        logprob = None if targets is None else self.logprob
+        _operation("solo_logprob_with_grad", True, logits, targets, grad_logprob, grad_entropy, logprob, self.entropy, out,
+                   C.addressof(shape), stream)
+        if shape.rows != self.rows:
+            return None if logprob is None else logprob[:shape.rows], self.entropy[:shape.rows], out
+        return logprob, self.entropy, out
 
 
 HBM_REGION_BYTES = 96 << 30      # an MI355X behaves as three such regions of physical memory
