@@ -335,7 +335,7 @@ int solo_embedding_grad(const void *grad_rows, const void *tokens, void *grad_ta
  * tokens), reading the logits from HBM once. */
 #define SOLO_TOP_MAX 32
 typedef struct solo_logits {
-    uint64_t rows, cols;        /* cols below 2^31                                               */
+    uint64_t rows, cols;        /* cols below 2^29                                               */
     uint64_t stride;            /* elements from row to row of logits, >= cols                   */
     uint64_t grad_stride;       /* the same of grad_logits                                       */
     uint32_t dtype;             /* of logits and grad_logits                                     */

@@ -19,7 +19,7 @@
 
 namespace solo {
 
-constexpr int kCandidates = 1024;      // of a row, before the slower selection takes over
+constexpr int kCandidates = 512;       // logits that are collected for the alternatives, before a slower selection takes over
 constexpr float kSlack = 8.0f;         // binary orders that a logit may lie above a thread's reference
 constexpr float kFloor = -1000.0f;     // e^d is 0 far above this; below it d is -inf or would be no number times 0
 
@@ -47,27 +47,34 @@ __device__ __forceinline__ void rebase(Sums &a, float at, float k)
     a.at = at;
 }
 
+__device__ __forceinline__ void add1(Sums &a, float x, float k)
+{
+    const float d = (x - a.at) * k, p = __builtin_amdgcn_exp2f(d);
+    a.s += p;
+    a.w = fmaf(p, fmaxf(d, kFloor), a.w);
+}
+
 __device__ __forceinline__ void add8(Sums &a, const float x[8], float k)
 {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float d = (x[e] - a.at) * k, p = __builtin_amdgcn_exp2f(d);
-        a.s += p;
-        a.w = fmaf(p, fmaxf(d, kFloor), a.w);
-    }
+    for (int e = 0; e < 8; ++e) add1(a, x[e], k);
 }
 
 __device__ __forceinline__ float max8(const float x[8])
 {
-    return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+    // (NaN wins; three operands an instruction, where fmaxf first quiets each of its own)
+    float m = __builtin_elementwise_maximum(__builtin_elementwise_maximum(x[0], x[1]), x[2]);
+    m = __builtin_elementwise_maximum(m, __builtin_elementwise_maximum(__builtin_elementwise_maximum(x[3], x[4]), x[5]));
+    return __builtin_elementwise_maximum(m, __builtin_elementwise_maximum(x[6], x[7]));
 }
 
-// Logits in the order of their values, as whole numbers; -0 and +0 are the same.  Behind it the column: the lower one is the larger key.
-__device__ __forceinline__ uint64_t key_of(float x, uint32_t column)
+// Logits in the order of their values, as whole numbers; -0 and +0 are the same.  A key has the column behind it: the lower one is larger.
+__device__ __forceinline__ uint32_t order_of(float x)
 {
     const uint32_t u = __float_as_uint(x + 0.0f);
-    return (uint64_t)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32 | (0xFFFFFFFFu - column);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+__device__ __forceinline__ uint64_t key_of(uint32_t order, uint32_t column) { return (uint64_t)order << 32 | (0xFFFFFFFFu - column); }
 __device__ __forceinline__ float value_of(uint64_t key)
 {
     const uint32_t u = (uint32_t)(key >> 32);
@@ -80,156 +87,275 @@ __device__ __forceinline__ int64_t target_of(const RowArgs &a, uint64_t row)
     return a.wide ? static_cast<const int64_t *>(a.targets)[row] : (int64_t)static_cast<const int32_t *>(a.targets)[row];
 }
 
-// Group g of eight columns of a row; columns behind the last are -inf.
+// A row is cut into groups of eight columns, dealt out to the threads in turn, and up to seven columns behind the last whole
+// group, one each to the first threads.
 template <bool BF16>
-__device__ __forceinline__ void read_group(const void *row, uint32_t g, uint32_t cols, float x[8])
-{
-    if (g * 8 + 8 <= cols) {
-        Elements<BF16>::unpack(Elements<BF16>::load8(row, g * 8), x);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = g * 8 + e < cols ? Elements<BF16>::load1(row, g * 8 + e) : -INFINITY;
-    }
-}
+struct Row {
+    const void *at;
+    uint32_t groups, rest;      // whole groups; columns behind them
 
-template <int THREADS>
-struct RowLds {
-    float at[THREADS / kLanes], s[THREADS / kLanes], w[THREADS / kLanes];
-    uint32_t above[THREADS / kLanes];
-    uint64_t key[THREADS];
-    uint32_t owner[SOLO_TOP_MAX];
-    uint64_t threshold, best;
-    uint32_t candidates;
-    uint64_t candidate[kCandidates];
+    __device__ __forceinline__ Row(const RowArgs &a, uint64_t r)
+        : at(static_cast<const char *>(a.logits) + r * a.stride * Elements<BF16>::kBytes), groups(a.cols / 8), rest(a.cols % 8) {}
+    __device__ __forceinline__ bool has_share(uint32_t thread) const { return thread < groups || thread < rest; }
+    __device__ __forceinline__ typename Elements<BF16>::Raw group(uint32_t g) const { return Elements<BF16>::load8_near(at, g * 8); }
+    __device__ __forceinline__ float one(uint32_t column) const { return Elements<BF16>::load1(at, column); }
 };
-template <int THREADS>
-struct RowLdsSmall { float at[THREADS / kLanes], s[THREADS / kLanes], w[THREADS / kLanes]; uint32_t above[THREADS / kLanes]; };
 
-// The sums of a row, for every thread; `largest` and `where`: this thread's largest logit and its group.
-template <bool BF16, bool TOP, bool RANK, int THREADS, typename Lds>
-__device__ __forceinline__ Sums row_sums(const void *row, uint32_t cols, float k, float target, Lds &lds, float &largest, uint32_t &where, uint32_t &above)
+template <int THREADS>
+struct SumLds { float at[THREADS / kLanes], s[THREADS / kLanes], w[THREADS / kLanes]; uint32_t above[THREADS / kLanes]; };
+
+template <int THREADS>
+struct TopLds : SumLds<THREADS> {
+    uint32_t largest[kLanes];                  // of the shares, as ordered whole numbers
+    uint32_t column[THREADS];                  // where the threshold stands first among a thread's logits
+    uint32_t threshold, last_column;
+    uint32_t holders, owners, candidates;
+    uint32_t owner[THREADS];
+    uint64_t candidate[kCandidates];
+    uint32_t before[kCandidates];              // candidates with a larger key
+    uint64_t best[THREADS / kLanes];
+};
+
+// What a thread remembers of its logits for the alternatives: the largest one of its groups, the number of that group (the
+// column behind the groups counts as one more) and the largest of the other groups.
+struct Largest {
+    float first = -INFINITY, second = -INFINITY;
+    uint32_t group = 0xFFFFFFFFu;
+    __device__ __forceinline__ void see(float m, uint32_t g)
+    {
+        if (!(m <= first)) {
+            second = first;
+            first = m;
+            group = g;
+        } else {
+            second = fmaxf(second, m);
+        }
+    }
+};
+
+// The sums of a row, for every thread.  `last`: its column behind the groups; with RESIDENT, for rows of no more than
+// THREADS * DEPTH groups, `raw` are its groups.  Otherwise the loads of the next DEPTH groups are under way while DEPTH are added.
+template <bool BF16, bool TOP, bool RANK, bool RESIDENT, int THREADS, int DEPTH>
+__device__ __forceinline__ Sums row_sums(const Row<BF16> &row, float k, float target, SumLds<THREADS> &lds,
+                                         typename Elements<BF16>::Raw raw[DEPTH], float &last, Largest &largest, uint32_t &above)
 {
     Sums a = {-FLT_MAX, 0.0f, 0.0f};
-    largest = -INFINITY;
-    where = threadIdx.x;
     uint32_t count = 0;
-    const uint32_t groups = (cols + 7) / 8;
-    for (uint32_t g = threadIdx.x; g < groups; g += THREADS) {
+    last = -INFINITY;
+    if (threadIdx.x < row.rest) last = row.one(row.groups * 8 + threadIdx.x);
+    auto add = [&](const typename Elements<BF16>::Raw &r, uint32_t g) {
         float x[8];
-        read_group<BF16>(row, g, cols, x);
+        Elements<BF16>::unpack(r, x);
         const float m = max8(x);
         if ((m - a.at) * k > kSlack) rebase(a, m, k);
-        if (TOP && m > largest) { largest = m; where = g; }
+        if (TOP) largest.see(m, g);
         if (RANK) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) count += x[e] > target;
         }
         add8(a, x, k);
-    }
-    // bring the sums of the wavefront, then of the workgroup, to one reference: the largest of the threads'
-    float at = a.at;
+    };
+    uint32_t g0 = 0;
+    if (!RESIDENT && row.groups >= THREADS * DEPTH) {
+        typename Elements<BF16>::Raw next[DEPTH];
 #pragma unroll
-    for (int d = 1; d < kLanes; d <<= 1) at = fmaxf(at, __shfl_xor(at, d));
+        for (int j = 0; j < DEPTH; ++j) next[j] = row.group(threadIdx.x + j * THREADS);
+        for (; g0 + THREADS * DEPTH <= row.groups; g0 += THREADS * DEPTH) {
+#pragma unroll
+            for (int j = 0; j < DEPTH; ++j) {
+                raw[j] = next[j];
+                next[j] = row.group(min(g0 + THREADS * DEPTH + j * THREADS + threadIdx.x, row.groups - 1));
+            }
+#pragma unroll
+            for (int j = 0; j < DEPTH; ++j) add(raw[j], g0 + j * THREADS + threadIdx.x);
+        }
+#pragma unroll
+        for (int j = 0; j < DEPTH; ++j)
+            if (g0 + j * THREADS + threadIdx.x < row.groups) add(next[j], g0 + j * THREADS + threadIdx.x);
+    } else if (row.groups != 0) {
+#pragma unroll
+        for (int j = 0; j < DEPTH; ++j) raw[j] = row.group(min(j * THREADS + threadIdx.x, row.groups - 1));
+#pragma unroll
+        for (int j = 0; j < DEPTH; ++j)
+            if (j * THREADS + threadIdx.x < row.groups) add(raw[j], j * THREADS + threadIdx.x);
+    }
+    if (threadIdx.x < row.rest) {
+        if ((last - a.at) * k > kSlack) rebase(a, last, k);
+        if (TOP) largest.see(last, row.groups);
+        if (RANK) count += last > target;
+        add1(a, last, k);
+    }
+    const float at = wave_max(a.at);
     rebase(a, at, k);
     a.s = wave_sum(a.s);
     a.w = wave_sum(a.w);
     if (RANK) count = wave_sum(count);
+    above = count;
+    if (THREADS == kLanes) return a;
     const int wave = threadIdx.x / kLanes;
     if (threadIdx.x % kLanes == 0) {
         lds.at[wave] = a.at; lds.s[wave] = a.s; lds.w[wave] = a.w;
         lds.above[wave] = count;
     }
     __syncthreads();
-    at = lds.at[0];
-    for (int w = 1; w < THREADS / kLanes; ++w) at = fmaxf(at, lds.at[w]);
-    Sums all = {at, 0.0f, 0.0f};
-    above = 0;
-    for (int w = 0; w < THREADS / kLanes; ++w) {
-        Sums part = {lds.at[w], lds.s[w], lds.w[w]};
-        rebase(part, at, k);
-        all.s += part.s;
-        all.w += part.w;
-        above += lds.above[w];
-    }
+    constexpr int kWaves = THREADS / kLanes;
+    const int part = threadIdx.x % kWaves;                 // every wavefront adds the wavefronts' sums, several times over
+    Sums all = {lds.at[part], lds.s[part], lds.w[part]};
+    above = lds.above[part];
+    rebase(all, wave_max<kWaves>(all.at), k);
+    all.s = wave_sum<kWaves>(all.s);
+    all.w = wave_sum<kWaves>(all.w);
+    if (RANK) above = wave_sum<kWaves>(above);
     return all;
 }
 
-// The a.top largest logits of a row, by key; `mine` is this thread's largest (0 if it has none).
+// The a.top largest logits of a row.  The threads of one lane number, one in each wavefront, have a share of the row; with T the
+// a.top-th largest of the 64 shares' largest logits, a.top logits at least are no smaller than T, and only threads whose own
+// largest is no smaller hold any.  These are few, unless many share the value T: then, C being the a.top-th lowest of the
+// columns where threads hold T first, a logit T behind column C is none of the alternatives.
 template <bool BF16, int THREADS>
-__device__ __forceinline__ void row_top(const RowArgs &a, const void *row, uint64_t out, uint64_t mine, const Sums &all, RowLds<THREADS> &lds)
+__device__ __forceinline__ void row_top(const RowArgs &a, const Row<BF16> &row, uint64_t out, const Largest &largest, const Sums &all, TopLds<THREADS> &lds)
 {
-    const uint32_t groups = (a.cols + 7) / 8, found = min(a.top, a.cols);
-    const float log_s = __builtin_amdgcn_logf(all.s);
-    float *const value = a.top_logprob + out * a.top;
-    int32_t *const token = a.top_token + out * a.top;
+    const uint32_t found = min(a.top, a.cols), each = (row.groups + THREADS - 1) / THREADS + 1;      // (groups of a thread, and its column behind them)
+    const float log_s = __builtin_amdgcn_logf(all.s) * kLn2;
+    const uint32_t lane = threadIdx.x % kLanes;
     auto put = [&](uint32_t at, uint64_t key) {
-        const float x = value_of(key);
-        value[at] = all.s == 0.0f ? -INFINITY : fmaf(x - all.at, a.scale, -log_s * kLn2);
-        token[at] = (int32_t)column_of(key);
+        a.top_logprob[out * a.top + at] = all.s == 0.0f ? -INFINITY : fmaf(value_of(key) - all.at, a.scale, -log_s);
+        a.top_token[out * a.top + at] = (int32_t)column_of(key);
     };
-    lds.key[threadIdx.x] = mine;
-    if (threadIdx.x == 0) lds.candidates = 0;
+    const bool any = row.has_share(threadIdx.x);
+    const uint32_t mine = any ? order_of(largest.first) : 0;
+    if (THREADS == kLanes) lds.largest[lane] = mine;
+    else atomicMax(&lds.largest[lane], mine);              // (0 from the row before)
     __syncthreads();
-    uint32_t larger = 0;
-    for (int t = 0; t < THREADS; ++t) larger += lds.key[t] > mine;
-    const uint32_t owners = min(found, min(groups, (uint32_t)THREADS));        // threads that have a key at all, at most a.top of them
-    if (mine != 0 && larger < owners) {
-        lds.owner[larger] = threadIdx.x;
-        if (larger == owners - 1) lds.threshold = owners == found ? mine : 0;  // (fewer threads than alternatives: every element is a candidate)
+    uint32_t threshold;
+    {
+        const uint32_t own = lds.largest[lane];
+        uint32_t larger = 0;
+#pragma unroll 4
+        for (int t = 0; t < kLanes; t += 4) {
+            const uint4 o = *reinterpret_cast<const uint4 *>(&lds.largest[t]);
+            larger += (o.x > own) + (o.y > own) + (o.z > own) + (o.w > own);
+        }
+        // the smallest that fewer than `found` exceed; 0 where there are fewer shares
+        threshold = ~wave_max(larger < found ? ~own : 0u);
     }
+    const bool holds = any && mine >= threshold;
+    bool counts = holds;
+    if (holds) atomicAdd(&lds.holders, 1u);
     __syncthreads();
-    const uint64_t threshold = lds.threshold;
-    // groups of the owners: owner, owner + THREADS, ...
-    const uint32_t each = (groups + THREADS - 1) / THREADS;
-    for (uint32_t i = threadIdx.x; i < owners * each; i += THREADS) {
-        const uint32_t g = lds.owner[i % owners] + i / owners * THREADS;
-        if (g >= groups) continue;
-        float x[8];
-        read_group<BF16>(row, g, a.cols, x);
+    const uint32_t holders = lds.holders;
+    uint32_t last_column = 0xFFFFFFFFu;
+    if (holders > (THREADS == kLanes ? found : 2 * found) + 8) {            // several hold the same value: their columns decide
+        uint32_t column = 0xFFFFFFFFu;
+        if (any && mine == threshold) {
+            for (uint32_t g = threadIdx.x; g < row.groups && column == 0xFFFFFFFFu; g += THREADS) {
+                float x[8];
+                Elements<BF16>::unpack(row.group(g), x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint64_t key = key_of(x[e], g * 8 + e);
-            if (g * 8 + e < a.cols && key >= threshold) {
-                const uint32_t at = atomicAdd(&lds.candidates, 1u);
-                if (at < kCandidates) lds.candidate[at] = key;
+                for (int e = 7; e >= 0; --e)
+                    if (order_of(x[e]) == threshold) column = g * 8 + e;
+            }
+            if (column == 0xFFFFFFFFu && threadIdx.x < row.rest) column = row.groups * 8 + threadIdx.x;
+        }
+        lds.column[threadIdx.x] = column;
+        __syncthreads();
+        if (threadIdx.x == 0) lds.last_column = 0xFFFFFFFFu;
+        uint32_t lower = 0;
+        if (column != 0xFFFFFFFFu) {
+#pragma unroll 2
+            for (int t = 0; t < THREADS; t += 4) {
+                const uint4 o = *reinterpret_cast<const uint4 *>(&lds.column[t]);
+                lower += (o.x < column) + (o.y < column) + (o.z < column) + (o.w < column);
             }
         }
+        __syncthreads();
+        if (column != 0xFFFFFFFFu && lower == found - 1) lds.last_column = column;     // (none where fewer hold it: then all of them count)
+        __syncthreads();
+        last_column = lds.last_column;
+        counts = holds && (mine > threshold || column <= last_column);
     }
+    auto look = [&](float x, uint32_t column, auto &&use) {
+        const uint32_t order = order_of(x);
+        if (order > threshold || (order == threshold && column <= last_column)) use(key_of(order, column));
+    };
+    auto look_at_group = [&](uint32_t g, uint32_t thread, auto &&use) {
+        if (g < row.groups) {
+            float x[8];
+            Elements<BF16>::unpack(row.group(g), x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) look(x[e], g * 8 + e, use);
+        } else if (g == row.groups && thread < row.rest) {
+            look(row.one(row.groups * 8 + thread), row.groups * 8 + thread, use);
+        }
+    };
+    auto collect = [&](uint64_t key) {
+        const uint32_t at = atomicAdd(&lds.candidates, 1u);
+        if (at < kCandidates) lds.candidate[at] = key;
+    };
+    // most threads hold theirs in one group; all groups of the others are looked through by everyone
+    const bool one_group = counts && order_of(largest.second) < threshold;
+    if (one_group) look_at_group(largest.group, threadIdx.x, collect);
+    else if (counts) lds.owner[atomicAdd(&lds.owners, 1u)] = threadIdx.x;
     __syncthreads();
+    const uint32_t owners = lds.owners;
+    auto keys_of = [&](uint32_t i, auto &&use) {
+        const uint32_t turn = i / owners, owner = lds.owner[i - turn * owners];
+        const uint32_t g = owner + turn * THREADS;
+        if (turn == each - 1) look_at_group(row.groups, owner, use);
+        else if (g < row.groups) look_at_group(g, owner, use);
+    };
+    for (uint32_t i = threadIdx.x; i < owners * each; i += THREADS) keys_of(i, collect);
+    if (owners != 0) __syncthreads();
     const uint32_t count = lds.candidates;
     if (count <= kCandidates) {
-        for (uint32_t i = threadIdx.x; i < count; i += THREADS) {
+        // a thread compares one candidate with every (THREADS / kLanes)-th
+        constexpr uint32_t kParts = THREADS / kLanes;
+        for (uint32_t i = lane; i < count; i += kLanes) {
             const uint64_t key = lds.candidate[i];
             uint32_t before = 0;
-            for (uint32_t j = 0; j < count; ++j) before += lds.candidate[j] > key;
-            if (before < found) put(before, key);
+#pragma unroll 4
+            for (uint32_t j = threadIdx.x / kLanes; j < count; j += kParts) before += lds.candidate[j] > key;
+            if (kParts == 1) {
+                if (before < found) put(before, key);
+            } else if (before) {
+                atomicAdd(&lds.before[i], before);         // (0 from the row before)
+            }
+        }
+        if (kParts > 1) {
+            __syncthreads();
+            for (uint32_t i = threadIdx.x; i < count; i += THREADS) {
+                const uint32_t before = lds.before[i];
+                lds.before[i] = 0;
+                if (before < found) put(before, lds.candidate[i]);
+            }
         }
     } else {                                               // large logits crowd in few threads: one alternative after the other
         uint64_t last = ~0ull;
         for (uint32_t r = 0; r < found; ++r) {
             uint64_t best = 0;
-            for (uint32_t i = threadIdx.x; i < owners * each; i += THREADS) {
-                const uint32_t g = lds.owner[i % owners] + i / owners * THREADS;
-                if (g >= groups) continue;
-                float x[8];
-                read_group<BF16>(row, g, a.cols, x);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint64_t key = key_of(x[e], g * 8 + e);
-                    if (g * 8 + e < a.cols && key < last && key > best) best = key;
-                }
-            }
+            auto better = [&](uint64_t key) { if (key < last && key > best) best = key; };
+            if (one_group) look_at_group(largest.group, threadIdx.x, better);
+            for (uint32_t i = threadIdx.x; i < owners * each; i += THREADS) keys_of(i, better);
+            best = wave_max(best);
+            __syncthreads();                               // (best of the round before)
+            if (lane == 0) lds.best[threadIdx.x / kLanes] = best;
             __syncthreads();
-            lds.key[threadIdx.x] = best;
-            __syncthreads();
-            for (int t = 0; t < THREADS; ++t) best = lds.key[t] > best ? lds.key[t] : best;
+            for (int w = 0; w < THREADS / kLanes; ++w) best = lds.best[w] > best ? lds.best[w] : best;
             if (threadIdx.x == 0) put(r, best);
             last = best;
         }
     }
     for (uint32_t r = found + threadIdx.x; r < a.top; r += THREADS) {
-        value[r] = -INFINITY;
-        token[r] = -1;
+        a.top_logprob[out * a.top + r] = -INFINITY;
+        a.top_token[out * a.top + r] = -1;
+    }
+    __syncthreads();
+    if (threadIdx.x < kLanes) lds.largest[threadIdx.x] = 0;
+    if (threadIdx.x == 0) {
+        lds.holders = 0;
+        lds.owners = 0;
+        lds.candidates = 0;
     }
 }
 
@@ -242,13 +368,22 @@ __device__ __forceinline__ float row_logprob(const Sums &all, float target, floa
     return all.s == 0.0f ? -INFINITY : fmaf(target - all.at, scale, -__builtin_amdgcn_logf(all.s) * kLn2);
 }
 
-template <bool BF16, bool TOP, bool RANK, int THREADS>
-__global__ __launch_bounds__(THREADS) void logprob_kernel(const RowArgs a)
+template <bool BF16, bool TOP, bool RANK, int THREADS, int DEPTH>
+__global__ __launch_bounds__(THREADS, !TOP ? 8 : THREADS < 512 ? 6 : 5) void logprob_kernel(const RowArgs a)
 {
-    __shared__ typename std::conditional<TOP, RowLds<THREADS>, RowLdsSmall<THREADS>>::type lds;
+    __shared__ __align__(16) typename std::conditional<TOP, TopLds<THREADS>, SumLds<THREADS>>::type lds;
     const float k = a.scale * kLog2E;
+    if constexpr (TOP) {                                   // (the barriers of row_sums stand between this and its first use)
+        if (threadIdx.x < kLanes) lds.largest[threadIdx.x] = 0;
+        for (uint32_t i = threadIdx.x; i < kCandidates; i += THREADS) lds.before[i] = 0;
+        if (threadIdx.x == 0) {
+            lds.holders = 0;
+            lds.owners = 0;
+            lds.candidates = 0;
+        }
+    }
     for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const char *row = static_cast<const char *>(a.logits) + r * a.stride * Elements<BF16>::kBytes;
+        const Row<BF16> row(a, r);
         const int64_t t = a.targets ? target_of(a, r) : 0;
         const bool has = a.targets != nullptr;
         if (has && (t < 0 || t >= (int64_t)a.cols)) {      // no target: the row is not read
@@ -265,107 +400,125 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(const RowArgs a)
                 }
             continue;
         }
-        const float target = has ? Elements<BF16>::load1(row, t) : 0.0f;
-        float largest;
-        uint32_t where, above;
-        const Sums all = row_sums<BF16, TOP, RANK, THREADS>(row, a.cols, k, target, lds, largest, where, above);
+        const float target = has ? row.one((uint32_t)t) : 0.0f;
+        float last;
+        Largest largest;
+        uint32_t above;
+        typename Elements<BF16>::Raw raw[DEPTH];
+        const Sums all = row_sums<BF16, TOP, RANK, false, THREADS, DEPTH>(row, k, target, lds, raw, last, largest, above);
         if (threadIdx.x == 0) {
             if (a.logprob && has) a.logprob[r] = row_logprob(all, target, a.scale);
             if (a.entropy) a.entropy[r] = row_entropy(all);
             if (RANK) a.rank[r] = (int32_t)above;
             if (a.stats) { a.stats[2 * r] = all.at; a.stats[2 * r + 1] = all.s; }
         }
-        if constexpr (TOP) {
-            uint64_t mine = 0;
-            if (where * 8 < a.cols) {                       // the lowest column of the group that holds the largest one
-                float x[8];
-                read_group<BF16>(row, where, a.cols, x);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint64_t key = key_of(x[e], where * 8 + e);
-                    if (where * 8 + e < a.cols && key > mine) mine = key;
-                }
-            }
-            row_top<BF16, THREADS>(a, row, r, mine, all, lds);
-        }
+        if constexpr (TOP) row_top<BF16, THREADS>(a, row, r, largest, all, lds);
         __syncthreads();                                   // (the sums in lds)
     }
 }
 
-// dx of group g; `at` and `s` of the row's sums.
-template <bool BF16>
-__device__ __forceinline__ void put_gradient(const void *row, void *out, uint32_t g, uint32_t cols, uint32_t target, float at, float s, float k, float scale, float a, float b, float entropy)
+// What the gradient of a row needs: p_j = 2^((x_j - at) k - log_s), dx_j = p_j (a + b (ln p_j + entropy)), and what is added at the target.
+struct Slope { float at, log_s, a, b, entropy, target; };
+
+__device__ __forceinline__ Slope slope_of(float at, float s, float entropy, float up, float up_entropy, float scale)
+{
+    // (no column of a row without probabilities has one: 2^-inf)
+    return Slope{at, s == 0.0f ? INFINITY : __builtin_amdgcn_logf(s), -scale * up, -scale * up_entropy, entropy, s == 0.0f ? 0.0f : scale * up};
+}
+
+template <bool ENTROPY>
+__device__ __forceinline__ float gradient_of(float x, const Slope &s, float k)
+{
+    const float d = fmaf(x - s.at, k, -s.log_s), p = __builtin_amdgcn_exp2f(d);
+    return p * (ENTROPY ? fmaf(s.b, fmaf(fmaxf(d, kFloor), kLn2, s.entropy), s.a) : s.a);
+}
+
+template <bool BF16, bool ENTROPY>
+__device__ __forceinline__ void put_gradient(const typename Elements<BF16>::Raw &raw, void *out, uint32_t g, uint32_t target, const Slope &s, float k)
 {
     float x[8];
-    read_group<BF16>(row, g, cols, x);
-    const float inverse = s == 0.0f ? 0.0f : 1.0f / s, log_s = s == 0.0f ? 0.0f : __builtin_amdgcn_logf(s);
+    Elements<BF16>::unpack(raw, x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float d = (x[e] - at) * k, p = __builtin_amdgcn_exp2f(d) * inverse;
-        const float inner = fmaxf(d - log_s, kFloor) * kLn2 + entropy;
-        x[e] = -p * fmaf(b, inner, a);
-        if (g * 8 + e == target && s != 0.0f) x[e] += a;
-        x[e] *= scale;
-    }
-    if (g * 8 + 8 <= cols) {
-        Elements<BF16>::store8(out, g * 8, x);
-    } else {
+    for (int e = 0; e < 8; ++e) x[e] = gradient_of<ENTROPY>(x[e], s, k);
+    if (g == target / 8) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (g * 8 + e < cols) Elements<BF16>::store1(out, g * 8 + e, x[e]);
+            if (e == (int)(target % 8)) x[e] += s.target;
     }
+    Elements<BF16>::store8_near(out, g * 8, x);
 }
 
-template <bool BF16>
-__device__ __forceinline__ void put_zeros(void *out, uint32_t g, uint32_t cols)
+// Wavefronts per SIMD that the registers have to leave room for.  Rows that stay in registers: two workgroups of 1024 threads, so that
+// one loads while the other computes, where 64 registers are enough; else as many as the row's own registers allow.
+constexpr int grad_waves(bool bf16, bool forward, bool resident, int threads, int depth)
 {
-    const float none[8] = {};
-    if (g * 8 + 8 <= cols) {
-        Elements<BF16>::store8(out, g * 8, none);
-    } else {
-        for (uint32_t c = g * 8; c < cols; ++c) Elements<BF16>::store1(out, c, 0.0f);
-    }
+    if (!forward || !resident) return 8;
+    if (depth > 4) return 4;
+    return bf16 ? 8 : threads == 1024 ? 4 : 5;
 }
 
-// FORWARD: the sums first, then the gradient, of a row that the caches still hold; else from the sums that are given.
-template <bool BF16, bool FORWARD, int THREADS>
-__global__ __launch_bounds__(THREADS) void logprob_grad_kernel(const RowArgs a)
+// FORWARD: the sums first, then the gradient; else from the sums that are given.  RESIDENT: the row has no more than THREADS * DEPTH
+// groups, which stay in registers between the two.
+template <bool BF16, bool FORWARD, bool RESIDENT, bool ENTROPY, int THREADS, int DEPTH>
+__global__ __launch_bounds__(THREADS, grad_waves(BF16, FORWARD, RESIDENT, THREADS, DEPTH)) void logprob_grad_kernel(const RowArgs a)
 {
-    __shared__ RowLdsSmall<THREADS> lds;
+    __shared__ SumLds<THREADS> lds;
     const float k = a.scale * kLog2E;
-    const uint32_t groups = (a.cols + 7) / 8;
     for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const char *row = static_cast<const char *>(a.logits) + r * a.stride * Elements<BF16>::kBytes;
+        const Row<BF16> row(a, r);
         char *out = static_cast<char *>(a.grad) + r * a.grad_stride * Elements<BF16>::kBytes;
         const int64_t t = a.targets ? target_of(a, r) : -1;
         if (a.targets && (t < 0 || t >= (int64_t)a.cols)) {
-            for (uint32_t g = threadIdx.x; g < groups; g += THREADS) put_zeros<BF16>(out, g, a.cols);
+            const float none[8] = {};
+            for (uint32_t g = threadIdx.x; g < row.groups; g += THREADS) Elements<BF16>::store8_near(out, g * 8, none);
+            if (threadIdx.x < row.rest) Elements<BF16>::store1(out, row.groups * 8 + threadIdx.x, 0.0f);
             if (FORWARD && threadIdx.x == 0) {
                 if (a.logprob) a.logprob[r] = 0.0f;
                 if (a.entropy) a.entropy[r] = 0.0f;
             }
             continue;
         }
-        const float up = a.grad_logprob && a.targets ? a.grad_logprob[r] : 0.0f, up_entropy = a.grad_entropy ? a.grad_entropy[r] : 0.0f;
-        Sums all;
-        float entropy;
+        const float up = a.grad_logprob && a.targets ? a.grad_logprob[r] : 0.0f, up_entropy = ENTROPY ? a.grad_entropy[r] : 0.0f;
+        typename Elements<BF16>::Raw raw[DEPTH];
+        float at, s, entropy, last = 0.0f;
         if (FORWARD) {
-            const float target = a.targets ? Elements<BF16>::load1(row, t) : 0.0f;
-            float largest;
-            uint32_t where, above;
-            all = row_sums<BF16, false, false, THREADS>(row, a.cols, k, target, lds, largest, where, above);
+            const float target = a.targets ? row.one((uint32_t)t) : 0.0f;
+            Largest largest;
+            uint32_t above;
+            const Sums all = row_sums<BF16, false, false, RESIDENT, THREADS, DEPTH>(row, k, target, lds, raw, last, largest, above);
+            at = all.at;
+            s = all.s;
             entropy = row_entropy(all);
             if (threadIdx.x == 0) {
                 if (a.logprob && a.targets) a.logprob[r] = row_logprob(all, target, a.scale);
                 if (a.entropy) a.entropy[r] = entropy;
             }
         } else {
-            all.at = a.stats[2 * r];
-            all.s = a.stats[2 * r + 1];
+            at = a.stats[2 * r];
+            s = a.stats[2 * r + 1];
             entropy = a.entropy[r];
         }
-        for (uint32_t g = threadIdx.x; g < groups; g += THREADS)
-            put_gradient<BF16>(row, out, g, a.cols, (uint32_t)t, all.at, all.s, k, a.scale, up, up_entropy, entropy);
+        const Slope slope = slope_of(at, s, entropy, up, up_entropy, a.scale);
+        if (!FORWARD && threadIdx.x < row.rest) last = row.one(row.groups * 8 + threadIdx.x);
+        for (uint32_t g0 = threadIdx.x; g0 < row.groups; g0 += THREADS * DEPTH) {
+            if (!(FORWARD && RESIDENT)) {
+#pragma unroll
+                for (int j = 0; j < DEPTH; ++j)
+                    if (g0 + j * THREADS < row.groups) raw[j] = row.group(g0 + j * THREADS);
+            }
+#pragma unroll
+            for (int j = 0; j < DEPTH; ++j)
+                if (g0 + j * THREADS < row.groups) {
+                    // (what has been unpacked for the sums is not kept: it would take twice the registers)
+                    if (FORWARD && RESIDENT) Elements<BF16>::forget(raw[j]);
+                    put_gradient<BF16, ENTROPY>(raw[j], out, g0 + j * THREADS, (uint32_t)t, slope, k);
+                }
+            if (FORWARD && RESIDENT) break;
+        }
+        if (threadIdx.x < row.rest) {
+            const uint32_t column = row.groups * 8 + threadIdx.x;
+            Elements<BF16>::store1(out, column, gradient_of<ENTROPY>(last, slope, k) + (column == (uint32_t)t ? slope.target : 0.0f));
+        }
         if (FORWARD) __syncthreads();
     }
 }
@@ -379,7 +532,7 @@ static int rows_args(RowArgs &a, const void *logits, const void *targets, const 
     if (s->rows != 0 && ((s->cols != 0 && !at_multiple(logits, element_bytes(s->dtype))) ||
                          (targets && !at_multiple(targets, s->target_bits / 8))))
         return SOLO_E_INVALID;
-    if (s->cols >= (1ull << 31) || s->rows >= (1ull << 40) || s->stride >= (1ull << 40) || s->grad_stride >= (1ull << 40)) return SOLO_E_UNSUPPORTED;
+    if (s->cols >= (1ull << 29) || s->rows >= (1ull << 40) || s->stride >= (1ull << 40) || s->grad_stride >= (1ull << 40)) return SOLO_E_UNSUPPORTED;
     a = RowArgs{};
     a.logits = logits; a.targets = targets;
     a.rows = s->rows; a.cols = (uint32_t)s->cols; a.stride = s->stride; a.grad_stride = s->grad_stride;
@@ -391,19 +544,49 @@ static bool optional_at(const void *p, uintptr_t size) { return !p || at_multipl
 
 static uint32_t row_grid(uint64_t rows) { return (uint32_t)(rows < (1u << 20) ? rows : 1u << 20); }
 
-template <int THREADS>
+template <int THREADS, int DEPTH>
 static void logprob_launch(const RowArgs &a, bool bf16, hipStream_t stream)
 {
     void (*kernel)(RowArgs);
     const bool top = a.top != 0, rank = a.rank != nullptr;
-    if (bf16) kernel = top ? (rank ? logprob_kernel<true, true, true, THREADS> : logprob_kernel<true, true, false, THREADS>)
-                           : (rank ? logprob_kernel<true, false, true, THREADS> : logprob_kernel<true, false, false, THREADS>);
-    else kernel = top ? (rank ? logprob_kernel<false, true, true, THREADS> : logprob_kernel<false, true, false, THREADS>)
-                      : (rank ? logprob_kernel<false, false, true, THREADS> : logprob_kernel<false, false, false, THREADS>);
+    if (bf16) kernel = top ? (rank ? logprob_kernel<true, true, true, THREADS, DEPTH> : logprob_kernel<true, true, false, THREADS, DEPTH>)
+                           : (rank ? logprob_kernel<true, false, true, THREADS, DEPTH> : logprob_kernel<true, false, false, THREADS, DEPTH>);
+    else kernel = top ? (rank ? logprob_kernel<false, true, true, THREADS, DEPTH> : logprob_kernel<false, true, false, THREADS, DEPTH>)
+                      : (rank ? logprob_kernel<false, false, true, THREADS, DEPTH> : logprob_kernel<false, false, false, THREADS, DEPTH>);
     hipLaunchKernelGGL(kernel, dim3(row_grid(a.rows)), dim3(THREADS), 0, stream, a);
 }
 
-constexpr uint64_t kFewRows = 512;     // up to so many rows a workgroup has 1024 threads instead of 256
+template <bool BF16, bool FORWARD, bool RESIDENT, int THREADS, int DEPTH>
+static void grad_launch(const RowArgs &a, hipStream_t stream)
+{
+    hipLaunchKernelGGL((a.grad_entropy ? logprob_grad_kernel<BF16, FORWARD, RESIDENT, true, THREADS, DEPTH>
+                                       : logprob_grad_kernel<BF16, FORWARD, RESIDENT, false, THREADS, DEPTH>),
+                       dim3(row_grid(a.rows)), dim3(THREADS), 0, stream, a);
+}
+
+template <bool BF16>
+static void with_grad_launch(const RowArgs &a, hipStream_t stream)
+{
+    const uint32_t groups = a.cols / 8;
+    if (groups <= 64 * 4) grad_launch<BF16, true, true, 64, 4>(a, stream);
+    else if (groups <= 256 * 4) grad_launch<BF16, true, true, 256, 4>(a, stream);
+    else if (groups <= 512 * 4) grad_launch<BF16, true, true, 512, 4>(a, stream);
+    else if (groups <= 1024 * 4) grad_launch<BF16, true, true, 1024, 4>(a, stream);
+    else if (groups <= 1024 * 8) grad_launch<BF16, true, true, 1024, 8>(a, stream);
+    else grad_launch<BF16, true, false, 1024, 2>(a, stream);
+}
+
+// Two or three groups of a row for each thread.
+template <bool BF16>
+static void only_grad_launch(const RowArgs &a, hipStream_t stream)
+{
+    const uint32_t groups = a.cols / 8;
+    if (groups <= 128) grad_launch<BF16, false, false, 64, 2>(a, stream);
+    else if (groups <= 256) grad_launch<BF16, false, false, 128, 2>(a, stream);
+    else if (groups <= 640) grad_launch<BF16, false, false, 256, 2>(a, stream);
+    else if (groups <= 1536) grad_launch<BF16, false, false, 512, 2>(a, stream);
+    else grad_launch<BF16, false, false, 1024, 2>(a, stream);
+}
 
 }  // namespace solo
 
@@ -421,8 +604,13 @@ int solo_logprob(const void *logits, const void *targets, float *logprob, float 
         ((logprob || rank) && !targets) || (shape->top != 0 && (!at_multiple(top_logprob, 4) || !at_multiple(top_token, 4))))
         return SOLO_E_INVALID;
     a.logprob = logprob; a.entropy = entropy; a.rank = rank; a.top_logprob = top_logprob; a.top_token = top_token; a.stats = stats;
-    if (a.rows <= kFewRows) logprob_launch<1024>(a, shape->dtype == SOLO_BF16, (hipStream_t)stream);
-    else logprob_launch<256>(a, shape->dtype == SOLO_BF16, (hipStream_t)stream);
+    const bool bf16 = shape->dtype == SOLO_BF16;
+    const uint32_t groups = a.cols / 8;
+    // A wavefront takes a row by itself where rows are short, or where there are enough of them that no compute unit waits and
+    // they are not so long that all wavefronts look for their alternatives at the same time; few rows get more threads each.
+    if (groups <= 256 || (a.rows >= 4096 && groups <= 2048)) logprob_launch<64, 2>(a, bf16, (hipStream_t)stream);
+    else if (a.rows >= 128 || groups <= 1024) logprob_launch<256, 2>(a, bf16, (hipStream_t)stream);
+    else logprob_launch<512, 2>(a, bf16, (hipStream_t)stream);
     return launched();
 }
 
@@ -440,8 +628,8 @@ int solo_logprob_grad(const void *logits, const void *targets, const float *entr
         return SOLO_E_INVALID;
     a.entropy = const_cast<float *>(entropy); a.stats = const_cast<float *>(stats);
     a.grad_logprob = grad_logprob; a.grad_entropy = grad_entropy; a.grad = grad_logits;
-    hipLaunchKernelGGL((shape->dtype == SOLO_BF16 ? logprob_grad_kernel<true, false, 256> : logprob_grad_kernel<false, false, 256>),
-                       dim3(row_grid(a.rows)), dim3(256), 0, (hipStream_t)stream, a);
+    if (shape->dtype == SOLO_BF16) only_grad_launch<true>(a, (hipStream_t)stream);
+    else only_grad_launch<false>(a, (hipStream_t)stream);
     return launched();
 }
 
@@ -460,8 +648,8 @@ int solo_logprob_with_grad(const void *logits, const void *targets, const float 
         return SOLO_E_INVALID;
     a.logprob = logprob; a.entropy = entropy;
     a.grad_logprob = grad_logprob; a.grad_entropy = grad_entropy; a.grad = grad_logits;
-    hipLaunchKernelGGL((shape->dtype == SOLO_BF16 ? logprob_grad_kernel<true, true, 512> : logprob_grad_kernel<false, true, 512>),
-                       dim3(row_grid(a.rows)), dim3(512), 0, (hipStream_t)stream, a);
+    if (shape->dtype == SOLO_BF16) with_grad_launch<true>(a, (hipStream_t)stream);
+    else with_grad_launch<false>(a, (hipStream_t)stream);
     return launched();
 }
 

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/solo.h"
 
 namespace solo {
@@ -52,6 +54,8 @@ struct Elements {
         for (int k = 0; k < (BF16 ? 1 : 2); ++k) r.q[k] = *reinterpret_cast<const Quad *>(at + 16 * k);
         return r;
     }
+    // The same where the offset is known to stay below 4 GiB of a base that is the same for the wavefront: one register of address.
+    __device__ __forceinline__ static Raw load8_near(const void *base, uint32_t i) { return load8(static_cast<const char *>(base) + i * kBytes, 0); }
     __device__ __forceinline__ static void unpack(const Raw &r, float x[8])
     {
 #pragma unroll
@@ -77,15 +81,67 @@ struct Elements {
         *reinterpret_cast<Quad *>(at) = a;
         if (!BF16) *reinterpret_cast<Quad *>(at + 16) = b;
     }
+    __device__ __forceinline__ static void store8_near(void *base, uint32_t i, const float x[8]) { store8(static_cast<char *>(base) + i * kBytes, 0, x); }
+    // From here on the compiler does not know what `r` holds.
+    __device__ __forceinline__ static void forget(Raw &r)
+    {
+#pragma unroll
+        for (int k = 0; k < (BF16 ? 1 : 2); ++k) asm volatile("" : "+v"(r.q[k]));
+    }
 };
 
-template <typename T>
-__device__ __forceinline__ T wave_sum(T x)
+// One step of a reduction: the values of the lanes of groups of D, which are all alike in a group, and of the neighbouring
+// groups of D.  By the data paths of the vector unit: through LDS a step takes several times as long.
+template <int D>
+__device__ __forceinline__ void neighbours(uint32_t x, uint32_t &a, uint32_t &b)
 {
-#pragma unroll
-    for (int d = 1; d < kLanes; d <<= 1) x += __shfl_xor(x, d);
-    return x;
+    if constexpr (D >= 16) {
+        const auto both = D == 16 ? __builtin_amdgcn_permlane16_swap(x, x, false, false) : __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        a = both[0];
+        b = both[1];
+    } else {                                               // quad_perm 1,0,3,2; quad_perm 2,3,0,1; half of a row mirrored; row rotated by 8
+        constexpr int kControl = D == 1 ? 0xB1 : D == 2 ? 0x4E : D == 4 ? 0x141 : 0x128;
+        a = x;
+        b = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kControl, 0xF, 0xF, true);
+    }
 }
+
+template <int D, typename T>
+__device__ __forceinline__ void neighbours(T x, T &a, T &b)
+{
+    if constexpr (sizeof(T) == 4) {
+        uint32_t p, q;
+        neighbours<D>(__builtin_bit_cast(uint32_t, x), p, q);
+        a = __builtin_bit_cast(T, p);
+        b = __builtin_bit_cast(T, q);
+    } else {
+        const uint64_t bits = __builtin_bit_cast(uint64_t, x);
+        uint32_t p, q, r, s;
+        neighbours<D>((uint32_t)bits, p, q);
+        neighbours<D>((uint32_t)(bits >> 32), r, s);
+        a = __builtin_bit_cast(T, (uint64_t)r << 32 | p);
+        b = __builtin_bit_cast(T, (uint64_t)s << 32 | q);
+    }
+}
+
+// op, which does not mind the order of its two, over the lanes of a wavefront, or of each group of LANES of them, for every lane.
+template <int LANES = kLanes, int D = 1, typename T, typename Op>
+__device__ __forceinline__ T wave_reduce(T x, Op op)
+{
+    if constexpr (D >= LANES) {
+        return x;
+    } else {
+        T a, b;
+        neighbours<D>(x, a, b);
+        return wave_reduce<LANES, 2 * D>(op(a, b), op);
+    }
+}
+template <int LANES = kLanes, typename T>
+__device__ __forceinline__ T wave_sum(T x) { return wave_reduce<LANES>(x, [](T a, T b) { return a + b; }); }
+template <int LANES = kLanes, typename T>
+__device__ __forceinline__ T wave_max(T x) { return wave_reduce<LANES>(x, [](T a, T b) { return a > b ? a : b; }); }
+template <int LANES = kLanes>
+__device__ __forceinline__ float wave_max(float x) { return wave_reduce<LANES>(x, [](float a, float b) { return fmaxf(a, b); }); }
 
 // Sum over a workgroup of `waves` wavefronts, for every thread of it, in an order that is always the same.
 template <typename T>
