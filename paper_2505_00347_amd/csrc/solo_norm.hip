@@ -15,6 +15,12 @@ constexpr int kNormThreads = 256;
 constexpr uint64_t kNormUnit = 16384;                      // elements of a unit of a small table
 constexpr uint64_t kNormUnits = 1 << 16;                   // a larger table has units of so many more elements that about this many are left
 constexpr int kFinishThreads = 1024;
+// Gradients of up to so many bytes are partly in the last-level cache (256 MiB) when the norm is known: the norm loads them
+// through the caches, and clipping, which is the last to look at them, loads and writes past them.  Of more nothing is left by
+// then: the norm loads past the caches.  Clipping 1.2e8 elements: bf16, 249 MB, 148 us with plain accesses throughout, 122 us;
+// fp32, 498 MB, 296 and 276 us.  Norm of 4e9 bf16 elements: 1.33 ms, past the caches 1.24 ms (6.45 TB/s).  The two sides
+// cross between 360 and 500 MB.
+constexpr uint64_t kLargeBytes = 384ull << 20;
 
 struct NormEntry {
     const void *grad;
@@ -23,7 +29,7 @@ struct NormEntry {
     uint64_t unit0;         // first unit of the tensor
     uint64_t unit_elems;    // elements of a unit, the same for all tensors of the table
     uint32_t bf16;
-    uint32_t reserved;
+    uint32_t large;         // the table's tensors are more than the last-level cache keeps, see kLargeBytes
 };
 static_assert(sizeof(NormEntry) == 48, "table layout");
 
@@ -40,18 +46,18 @@ struct NormArgs {
 // Sum of the squares of elements [begin, end) over the workgroup's threads (each thread's part of it).
 // Squares and sums are binary64: the square of a finite binary32 value never overflows or vanishes there, and the kernel
 // waits for memory, not for the additions.
-template <bool BF16>
-__device__ __forceinline__ double square_sum(const void *grad, uint64_t begin, uint64_t end)
+template <bool BF16, bool PAST>
+__device__ __forceinline__ double square_sum(const void *grad, uint64_t begin, uint64_t end, uint32_t thread)
 {
     using E = Elements<BF16>;
     constexpr int kAhead = BF16 ? 8 : 4;
     constexpr uint64_t kStep = kNormThreads * 8;
     double sum[4] = {0.0, 0.0, 0.0, 0.0};
-    uint64_t i = begin + threadIdx.x * 8;
+    uint64_t i = begin + thread * 8;
     for (; i + (kAhead - 1) * kStep + 8 <= end; i += kAhead * kStep) {
         typename E::Raw raw[kAhead];
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) raw[a] = E::load8(grad, i + a * kStep);
+        for (int a = 0; a < kAhead; ++a) raw[a] = PAST ? E::load8_past(grad, i + a * kStep) : E::load8(grad, i + a * kStep);
 #pragma unroll
         for (int a = 0; a < kAhead; ++a) {
             float x[8];
@@ -73,45 +79,102 @@ __device__ __forceinline__ double square_sum(const void *grad, uint64_t begin, u
     return (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 
+__device__ __forceinline__ double unit_square_sum(const NormEntry &e, uint32_t unit, uint32_t thread)
+{
+    const uint64_t begin = (unit - e.unit0) * e.unit_elems, end = min(begin + e.unit_elems, e.n);
+    if (e.large) return e.bf16 ? square_sum<true, true>(e.grad, begin, end, thread) : square_sum<false, true>(e.grad, begin, end, thread);
+    return e.bf16 ? square_sum<true, false>(e.grad, begin, end, thread) : square_sum<false, false>(e.grad, begin, end, thread);
+}
+
 __global__ __launch_bounds__(kNormThreads) void norm_units_kernel(const NormArgs a)
 {
     __shared__ double lds[kNormThreads / kLanes];
     const uint32_t unit = blockIdx.x;
-    const NormEntry e = a.entries[a.map[unit]];
-    const uint64_t begin = (unit - e.unit0) * e.unit_elems;
-    const uint64_t end = min(begin + e.unit_elems, e.n);
-    double sum = e.bf16 ? square_sum<true>(e.grad, begin, end) : square_sum<false>(e.grad, begin, end);
+    double sum = unit_square_sum(a.entries[a.map[unit]], unit, threadIdx.x);
     sum = group_sum(sum, lds, kNormThreads / kLanes);
     if (threadIdx.x == 0) a.partial[unit] = sum;
 }
 
+__device__ __forceinline__ double unscale_of(const NormArgs &a) { return a.unscale ? (double)*a.unscale : 1.0; }
+
+__device__ __forceinline__ void put_norm(const NormArgs &a, double total, double u)
+{
+    const float norm = (float)(sqrt(total) * fabs(u));
+    *a.norm = norm;
+    *a.scale = !isfinite(norm) ? 0.0f : (float)(norm > a.max_norm ? u * ((double)a.max_norm / (double)norm) : u);
+}
+
+// Sum of values[0 .. n), over every `step`-th from `first` on, with eight loads under way.
+__device__ __forceinline__ double strided_sum(const double *values, uint64_t n, uint64_t first, uint64_t step)
+{
+    double sum[8] = {};
+    for (uint64_t i = first; i < n; i += 8 * step) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const double x = values[min(i + k * step, n - 1)];
+            sum[k] += i + k * step < n ? x : 0.0;
+        }
+    }
+    return ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
+}
+
+// The first workgroup adds all units, the others those of a tensor per wavefront.
 __global__ __launch_bounds__(kFinishThreads) void norm_finish_kernel(const NormArgs a)
 {
     __shared__ double lds[kFinishThreads / kLanes];
-    const double u = a.unscale ? (double)*a.unscale : 1.0;
-    double total = 0.0;
-    for (uint32_t i = threadIdx.x; i < a.units; i += kFinishThreads) total += a.partial[i];
-    total = group_sum(total, lds, kFinishThreads / kLanes);
+    const double u = unscale_of(a);
+    if (blockIdx.x == 0) {
+        const double total = group_sum(strided_sum(a.partial, a.units, threadIdx.x, kFinishThreads), lds, kFinishThreads / kLanes);
+        if (threadIdx.x == 0) put_norm(a, total, u);
+        return;
+    }
+    const uint32_t waves = (gridDim.x - 1) * (kFinishThreads / kLanes);
+    for (uint32_t k = (blockIdx.x - 1) * (kFinishThreads / kLanes) + threadIdx.x / kLanes; k < a.count; k += waves) {
+        const NormEntry &e = a.entries[k];
+        const double sum = wave_sum(strided_sum(a.partial + e.unit0, (e.n + e.unit_elems - 1) / e.unit_elems, threadIdx.x % kLanes, kLanes));
+        if (threadIdx.x % kLanes == 0) a.tensor_norm[k] = (float)(sqrt(sum) * fabs(u));
+    }
+}
+
+// All of it by one workgroup, a quarter of it for a unit: tables of up to four units.  A vector of 4096 elements takes 4.9 us a call
+// instead of 6.9 with two launches; five units and more are read faster by as many compute units.
+constexpr uint32_t kSmallUnits = kFinishThreads / kNormThreads;
+
+__global__ __launch_bounds__(kFinishThreads) void norm_small_kernel(const NormArgs a)
+{
+    __shared__ double lds[kFinishThreads / kLanes];
+    __shared__ double partial[kSmallUnits];
+    const uint32_t unit = threadIdx.x / kNormThreads, thread = threadIdx.x % kNormThreads;
+    const double u = unscale_of(a);
+    double sum = 0.0;
+    if (unit < a.units) sum = unit_square_sum(a.entries[a.map[unit]], unit, thread);
+    sum = wave_sum(sum);
+    if (threadIdx.x % kLanes == 0) lds[threadIdx.x / kLanes] = sum;
+    __syncthreads();
+    constexpr uint32_t kWaves = kNormThreads / kLanes;
+    if (threadIdx.x < kSmallUnits) {
+        double s = lds[threadIdx.x * kWaves];
+        for (uint32_t w = 1; w < kWaves; ++w) s += lds[threadIdx.x * kWaves + w];
+        partial[threadIdx.x] = s;
+    }
+    __syncthreads();
     if (threadIdx.x == 0) {
-        const float norm = (float)(sqrt(total) * fabs(u));
-        *a.norm = norm;
-        float c = 0.0f;
-        if (isfinite(norm)) c = (float)(norm > a.max_norm ? u * ((double)a.max_norm / (double)norm) : u);
-        *a.scale = c;
+        double total = 0.0;
+        for (uint32_t k = 0; k < a.units; ++k) total += partial[k];
+        put_norm(a, total, u);
     }
     if (!a.tensor_norm) return;
-    const int wave = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
-    for (uint32_t k = wave; k < a.count; k += kFinishThreads / kLanes) {
-        const uint64_t first = a.entries[k].unit0, units = (a.entries[k].n + a.entries[k].unit_elems - 1) / a.entries[k].unit_elems;
-        double sum = 0.0;
-        for (uint64_t i = lane; i < units; i += kLanes) sum += a.partial[first + i];
-        sum = wave_sum(sum);
-        if (lane == 0) a.tensor_norm[k] = (float)(sqrt(sum) * fabs(u));
+    for (uint32_t k = threadIdx.x; k < a.count; k += kFinishThreads) {
+        const NormEntry &e = a.entries[k];
+        const uint32_t units = (uint32_t)((e.n + e.unit_elems - 1) / e.unit_elems);
+        double s = 0.0;
+        for (uint32_t i = 0; i < units; ++i) s += partial[e.unit0 + i];
+        a.tensor_norm[k] = (float)(sqrt(s) * fabs(u));
     }
 }
 
 // A factor of 0 (a norm that is not finite, max_norm = 0) writes zeros, also over gradients that are not finite.
-template <bool BF16>
+template <bool BF16, bool PAST>
 __device__ __forceinline__ void scale_unit(const void *grad, void *out, uint64_t begin, uint64_t end, float c)
 {
     using E = Elements<BF16>;
@@ -122,14 +185,15 @@ __device__ __forceinline__ void scale_unit(const void *grad, void *out, uint64_t
     for (; i + (kAhead - 1) * kStep + 8 <= end; i += kAhead * kStep) {
         typename E::Raw raw[kAhead];
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) raw[a] = E::load8(grad, i + a * kStep);
+        for (int a = 0; a < kAhead; ++a) raw[a] = PAST ? E::load8_past(grad, i + a * kStep) : E::load8(grad, i + a * kStep);
 #pragma unroll
         for (int a = 0; a < kAhead; ++a) {
             float x[8];
             E::unpack(raw[a], x);
 #pragma unroll
             for (int k = 0; k < 8; ++k) x[k] = zero ? 0.0f : x[k] * c;
-            E::store8(out, i + a * kStep, x);
+            if (PAST) E::store8_past(out, i + a * kStep, x);
+            else E::store8(out, i + a * kStep, x);
         }
     }
     for (; i + 8 <= end; i += kStep) {
@@ -150,8 +214,13 @@ __global__ __launch_bounds__(kNormThreads) void clip_units_kernel(const NormArgs
     if (!e.clipped || (c == 1.0f && e.clipped == e.grad)) return;            // nothing to write
     const uint64_t begin = (unit - e.unit0) * e.unit_elems;
     const uint64_t end = min(begin + e.unit_elems, e.n);
-    if (e.bf16) scale_unit<true>(e.grad, e.clipped, begin, end, c);
-    else scale_unit<false>(e.grad, e.clipped, begin, end, c);
+    if (e.large) {
+        if (e.bf16) scale_unit<true, false>(e.grad, e.clipped, begin, end, c);
+        else scale_unit<false, false>(e.grad, e.clipped, begin, end, c);
+    } else {
+        if (e.bf16) scale_unit<true, true>(e.grad, e.clipped, begin, end, c);
+        else scale_unit<false, true>(e.grad, e.clipped, begin, end, c);
+    }
 }
 
 static uint64_t unit_elems(const solo_grad *grads, uint32_t count)
@@ -191,8 +260,13 @@ static int norm_args(NormArgs &a, const void *table, uint32_t count, uint64_t un
 
 static int norm(const NormArgs &a, hipStream_t stream)
 {
-    if (a.units) hipLaunchKernelGGL(norm_units_kernel, dim3(a.units), dim3(kNormThreads), 0, stream, a);
-    hipLaunchKernelGGL(norm_finish_kernel, dim3(1), dim3(kFinishThreads), 0, stream, a);
+    if (a.units <= kSmallUnits) {
+        hipLaunchKernelGGL(norm_small_kernel, dim3(1), dim3(kFinishThreads), 0, stream, a);
+        return launched();
+    }
+    hipLaunchKernelGGL(norm_units_kernel, dim3(a.units), dim3(kNormThreads), 0, stream, a);
+    const uint32_t tensors = a.tensor_norm ? (a.count + kFinishThreads / kLanes - 1) / (kFinishThreads / kLanes) : 0;
+    hipLaunchKernelGGL(norm_finish_kernel, dim3(1 + (tensors < 256 ? tensors : 256)), dim3(kFinishThreads), 0, stream, a);
     return launched();
 }
 
@@ -225,13 +299,14 @@ int solo_norm_table_build(const solo_grad *grads, uint32_t count, void *table_ho
     if (table_bytes < solo_norm_table_bytes(count, units)) return SOLO_E_INVALID;
     solo::NormEntry *entries = static_cast<solo::NormEntry *>(table_host);
     uint32_t *map = reinterpret_cast<uint32_t *>(entries + count);
-    uint64_t unit0 = 0;
+    uint64_t unit0 = 0, bytes = 0;
+    for (uint32_t k = 0; k < count; ++k) bytes += grads[k].n * solo::element_bytes(grads[k].dtype);
     for (uint32_t k = 0; k < count; ++k) {
         const solo_grad &g = grads[k];
         if (!solo::dtype_ok(g.dtype) || g.reserved != 0) return SOLO_E_INVALID;
         const uintptr_t size = solo::element_bytes(g.dtype);
         if (g.n != 0 && (!solo::at_multiple(g.grad, size) || (g.clipped && !solo::at_multiple(g.clipped, size)))) return SOLO_E_INVALID;
-        entries[k] = solo::NormEntry{g.grad, g.clipped, g.n, unit0, unit, g.dtype == SOLO_BF16 ? 1u : 0u, 0u};
+        entries[k] = solo::NormEntry{g.grad, g.clipped, g.n, unit0, unit, g.dtype == SOLO_BF16 ? 1u : 0u, bytes > solo::kLargeBytes ? 1u : 0u};
         for (uint64_t u = 0; u < solo::units_of(g.n, unit); ++u) map[unit0++] = k;
     }
     return SOLO_OK;

@@ -81,6 +81,27 @@ struct Elements {
         *reinterpret_cast<Quad *>(at) = a;
         if (!BF16) *reinterpret_cast<Quad *>(at + 16) = b;
     }
+    // Past the caches: what is written once and not read soon.
+    __device__ __forceinline__ static void store8_past(void *base, uint64_t i, const float x[8])
+    {
+        char *at = static_cast<char *>(base) + i * kBytes;
+        Quad a, b;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            a[k] = BF16 ? to_bf16(x[2 * k], x[2 * k + 1]) : __float_as_uint(x[k]);
+            b[k] = __float_as_uint(x[4 + k]);
+        }
+        __builtin_nontemporal_store(a, reinterpret_cast<Quad *>(at));
+        if (!BF16) __builtin_nontemporal_store(b, reinterpret_cast<Quad *>(at + 16));
+    }
+    __device__ __forceinline__ static Raw load8_past(const void *base, uint64_t i)
+    {
+        Raw r;
+        const char *at = static_cast<const char *>(base) + i * kBytes;
+#pragma unroll
+        for (int k = 0; k < (BF16 ? 1 : 2); ++k) r.q[k] = __builtin_nontemporal_load(reinterpret_cast<const Quad *>(at + 16 * k));
+        return r;
+    }
     __device__ __forceinline__ static void store8_near(void *base, uint32_t i, const float x[8]) { store8(static_cast<char *>(base) + i * kBytes, 0, x); }
     // From here on the compiler does not know what `r` holds.
     __device__ __forceinline__ static void forget(Raw &r)
