@@ -16,6 +16,7 @@
 namespace solo {
 
 constexpr int kSortWaves = 16;
+constexpr int kSortDepth = 8;                             // tokens of a lane that are under way, and in registers, together
 constexpr uint32_t kBuckets = 512;                         // buckets of a table, about (a bucket has 16 rows at least, 512 at most)
 constexpr uint32_t kMinBucketBits = 4, kMaxBucketBits = 9;
 constexpr int kEmbedThreads = 256;
@@ -35,7 +36,9 @@ struct EmbedArgs {
     uint32_t bucket_bits, piece, team_bits, tiles;
     uint32_t pieces;        // pieces of n sorted tokens
     uint32_t add;           // the gradient is added to what is there
-    uint32_t zero_groups;   // workgroups that write the rows without a token
+    uint32_t zero_groups;   // workgroups that write the rows without a token,
+    uint32_t zero_rows;     // so many a wavefront, 64 at most
+    uint32_t zero_team_bits;
 };
 
 template <bool WIDE>
@@ -101,13 +104,19 @@ __global__ __launch_bounds__(kSortWaves * kLanes) void embed_sort_kernel(const E
     uint32_t *const mine = count + wave * rows;
     for (uint32_t r = threadIdx.x; r < kSortWaves * rows; r += kSortWaves * kLanes) count[r] = 0;
     __syncthreads();
-    uint32_t below = 0;
-    for (uint64_t i = begin + lane; i < end; i += 4 * kLanes) {
-        uint32_t t[4];
+    uint32_t t[kSortDepth], below = 0;
+    auto load = [&](uint64_t i0) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) t[k] = i + k * kLanes < end ? token_at<WIDE>(a.tokens, i + k * kLanes, a.vocab) : 0xFFFFFFFFu;
+        for (int k = 0; k < kSortDepth; ++k) {
+            const uint64_t i = i0 + k * kLanes + lane;
+            t[k] = token_at<WIDE>(a.tokens, min(i, (uint64_t)a.n - 1), a.vocab);
+            if (i >= end) t[k] = 0xFFFFFFFFu;
+        }
+    };
+    for (uint64_t i0 = begin; i0 < end; i0 += kSortDepth * kLanes) {
+        load(i0);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < kSortDepth; ++k) {
             below += t[k] < first;
             if (t[k] != 0xFFFFFFFFu && t[k] - first < rows) atomicAdd(&mine[t[k] - first], 1u);
         }
@@ -143,13 +152,10 @@ __global__ __launch_bounds__(kSortWaves * kLanes) void embed_sort_kernel(const E
         }
     }
     __syncthreads();
-    for (uint64_t i0 = begin; i0 < end; i0 += 4 * kLanes) {
-        uint32_t t[4];
-        const uint64_t i = i0 + lane;
+    for (uint64_t i0 = begin; i0 < end; i0 += kSortDepth * kLanes) {
+        if (share > kSortDepth * kLanes) load(i0);         // (else the registers still hold them)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) t[k] = i + k * kLanes < end ? token_at<WIDE>(a.tokens, i + k * kLanes, a.vocab) : 0xFFFFFFFFu;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < kSortDepth; ++k) {
             const uint32_t row = t[k] - first;
             const bool in = t[k] != 0xFFFFFFFFu && row < rows;
             if (!__any(in)) continue;
@@ -157,7 +163,7 @@ __global__ __launch_bounds__(kSortWaves * kLanes) void embed_sort_kernel(const E
             const uint32_t before = __popcll(same & ((1ull << lane) - 1));
             if (in) {
                 const uint32_t at = mine[row] + before;
-                a.order[at] = (uint32_t)(i + k * kLanes);
+                a.order[at] = (uint32_t)(i0 + k * kLanes + lane);
                 a.sorted[at] = t[k];
             }
             __builtin_amdgcn_wave_barrier();
@@ -172,10 +178,10 @@ __global__ __launch_bounds__(kSortWaves * kLanes) void embed_sort_kernel(const E
 // that begin inside the piece, to their ends where they have no more than `piece` tokens.  A longer row ("hot") is added
 // piece by piece: the part in the piece where it begins goes to that piece's second row of `partial`, the part in every
 // later piece to that one's first, and embed_join_kernel adds these.
-template <bool IN16, bool OUT16>
+template <bool OUT16>
 __device__ __forceinline__ void put_row(const EmbedArgs &a, uint32_t row, uint32_t c, const float sum[8])
 {
-    char *to = static_cast<char *>(a.out) + row * a.out_stride * Elements<OUT16>::kBytes;
+    char *to = static_cast<char *>(a.out) + (uint64_t)row * a.out_stride * Elements<OUT16>::kBytes;
     float x[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) x[k] = sum[k] * a.scale;
@@ -192,6 +198,20 @@ __device__ __forceinline__ void put_row(const EmbedArgs &a, uint32_t row, uint32
 #pragma unroll
     for (int k = 0; k < 8; ++k)
         if (c + k < a.dim) Elements<OUT16>::store1(to, c + k, x[k] + (a.add ? Elements<OUT16>::load1(to, c + k) : 0.0f));
+}
+
+// Columns c .. c + 7 of a row, of the sums of columns from .. from + 7 (from < c only in the shorter last group).
+template <bool OUT16>
+__device__ __forceinline__ void put_columns(const EmbedArgs &a, uint32_t row, uint32_t c, uint32_t from, const float sum[8])
+{
+    if (from == c) {
+        put_row<OUT16>(a, row, c, sum);
+        return;
+    }
+    char *to = static_cast<char *>(a.out) + row * a.out_stride * Elements<OUT16>::kBytes;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (from + k >= c) Elements<OUT16>::store1(to, from + k, sum[k] * a.scale + (a.add ? Elements<OUT16>::load1(to, from + k) : 0.0f));
 }
 
 __device__ __forceinline__ void put_partial(const EmbedArgs &a, uint64_t slot, uint32_t c, const float sum[8])
@@ -253,7 +273,7 @@ __device__ __forceinline__ void sum_piece(const EmbedArgs &a, uint32_t piece, ui
             if (s + k >= hi) break;
             if (next[k] != row) {
                 if (head) put_partial(a, 2ull * piece, c, sum);
-                else put_row<IN16, OUT16>(a, row, c, sum);
+                else put_row<OUT16>(a, row, c, sum);
                 head = false;
                 row = next[k];
 #pragma unroll
@@ -267,66 +287,239 @@ __device__ __forceinline__ void sum_piece(const EmbedArgs &a, uint32_t piece, ui
     }
     if (head) put_partial(a, 2ull * piece, c, sum);
     else if (tail) put_partial(a, 2ull * piece + 1, c, sum);
-    else put_row<IN16, OUT16>(a, row, c, sum);
+    else put_row<OUT16>(a, row, c, sum);
 }
 
-template <bool OUT16>
-__device__ __forceinline__ void zero_rows(const EmbedArgs &a, uint32_t group)
-{
-    const float none[8] = {};
-    for (uint32_t row = group; row < a.vocab; row += a.zero_groups) {
-        if (a.n != 0 && a.start[row] != a.start[row + 1]) continue;
-        char *to = static_cast<char *>(a.out) + row * a.out_stride * Elements<OUT16>::kBytes;
-        uint32_t c = threadIdx.x * 8;
-        for (; c + 8 <= a.dim; c += kEmbedThreads * 8) Elements<OUT16>::store8(to, c, none);
-        for (; c < a.dim; ++c) Elements<OUT16>::store1(to, c, 0.0f);
-    }
-}
-
+// The same by a whole wavefront, for rows of more than 256 columns: the places of the list are a lane each, so that rows and
+// positions are scalars, and a batch of rows is under way while the one before is added and written.  (A wait for loads also waits
+// for the stores in front of them: stores of a batch come behind the loads of the next.)
 template <bool IN16, bool OUT16>
+__device__ __forceinline__ void sum_piece_wave(const EmbedArgs &a, uint32_t piece, uint32_t c)
+{
+    constexpr int kBatch = IN16 ? 8 : 4;
+    const uint32_t begin = piece * a.piece, lane = threadIdx.x % kLanes, total = a.start[a.vocab];
+    const uint32_t at = min(begin + lane, a.n - 1);
+    const uint32_t token = a.sorted[at], position = a.order[at];               // (behind `total`: not set, and not used)
+    const uint32_t edge = min(begin + a.piece, total);
+    if (begin >= edge) return;
+    const uint32_t first = __builtin_amdgcn_readfirstlane(token), last = __builtin_amdgcn_readlane(token, edge - 1 - begin);
+    const uint32_t first_start = a.start[first], first_end = a.start[first + 1], last_start = a.start[last], last_end = a.start[last + 1];
+    const bool head = first_start < begin && first_end - first_start > a.piece;
+    const bool tail = last_end > edge && last_end - last_start > a.piece && last_start >= begin;
+    const uint32_t lo = first_start < begin && !head ? first_end : begin;
+    const uint32_t hi = last_end > edge && last_end - last_start <= a.piece && last_start >= begin ? last_end : edge;
+    if (lo >= hi) return;
+    // a lane whose group is the shorter last one takes the last eight columns of the row; one behind it writes nothing
+    const uint32_t from = min(c, a.dim - 8);
+    const bool writes = c < a.dim;
+    const char *const in = static_cast<const char *>(a.in) + (uint64_t)from * Elements<IN16>::kBytes;
+    const uint32_t k0 = lo - begin, k1 = hi - begin;        // at most 64 places: `piece`, and one less of the last row
+    float sum[8] = {};
+    uint32_t row = __builtin_amdgcn_readlane(token, k0);
+    bool in_head = head;
+    typename Elements<IN16>::Raw raw[2][kBatch];
+    auto load = [&](typename Elements<IN16>::Raw *r, uint32_t k) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const uint64_t at_row = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(position, min(k + j, k1 - 1)) * a.in_stride;
+            r[j] = Elements<IN16>::load8(in + at_row * Elements<IN16>::kBytes, 0);
+        }
+    };
+    auto put = [&](uint32_t row, bool head, bool tail) {
+        if (!writes) return;
+        if (head || tail) put_partial(a, 2ull * piece + (head ? 0 : 1), c, sum);
+        else put_columns<OUT16>(a, row, c, from, sum);
+    };
+    auto add = [&](const typename Elements<IN16>::Raw *r, uint32_t k) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            if (k + j >= k1) break;
+            const uint32_t next = __builtin_amdgcn_readlane(token, k + j);
+            if (next != row) {
+                put(row, in_head, false);
+                in_head = false;
+                row = next;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+            }
+            float x[8];
+            Elements<IN16>::unpack(r[j], x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += x[e];
+        }
+    };
+    load(raw[0], k0);
+    for (uint32_t k = k0; k < k1; k += 2 * kBatch) {
+        if (k + kBatch < k1) load(raw[1], k + kBatch);
+        add(raw[0], k);
+        if (k + kBatch >= k1) break;
+        if (k + 2 * kBatch < k1) load(raw[0], k + 2 * kBatch);
+        add(raw[1], k + kBatch);
+    }
+    put(row, in_head, tail);
+}
+
+// Rows without a token, past the caches: a wavefront looks at up to 64 rows, a lane each, and its teams write those that are empty,
+// 16 bytes a lane.  (154 MB of zeros in rows of 3 KB: 53 us through the caches, 35 us past them.)
+__device__ __forceinline__ void zero_row(char *to, uint32_t bytes, uint32_t lane, uint32_t lanes)
+{
+    const Quad none = {};
+    uint32_t i = lane * 16;
+    for (; i + 16 <= bytes; i += lanes * 16) __builtin_nontemporal_store(none, reinterpret_cast<Quad *>(to + i));
+    for (; i < bytes; i += 2) *reinterpret_cast<uint16_t *>(to + i) = 0;       // (one lane's: what is left is less than 16 bytes)
+}
+
+// `empty`: bit r is set where row first + r has no token.
+template <bool OUT16>
+__device__ __forceinline__ void zero_rows(const EmbedArgs &a, uint32_t first, uint64_t empty)
+{
+    const uint32_t lanes = 1u << a.zero_team_bits, lane = threadIdx.x & (lanes - 1), team = threadIdx.x % kLanes >> a.zero_team_bits;
+    for (uint32_t r = team; r < a.zero_rows; r += kLanes >> a.zero_team_bits)
+        if (empty >> r & 1)
+            zero_row(static_cast<char *>(a.out) + (uint64_t)(first + r) * a.out_stride * Elements<OUT16>::kBytes, a.dim * Elements<OUT16>::kBytes, lane, lanes);
+}
+
+template <bool IN16, bool OUT16, bool WAVE>
 __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedArgs a)
 {
-    const uint64_t teams = (uint64_t)(gridDim.x - a.zero_groups) * kEmbedThreads >> a.team_bits;
+    const uint32_t lane = threadIdx.x % kLanes;
     if (blockIdx.x >= gridDim.x - a.zero_groups) {
-        zero_rows<OUT16>(a, blockIdx.x - (gridDim.x - a.zero_groups));
+        const uint64_t wave = ((uint64_t)(blockIdx.x - (gridDim.x - a.zero_groups)) * kEmbedThreads + threadIdx.x) / kLanes;
+        const uint64_t first = wave * a.zero_rows, mine = first + lane;
+        const bool empty = lane < a.zero_rows && mine < a.vocab && (a.n == 0 || a.start[mine] == a.start[mine + 1]);
+        zero_rows<OUT16>(a, (uint32_t)first, __ballot(empty));
         return;
     }
-    const uint32_t lane = threadIdx.x & ((1u << a.team_bits) - 1), total = a.start[a.vocab];
-    for (uint64_t item = ((uint64_t)blockIdx.x * kEmbedThreads + threadIdx.x) >> a.team_bits; item < (uint64_t)a.pieces * a.tiles; item += teams) {
-        const uint32_t piece = (uint32_t)(item / a.tiles), c = ((uint32_t)(item % a.tiles) << a.team_bits | lane) * 8;
-        if (c < a.dim) sum_piece<IN16, OUT16>(a, piece, c, total);
+    const uint64_t items = (uint64_t)a.pieces * a.tiles, teams = (uint64_t)(gridDim.x - a.zero_groups) * kEmbedThreads >> a.team_bits;
+    const uint64_t team = ((uint64_t)blockIdx.x * kEmbedThreads + threadIdx.x) >> a.team_bits;
+    if (WAVE) {
+        for (uint64_t item = __builtin_amdgcn_readfirstlane((uint32_t)team); item < items; item += teams) {
+            const uint32_t piece = (uint32_t)(item / a.tiles), c = ((uint32_t)(item % a.tiles) << 6 | lane) * 8;
+            sum_piece_wave<IN16, OUT16>(a, piece, c);
+        }
+        return;
     }
+    const uint32_t total = a.start[a.vocab], c = (threadIdx.x & ((1u << a.team_bits) - 1)) * 8;        // (one tile)
+    for (uint64_t item = team; item < items; item += teams)
+        if (c < a.dim) sum_piece<IN16, OUT16>(a, (uint32_t)item, c, total);
 }
 
-// The rows with more than `piece` tokens: the piece where such a row begins adds its parts.
-template <bool IN16, bool OUT16>
-__global__ __launch_bounds__(kEmbedThreads) void embed_join_kernel(const EmbedArgs a)
+// ---- few tokens ------------------------------------------------------------------------------
+// One launch without a sort: every workgroup holds all tokens in LDS.  The wavefront of a token's first position adds the rows of
+// all its positions; the zeros go to the rows that no token names.  96 tokens of a table of 50257 x 768: 30 us instead of
+// 43 with the sort.  The line is where one wavefront's run over all tokens, if they are the same, takes as long as the launches saved.
+constexpr uint32_t kFewTokens = 256;
+
+template <bool IN16, bool OUT16, bool WIDE>
+__global__ __launch_bounds__(kEmbedThreads) void embed_few_kernel(const EmbedArgs a)
 {
+    __shared__ uint32_t tokens[kFewTokens];
+    __shared__ uint32_t named[kEmbedThreads / kLanes][2];
+    const uint32_t lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
+    tokens[threadIdx.x] = threadIdx.x < a.n ? token_at<WIDE>(a.tokens, threadIdx.x, a.vocab) : 0xFFFFFFFFu;
+    if (lane < 2) named[wave][lane] = 0;
+    __syncthreads();
+    if (blockIdx.x >= gridDim.x - a.zero_groups) {
+        const uint64_t first = ((uint64_t)(blockIdx.x - (gridDim.x - a.zero_groups)) * (kEmbedThreads / kLanes) + wave) * a.zero_rows;
+#pragma unroll
+        for (uint32_t k = 0; k < kFewTokens; k += kLanes) {
+            const uint32_t r = tokens[k + lane] - (uint32_t)first;             // (no token: larger than any row number)
+            if (tokens[k + lane] >= first && r < a.zero_rows) atomicOr(&named[wave][r / 32], 1u << r % 32);
+        }
+        __builtin_amdgcn_wave_barrier();
+        const uint64_t mask = (uint64_t)*(volatile uint32_t *)&named[wave][1] << 32 | *(volatile uint32_t *)&named[wave][0];
+        zero_rows<OUT16>(a, (uint32_t)first, __ballot(lane < a.zero_rows && first + lane < a.vocab) & ~mask);
+        return;
+    }
+    const uint32_t item = __builtin_amdgcn_readfirstlane(blockIdx.x * (kEmbedThreads / kLanes) + wave), i = item / a.tiles;
+    if (i >= a.n) return;
+    const uint32_t row = __builtin_amdgcn_readfirstlane(tokens[i]), c = (item % a.tiles * kLanes + lane) * 8;
+    if (row == 0xFFFFFFFFu) return;
+    uint64_t same[kFewTokens / kLanes];
+#pragma unroll
+    for (uint32_t k = 0; k < kFewTokens / kLanes; ++k) same[k] = __ballot(tokens[k * kLanes + lane] == row);
+#pragma unroll
+    for (uint32_t k = 0; k < kFewTokens / kLanes; ++k) {                       // an earlier position has it all
+        const uint64_t before = k < i / kLanes ? ~0ull : k == i / kLanes ? (1ull << i % kLanes) - 1 : 0;
+        if (same[k] & before) return;
+    }
+    const bool whole = c + 8 <= a.dim;
+    float sum[8] = {};
+#pragma unroll
+    for (uint32_t k = 0; k < kFewTokens / kLanes; ++k) {
+        uint64_t left = same[k];
+        while (left) {
+            constexpr int kBatch = 4;
+            typename Elements<IN16>::Raw raw[kBatch];
+            float x[kBatch][8];
+            int count = 0;
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                if (left == 0) break;
+                const uint32_t position = k * kLanes + __builtin_ctzll(left);
+                left &= left - 1;
+                if (c < a.dim) row_part<IN16>(a, position, c, raw[j], x[j], whole);
+                count = j + 1;
+            }
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                if (j >= count) break;
+                if (whole) Elements<IN16>::unpack(raw[j], x[j]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += x[j][e];
+            }
+        }
+    }
+    if (c < a.dim) put_row<OUT16>(a, row, c, sum);
+}
+
+// The rows with more than `piece` tokens: the piece where such a row begins adds its parts, each wavefront of the workgroup a
+// run of them.
+constexpr int kJoinWaves = 8;
+template <bool IN16, bool OUT16>
+__global__ __launch_bounds__(kJoinWaves * kLanes) void embed_join_kernel(const EmbedArgs a)
+{
+    __shared__ float lds[kJoinWaves][8][kLanes];
     const uint32_t piece = blockIdx.x, total = a.start[a.vocab];
     const uint64_t edge = (uint64_t)(piece + 1) * a.piece;
     if (edge >= total) return;
     const uint32_t row = a.sorted[edge - 1], from = a.start[row], to = a.start[row + 1];
     if (to <= edge || to - from <= a.piece || from < piece * a.piece) return;
-    const uint32_t last = (to - 1) / a.piece;
+    const uint32_t parts = (to - 1) / a.piece - piece + 1;                     // the first is the second row of its piece
     const uint64_t stride = ((uint64_t)a.dim + 7) / 8 * 8;
-    const uint32_t c = (blockIdx.y * kEmbedThreads + threadIdx.x) * 8;
-    if (c >= a.dim) return;
-    float sum[8];
-    Elements<false>::unpack(Elements<false>::load8(a.partial + (2ull * piece + 1) * stride, c), sum);
-    for (uint32_t p = piece + 1; p <= last; p += kAheadRows) {
-        Elements<false>::Raw raw[kAheadRows];
+    const uint32_t lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
+    const uint32_t run = (parts + kJoinWaves - 1) / kJoinWaves, begin = wave * run, end = min(begin + run, parts);
+    for (uint32_t c0 = blockIdx.y * kLanes * 8; c0 < a.dim; c0 += gridDim.y * kLanes * 8) {
+        const uint32_t c = min(c0 + lane * 8, (uint32_t)stride - 8), from_column = a.team_bits == 6 ? min(c, a.dim - 8) : c;
+        float sum[8] = {};
+        for (uint32_t p = begin; p < end; p += kAheadRows) {
+            Elements<false>::Raw raw[kAheadRows];
 #pragma unroll
-        for (int k = 0; k < kAheadRows; ++k) raw[k] = Elements<false>::load8(a.partial + 2ull * min(p + k, last) * stride, c);
+            for (int k = 0; k < kAheadRows; ++k) {
+                const uint32_t part = min(p + k, end - 1);
+                raw[k] = Elements<false>::load8(a.partial + (2ull * (piece + part) + (part == 0)) * stride, c);
+            }
 #pragma unroll
-        for (int k = 0; k < kAheadRows; ++k) {
-            if (p + k > last) break;
-            float x[8];
-            Elements<false>::unpack(raw[k], x);
+            for (int k = 0; k < kAheadRows; ++k) {
+                if (p + k >= end) break;
+                float x[8];
+                Elements<false>::unpack(raw[k], x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += x[e];
+                for (int e = 0; e < 8; ++e) sum[e] += x[e];
+            }
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) lds[wave][e][lane] = sum[e];
+        __syncthreads();
+        if (wave == 0) {
+            const uint32_t waves = (parts + run - 1) / run;
+            for (uint32_t w = 1; w < waves; ++w)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += lds[w][e][lane];
+            if (c0 + lane * 8 < a.dim) put_columns<OUT16>(a, row, c, from_column, sum);
+        }
+        __syncthreads();
     }
-    put_row<IN16, OUT16>(a, row, c, sum);
 }
 
 // ---- host ------------------------------------------------------------------------------------
@@ -369,13 +562,20 @@ static EmbedPlan embed_plan(const solo_embedding_shape *s)
 }
 
 template <bool IN16, bool OUT16>
+static void few_tokens(const EmbedArgs &a, bool wide, hipStream_t stream)
+{
+    const uint32_t waves = kEmbedThreads / kLanes, grid = (a.n * a.tiles + waves - 1) / waves + a.zero_groups;
+    hipLaunchKernelGGL((wide ? embed_few_kernel<IN16, OUT16, true> : embed_few_kernel<IN16, OUT16, false>), dim3(grid), dim3(kEmbedThreads), 0, stream, a);
+}
+
+template <bool IN16, bool OUT16>
 static void sum_rows(const EmbedArgs &a, const EmbedPlan &p, uint32_t sum_groups, hipStream_t stream)
 {
     const uint32_t grid = sum_groups + a.zero_groups;
-    if (grid) hipLaunchKernelGGL((embed_sum_kernel<IN16, OUT16>), dim3(grid), dim3(kEmbedThreads), 0, stream, a);
+    if (grid) hipLaunchKernelGGL((p.team_bits == 6 ? embed_sum_kernel<IN16, OUT16, true> : embed_sum_kernel<IN16, OUT16, false>), dim3(grid), dim3(kEmbedThreads), 0, stream, a);
+    const uint32_t tiles = (a.dim + kLanes * 8 - 1) / (kLanes * 8);
     if (p.pieces > 1)
-        hipLaunchKernelGGL((embed_join_kernel<IN16, OUT16>), dim3(p.pieces, (a.dim + kEmbedThreads * 8 - 1) / (kEmbedThreads * 8)),
-                           dim3(kEmbedThreads), 0, stream, a);
+        hipLaunchKernelGGL((embed_join_kernel<IN16, OUT16>), dim3(p.pieces, tiles < 16 ? tiles : 16), dim3(kJoinWaves * kLanes), 0, stream, a);
 }
 
 }  // namespace solo
@@ -440,16 +640,29 @@ int solo_embedding_grad(const void *grad_rows, const void *tokens, void *grad_ta
     a.scale = shape->scale;
     a.bucket_bits = p.bucket_bits; a.piece = p.piece; a.pieces = p.pieces; a.team_bits = p.team_bits; a.tiles = p.tiles;
     a.add = add ? 1u : 0u;
-    a.zero_groups = add ? 0 : a.vocab < 4096 ? a.vocab : 4096;
+    if (!add) {
+        const uint32_t row_bytes = a.dim * (uint32_t)element_bytes(shape->table_dtype);
+        a.zero_team_bits = bits_for((row_bytes + 15) / 16);
+        if (a.zero_team_bits > 6) a.zero_team_bits = 6;
+        a.zero_rows = row_bytes >= 4096 ? 1 : 4096 / row_bytes < kLanes ? 4096 / row_bytes : kLanes;
+        const uint32_t waves = (a.vocab + a.zero_rows - 1) / a.zero_rows;
+        a.zero_groups = (waves + kEmbedThreads / kLanes - 1) / (kEmbedThreads / kLanes);
+    }
     hipStream_t s = (hipStream_t)stream;
+    const bool in16 = shape->rows_dtype == SOLO_BF16, out16 = shape->table_dtype == SOLO_BF16, wide = shape->token_bits == 64;
+    if (a.n != 0 && a.n <= kFewTokens) {
+        a.tiles = (a.dim + kLanes * 8 - 1) / (kLanes * 8);
+        if (in16) out16 ? few_tokens<true, true>(a, wide, s) : few_tokens<true, false>(a, wide, s);
+        else out16 ? few_tokens<false, true>(a, wide, s) : few_tokens<false, false>(a, wide, s);
+        return launched();
+    }
     if (a.n != 0) {
         const uint32_t lds = (kSortWaves * (1u << p.bucket_bits) + kSortWaves) * (uint32_t)sizeof(uint32_t);
-        if (shape->token_bits == 64) hipLaunchKernelGGL(embed_sort_kernel<true>, dim3(p.buckets), dim3(kSortWaves * kLanes), lds, s, a);
+        if (wide) hipLaunchKernelGGL(embed_sort_kernel<true>, dim3(p.buckets), dim3(kSortWaves * kLanes), lds, s, a);
         else hipLaunchKernelGGL(embed_sort_kernel<false>, dim3(p.buckets), dim3(kSortWaves * kLanes), lds, s, a);
     }
     uint64_t items = (uint64_t)p.pieces * p.tiles, groups = ((items << p.team_bits) + kEmbedThreads - 1) / kEmbedThreads;
     if (groups > (1u << 22)) groups = 1u << 22;
-    const bool in16 = shape->rows_dtype == SOLO_BF16, out16 = shape->table_dtype == SOLO_BF16;
     if (in16) out16 ? sum_rows<true, true>(a, p, (uint32_t)groups, s) : sum_rows<true, false>(a, p, (uint32_t)groups, s);
     else out16 ? sum_rows<false, true>(a, p, (uint32_t)groups, s) : sum_rows<false, false>(a, p, (uint32_t)groups, s);
     return launched();

@@ -178,7 +178,7 @@ template <bool BF16, bool PAST>
 __device__ __forceinline__ void scale_unit(const void *grad, void *out, uint64_t begin, uint64_t end, float c)
 {
     using E = Elements<BF16>;
-    constexpr int kAhead = 4;
+    constexpr int kAhead = BF16 ? 8 : 4;
     constexpr uint64_t kStep = kNormThreads * 8;
     const bool zero = c == 0.0f;
     uint64_t i = begin + threadIdx.x * 8;
