@@ -6,9 +6,10 @@
 // other, in the order of their positions, and the sorted list is cut into pieces of the same length, whatever the tokens
 // are.  The sums and their order are therefore the same on every call.
 //
-// Sorting takes one launch: a workgroup owns a bucket of consecutive table rows, reads all tokens twice (they lie in the
-// caches) and needs nothing from the others: the first time it counts the tokens of every row of its bucket, by wavefront, and
-// those below the bucket, which is where its part of the sorted list begins; the second time it places them.
+// Sorting takes one launch: a workgroup owns a bucket of table rows, every 256th one or so (the frequent tokens of a vocabulary
+// are neighbours, and half of a text is a few hundred of them), reads all tokens (they lie in the caches) and needs nothing from the
+// others.  It counts the tokens of the buckets before its own, which is where its part of the sorted list begins, and its own by row
+// and wavefront; then it places them.
 #include "solo_ops.h"
 
 #include <math.h>
@@ -16,9 +17,10 @@
 namespace solo {
 
 constexpr int kSortWaves = 16;
+constexpr uint32_t kListed = 256;                          // tokens of its bucket that a wavefront keeps in LDS
 constexpr int kSortDepth = 8;                             // tokens of a lane that are under way, and in registers, together
-constexpr uint32_t kBuckets = 512;                         // buckets of a table, about (a bucket has 16 rows at least, 512 at most)
-constexpr uint32_t kMinBucketBits = 4, kMaxBucketBits = 9;
+constexpr uint32_t kMinBuckets = 256;                      // workgroups that sort: one for each compute unit
+constexpr uint32_t kMaxRowBits = 9;                        // rows of a bucket: 512 at most (counters by wavefront: 32 KB of LDS)
 constexpr int kEmbedThreads = 256;
 constexpr int kAheadRows = 8;                              // rows of dy that a team has under way
 
@@ -28,12 +30,12 @@ struct EmbedArgs {
     void *out;              // looked-up rows, or gradient of the table
     uint32_t *order;        // positions of the tokens inside the table, sorted by token
     uint32_t *sorted;       // their tokens
-    uint32_t *start;        // first place of every row's tokens in both, and their number behind it: [vocab + 1]
+    uint2 *span;            // where the tokens of every row begin and end in both; behind the last row: the number of all
     float *partial;         // two rows of sums per piece, see embed_sum_kernel
     uint64_t in_stride, out_stride;
     uint32_t vocab, dim, n;
     float scale;
-    uint32_t bucket_bits, piece, team_bits, tiles;
+    uint32_t bucket_bits, row_bits, piece, team_bits, tiles;
     uint32_t pieces;        // pieces of n sorted tokens
     uint32_t add;           // the gradient is added to what is there
     uint32_t zero_groups;   // workgroups that write the rows without a token,
@@ -41,14 +43,18 @@ struct EmbedArgs {
     uint32_t zero_team_bits;
 };
 
+// A token as a number of 32 bits; what is negative or does not fit becomes one that no table has (tables have fewer than 2^31 rows).
+template <bool WIDE>
+__device__ __forceinline__ uint32_t token_at(const void *tokens, uint64_t i)
+{
+    if (!WIDE) return static_cast<const uint32_t *>(tokens)[i];
+    const uint2 t = static_cast<const uint2 *>(tokens)[i];
+    return t.y == 0 ? t.x : 0xFFFFFFFFu;
+}
 template <bool WIDE>
 __device__ __forceinline__ uint32_t token_at(const void *tokens, uint64_t i, uint32_t vocab)
 {
-    if (WIDE) {
-        const uint64_t t = static_cast<const uint64_t *>(tokens)[i];
-        return t < vocab ? (uint32_t)t : 0xFFFFFFFFu;
-    }
-    const uint32_t t = static_cast<const uint32_t *>(tokens)[i];
+    const uint32_t t = token_at<WIDE>(tokens, i);
     return t < vocab ? t : 0xFFFFFFFFu;
 }
 
@@ -80,13 +86,18 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_lookup_kernel(const Embed
 }
 
 // ---- sort ------------------------------------------------------------------------------------
-// Lanes of the wavefront whose token lies in the same row of the bucket as this lane's (of those in it).
+// Lanes of the wavefront, of those with `in`, whose token lies in the same row of the bucket as this lane's.
 __device__ __forceinline__ uint64_t same_row(uint32_t row, bool in, uint32_t bits)
 {
     uint64_t same = __ballot(in);
-    for (uint32_t b = 0; b < bits; ++b) {
-        const uint64_t ones = __ballot((row >> b) & 1u);
-        same &= (row >> b) & 1u ? ones : ~ones;
+    if (same != 0 && !__any(in && row != (uint32_t)__builtin_amdgcn_readlane(row, __builtin_ctzll(same)))) return same;        // (one token all over)
+#pragma unroll
+    for (uint32_t b = 0; b < kMaxRowBits; ++b) {
+        if (b < bits) {
+            const uint32_t own = (uint32_t)((int32_t)(row << (31 - b)) >> 31); // all ones where the bit is set
+            const uint64_t ones = __ballot(own != 0);
+            same &= ~(ones ^ ((uint64_t)own << 32 | own));
+        }
     }
     return same;
 }
@@ -94,40 +105,46 @@ __device__ __forceinline__ uint64_t same_row(uint32_t row, bool in, uint32_t bit
 template <bool WIDE>
 __global__ __launch_bounds__(kSortWaves * kLanes) void embed_sort_kernel(const EmbedArgs a)
 {
-    extern __shared__ uint32_t count[];                    // [wavefront][row of the bucket], then one word per wavefront
-    const uint32_t rows = 1u << a.bucket_bits;
-    uint32_t *const below_of = count + kSortWaves * rows;
+    extern __shared__ uint32_t count[];                    // [wavefront][row of the bucket]
+    __shared__ uint32_t below_of[kSortWaves], sums[kSortWaves];
+    __shared__ uint32_t list[kSortWaves][kListed];         // a wavefront's tokens of the bucket: where they are, from its first on
+    __shared__ uint16_t list_row[kSortWaves][kListed];
     const uint32_t wave = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
-    const uint32_t first = blockIdx.x << a.bucket_bits;    // the bucket's first row
+    const uint32_t bucket = blockIdx.x, bits = a.bucket_bits, low = (1u << bits) - 1, rows = 1u << a.row_bits;
     const uint32_t share = (a.n + kSortWaves * kLanes - 1) / (kSortWaves * kLanes) * kLanes;        // tokens of a wavefront
     const uint64_t begin = (uint64_t)wave * share, end = min(begin + share, (uint64_t)a.n);
     uint32_t *const mine = count + wave * rows;
     for (uint32_t r = threadIdx.x; r < kSortWaves * rows; r += kSortWaves * kLanes) count[r] = 0;
     __syncthreads();
-    uint32_t t[kSortDepth], below = 0;
-    auto load = [&](uint64_t i0) {
+    uint32_t below = 0, listed = 0;
+    for (uint64_t i0 = begin; i0 < end; i0 += kSortDepth * kLanes) {
+        uint32_t t[kSortDepth];
+#pragma unroll
+        for (int k = 0; k < kSortDepth; ++k) t[k] = token_at<WIDE>(a.tokens, min(i0 + k * kLanes + lane, end - 1));
 #pragma unroll
         for (int k = 0; k < kSortDepth; ++k) {
             const uint64_t i = i0 + k * kLanes + lane;
-            t[k] = token_at<WIDE>(a.tokens, min(i, (uint64_t)a.n - 1), a.vocab);
-            if (i >= end) t[k] = 0xFFFFFFFFu;
-        }
-    };
-    for (uint64_t i0 = begin; i0 < end; i0 += kSortDepth * kLanes) {
-        load(i0);
-#pragma unroll
-        for (int k = 0; k < kSortDepth; ++k) {
-            below += t[k] < first;
-            if (t[k] != 0xFFFFFFFFu && t[k] - first < rows) atomicAdd(&mine[t[k] - first], 1u);
+            const bool known = t[k] < a.vocab && i < end;
+            below += __popcll(__ballot(known && (t[k] & low) < bucket));
+            const bool in = known && (t[k] & low) == bucket;
+            const uint64_t all = __ballot(in);
+            if (all == 0) continue;
+            if (in) {
+                const uint32_t row = t[k] >> bits, at = listed + __popcll(all & ((1ull << lane) - 1));
+                atomicAdd(&mine[row], 1u);
+                if (at < kListed) {
+                    list[wave][at] = (uint32_t)(i - begin);
+                    list_row[wave][at] = (uint16_t)row;
+                }
+            }
+            listed += __popcll(all);
         }
     }
-    below = wave_sum(below);
     if (lane == 0) below_of[wave] = below;
     __syncthreads();
     below = 0;
     for (int w = 0; w < kSortWaves; ++w) below += below_of[w];
     // where the tokens of row r that wavefront w has found go: behind the rows before it, and the wavefronts before this one
-    __shared__ uint32_t sums[kSortWaves];
     const uint32_t r = threadIdx.x;
     uint32_t total = 0;
     if (r < rows)
@@ -143,8 +160,9 @@ __global__ __launch_bounds__(kSortWaves * kLanes) void embed_sort_kernel(const E
     uint32_t place = below + upto - total;
     for (uint32_t w = 0; w < wave; ++w) place += sums[w];
     if (r < rows) {
-        if (first + r < a.vocab) a.start[first + r] = place;
-        if (first + r + 1 == a.vocab) a.start[a.vocab] = place + total;
+        const uint64_t row = (uint64_t)r << bits | bucket;
+        if (row < a.vocab) a.span[row] = make_uint2(place, place + total);
+        if (r == rows - 1 && bucket == gridDim.x - 1) a.span[a.vocab] = make_uint2(place + total, 0);
         for (int w = 0; w < kSortWaves; ++w) {
             const uint32_t c = count[w * rows + r];
             count[w * rows + r] = place;
@@ -152,25 +170,50 @@ __global__ __launch_bounds__(kSortWaves * kLanes) void embed_sort_kernel(const E
         }
     }
     __syncthreads();
-    for (uint64_t i0 = begin; i0 < end; i0 += kSortDepth * kLanes) {
-        if (share > kSortDepth * kLanes) load(i0);         // (else the registers still hold them)
+    auto put = [&](bool in, uint32_t row, uint32_t position) {
+        const uint64_t same = same_row(row, in, a.row_bits);
+        const uint32_t before = __popcll(same & ((1ull << lane) - 1));
+        if (in) {
+            const uint32_t at = mine[row] + before;
+            a.order[at] = position;
+            a.sorted[at] = row << bits | bucket;
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (in && before == 0) mine[row] += __popcll(same);
+        __builtin_amdgcn_wave_barrier();
+    };
+    auto put_listed = [&](uint32_t k, uint32_t n) {        // entries k .. k + 63 of the first n, of a list that begins again behind its end
+        const bool in = k + lane < n;
+        const uint32_t at = (k + lane) % kListed;
+        put(in, in ? list_row[wave][at] : 0, (uint32_t)begin + (in ? list[wave][at] : 0));
+    };
+    uint32_t done = 0;
+    if (listed > kListed) {                                // more than the list holds: from the beginning, 64 at a time
+        listed = 0;
+        for (uint64_t i0 = begin; i0 < end; i0 += kSortDepth * kLanes) {
+            uint32_t t[kSortDepth];
 #pragma unroll
-        for (int k = 0; k < kSortDepth; ++k) {
-            const uint32_t row = t[k] - first;
-            const bool in = t[k] != 0xFFFFFFFFu && row < rows;
-            if (!__any(in)) continue;
-            const uint64_t same = same_row(row, in, a.bucket_bits);
-            const uint32_t before = __popcll(same & ((1ull << lane) - 1));
-            if (in) {
-                const uint32_t at = mine[row] + before;
-                a.order[at] = (uint32_t)(i0 + k * kLanes + lane);
-                a.sorted[at] = t[k];
+            for (int k = 0; k < kSortDepth; ++k) t[k] = token_at<WIDE>(a.tokens, min(i0 + k * kLanes + lane, end - 1));
+#pragma unroll
+            for (int k = 0; k < kSortDepth; ++k) {
+                const uint64_t i = i0 + k * kLanes + lane;
+                const bool in = t[k] < a.vocab && (t[k] & low) == bucket && i < end;
+                const uint64_t all = __ballot(in);
+                if (in) {
+                    const uint32_t at = (listed + __popcll(all & ((1ull << lane) - 1))) % kListed;
+                    list[wave][at] = (uint32_t)(i - begin);
+                    list_row[wave][at] = (uint16_t)(t[k] >> bits);
+                }
+                listed += __popcll(all);
+                __builtin_amdgcn_wave_barrier();
+                if (listed - done >= kLanes) {
+                    put_listed(done, listed);
+                    done += kLanes;
+                }
             }
-            __builtin_amdgcn_wave_barrier();
-            if (in && before == 0) mine[row] += __popcll(same);
-            __builtin_amdgcn_wave_barrier();
         }
     }
+    for (; done < listed; done += kLanes) put_listed(done, listed);
 }
 
 // ---- sums ------------------------------------------------------------------------------------
@@ -214,22 +257,33 @@ __device__ __forceinline__ void put_columns(const EmbedArgs &a, uint32_t row, ui
         if (from + k >= c) Elements<OUT16>::store1(to, from + k, sum[k] * a.scale + (a.add ? Elements<OUT16>::load1(to, from + k) : 0.0f));
 }
 
-__device__ __forceinline__ void put_partial(const EmbedArgs &a, uint64_t slot, uint32_t c, const float sum[8])
+// Where a piece's part of a hot row lies, columns c on: first or second row of the piece.  The parts of neighbouring pieces are
+// neighbours, for the columns of a team: join reads them one behind the other.
+__device__ __forceinline__ float *partial_at(const EmbedArgs &a, uint32_t piece, bool second, uint32_t c)
 {
-    float *to = a.partial + slot * (((uint64_t)a.dim + 7) / 8 * 8) + c;     // (rows of whole groups of eight)
-    Elements<false>::store8(to, 0, sum);
+    const uint32_t width = 8u << a.team_bits, tile = c / width;
+    return a.partial + (((uint64_t)tile * 2 + second) * a.pieces + piece) * width + c % width;
 }
 
-template <bool IN16>
-__device__ __forceinline__ void row_part(const EmbedArgs &a, uint32_t position, uint32_t c, typename Elements<IN16>::Raw &raw, float tail[8], bool whole)
+__device__ __forceinline__ void put_partial(const EmbedArgs &a, uint32_t piece, bool second, uint32_t c, const float sum[8])
 {
-    const char *from = static_cast<const char *>(a.in) + position * a.in_stride * Elements<IN16>::kBytes;
-    if (whole) {
-        raw = Elements<IN16>::load8(from, c);
-    } else {
+    Elements<false>::store8(partial_at(a, piece, second, c), 0, sum);
+}
+
+// The lane with the shorter last group of a row takes the last eight columns instead, where there are eight.
+__device__ __forceinline__ uint32_t first_column(const EmbedArgs &a, uint32_t c) { return a.dim >= 8 ? min(c, a.dim - 8) : 0; }
+
+template <bool IN16>
+__device__ __forceinline__ typename Elements<IN16>::Raw load_columns(const EmbedArgs &a, uint32_t position, uint32_t from)
+{
+    const char *at = static_cast<const char *>(a.in) + ((uint64_t)position * a.in_stride + from) * Elements<IN16>::kBytes;
+    if (a.dim >= 8) return Elements<IN16>::load8(at, 0);
+    float x[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) tail[k] = c + k < a.dim ? Elements<IN16>::load1(from, c + k) : 0.0f;
-    }
+    for (int k = 0; k < 8; ++k) x[k] = k < (int)a.dim ? Elements<IN16>::load1(at, k) : 0.0f;
+    typename Elements<IN16>::Raw r;
+    Elements<IN16>::store8(&r, 0, x);
+    return r;
 }
 
 template <bool IN16, bool OUT16>
@@ -240,54 +294,50 @@ __device__ __forceinline__ void sum_piece(const EmbedArgs &a, uint32_t piece, ui
     uint32_t lo = begin, hi = edge;
     bool head = false, tail = false;                       // the first row is the rest of a hot one; the last row is the beginning of one
     uint32_t row = a.sorted[begin];
-    if (a.start[row] < begin) {
-        if (a.start[row + 1] - a.start[row] > a.piece) head = true;
-        else lo = a.start[row + 1];
-    }
     const uint32_t last = a.sorted[edge - 1];
-    if (a.start[last + 1] > edge) {
-        if (a.start[last + 1] - a.start[last] > a.piece) tail = a.start[last] >= begin;
-        else if (a.start[last] >= begin) hi = a.start[last + 1];
+    const uint2 first_span = a.span[row], last_span = a.span[last];
+    if (first_span.x < begin) {
+        if (first_span.y - first_span.x > a.piece) head = true;
+        else lo = first_span.y;
+    }
+    if (last_span.y > edge && last_span.x >= begin) {
+        if (last_span.y - last_span.x > a.piece) tail = true;
+        else hi = last_span.y;
     }
     if (lo >= hi) return;
-    row = a.sorted[lo];
-    const bool whole = c + 8 <= a.dim;
+    const uint32_t from = first_column(a, c);
     float sum[8] = {};
+    auto put = [&](bool to_head, bool to_tail) {
+        if (to_head || to_tail) put_partial(a, piece, to_tail, c, sum);
+        else put_columns<OUT16>(a, row, c, from, sum);
+    };
+    row = a.sorted[lo];
     for (uint32_t s = lo; s < hi; s += kAheadRows) {
         typename Elements<IN16>::Raw raw[kAheadRows];
         uint32_t next[kAheadRows];
-        float x[8];
-        if (whole) {
 #pragma unroll
-            for (int k = 0; k < kAheadRows; ++k) {
-                const uint32_t at = min(s + k, hi - 1);
-                next[k] = a.sorted[at];
-                row_part<IN16>(a, a.order[at], c, raw[k], x, true);
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < kAheadRows; ++k) next[k] = a.sorted[min(s + k, hi - 1)];
+        for (int k = 0; k < kAheadRows; ++k) {
+            const uint32_t at = min(s + k, hi - 1);
+            next[k] = a.sorted[at];
+            raw[k] = load_columns<IN16>(a, a.order[at], from);
         }
 #pragma unroll
         for (int k = 0; k < kAheadRows; ++k) {
             if (s + k >= hi) break;
             if (next[k] != row) {
-                if (head) put_partial(a, 2ull * piece, c, sum);
-                else put_row<OUT16>(a, row, c, sum);
+                put(head, false);
                 head = false;
                 row = next[k];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
             }
-            if (whole) Elements<IN16>::unpack(raw[k], x);
-            else row_part<IN16>(a, a.order[s + k], c, raw[k], x, false);
+            float x[8];
+            Elements<IN16>::unpack(raw[k], x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] += x[e];
         }
     }
-    if (head) put_partial(a, 2ull * piece, c, sum);
-    else if (tail) put_partial(a, 2ull * piece + 1, c, sum);
-    else put_row<OUT16>(a, row, c, sum);
+    put(head, tail);
 }
 
 // The same by a whole wavefront, for rows of more than 256 columns: the places of the list are a lane each, so that rows and
@@ -297,21 +347,21 @@ template <bool IN16, bool OUT16>
 __device__ __forceinline__ void sum_piece_wave(const EmbedArgs &a, uint32_t piece, uint32_t c)
 {
     constexpr int kBatch = IN16 ? 8 : 4;
-    const uint32_t begin = piece * a.piece, lane = threadIdx.x % kLanes, total = a.start[a.vocab];
+    const uint32_t begin = piece * a.piece, lane = threadIdx.x % kLanes, total = a.span[a.vocab].x;
     const uint32_t at = min(begin + lane, a.n - 1);
     const uint32_t token = a.sorted[at], position = a.order[at];               // (behind `total`: not set, and not used)
     const uint32_t edge = min(begin + a.piece, total);
     if (begin >= edge) return;
     const uint32_t first = __builtin_amdgcn_readfirstlane(token), last = __builtin_amdgcn_readlane(token, edge - 1 - begin);
-    const uint32_t first_start = a.start[first], first_end = a.start[first + 1], last_start = a.start[last], last_end = a.start[last + 1];
+    const uint2 first_span = a.span[first], last_span = a.span[last];
+    const uint32_t first_start = first_span.x, first_end = first_span.y, last_start = last_span.x, last_end = last_span.y;
     const bool head = first_start < begin && first_end - first_start > a.piece;
     const bool tail = last_end > edge && last_end - last_start > a.piece && last_start >= begin;
     const uint32_t lo = first_start < begin && !head ? first_end : begin;
     const uint32_t hi = last_end > edge && last_end - last_start <= a.piece && last_start >= begin ? last_end : edge;
     if (lo >= hi) return;
-    // a lane whose group is the shorter last one takes the last eight columns of the row; one behind it writes nothing
-    const uint32_t from = min(c, a.dim - 8);
-    const bool writes = c < a.dim;
+    const uint32_t from = first_column(a, c);
+    const bool writes = c < a.dim;                          // (the last team's lanes behind the row take part, and write nothing)
     const char *const in = static_cast<const char *>(a.in) + (uint64_t)from * Elements<IN16>::kBytes;
     const uint32_t k0 = lo - begin, k1 = hi - begin;        // at most 64 places: `piece`, and one less of the last row
     float sum[8] = {};
@@ -327,7 +377,7 @@ __device__ __forceinline__ void sum_piece_wave(const EmbedArgs &a, uint32_t piec
     };
     auto put = [&](uint32_t row, bool head, bool tail) {
         if (!writes) return;
-        if (head || tail) put_partial(a, 2ull * piece + (head ? 0 : 1), c, sum);
+        if (head || tail) put_partial(a, piece, tail && !head, c, sum);
         else put_columns<OUT16>(a, row, c, from, sum);
     };
     auto add = [&](const typename Elements<IN16>::Raw *r, uint32_t k) {
@@ -356,7 +406,7 @@ __device__ __forceinline__ void sum_piece_wave(const EmbedArgs &a, uint32_t piec
         if (k + 2 * kBatch < k1) load(raw[0], k + 2 * kBatch);
         add(raw[1], k + kBatch);
     }
-    put(row, in_head, tail);
+    put(row, in_head, tail && !in_head);
 }
 
 // Rows without a token, past the caches: a wavefront looks at up to 64 rows, a lane each, and its teams write those that are empty,
@@ -386,7 +436,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedArg
     if (blockIdx.x >= gridDim.x - a.zero_groups) {
         const uint64_t wave = ((uint64_t)(blockIdx.x - (gridDim.x - a.zero_groups)) * kEmbedThreads + threadIdx.x) / kLanes;
         const uint64_t first = wave * a.zero_rows, mine = first + lane;
-        const bool empty = lane < a.zero_rows && mine < a.vocab && (a.n == 0 || a.start[mine] == a.start[mine + 1]);
+        const bool empty = lane < a.zero_rows && mine < a.vocab && (a.n == 0 || a.span[mine].x == a.span[mine].y);
         zero_rows<OUT16>(a, (uint32_t)first, __ballot(empty));
         return;
     }
@@ -399,7 +449,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedArg
         }
         return;
     }
-    const uint32_t total = a.start[a.vocab], c = (threadIdx.x & ((1u << a.team_bits) - 1)) * 8;        // (one tile)
+    const uint32_t total = a.span[a.vocab].x, c = (threadIdx.x & ((1u << a.team_bits) - 1)) * 8;        // (one tile)
     for (uint64_t item = team; item < items; item += teams)
         if (c < a.dim) sum_piece<IN16, OUT16>(a, (uint32_t)item, c, total);
 }
@@ -443,7 +493,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_few_kernel(const EmbedArg
         const uint64_t before = k < i / kLanes ? ~0ull : k == i / kLanes ? (1ull << i % kLanes) - 1 : 0;
         if (same[k] & before) return;
     }
-    const bool whole = c + 8 <= a.dim;
+    const uint32_t from = first_column(a, c);
     float sum[8] = {};
 #pragma unroll
     for (uint32_t k = 0; k < kFewTokens / kLanes; ++k) {
@@ -451,74 +501,83 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_few_kernel(const EmbedArg
         while (left) {
             constexpr int kBatch = 4;
             typename Elements<IN16>::Raw raw[kBatch];
-            float x[kBatch][8];
             int count = 0;
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
                 if (left == 0) break;
                 const uint32_t position = k * kLanes + __builtin_ctzll(left);
                 left &= left - 1;
-                if (c < a.dim) row_part<IN16>(a, position, c, raw[j], x[j], whole);
+                raw[j] = load_columns<IN16>(a, position, from);
                 count = j + 1;
             }
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
                 if (j >= count) break;
-                if (whole) Elements<IN16>::unpack(raw[j], x[j]);
+                float x[8];
+                Elements<IN16>::unpack(raw[j], x);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] += x[j][e];
+                for (int e = 0; e < 8; ++e) sum[e] += x[e];
             }
         }
     }
-    if (c < a.dim) put_row<OUT16>(a, row, c, sum);
+    if (c < a.dim) put_columns<OUT16>(a, row, c, from, sum);
 }
 
 // The rows with more than `piece` tokens: the piece where such a row begins adds its parts, each wavefront of the workgroup a
 // run of them.
 constexpr int kJoinWaves = 8;
+constexpr uint32_t kJoinPieces = 4;                        // pieces of a workgroup
 template <bool IN16, bool OUT16>
 __global__ __launch_bounds__(kJoinWaves * kLanes) void embed_join_kernel(const EmbedArgs a)
 {
     __shared__ float lds[kJoinWaves][8][kLanes];
-    const uint32_t piece = blockIdx.x, total = a.start[a.vocab];
-    const uint64_t edge = (uint64_t)(piece + 1) * a.piece;
-    if (edge >= total) return;
-    const uint32_t row = a.sorted[edge - 1], from = a.start[row], to = a.start[row + 1];
-    if (to <= edge || to - from <= a.piece || from < piece * a.piece) return;
-    const uint32_t parts = (to - 1) / a.piece - piece + 1;                     // the first is the second row of its piece
-    const uint64_t stride = ((uint64_t)a.dim + 7) / 8 * 8;
-    const uint32_t lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
-    const uint32_t run = (parts + kJoinWaves - 1) / kJoinWaves, begin = wave * run, end = min(begin + run, parts);
-    for (uint32_t c0 = blockIdx.y * kLanes * 8; c0 < a.dim; c0 += gridDim.y * kLanes * 8) {
-        const uint32_t c = min(c0 + lane * 8, (uint32_t)stride - 8), from_column = a.team_bits == 6 ? min(c, a.dim - 8) : c;
-        float sum[8] = {};
-        for (uint32_t p = begin; p < end; p += kAheadRows) {
-            Elements<false>::Raw raw[kAheadRows];
+    const uint32_t lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes, total = a.span[a.vocab].x;
+    // a lane looks at a piece
+    const uint64_t at = (uint64_t)blockIdx.x * kJoinPieces + lane, at_edge = (at + 1) * a.piece;
+    uint32_t its_row = 0, its_start = 0, its_end = 0;
+    bool begins = lane < kJoinPieces && at_edge < total;
+    if (begins) {
+        its_row = a.sorted[at_edge - 1];
+        const uint2 span = a.span[its_row];
+        its_start = span.x;
+        its_end = span.y;
+        begins = its_end > at_edge && its_end - its_start > a.piece && its_start >= at * a.piece;
+    }
+    for (uint64_t left = __ballot(begins); left != 0; left &= left - 1) {
+        const uint32_t which = __builtin_ctzll(left), piece = blockIdx.x * kJoinPieces + which;
+        const uint32_t row = __builtin_amdgcn_readlane(its_row, which), to = __builtin_amdgcn_readlane(its_end, which);
+        const uint32_t parts = (to - 1) / a.piece - piece + 1;                 // the first is the second row of its piece
+        const uint32_t run = (parts + kJoinWaves - 1) / kJoinWaves, begin = wave * run, end = min(begin + run, parts);
+        for (uint32_t c0 = blockIdx.y * kLanes * 8; c0 < a.dim; c0 += gridDim.y * kLanes * 8) {
+            const uint32_t c = min(c0 + lane * 8, (a.dim - 1) / 8 * 8), from = first_column(a, c);
+            float sum[8] = {};
+            for (uint32_t p = begin; p < end; p += kAheadRows) {
+                Elements<false>::Raw raw[kAheadRows];
 #pragma unroll
-            for (int k = 0; k < kAheadRows; ++k) {
-                const uint32_t part = min(p + k, end - 1);
-                raw[k] = Elements<false>::load8(a.partial + (2ull * (piece + part) + (part == 0)) * stride, c);
+                for (int k = 0; k < kAheadRows; ++k) {
+                    const uint32_t part = min(p + k, end - 1);
+                    raw[k] = Elements<false>::load8(partial_at(a, piece + part, part == 0, c), 0);
+                }
+#pragma unroll
+                for (int k = 0; k < kAheadRows; ++k) {
+                    float x[8];
+                    Elements<false>::unpack(raw[k], x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[e] += p + k < end ? x[e] : 0.0f;       // (no branch: behind one a load would be moved)
+                }
             }
 #pragma unroll
-            for (int k = 0; k < kAheadRows; ++k) {
-                if (p + k >= end) break;
-                float x[8];
-                Elements<false>::unpack(raw[k], x);
+            for (int e = 0; e < 8; ++e) lds[wave][e][lane] = sum[e];
+            __syncthreads();
+            if (wave == 0) {
+                const uint32_t waves = (parts + run - 1) / run;
+                for (uint32_t w = 1; w < waves; ++w)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] += x[e];
+                    for (int e = 0; e < 8; ++e) sum[e] += lds[w][e][lane];
+                if (c0 + lane * 8 < a.dim) put_columns<OUT16>(a, row, c, from, sum);
             }
+            __syncthreads();
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) lds[wave][e][lane] = sum[e];
-        __syncthreads();
-        if (wave == 0) {
-            const uint32_t waves = (parts + run - 1) / run;
-            for (uint32_t w = 1; w < waves; ++w)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] += lds[w][e][lane];
-            if (c0 + lane * 8 < a.dim) put_columns<OUT16>(a, row, c, from_column, sum);
-        }
-        __syncthreads();
     }
 }
 
@@ -537,26 +596,27 @@ static bool shape_fits(const solo_embedding_shape *s)
 
 static uint32_t bits_for(uint64_t n) { uint32_t b = 0; while ((1ull << b) < n) ++b; return b; }
 
-struct EmbedPlan { uint32_t bucket_bits, buckets, piece, pieces, team_bits, tiles; size_t order, sorted, start, partial, bytes; };
+struct EmbedPlan { uint32_t bucket_bits, row_bits, piece, pieces, team_bits, tiles; size_t order, sorted, span, partial, bytes; };
 
 static EmbedPlan embed_plan(const solo_embedding_shape *s)
 {
     EmbedPlan p;
     const uint64_t n = s->tokens, groups = (s->dim + 7) / 8;
-    p.bucket_bits = bits_for((s->vocab + kBuckets - 1) / kBuckets);
-    p.bucket_bits = p.bucket_bits < kMinBucketBits ? kMinBucketBits : p.bucket_bits > kMaxBucketBits ? kMaxBucketBits : p.bucket_bits;
-    p.buckets = (uint32_t)((s->vocab + (1u << p.bucket_bits) - 1) >> p.bucket_bits);
+    const uint64_t rows = s->vocab ? s->vocab : 1;
+    p.bucket_bits = bits_for(kMinBuckets);
+    while (((rows - 1) >> p.bucket_bits) >> kMaxRowBits) ++p.bucket_bits;
+    p.row_bits = bits_for(((rows - 1) >> p.bucket_bits) + 1);
     p.team_bits = bits_for(groups);
     if (p.team_bits > 6) p.team_bits = 6;
     p.tiles = (uint32_t)((groups + (1u << p.team_bits) - 1) >> p.team_bits);
-    p.piece = 32;
+    p.piece = p.team_bits == 6 ? 32 : 8;
     p.pieces = (uint32_t)((n + p.piece - 1) / p.piece);
     size_t at = 0;
     auto take = [&](uint64_t bytes) { const size_t was = at; at += (size_t)((bytes + 255) / 256 * 256); return was; };
     p.order = take(4 * n);
     p.sorted = take(4 * n);
-    p.start = take(4 * (s->vocab + 1));
-    p.partial = take(n > p.piece ? 2ull * p.pieces * groups * 8 * sizeof(float) : 0);
+    p.span = take(8 * (s->vocab + 1));
+    p.partial = take(n > p.piece ? 2ull * p.pieces * p.tiles * (8ull << p.team_bits) * sizeof(float) : 0);
     p.bytes = at;
     return p;
 }
@@ -575,7 +635,7 @@ static void sum_rows(const EmbedArgs &a, const EmbedPlan &p, uint32_t sum_groups
     if (grid) hipLaunchKernelGGL((p.team_bits == 6 ? embed_sum_kernel<IN16, OUT16, true> : embed_sum_kernel<IN16, OUT16, false>), dim3(grid), dim3(kEmbedThreads), 0, stream, a);
     const uint32_t tiles = (a.dim + kLanes * 8 - 1) / (kLanes * 8);
     if (p.pieces > 1)
-        hipLaunchKernelGGL((embed_join_kernel<IN16, OUT16>), dim3(p.pieces, tiles < 16 ? tiles : 16), dim3(kJoinWaves * kLanes), 0, stream, a);
+        hipLaunchKernelGGL((embed_join_kernel<IN16, OUT16>), dim3((p.pieces + kJoinPieces - 1) / kJoinPieces, tiles < 16 ? tiles : 16), dim3(kJoinWaves * kLanes), 0, stream, a);
 }
 
 }  // namespace solo
@@ -634,11 +694,12 @@ int solo_embedding_grad(const void *grad_rows, const void *tokens, void *grad_ta
     a.in = grad_rows; a.tokens = tokens; a.out = grad_table;
     char *const ws = static_cast<char *>(workspace);
     a.order = reinterpret_cast<uint32_t *>(ws + p.order); a.sorted = reinterpret_cast<uint32_t *>(ws + p.sorted);
-    a.start = reinterpret_cast<uint32_t *>(ws + p.start); a.partial = reinterpret_cast<float *>(ws + p.partial);
+    a.span = reinterpret_cast<uint2 *>(ws + p.span); a.partial = reinterpret_cast<float *>(ws + p.partial);
     a.in_stride = shape->rows_stride; a.out_stride = shape->table_stride;
     a.vocab = (uint32_t)shape->vocab; a.dim = (uint32_t)shape->dim; a.n = (uint32_t)shape->tokens;
     a.scale = shape->scale;
-    a.bucket_bits = p.bucket_bits; a.piece = p.piece; a.pieces = p.pieces; a.team_bits = p.team_bits; a.tiles = p.tiles;
+    a.bucket_bits = p.bucket_bits; a.row_bits = p.row_bits;
+    a.piece = p.piece; a.pieces = p.pieces; a.team_bits = p.team_bits; a.tiles = p.tiles;
     a.add = add ? 1u : 0u;
     if (!add) {
         const uint32_t row_bytes = a.dim * (uint32_t)element_bytes(shape->table_dtype);
@@ -657,9 +718,9 @@ int solo_embedding_grad(const void *grad_rows, const void *tokens, void *grad_ta
         return launched();
     }
     if (a.n != 0) {
-        const uint32_t lds = (kSortWaves * (1u << p.bucket_bits) + kSortWaves) * (uint32_t)sizeof(uint32_t);
-        if (wide) hipLaunchKernelGGL(embed_sort_kernel<true>, dim3(p.buckets), dim3(kSortWaves * kLanes), lds, s, a);
-        else hipLaunchKernelGGL(embed_sort_kernel<false>, dim3(p.buckets), dim3(kSortWaves * kLanes), lds, s, a);
+        const uint32_t lds = kSortWaves * (1u << p.row_bits) * (uint32_t)sizeof(uint32_t);
+        if (wide) hipLaunchKernelGGL(embed_sort_kernel<true>, dim3(1u << p.bucket_bits), dim3(kSortWaves * kLanes), lds, s, a);
+        else hipLaunchKernelGGL(embed_sort_kernel<false>, dim3(1u << p.bucket_bits), dim3(kSortWaves * kLanes), lds, s, a);
     }
     uint64_t items = (uint64_t)p.pieces * p.tiles, groups = ((items << p.team_bits) + kEmbedThreads - 1) / kEmbedThreads;
     if (groups > (1u << 22)) groups = 1u << 22;
