@@ -22,6 +22,10 @@ constexpr int kSortDepth = 8;                             // tokens of a lane th
 constexpr uint32_t kMinBuckets = 256;                      // workgroups that sort: one for each compute unit
 constexpr uint32_t kMaxRowBits = 9;                        // rows of a bucket: 512 at most (counters by wavefront: 32 KB of LDS)
 constexpr int kEmbedThreads = 256;
+// Looked-up rows of more bytes than this are written past the caches, and gradients of more are read past them: a quarter of the
+// last-level cache.  Lookup of 134 MB 43 us through the caches, 32 us past them, of 16 MB no difference; gradient of 134 MB 94 and 84 us,
+// but of 40 MB, which the backward pass has left in the caches, 38 and 51 us.
+constexpr uint64_t kPastBytes = 64ull << 20;
 constexpr int kAheadRows = 8;                              // rows of dy that a team has under way
 
 struct EmbedArgs {
@@ -60,7 +64,7 @@ __device__ __forceinline__ uint32_t token_at(const void *tokens, uint64_t i, uin
 
 // ---- lookup ----------------------------------------------------------------------------------
 // Teams of 2^team_bits lanes take one token each; a lane copies eight elements at a time.
-template <bool IN16, bool OUT16, bool WIDE>
+template <bool IN16, bool OUT16, bool WIDE, bool PAST>
 __global__ __launch_bounds__(kEmbedThreads) void embed_lookup_kernel(const EmbedArgs a)
 {
     const uint32_t team = 1u << a.team_bits, lane = threadIdx.x & (team - 1);
@@ -76,7 +80,8 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_lookup_kernel(const Embed
             if (known) Elements<IN16>::unpack(Elements<IN16>::load8(from, c), x);
 #pragma unroll
             for (int k = 0; k < 8; ++k) x[k] *= a.scale;
-            Elements<OUT16>::store8(to, c, x);
+            if (PAST) Elements<OUT16>::store8_past(to, c, x);
+            else Elements<OUT16>::store8(to, c, x);
         }
         const uint32_t c = whole + lane;
         if (c < a.dim) Elements<OUT16>::store1(to, c, known ? Elements<IN16>::load1(from, c) * a.scale : 0.0f);
@@ -343,7 +348,7 @@ __device__ __forceinline__ void sum_piece(const EmbedArgs &a, uint32_t piece, ui
 // The same by a whole wavefront, for rows of more than 256 columns: the places of the list are a lane each, so that rows and
 // positions are scalars, and a batch of rows is under way while the one before is added and written.  (A wait for loads also waits
 // for the stores in front of them: stores of a batch come behind the loads of the next.)
-template <bool IN16, bool OUT16>
+template <bool IN16, bool OUT16, bool PAST>
 __device__ __forceinline__ void sum_piece_wave(const EmbedArgs &a, uint32_t piece, uint32_t c)
 {
     constexpr int kBatch = IN16 ? 8 : 4;
@@ -372,7 +377,8 @@ __device__ __forceinline__ void sum_piece_wave(const EmbedArgs &a, uint32_t piec
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
             const uint64_t at_row = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(position, min(k + j, k1 - 1)) * a.in_stride;
-            r[j] = Elements<IN16>::load8(in + at_row * Elements<IN16>::kBytes, 0);
+            const char *const at = in + at_row * Elements<IN16>::kBytes;
+            r[j] = PAST ? Elements<IN16>::load8_past(at, 0) : Elements<IN16>::load8(at, 0);
         }
     };
     auto put = [&](uint32_t row, bool head, bool tail) {
@@ -429,7 +435,7 @@ __device__ __forceinline__ void zero_rows(const EmbedArgs &a, uint32_t first, ui
             zero_row(static_cast<char *>(a.out) + (uint64_t)(first + r) * a.out_stride * Elements<OUT16>::kBytes, a.dim * Elements<OUT16>::kBytes, lane, lanes);
 }
 
-template <bool IN16, bool OUT16, bool WAVE>
+template <bool IN16, bool OUT16, bool WAVE, bool PAST>
 __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedArgs a)
 {
     const uint32_t lane = threadIdx.x % kLanes;
@@ -445,7 +451,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedArg
     if (WAVE) {
         for (uint64_t item = __builtin_amdgcn_readfirstlane((uint32_t)team); item < items; item += teams) {
             const uint32_t piece = (uint32_t)(item / a.tiles), c = ((uint32_t)(item % a.tiles) << 6 | lane) * 8;
-            sum_piece_wave<IN16, OUT16>(a, piece, c);
+            sum_piece_wave<IN16, OUT16, PAST>(a, piece, c);
         }
         return;
     }
@@ -621,6 +627,16 @@ static EmbedPlan embed_plan(const solo_embedding_shape *s)
     return p;
 }
 
+static bool past_caches(const solo_embedding_shape *s) { return s->tokens * s->dim * element_bytes(s->rows_dtype) > kPastBytes; }
+
+template <bool IN16, bool OUT16>
+static void lookup(const EmbedArgs &a, bool wide, bool past, uint64_t grid, void *stream)
+{
+    void (*kernel)(EmbedArgs) = wide ? (past ? embed_lookup_kernel<IN16, OUT16, true, true> : embed_lookup_kernel<IN16, OUT16, true, false>)
+                                     : (past ? embed_lookup_kernel<IN16, OUT16, false, true> : embed_lookup_kernel<IN16, OUT16, false, false>);
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)grid), dim3(kEmbedThreads), 0, (hipStream_t)stream, a);
+}
+
 template <bool IN16, bool OUT16>
 static void few_tokens(const EmbedArgs &a, bool wide, hipStream_t stream)
 {
@@ -629,10 +645,11 @@ static void few_tokens(const EmbedArgs &a, bool wide, hipStream_t stream)
 }
 
 template <bool IN16, bool OUT16>
-static void sum_rows(const EmbedArgs &a, const EmbedPlan &p, uint32_t sum_groups, hipStream_t stream)
+static void sum_rows(const EmbedArgs &a, const EmbedPlan &p, uint32_t sum_groups, bool past, hipStream_t stream)
 {
     const uint32_t grid = sum_groups + a.zero_groups;
-    if (grid) hipLaunchKernelGGL((p.team_bits == 6 ? embed_sum_kernel<IN16, OUT16, true> : embed_sum_kernel<IN16, OUT16, false>), dim3(grid), dim3(kEmbedThreads), 0, stream, a);
+    if (grid) hipLaunchKernelGGL((p.team_bits < 6 ? embed_sum_kernel<IN16, OUT16, false, false>
+                                     : past ? embed_sum_kernel<IN16, OUT16, true, true> : embed_sum_kernel<IN16, OUT16, true, false>), dim3(grid), dim3(kEmbedThreads), 0, stream, a);
     const uint32_t tiles = (a.dim + kLanes * 8 - 1) / (kLanes * 8);
     if (p.pieces > 1)
         hipLaunchKernelGGL((embed_join_kernel<IN16, OUT16>), dim3((p.pieces + kJoinPieces - 1) / kJoinPieces, tiles < 16 ? tiles : 16), dim3(kJoinWaves * kLanes), 0, stream, a);
@@ -661,12 +678,9 @@ int solo_embedding(const void *table, const void *tokens, void *rows, const solo
     uint64_t grid = ((shape->tokens << a.team_bits) + kEmbedThreads - 1) / kEmbedThreads;
     if (grid > (1u << 20)) grid = 1u << 20;
     const bool in16 = shape->table_dtype == SOLO_BF16, out16 = shape->rows_dtype == SOLO_BF16, wide = shape->token_bits == 64;
-    void (*kernel)(EmbedArgs) =
-        in16 ? (out16 ? (wide ? embed_lookup_kernel<true, true, true> : embed_lookup_kernel<true, true, false>)
-                      : (wide ? embed_lookup_kernel<true, false, true> : embed_lookup_kernel<true, false, false>))
-             : (out16 ? (wide ? embed_lookup_kernel<false, true, true> : embed_lookup_kernel<false, true, false>)
-                      : (wide ? embed_lookup_kernel<false, false, true> : embed_lookup_kernel<false, false, false>));
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)grid), dim3(kEmbedThreads), 0, (hipStream_t)stream, a);
+    const bool past = past_caches(shape);
+    if (in16) out16 ? lookup<true, true>(a, wide, past, grid, stream) : lookup<true, false>(a, wide, past, grid, stream);
+    else out16 ? lookup<false, true>(a, wide, past, grid, stream) : lookup<false, false>(a, wide, past, grid, stream);
     return launched();
 }
 
@@ -724,8 +738,8 @@ int solo_embedding_grad(const void *grad_rows, const void *tokens, void *grad_ta
     }
     uint64_t items = (uint64_t)p.pieces * p.tiles, groups = ((items << p.team_bits) + kEmbedThreads - 1) / kEmbedThreads;
     if (groups > (1u << 22)) groups = 1u << 22;
-    if (in16) out16 ? sum_rows<true, true>(a, p, (uint32_t)groups, s) : sum_rows<true, false>(a, p, (uint32_t)groups, s);
-    else out16 ? sum_rows<false, true>(a, p, (uint32_t)groups, s) : sum_rows<false, false>(a, p, (uint32_t)groups, s);
+    if (in16) out16 ? sum_rows<true, true>(a, p, (uint32_t)groups, past_caches(shape), s) : sum_rows<true, false>(a, p, (uint32_t)groups, past_caches(shape), s);
+    else out16 ? sum_rows<false, true>(a, p, (uint32_t)groups, past_caches(shape), s) : sum_rows<false, false>(a, p, (uint32_t)groups, past_caches(shape), s);
     return launched();
 }
 
