@@ -54,18 +54,14 @@ __device__ __forceinline__ void add1(Sums &a, float x, float k)
     a.w = fmaf(p, fmaxf(d, kFloor), a.w);
 }
 
-__device__ __forceinline__ void add8(Sums &a, const float x[8], float k)
+// (NaN wins; three operands an instruction, where fmaxf first quiets each of its own)
+template <int N>
+__device__ __forceinline__ float max_of(const float x[N])
 {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) add1(a, x[e], k);
-}
-
-__device__ __forceinline__ float max8(const float x[8])
-{
-    // (NaN wins; three operands an instruction, where fmaxf first quiets each of its own)
     float m = __builtin_elementwise_maximum(__builtin_elementwise_maximum(x[0], x[1]), x[2]);
-    m = __builtin_elementwise_maximum(m, __builtin_elementwise_maximum(__builtin_elementwise_maximum(x[3], x[4]), x[5]));
-    return __builtin_elementwise_maximum(m, __builtin_elementwise_maximum(x[6], x[7]));
+    if constexpr (N == 4) return __builtin_elementwise_maximum(m, x[3]);
+    m = __builtin_elementwise_maximum(m, __builtin_elementwise_maximum(__builtin_elementwise_maximum(x[3 % N], x[4 % N]), x[5 % N]));
+    return __builtin_elementwise_maximum(m, __builtin_elementwise_maximum(x[6 % N], x[7 % N]));
 }
 
 // Logits in the order of their values, as whole numbers; -0 and +0 are the same.  A key has the column behind it: the lower one is larger.
@@ -87,18 +83,23 @@ __device__ __forceinline__ int64_t target_of(const RowArgs &a, uint64_t row)
     return a.wide ? static_cast<const int64_t *>(a.targets)[row] : (int64_t)static_cast<const int32_t *>(a.targets)[row];
 }
 
-// A row is cut into groups of eight columns, dealt out to the threads in turn, and up to seven columns behind the last whole
+// A row is cut into groups of columns, 16 bytes each, dealt out to the threads in turn, and the few columns behind the last whole
 // group, one each to the first threads.
 template <bool BF16>
 struct Row {
+    using Lane = Lane16<BF16>;
+    static constexpr uint32_t kPer = Lane::kPer;
     const void *at;
     uint32_t groups, rest;      // whole groups; columns behind them
 
     __device__ __forceinline__ Row(const RowArgs &a, uint64_t r)
-        : at(static_cast<const char *>(a.logits) + r * a.stride * Elements<BF16>::kBytes), groups(a.cols / 8), rest(a.cols % 8) {}
+        : at(static_cast<const char *>(a.logits) + r * a.stride * Lane::kBytes), groups(a.cols / kPer), rest(a.cols % kPer) {}
     __device__ __forceinline__ bool has_share(uint32_t thread) const { return thread < groups || thread < rest; }
-    __device__ __forceinline__ typename Elements<BF16>::Raw group(uint32_t g) const { return Elements<BF16>::load8_near(at, g * 8); }
+    template <bool PAST = false>
+    __device__ __forceinline__ Quad group(uint32_t g) const { return Lane::template load_near<PAST>(at, g * kPer); }
     __device__ __forceinline__ float one(uint32_t column) const { return Elements<BF16>::load1(at, column); }
+    // The column behind the groups that a thread has (if it is less than `rest`).
+    __device__ __forceinline__ uint32_t last_column(uint32_t thread) const { return groups * kPer + thread; }
 };
 
 template <int THREADS>
@@ -116,69 +117,66 @@ struct TopLds : SumLds<THREADS> {
     uint64_t best[THREADS / kLanes];
 };
 
-// What a thread remembers of its logits for the alternatives: the largest one of its groups, the number of that group (the
-// column behind the groups counts as one more) and the largest of the other groups.
+// What a thread remembers of its logits for the alternatives: the largest one, the group that holds it, and the largest one of its
+// other groups.  (The column behind the groups counts as a group, with the number behind theirs.)
 struct Largest {
     float first = -INFINITY, second = -INFINITY;
     uint32_t group = 0xFFFFFFFFu;
     __device__ __forceinline__ void see(float m, uint32_t g)
     {
-        if (!(m <= first)) {
-            second = first;
-            first = m;
-            group = g;
-        } else {
-            second = fmaxf(second, m);
-        }
+        second = __builtin_amdgcn_fmed3f(second, m, first);        // (of second <= first and m, the middle one)
+        group = m > first ? g : group;
+        first = m > first ? m : first;
     }
 };
 
-// The sums of a row, for every thread.  `last`: its column behind the groups; with RESIDENT, for rows of no more than
-// THREADS * DEPTH groups, `raw` are its groups.  Otherwise the loads of the next DEPTH groups are under way while DEPTH are added.
-template <bool BF16, bool TOP, bool RANK, bool RESIDENT, int THREADS, int DEPTH>
-__device__ __forceinline__ Sums row_sums(const Row<BF16> &row, float k, float target, SumLds<THREADS> &lds,
-                                         typename Elements<BF16>::Raw raw[DEPTH], float &last, Largest &largest, uint32_t &above)
+// The first DEPTH groups of a thread; one that it does not have is another's.
+template <bool BF16, bool PAST, int THREADS, int DEPTH>
+__device__ __forceinline__ void first_groups(const Row<BF16> &row, Quad q[DEPTH])
+{
+    if (row.groups == 0) return;
+#pragma unroll
+    for (int j = 0; j < DEPTH; ++j) q[j] = row.template group<PAST>(min(j * THREADS + threadIdx.x, row.groups - 1));
+}
+
+// The sums of a row, for every thread.  `q`: first_groups() of the row, which with RESIDENT, for rows of no more than THREADS * DEPTH
+// groups, are all of them; otherwise the loads of the next DEPTH groups are under way while DEPTH are added.  `last`: the thread's
+// column behind the groups.
+template <bool BF16, bool TOP, bool RANK, bool RESIDENT, bool PAST, int THREADS, int DEPTH>
+__device__ __forceinline__ Sums row_sums(const Row<BF16> &row, float k, float target, SumLds<THREADS> &lds, Quad q[DEPTH],
+                                         float last, Largest &largest, uint32_t &above)
 {
     Sums a = {-FLT_MAX, 0.0f, 0.0f};
     uint32_t count = 0;
-    last = -INFINITY;
-    if (threadIdx.x < row.rest) last = row.one(row.groups * 8 + threadIdx.x);
-    auto add = [&](const typename Elements<BF16>::Raw &r, uint32_t g) {
-        float x[8];
-        Elements<BF16>::unpack(r, x);
-        const float m = max8(x);
+    constexpr int kPer = Row<BF16>::kPer;
+    auto add = [&](const Quad &quad, uint32_t g) {
+        float x[kPer];
+        Lane16<BF16>::unpack(quad, x);
+        const float m = max_of<kPer>(x);
         if ((m - a.at) * k > kSlack) rebase(a, m, k);
         if (TOP) largest.see(m, g);
         if (RANK) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) count += x[e] > target;
+            for (int e = 0; e < kPer; ++e) count += x[e] > target;
         }
-        add8(a, x, k);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) add1(a, x[e], k);
     };
     uint32_t g0 = 0;
-    if (!RESIDENT && row.groups >= THREADS * DEPTH) {
-        typename Elements<BF16>::Raw next[DEPTH];
-#pragma unroll
-        for (int j = 0; j < DEPTH; ++j) next[j] = row.group(threadIdx.x + j * THREADS);
+    if (!RESIDENT)
         for (; g0 + THREADS * DEPTH <= row.groups; g0 += THREADS * DEPTH) {
+            Quad now[DEPTH];
 #pragma unroll
             for (int j = 0; j < DEPTH; ++j) {
-                raw[j] = next[j];
-                next[j] = row.group(min(g0 + THREADS * DEPTH + j * THREADS + threadIdx.x, row.groups - 1));
+                now[j] = q[j];
+                q[j] = row.template group<PAST>(min(g0 + THREADS * DEPTH + j * THREADS + threadIdx.x, row.groups - 1));
             }
 #pragma unroll
-            for (int j = 0; j < DEPTH; ++j) add(raw[j], g0 + j * THREADS + threadIdx.x);
+            for (int j = 0; j < DEPTH; ++j) add(now[j], g0 + j * THREADS + threadIdx.x);
         }
 #pragma unroll
-        for (int j = 0; j < DEPTH; ++j)
-            if (g0 + j * THREADS + threadIdx.x < row.groups) add(next[j], g0 + j * THREADS + threadIdx.x);
-    } else if (row.groups != 0) {
-#pragma unroll
-        for (int j = 0; j < DEPTH; ++j) raw[j] = row.group(min(j * THREADS + threadIdx.x, row.groups - 1));
-#pragma unroll
-        for (int j = 0; j < DEPTH; ++j)
-            if (j * THREADS + threadIdx.x < row.groups) add(raw[j], j * THREADS + threadIdx.x);
-    }
+    for (int j = 0; j < DEPTH; ++j)
+        if (g0 + j * THREADS + threadIdx.x < row.groups) add(q[j], g0 + j * THREADS + threadIdx.x);
     if (threadIdx.x < row.rest) {
         if ((last - a.at) * k > kSlack) rebase(a, last, k);
         if (TOP) largest.see(last, row.groups);
@@ -223,13 +221,16 @@ __device__ __forceinline__ void row_top(const RowArgs &a, const Row<BF16> &row, 
         a.top_logprob[out * a.top + at] = all.s == 0.0f ? -INFINITY : fmaf(value_of(key) - all.at, a.scale, -log_s);
         a.top_token[out * a.top + at] = (int32_t)column_of(key);
     };
+    auto put_none = [&](uint32_t at) {
+        a.top_logprob[out * a.top + at] = -INFINITY;
+        a.top_token[out * a.top + at] = -1;
+    };
     const bool any = row.has_share(threadIdx.x);
     const uint32_t mine = any ? order_of(largest.first) : 0;
     if (THREADS == kLanes) lds.largest[lane] = mine;
     else atomicMax(&lds.largest[lane], mine);              // (0 from the row before)
     __syncthreads();
-    uint32_t threshold;
-    {
+    if (threadIdx.x < kLanes) {
         const uint32_t own = lds.largest[lane];
         uint32_t larger = 0;
 #pragma unroll 4
@@ -238,11 +239,16 @@ __device__ __forceinline__ void row_top(const RowArgs &a, const Row<BF16> &row, 
             larger += (o.x > own) + (o.y > own) + (o.z > own) + (o.w > own);
         }
         // the smallest that fewer than `found` exceed; 0 where there are fewer shares
-        threshold = ~wave_max(larger < found ? ~own : 0u);
+        const uint32_t it = ~wave_max(larger < found ? ~own : 0u);
+        if (lane == 0) lds.threshold = it;
     }
+    __syncthreads();
+    const uint32_t threshold = lds.threshold;
+    const float at_least = threshold == 0 ? -INFINITY : value_of((uint64_t)threshold << 32);
     const bool holds = any && mine >= threshold;
     bool counts = holds;
-    if (holds) atomicAdd(&lds.holders, 1u);
+    const uint64_t holding = __ballot(holds);
+    if (lane == 0 && holding != 0) atomicAdd(&lds.holders, (uint32_t)__popcll(holding));
     __syncthreads();
     const uint32_t holders = lds.holders;
     uint32_t last_column = 0xFFFFFFFFu;
@@ -250,13 +256,13 @@ __device__ __forceinline__ void row_top(const RowArgs &a, const Row<BF16> &row, 
         uint32_t column = 0xFFFFFFFFu;
         if (any && mine == threshold) {
             for (uint32_t g = threadIdx.x; g < row.groups && column == 0xFFFFFFFFu; g += THREADS) {
-                float x[8];
-                Elements<BF16>::unpack(row.group(g), x);
+                float x[Row<BF16>::kPer];
+                Lane16<BF16>::unpack(row.group(g), x);
 #pragma unroll
-                for (int e = 7; e >= 0; --e)
-                    if (order_of(x[e]) == threshold) column = g * 8 + e;
+                for (int e = Row<BF16>::kPer - 1; e >= 0; --e)
+                    if (order_of(x[e]) == threshold) column = g * Row<BF16>::kPer + e;
             }
-            if (column == 0xFFFFFFFFu && threadIdx.x < row.rest) column = row.groups * 8 + threadIdx.x;
+            if (column == 0xFFFFFFFFu && threadIdx.x < row.rest) column = row.last_column(threadIdx.x);
         }
         lds.column[threadIdx.x] = column;
         __syncthreads();
@@ -275,18 +281,29 @@ __device__ __forceinline__ void row_top(const RowArgs &a, const Row<BF16> &row, 
         last_column = lds.last_column;
         counts = holds && (mine > threshold || column <= last_column);
     }
-    auto look = [&](float x, uint32_t column, auto &&use) {
-        const uint32_t order = order_of(x);
-        if (order > threshold || (order == threshold && column <= last_column)) use(key_of(order, column));
+    // the logits of a group, from column `column` on, that count (a NaN does not)
+    auto look = [&](const float *x, int n, uint32_t column, auto &&use) {
+        uint32_t hits = 0;
+#pragma unroll
+        for (int e = 0; e < n; ++e)
+            hits |= (x[e] > at_least || (x[e] == at_least && column + e <= last_column) ? 1u : 0u) << e;
+        while (hits != 0) {                                // (one, mostly)
+            const uint32_t e = __builtin_ctz(hits);
+            hits &= hits - 1;
+            float it = x[0];
+#pragma unroll
+            for (int o = 1; o < n; ++o) it = (int)e == o ? x[o] : it;
+            use(key_of(order_of(it), column + e));
+        }
     };
     auto look_at_group = [&](uint32_t g, uint32_t thread, auto &&use) {
+        float x[Row<BF16>::kPer];
         if (g < row.groups) {
-            float x[8];
-            Elements<BF16>::unpack(row.group(g), x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) look(x[e], g * 8 + e, use);
+            Lane16<BF16>::unpack(row.group(g), x);
+            look(x, Row<BF16>::kPer, g * Row<BF16>::kPer, use);
         } else if (g == row.groups && thread < row.rest) {
-            look(row.one(row.groups * 8 + thread), row.groups * 8 + thread, use);
+            x[0] = row.one(row.last_column(thread));
+            look(x, 1, row.last_column(thread), use);
         }
     };
     auto collect = [&](uint64_t key) {
@@ -342,14 +359,15 @@ __device__ __forceinline__ void row_top(const RowArgs &a, const Row<BF16> &row, 
             if (lane == 0) lds.best[threadIdx.x / kLanes] = best;
             __syncthreads();
             for (int w = 0; w < THREADS / kLanes; ++w) best = lds.best[w] > best ? lds.best[w] : best;
-            if (threadIdx.x == 0) put(r, best);
+            if (threadIdx.x == 0) {
+                if (best != 0) put(r, best);
+                else put_none(r);
+            }
             last = best;
         }
     }
-    for (uint32_t r = found + threadIdx.x; r < a.top; r += THREADS) {
-        a.top_logprob[out * a.top + r] = -INFINITY;
-        a.top_token[out * a.top + r] = -1;
-    }
+    // behind the last column (and in a row of NaN)
+    for (uint32_t r = min(found, count) + threadIdx.x; r < a.top; r += THREADS) put_none(r);
     __syncthreads();
     if (threadIdx.x < kLanes) lds.largest[threadIdx.x] = 0;
     if (threadIdx.x == 0) {
@@ -368,8 +386,11 @@ __device__ __forceinline__ float row_logprob(const Sums &all, float target, floa
     return all.s == 0.0f ? -INFINITY : fmaf(target - all.at, scale, -__builtin_amdgcn_logf(all.s) * kLn2);
 }
 
-template <bool BF16, bool TOP, bool RANK, int THREADS, int DEPTH>
-__global__ __launch_bounds__(THREADS, !TOP ? 8 : THREADS < 512 ? 6 : 5) void logprob_kernel(const RowArgs a)
+// Wavefronts per SIMD that the registers have to leave room for.
+constexpr int forward_waves(bool top, int threads) { return !top ? 8 : threads < 512 ? 6 : 5; }
+
+template <bool BF16, bool TOP, bool RANK, bool PAST, int THREADS, int DEPTH>
+__global__ __launch_bounds__(THREADS, forward_waves(TOP, THREADS)) void logprob_kernel(const RowArgs a)
 {
     __shared__ __align__(16) typename std::conditional<TOP, TopLds<THREADS>, SumLds<THREADS>>::type lds;
     const float k = a.scale * kLog2E;
@@ -384,8 +405,8 @@ __global__ __launch_bounds__(THREADS, !TOP ? 8 : THREADS < 512 ? 6 : 5) void log
     }
     for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const Row<BF16> row(a, r);
-        const int64_t t = a.targets ? target_of(a, r) : 0;
         const bool has = a.targets != nullptr;
+        const int64_t t = has ? target_of(a, r) : 0;
         if (has && (t < 0 || t >= (int64_t)a.cols)) {      // no target: the row is not read
             if (threadIdx.x == 0) {
                 if (a.logprob) a.logprob[r] = 0.0f;
@@ -400,12 +421,13 @@ __global__ __launch_bounds__(THREADS, !TOP ? 8 : THREADS < 512 ? 6 : 5) void log
                 }
             continue;
         }
+        Quad q[DEPTH];
+        first_groups<BF16, PAST, THREADS, DEPTH>(row, q);
         const float target = has ? row.one((uint32_t)t) : 0.0f;
-        float last;
+        const float last = threadIdx.x < row.rest ? row.one(row.last_column(threadIdx.x)) : -INFINITY;
         Largest largest;
         uint32_t above;
-        typename Elements<BF16>::Raw raw[DEPTH];
-        const Sums all = row_sums<BF16, TOP, RANK, false, THREADS, DEPTH>(row, k, target, lds, raw, last, largest, above);
+        const Sums all = row_sums<BF16, TOP, RANK, false, PAST, THREADS, DEPTH>(row, k, target, lds, q, last, largest, above);
         if (threadIdx.x == 0) {
             if (a.logprob && has) a.logprob[r] = row_logprob(all, target, a.scale);
             if (a.entropy) a.entropy[r] = row_entropy(all);
@@ -433,19 +455,20 @@ __device__ __forceinline__ float gradient_of(float x, const Slope &s, float k)
     return p * (ENTROPY ? fmaf(s.b, fmaf(fmaxf(d, kFloor), kLn2, s.entropy), s.a) : s.a);
 }
 
-template <bool BF16, bool ENTROPY>
-__device__ __forceinline__ void put_gradient(const typename Elements<BF16>::Raw &raw, void *out, uint32_t g, uint32_t target, const Slope &s, float k)
+template <bool BF16, bool ENTROPY, bool PAST>
+__device__ __forceinline__ void put_gradient(const Quad &q, void *out, uint32_t g, uint32_t target, const Slope &s, float k)
 {
-    float x[8];
-    Elements<BF16>::unpack(raw, x);
+    constexpr int kPer = Row<BF16>::kPer;
+    float x[kPer];
+    Lane16<BF16>::unpack(q, x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = gradient_of<ENTROPY>(x[e], s, k);
-    if (g == target / 8) {
+    for (int e = 0; e < kPer; ++e) x[e] = gradient_of<ENTROPY>(x[e], s, k);
+    if (g == target / kPer) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e == (int)(target % 8)) x[e] += s.target;
+        for (int e = 0; e < kPer; ++e)
+            if (e == (int)(target % kPer)) x[e] += s.target;
     }
-    Elements<BF16>::store8_near(out, g * 8, x);
+    Lane16<BF16>::template store_near<PAST>(out, g * kPer, x);
 }
 
 // Wavefronts per SIMD that the registers have to leave room for.  Rows that stay in registers: two workgroups of 1024 threads, so that
@@ -453,13 +476,13 @@ __device__ __forceinline__ void put_gradient(const typename Elements<BF16>::Raw 
 constexpr int grad_waves(bool bf16, bool forward, bool resident, int threads, int depth)
 {
     if (!forward || !resident) return 8;
-    if (depth > 4) return 4;
+    if (depth > (bf16 ? 4 : 8)) return 4;
     return bf16 ? 8 : threads == 1024 ? 4 : 5;
 }
 
 // FORWARD: the sums first, then the gradient; else from the sums that are given.  RESIDENT: the row has no more than THREADS * DEPTH
 // groups, which stay in registers between the two.
-template <bool BF16, bool FORWARD, bool RESIDENT, bool ENTROPY, int THREADS, int DEPTH>
+template <bool BF16, bool FORWARD, bool RESIDENT, bool ENTROPY, int PAST, int THREADS, int DEPTH>
 __global__ __launch_bounds__(THREADS, grad_waves(BF16, FORWARD, RESIDENT, THREADS, DEPTH)) void logprob_grad_kernel(const RowArgs a)
 {
     __shared__ SumLds<THREADS> lds;
@@ -469,9 +492,9 @@ __global__ __launch_bounds__(THREADS, grad_waves(BF16, FORWARD, RESIDENT, THREAD
         char *out = static_cast<char *>(a.grad) + r * a.grad_stride * Elements<BF16>::kBytes;
         const int64_t t = a.targets ? target_of(a, r) : -1;
         if (a.targets && (t < 0 || t >= (int64_t)a.cols)) {
-            const float none[8] = {};
-            for (uint32_t g = threadIdx.x; g < row.groups; g += THREADS) Elements<BF16>::store8_near(out, g * 8, none);
-            if (threadIdx.x < row.rest) Elements<BF16>::store1(out, row.groups * 8 + threadIdx.x, 0.0f);
+            const float none[Row<BF16>::kPer] = {};
+            for (uint32_t g = threadIdx.x; g < row.groups; g += THREADS) Lane16<BF16>::template store_near<(PAST > 0)>(out, g * Row<BF16>::kPer, none);
+            if (threadIdx.x < row.rest) Elements<BF16>::store1(out, row.last_column(threadIdx.x), 0.0f);
             if (FORWARD && threadIdx.x == 0) {
                 if (a.logprob) a.logprob[r] = 0.0f;
                 if (a.entropy) a.entropy[r] = 0.0f;
@@ -479,13 +502,15 @@ __global__ __launch_bounds__(THREADS, grad_waves(BF16, FORWARD, RESIDENT, THREAD
             continue;
         }
         const float up = a.grad_logprob && a.targets ? a.grad_logprob[r] : 0.0f, up_entropy = ENTROPY ? a.grad_entropy[r] : 0.0f;
-        typename Elements<BF16>::Raw raw[DEPTH];
-        float at, s, entropy, last = 0.0f;
+        Quad raw[DEPTH];
+        float at, s, entropy;
+        const float last = threadIdx.x < row.rest ? row.one(row.last_column(threadIdx.x)) : -INFINITY;
         if (FORWARD) {
             const float target = a.targets ? row.one((uint32_t)t) : 0.0f;
             Largest largest;
             uint32_t above;
-            const Sums all = row_sums<BF16, false, false, RESIDENT, THREADS, DEPTH>(row, k, target, lds, raw, last, largest, above);
+            first_groups<BF16, (PAST > 1), THREADS, DEPTH>(row, raw);
+            const Sums all = row_sums<BF16, false, false, RESIDENT, (PAST > 1), THREADS, DEPTH>(row, k, target, lds, raw, last, largest, above);
             at = all.at;
             s = all.s;
             entropy = row_entropy(all);
@@ -499,24 +524,23 @@ __global__ __launch_bounds__(THREADS, grad_waves(BF16, FORWARD, RESIDENT, THREAD
             entropy = a.entropy[r];
         }
         const Slope slope = slope_of(at, s, entropy, up, up_entropy, a.scale);
-        if (!FORWARD && threadIdx.x < row.rest) last = row.one(row.groups * 8 + threadIdx.x);
         for (uint32_t g0 = threadIdx.x; g0 < row.groups; g0 += THREADS * DEPTH) {
             if (!(FORWARD && RESIDENT)) {
 #pragma unroll
                 for (int j = 0; j < DEPTH; ++j)
-                    if (g0 + j * THREADS < row.groups) raw[j] = row.group(g0 + j * THREADS);
+                    if (g0 + j * THREADS < row.groups) raw[j] = row.template group<(PAST > 1)>(g0 + j * THREADS);
             }
 #pragma unroll
             for (int j = 0; j < DEPTH; ++j)
                 if (g0 + j * THREADS < row.groups) {
                     // (what has been unpacked for the sums is not kept: it would take twice the registers)
-                    if (FORWARD && RESIDENT) Elements<BF16>::forget(raw[j]);
-                    put_gradient<BF16, ENTROPY>(raw[j], out, g0 + j * THREADS, (uint32_t)t, slope, k);
+                    if (FORWARD && RESIDENT) forget(raw[j]);
+                    put_gradient<BF16, ENTROPY, (PAST > 0)>(raw[j], out, g0 + j * THREADS, (uint32_t)t, slope, k);
                 }
             if (FORWARD && RESIDENT) break;
         }
         if (threadIdx.x < row.rest) {
-            const uint32_t column = row.groups * 8 + threadIdx.x;
+            const uint32_t column = row.last_column(threadIdx.x);
             Elements<BF16>::store1(out, column, gradient_of<ENTROPY>(last, slope, k) + (column == (uint32_t)t ? slope.target : 0.0f));
         }
         if (FORWARD) __syncthreads();
@@ -544,26 +568,56 @@ static bool optional_at(const void *p, uintptr_t size) { return !p || at_multipl
 
 static uint32_t row_grid(uint64_t rows) { return (uint32_t)(rows < (1u << 20) ? rows : 1u << 20); }
 
-template <int THREADS, int DEPTH>
-static void logprob_launch(const RowArgs &a, bool bf16, hipStream_t stream)
+// Logits of more bytes than the last-level cache (256 MiB) keeps are read past the caches, and gradients that are not small are
+// written past them.
+constexpr uint64_t kPastLoads = 256ull << 20, kPastStores = 32ull << 20;
+
+static uint64_t logits_bytes(const RowArgs &a, bool bf16) { return a.rows * a.cols * (bf16 ? 2 : 4); }
+
+template <bool BF16, bool TOP, int THREADS, int DEPTH>
+static void logprob_launch(const RowArgs &a, hipStream_t stream)
 {
+    const bool rank = a.rank != nullptr;
     void (*kernel)(RowArgs);
-    const bool top = a.top != 0, rank = a.rank != nullptr;
-    if (bf16) kernel = top ? (rank ? logprob_kernel<true, true, true, THREADS, DEPTH> : logprob_kernel<true, true, false, THREADS, DEPTH>)
-                           : (rank ? logprob_kernel<true, false, true, THREADS, DEPTH> : logprob_kernel<true, false, false, THREADS, DEPTH>);
-    else kernel = top ? (rank ? logprob_kernel<false, true, true, THREADS, DEPTH> : logprob_kernel<false, true, false, THREADS, DEPTH>)
-                      : (rank ? logprob_kernel<false, false, true, THREADS, DEPTH> : logprob_kernel<false, false, false, THREADS, DEPTH>);
+    if (logits_bytes(a, BF16) > kPastLoads)
+        kernel = rank ? logprob_kernel<BF16, TOP, true, true, THREADS, DEPTH> : logprob_kernel<BF16, TOP, false, true, THREADS, DEPTH>;
+    else
+        kernel = rank ? logprob_kernel<BF16, TOP, true, false, THREADS, DEPTH> : logprob_kernel<BF16, TOP, false, false, THREADS, DEPTH>;
     hipLaunchKernelGGL(kernel, dim3(row_grid(a.rows)), dim3(THREADS), 0, stream, a);
 }
 
 template <bool BF16, bool FORWARD, bool RESIDENT, int THREADS, int DEPTH>
 static void grad_launch(const RowArgs &a, hipStream_t stream)
 {
-    hipLaunchKernelGGL((a.grad_entropy ? logprob_grad_kernel<BF16, FORWARD, RESIDENT, true, THREADS, DEPTH>
-                                       : logprob_grad_kernel<BF16, FORWARD, RESIDENT, false, THREADS, DEPTH>),
-                       dim3(row_grid(a.rows)), dim3(THREADS), 0, stream, a);
+    constexpr int kDepth = BF16 ? DEPTH : 2 * DEPTH;
+    const uint64_t bytes = logits_bytes(a, BF16);
+    void (*kernel)(RowArgs);
+    constexpr int kBoth = FORWARD && !RESIDENT ? 1 : 2;    // (a row that is read twice stays in the caches)
+    if (a.grad_entropy) kernel = bytes > kPastLoads    ? logprob_grad_kernel<BF16, FORWARD, RESIDENT, true, kBoth, THREADS, kDepth>
+                                 : bytes > kPastStores ? logprob_grad_kernel<BF16, FORWARD, RESIDENT, true, 1, THREADS, kDepth>
+                                                       : logprob_grad_kernel<BF16, FORWARD, RESIDENT, true, 0, THREADS, kDepth>;
+    else kernel = bytes > kPastLoads    ? logprob_grad_kernel<BF16, FORWARD, RESIDENT, false, kBoth, THREADS, kDepth>
+                  : bytes > kPastStores ? logprob_grad_kernel<BF16, FORWARD, RESIDENT, false, 1, THREADS, kDepth>
+                                        : logprob_grad_kernel<BF16, FORWARD, RESIDENT, false, 0, THREADS, kDepth>;
+    hipLaunchKernelGGL(kernel, dim3(row_grid(a.rows)), dim3(THREADS), 0, stream, a);
 }
 
+// A wavefront takes a row by itself where rows are short, or where there are enough of them that no compute unit waits and they
+// are not so long that all wavefronts look for their alternatives at the same time; few rows get more threads each.  (16384 rows of
+// 4096 columns, bf16, five alternatives: 40 us, with 256 threads 78; 4096 rows of 50304, twenty: 105 us, with 256 threads 83;
+// one row of 50257: 26 us, with 512 threads 10.)  With alternatives, 256 threads have one load of bf16 ahead instead of two: the
+// registers leave room for another wavefront, 83 instead of 86 us.  (groups: of eight columns)
+template <bool BF16, bool TOP>
+static void logprob_rows(const RowArgs &a, hipStream_t stream)
+{
+    const uint32_t groups = a.cols / 8;
+    constexpr int kDepth = BF16 ? 2 : 4;
+    if (groups <= 256 || (a.rows >= 4096 && groups <= 2048)) logprob_launch<BF16, TOP, 64, kDepth>(a, stream);
+    else if (a.rows >= 128 || groups <= 1024) logprob_launch<BF16, TOP, 256, BF16 && TOP ? 1 : kDepth>(a, stream);
+    else logprob_launch<BF16, TOP, 512, kDepth>(a, stream);
+}
+
+// (groups of eight columns)
 template <bool BF16>
 static void with_grad_launch(const RowArgs &a, hipStream_t stream)
 {
@@ -604,13 +658,9 @@ int solo_logprob(const void *logits, const void *targets, float *logprob, float 
         ((logprob || rank) && !targets) || (shape->top != 0 && (!at_multiple(top_logprob, 4) || !at_multiple(top_token, 4))))
         return SOLO_E_INVALID;
     a.logprob = logprob; a.entropy = entropy; a.rank = rank; a.top_logprob = top_logprob; a.top_token = top_token; a.stats = stats;
-    const bool bf16 = shape->dtype == SOLO_BF16;
-    const uint32_t groups = a.cols / 8;
-    // A wavefront takes a row by itself where rows are short, or where there are enough of them that no compute unit waits and
-    // they are not so long that all wavefronts look for their alternatives at the same time; few rows get more threads each.
-    if (groups <= 256 || (a.rows >= 4096 && groups <= 2048)) logprob_launch<64, 2>(a, bf16, (hipStream_t)stream);
-    else if (a.rows >= 128 || groups <= 1024) logprob_launch<256, 2>(a, bf16, (hipStream_t)stream);
-    else logprob_launch<512, 2>(a, bf16, (hipStream_t)stream);
+    const hipStream_t s = (hipStream_t)stream;
+    if (shape->dtype == SOLO_BF16) a.top ? logprob_rows<true, true>(a, s) : logprob_rows<true, false>(a, s);
+    else a.top ? logprob_rows<false, true>(a, s) : logprob_rows<false, false>(a, s);
     return launched();
 }
 

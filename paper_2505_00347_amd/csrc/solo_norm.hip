@@ -49,31 +49,27 @@ struct NormArgs {
 template <bool BF16, bool PAST>
 __device__ __forceinline__ double square_sum(const void *grad, uint64_t begin, uint64_t end, uint32_t thread)
 {
-    using E = Elements<BF16>;
-    constexpr int kAhead = BF16 ? 8 : 4;
-    constexpr uint64_t kStep = kNormThreads * 8;
+    using Lane = Lane16<BF16>;
+    constexpr int kPer = Lane::kPer, kAhead = 8;
+    constexpr uint64_t kStep = kNormThreads * kPer;
     double sum[4] = {0.0, 0.0, 0.0, 0.0};
-    uint64_t i = begin + thread * 8;
-    for (; i + (kAhead - 1) * kStep + 8 <= end; i += kAhead * kStep) {
-        typename E::Raw raw[kAhead];
+    auto add = [&](const Quad &q) {
+        float x[kPer];
+        Lane::unpack(q, x);
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) raw[a] = PAST ? E::load8_past(grad, i + a * kStep) : E::load8(grad, i + a * kStep);
+        for (int k = 0; k < kPer; ++k) sum[k & 3] = fma((double)x[k], (double)x[k], sum[k & 3]);
+    };
+    uint64_t i = begin + thread * kPer;
+    for (; i + (kAhead - 1) * kStep + kPer <= end; i += kAhead * kStep) {
+        Quad q[kAhead];
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-            float x[8];
-            E::unpack(raw[a], x);
+        for (int a = 0; a < kAhead; ++a) q[a] = Lane::template load<PAST>(grad, i + a * kStep);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum[k & 3] = fma((double)x[k], (double)x[k], sum[k & 3]);
-        }
+        for (int a = 0; a < kAhead; ++a) add(q[a]);
     }
-    for (; i + 8 <= end; i += kStep) {
-        float x[8];
-        E::unpack(E::load8(grad, i), x);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) sum[k & 3] = fma((double)x[k], (double)x[k], sum[k & 3]);
-    }
-    for (; i < end; ++i) {                                  // the last, shorter group of eight: one thread's
-        const double x = E::load1(grad, i);
+    for (; i + kPer <= end; i += kStep) add(Lane::template load<false>(grad, i));
+    for (; i < end; ++i) {                                 // the last, shorter group: one thread's
+        const double x = Elements<BF16>::load1(grad, i);
         sum[0] = fma(x, x, sum[0]);
     }
     return (sum[0] + sum[1]) + (sum[2] + sum[3]);
@@ -177,33 +173,33 @@ __global__ __launch_bounds__(kFinishThreads) void norm_small_kernel(const NormAr
 template <bool BF16, bool PAST>
 __device__ __forceinline__ void scale_unit(const void *grad, void *out, uint64_t begin, uint64_t end, float c)
 {
-    using E = Elements<BF16>;
-    constexpr int kAhead = BF16 ? 8 : 4;
-    constexpr uint64_t kStep = kNormThreads * 8;
+    using Lane = Lane16<BF16>;
+    constexpr int kPer = Lane::kPer, kAhead = 8;
+    constexpr uint64_t kStep = kNormThreads * kPer;
     const bool zero = c == 0.0f;
-    uint64_t i = begin + threadIdx.x * 8;
-    for (; i + (kAhead - 1) * kStep + 8 <= end; i += kAhead * kStep) {
-        typename E::Raw raw[kAhead];
+    auto scaled = [&](const Quad &q, float x[kPer]) {
+        Lane::unpack(q, x);
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) raw[a] = PAST ? E::load8_past(grad, i + a * kStep) : E::load8(grad, i + a * kStep);
+        for (int k = 0; k < kPer; ++k) x[k] = zero ? 0.0f : x[k] * c;
+    };
+    uint64_t i = begin + threadIdx.x * kPer;
+    for (; i + (kAhead - 1) * kStep + kPer <= end; i += kAhead * kStep) {
+        Quad q[kAhead];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) q[a] = Lane::template load<PAST>(grad, i + a * kStep);
 #pragma unroll
         for (int a = 0; a < kAhead; ++a) {
-            float x[8];
-            E::unpack(raw[a], x);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = zero ? 0.0f : x[k] * c;
-            if (PAST) E::store8_past(out, i + a * kStep, x);
-            else E::store8(out, i + a * kStep, x);
+            float x[kPer];
+            scaled(q[a], x);
+            Lane::template store<PAST>(out, i + a * kStep, x);
         }
     }
-    for (; i + 8 <= end; i += kStep) {
-        float x[8];
-        E::unpack(E::load8(grad, i), x);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = zero ? 0.0f : x[k] * c;
-        E::store8(out, i, x);
+    for (; i + kPer <= end; i += kStep) {
+        float x[kPer];
+        scaled(Lane::template load<false>(grad, i), x);
+        Lane::template store<false>(out, i, x);
     }
-    for (; i < end; ++i) E::store1(out, i, zero ? 0.0f : E::load1(grad, i) * c);
+    for (; i < end; ++i) Elements<BF16>::store1(out, i, zero ? 0.0f : Elements<BF16>::load1(grad, i) * c);
 }
 
 __global__ __launch_bounds__(kNormThreads) void clip_units_kernel(const NormArgs a)

@@ -54,8 +54,6 @@ struct Elements {
         for (int k = 0; k < (BF16 ? 1 : 2); ++k) r.q[k] = *reinterpret_cast<const Quad *>(at + 16 * k);
         return r;
     }
-    // The same where the offset is known to stay below 4 GiB of a base that is the same for the wavefront: one register of address.
-    __device__ __forceinline__ static Raw load8_near(const void *base, uint32_t i) { return load8(static_cast<const char *>(base) + i * kBytes, 0); }
     __device__ __forceinline__ static void unpack(const Raw &r, float x[8])
     {
 #pragma unroll
@@ -102,14 +100,52 @@ struct Elements {
         for (int k = 0; k < (BF16 ? 1 : 2); ++k) r.q[k] = __builtin_nontemporal_load(reinterpret_cast<const Quad *>(at + 16 * k));
         return r;
     }
-    __device__ __forceinline__ static void store8_near(void *base, uint32_t i, const float x[8]) { store8(static_cast<char *>(base) + i * kBytes, 0, x); }
-    // From here on the compiler does not know what `r` holds.
-    __device__ __forceinline__ static void forget(Raw &r)
+};
+
+// 16 bytes a lane: eight bf16 or four fp32 elements, so that an instruction of a wavefront reads or writes 1 KB without gaps.
+// (Eight fp32 elements a lane, as two halves, leave gaps of 16 bytes: stores past the caches then take half as long again.)
+// `i` is an element; `near`: less than 4 GiB behind a base that is the same for the wavefront, which saves registers of address.
+template <bool BF16>
+struct Lane16 {
+    static constexpr int kBytes = BF16 ? 2 : 4, kPer = 16 / kBytes;
+
+    template <bool PAST>
+    __device__ __forceinline__ static Quad load(const void *base, uint64_t i)
+    {
+        const Quad *at = reinterpret_cast<const Quad *>(static_cast<const char *>(base) + i * kBytes);
+        if (PAST) return __builtin_nontemporal_load(at);
+        return *at;
+    }
+    template <bool PAST>
+    __device__ __forceinline__ static Quad load_near(const void *base, uint32_t i) { return load<PAST>(static_cast<const char *>(base) + i * kBytes, 0); }
+    __device__ __forceinline__ static void unpack(const Quad &q, float x[kPer])
     {
 #pragma unroll
-        for (int k = 0; k < (BF16 ? 1 : 2); ++k) asm volatile("" : "+v"(r.q[k]));
+        for (int k = 0; k < 4; ++k) {
+            if (BF16) {
+                x[2 * k] = bf16_low(q[k]);
+                x[(2 * k + 1) % kPer] = bf16_high(q[k]);
+            } else {
+                x[k] = __uint_as_float(q[k]);
+            }
+        }
     }
+    template <bool PAST>
+    __device__ __forceinline__ static void store(void *base, uint64_t i, const float x[kPer])
+    {
+        Quad *at = reinterpret_cast<Quad *>(static_cast<char *>(base) + i * kBytes);
+        Quad q;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q[k] = BF16 ? to_bf16(x[2 * k % kPer], x[(2 * k + 1) % kPer]) : __float_as_uint(x[k]);
+        if (PAST) __builtin_nontemporal_store(q, at);
+        else *at = q;
+    }
+    template <bool PAST>
+    __device__ __forceinline__ static void store_near(void *base, uint32_t i, const float x[kPer]) { store<PAST>(static_cast<char *>(base) + i * kBytes, 0, x); }
 };
+
+// From here on the compiler does not know what `q` holds.
+__device__ __forceinline__ void forget(Quad &q) { asm volatile("" : "+v"(q)); }
 
 // One step of a reduction: the values of the lanes of groups of D, which are all alike in a group, and of the neighbouring
 // groups of D.  By the data paths of the vector unit: through LDS a step takes several times as long.
