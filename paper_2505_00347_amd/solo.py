@@ -385,9 +385,24 @@ def _row_stride(tensor, rows, cols, name):
     return stride
 
 
-def _row_weights(tensor, rows, name):
-    if tensor is not None and (tensor.dtype is not _torch.float32 or tuple(tensor.shape) != (rows,) or not tensor.is_contiguous()):
+def _row_weights(tensor, rows, name, device):
+    if tensor is None:
+        return
+    if tensor.dtype is not _torch.float32 or tensor.dim() != 1 or tensor.numel() != rows or not tensor.is_contiguous():
         raise ValueError(f"{name}: {rows} contiguous float32 values expected")
+    if tensor.device.type != device:
+        raise ValueError(f"{name}: on {device} expected, got {tensor.device}")
+
+
+def _layout(tensor):
+    """What a handle's checks look at."""
+    return None if tensor is None else (tensor.shape, tensor.stride(), tensor.dtype, tensor.device)
+
+
+def _on(device, *tensors):
+    for t in tensors:
+        if t is not None and t.device.type != device:
+            raise ValueError(f"tensors on {device} expected, got {t.device}")
 
 
 class SoloGradNorm:
@@ -403,11 +418,13 @@ class SoloGradNorm:
         self.count = len(grads)
         if clipped is not None and len(clipped) != self.count:
             raise ValueError(f"{self.count} clipped tensors expected, got {len(clipped)}")
+        where = _torch.device(device).type
         arr = (solo_grad * self.count)()
         for k, g in enumerate(grads):
             c = clipped[k] if clipped is not None else None
             if not g.is_contiguous() or (c is not None and (not c.is_contiguous() or c.dtype is not g.dtype or c.shape != g.shape)):
                 raise ValueError(f"tensor {k}: contiguous gradients, and clipped ones of the same shapes and types, expected")
+            _on(where, g, c)
             arr[k] = solo_grad(_ptr(g), _ptr(c), g.numel(), _dtype(g), 0)
         self.units = solo_norm_units(arr, self.count)
         nbytes = solo_norm_table_bytes(self.count, self.units)
@@ -421,8 +438,11 @@ class SoloGradNorm:
         self._keep = grads, clipped                # the buffers the table points to
 
     def _run(self, name, max_norm, unscale, stream):
-        if unscale is not None and unscale.dtype is not _torch.float32:
-            raise TypeError(f"unscale: float32 expected, got {unscale.dtype}")
+        if unscale is not None:
+            if unscale.dtype is not _torch.float32 or unscale.numel() != 1:
+                raise TypeError(f"unscale: one float32 value expected, got {unscale.numel()} of {unscale.dtype}")
+            if unscale.device != self.table.device:
+                raise ValueError(f"unscale: on {self.table.device} expected, got {unscale.device}")
         _operation(name, True, self.table, self.count, self.units, unscale, max_norm, *self.results, self.workspace, stream)
         return self.results
 
@@ -442,7 +462,8 @@ class SoloEmbedding:
 
     def __init__(self, vocab, dim, tokens, scale=1.0, device="cuda"):
         lib()
-        self.vocab, self.dim, self.tokens, self.scale, self.device = vocab, dim, tokens, scale, device
+        self.vocab, self.dim, self.tokens, self.scale, self.device = vocab, dim, tokens, scale, _torch.device(device)
+        self._seen = self._made = None
         shape = solo_embedding_shape(vocab, dim, tokens, dim, dim, SOLO_FP32, SOLO_FP32, 64, 0, scale, 0)
         self.workspace_bytes = solo_embedding_workspace_bytes(shape)
         if not self.workspace_bytes:
@@ -450,12 +471,19 @@ class SoloEmbedding:
         self.workspace = None                      # of the first gradient
 
     def _shape(self, table, rows, ids, flags):
-        n = ids.numel()
-        if n > self.tokens:
-            raise ValueError(f"at most {self.tokens} tokens expected, got {n}")
-        return solo_embedding_shape(self.vocab, self.dim, n, _row_stride(table, self.vocab, self.dim, "table"),
-                                    _row_stride(rows, n, self.dim, "rows"), _dtype(table), _dtype(rows), _token_bits(ids, n),
-                                    flags, self.scale, 0)
+        """The C struct of these tensors.  The checks and the struct are made when the tensors' layout is another than in the
+        call before: 3.6 us of the 5.9 that a lookup of a few tokens took."""
+        seen = _layout(table), _layout(rows), _layout(ids), flags, self.scale
+        if seen != self._seen:
+            n = ids.numel()
+            if n > self.tokens:
+                raise ValueError(f"at most {self.tokens} tokens expected, got {n}")
+            made = solo_embedding_shape(self.vocab, self.dim, n, _row_stride(table, self.vocab, self.dim, "table"),
+                                        _row_stride(rows, n, self.dim, "rows"), _dtype(table), _dtype(rows), _token_bits(ids, n),
+                                        flags, self.scale, 0)
+            _on(self.device.type, table, rows, ids)
+            self._made, self._seen = made, seen
+        return self._made
 
     def lookup(self, table, ids, out, stream=None):
         """out[i] = scale * table[ids[i]]"""
@@ -481,7 +509,8 @@ class SoloLogprob:
         lib()
         if not 0 <= top <= SOLO_TOP_MAX:
             raise ValueError(f"0 to {SOLO_TOP_MAX} alternatives expected, got {top}")
-        self.rows, self.cols, self.top, self.scale = rows, cols, top, scale
+        self.rows, self.cols, self.top, self.scale, self.device = rows, cols, top, scale, _torch.device(device).type
+        self._seen = self._made = None
         f32, i32 = dict(dtype=_torch.float32, device=device), dict(dtype=_torch.int32, device=device)
         self.logprob, self.entropy = _torch.empty(rows, **f32), _torch.empty(rows, **f32)
         self.stats = _torch.empty((rows, 2), **f32)
@@ -490,17 +519,23 @@ class SoloLogprob:
         self.top_token = _torch.empty((rows, top), **i32) if top else None
 
     def _shape(self, logits, targets, out=None):
-        r = logits.shape[0]
-        if r > self.rows:
-            raise ValueError(f"at most {self.rows} rows expected, got {r}")
-        stride = _row_stride(logits, r, self.cols, "logits")
-        grad_stride = stride
-        if out is not None:
-            grad_stride = _row_stride(out, r, self.cols, "gradient")
-            if out.dtype is not logits.dtype:
-                raise TypeError(f"gradient: {logits.dtype} expected, got {out.dtype}")
-        return solo_logits(r, self.cols, stride, grad_stride, _dtype(logits), 64 if targets is None else _token_bits(targets, r),
-                           self.top, 0, self.scale, 0)
+        """The C struct of these tensors, made when their layout is another than in the call before."""
+        seen = _layout(logits), _layout(targets), _layout(out), self.scale
+        if seen != self._seen:
+            r = logits.shape[0]
+            if r > self.rows:
+                raise ValueError(f"at most {self.rows} rows expected, got {r}")
+            stride = _row_stride(logits, r, self.cols, "logits")
+            grad_stride = stride
+            if out is not None:
+                grad_stride = _row_stride(out, r, self.cols, "gradient")
+                if out.dtype is not logits.dtype:
+                    raise TypeError(f"gradient: {logits.dtype} expected, got {out.dtype}")
+            made = solo_logits(r, self.cols, stride, grad_stride, _dtype(logits), 64 if targets is None else _token_bits(targets, r),
+                               self.top, 0, self.scale, 0)
+            _on(self.device, logits, targets, out)
+            self._made, self._seen = made, seen
+        return self._made
 
     def forward(self, logits, targets, stream=None):
         """(logprob, entropy[, rank][, top_logprob, top_token]); without targets, logprob and rank are None."""
@@ -519,8 +554,8 @@ class SoloLogprob:
     def grad(self, logits, targets, grad_logprob, grad_entropy, out, stream=None):
         """Gradient of the logits behind forward() on the same ones, for the gradients of logprob and entropy (or None)."""
         shape = self._shape(logits, targets, out)
-        _row_weights(grad_logprob, shape.rows, "grad_logprob")
-        _row_weights(grad_entropy, shape.rows, "grad_entropy")
+        _row_weights(grad_logprob, shape.rows, "grad_logprob", self.device)
+        _row_weights(grad_entropy, shape.rows, "grad_entropy", self.device)
         _operation("solo_logprob_grad", True, logits, targets, self.entropy, self.stats, grad_logprob, grad_entropy, out,
                    C.addressof(shape), stream)
         return out
@@ -528,8 +563,8 @@ class SoloLogprob:
     def forward_grad(self, logits, targets, grad_logprob, grad_entropy, out, stream=None):
         """(logprob, entropy, gradient) in one pass, for row weights that are known beforehand."""
         shape = self._shape(logits, targets, out)
-        _row_weights(grad_logprob, shape.rows, "grad_logprob")
-        _row_weights(grad_entropy, shape.rows, "grad_entropy")
+        _row_weights(grad_logprob, shape.rows, "grad_logprob", self.device)
+        _row_weights(grad_entropy, shape.rows, "grad_entropy", self.device)
         logprob = None if targets is None else self.logprob
         _operation("solo_logprob_with_grad", True, logits, targets, grad_logprob, grad_entropy, logprob, self.entropy, out,
                    C.addressof(shape), stream)
