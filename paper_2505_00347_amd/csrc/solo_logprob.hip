@@ -621,7 +621,7 @@ static void logprob_rows(const RowArgs &a, hipStream_t stream)
 template <bool BF16>
 static void with_grad_launch(const RowArgs &a, hipStream_t stream)
 {
-    const uint32_t groups = a.cols / 8;
+    const uint32_t groups = (a.cols + 7) / 8;              // (all of them have to fit)
     if (groups <= 64 * 4) grad_launch<BF16, true, true, 64, 4>(a, stream);
     else if (groups <= 256 * 4) grad_launch<BF16, true, true, 256, 4>(a, stream);
     else if (groups <= 512 * 4) grad_launch<BF16, true, true, 512, 4>(a, stream);

@@ -577,3 +577,28 @@ def test_graph():
         call()
         torch.cuda.synchronize()
         assert all(torch.equal(o, w) for o, w in zip(outs, got))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,top", [(1, 16384, 5), (128, 16389, 3), (7, 20_001, 32), (1, 300_003, 20), (2, 400_001, 0), (5, 65_537, 1)])
+def test_few_long_rows(rows, cols, top, dtype):
+    x = randn((rows, cols + 1), dtype, 1, 3.0)[:, 1:]
+    t = torch.randint(0, cols, (rows,), generator=generator(9), device="cuda")
+    if rows > 4:
+        x[1] = -math.inf
+        x[2, : cols - 5] = -math.inf
+        x[3] = torch.finfo(dtype).min
+        t[4] = -100
+        x[4] = math.nan
+    check_rows(x, t, 0.9, top, in_place=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("last", [2048, 8192, 16384, 32768, 65536])
+@pytest.mark.parametrize("more", [0, 1, 3, 4, 5, 7, 8])
+def test_rows_that_just_stay_in_registers_and_just_do_not(last, more, dtype):
+    cols = last + more
+    x = randn((3, cols), dtype, more, 3.0)
+    x[:, last - 9:] += 9.0                                 # (what lies behind the line counts)
+    check_rows(x, torch.tensor([cols - 1, 0, last - 1], device="cuda"), 1.0, 2)
+
