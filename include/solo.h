@@ -294,7 +294,7 @@ int solo_grad_clip(const void *table_device, uint32_t count, uint64_t units, con
  * touched. */
 #define SOLO_EMBEDDING_ACCUMULATE 1u
 typedef struct solo_embedding_shape {
-    uint64_t vocab, dim;        /* rows and columns of the table; below 2^31 and 2^24            */
+    uint64_t vocab, dim;        /* rows and columns of the table; below 2^30 and 2^24            */
     uint64_t tokens;            /* below 2^28                                                    */
     uint64_t table_stride;      /* elements from row to row, >= dim, below 2^31                  */
     uint64_t rows_stride;       /* the same of rows / grad_rows                                  */

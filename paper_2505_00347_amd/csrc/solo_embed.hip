@@ -10,6 +10,9 @@
 // are neighbours, and half of a text is a few hundred of them), reads all tokens (they lie in the caches) and needs nothing from the
 // others.  It counts the tokens of the buckets before its own, which is where its part of the sorted list begins, and its own by row
 // and wavefront; then it places them.
+//
+// Bound by memory.  16384 tokens of a bf16 table of 32000 x 4096: lookup 31 us (178 MB with every row that occurs once), gradient 83 us
+// (396 MB; the sort 8.8, the sums and zeros 67, the parts of frequent tokens 7.6 us); 396 MB take 72 us at the rate of a large copy.
 #include "solo_ops.h"
 
 #include <math.h>
@@ -416,7 +419,7 @@ __device__ __forceinline__ void sum_piece_wave(const EmbedArgs &a, uint32_t piec
 }
 
 // Rows without a token, past the caches: a wavefront looks at up to 64 rows, a lane each, and its teams write those that are empty,
-// 16 bytes a lane.  (154 MB of zeros in rows of 3 KB: 53 us through the caches, 35 us past them.)
+// 16 bytes a lane.  (Gradient of 96 tokens, 154 MB of zeros in rows of 3 KB: 62 us through the caches, 41 us past them, by the sort.)
 __device__ __forceinline__ void zero_row(char *to, uint32_t bytes, uint32_t lane, uint32_t lanes)
 {
     const Quad none = {};
@@ -462,8 +465,8 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedArg
 
 // ---- few tokens ------------------------------------------------------------------------------
 // One launch without a sort: every workgroup holds all tokens in LDS.  The wavefront of a token's first position adds the rows of
-// all its positions; the zeros go to the rows that no token names.  96 tokens of a table of 50257 x 768: 30 us instead of
-// 43 with the sort.  The line is where one wavefront's run over all tokens, if they are the same, takes as long as the launches saved.
+// all its positions; the zeros go to the rows that no token names.  96 tokens of a table of 50257 x 768: 27 us instead of
+// 41 with the sort.  The line is where one wavefront's run over all tokens, if they are the same, takes as long as the launches saved.
 constexpr uint32_t kFewTokens = 256;
 
 template <bool IN16, bool OUT16, bool WIDE>
@@ -597,7 +600,7 @@ static bool shape_ok(const solo_embedding_shape *s)
 // Offsets of a row are 64 bits wide, counts and places 32.
 static bool shape_fits(const solo_embedding_shape *s)
 {
-    return s->vocab < (1ull << 31) && s->dim < (1ull << 24) && s->tokens < (1ull << 28) && s->table_stride < (1ull << 31) && s->rows_stride < (1ull << 31);
+    return s->vocab < (1ull << 30) && s->dim < (1ull << 24) && s->tokens < (1ull << 28) && s->table_stride < (1ull << 31) && s->rows_stride < (1ull << 31);
 }
 
 static uint32_t bits_for(uint64_t n) { uint32_t b = 0; while ((1ull << b) < n) ++b; return b; }
@@ -615,6 +618,8 @@ static EmbedPlan embed_plan(const solo_embedding_shape *s)
     p.team_bits = bits_for(groups);
     if (p.team_bits > 6) p.team_bits = 6;
     p.tiles = (uint32_t)((groups + (1u << p.team_bits) - 1) >> p.team_bits);
+    // (wide rows: pieces of 16 write twice as many parts of frequent tokens, 111 instead of 106 us for 16384 x 4096, and 64 are too few
+    // wavefronts; narrow ones have few lanes a piece: 40000 tokens of 5000 x 100 85 us with 32, 66 us with 8)
     p.piece = p.team_bits == 6 ? 32 : 8;
     p.pieces = (uint32_t)((n + p.piece - 1) / p.piece);
     size_t at = 0;
@@ -735,6 +740,7 @@ int solo_embedding_grad(const void *grad_rows, const void *tokens, void *grad_ta
         const uint32_t lds = kSortWaves * (1u << p.row_bits) * (uint32_t)sizeof(uint32_t);
         if (wide) hipLaunchKernelGGL(embed_sort_kernel<true>, dim3(1u << p.bucket_bits), dim3(kSortWaves * kLanes), lds, s, a);
         else hipLaunchKernelGGL(embed_sort_kernel<false>, dim3(1u << p.bucket_bits), dim3(kSortWaves * kLanes), lds, s, a);
+        if (launched() != SOLO_OK) return SOLO_E_HIP;      // (what follows reads what the sort writes)
     }
     uint64_t items = (uint64_t)p.pieces * p.tiles, groups = ((items << p.team_bits) + kEmbedThreads - 1) / kEmbedThreads;
     if (groups > (1u << 22)) groups = 1u << 22;

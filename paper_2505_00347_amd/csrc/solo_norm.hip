@@ -5,6 +5,11 @@
 // The tensors are cut into units of the same number of elements, one workgroup each; a map names every unit's tensor.
 // norm_units_kernel writes one partial sum per unit, norm_finish_kernel adds them in the order of the units, per tensor
 // and over all, so the result does not depend on the order in which workgroups run.
+//
+// Bound by memory: two operations per element beside 2 or 4 bytes.  The 291 tensors of the 7B shapes in bf16, 13.5 GB: 1.90 ms, 7.1 TB/s
+// (a large copy reaches 5.4, reads alone through the caches 6.1), 9 us of them the sums of 51000 units.  Clipping reads twice,
+// since no element can be scaled before the last one is known, and writes once: 1.31e9 bf16 elements 1.39 ms (7.9 GB), 1.24e8 fp32 elements
+// 266 us (1.5 GB).
 #include "solo_ops.h"
 
 #include <math.h>
@@ -132,8 +137,8 @@ __global__ __launch_bounds__(kFinishThreads) void norm_finish_kernel(const NormA
     }
 }
 
-// All of it by one workgroup, a quarter of it for a unit: tables of up to four units.  A vector of 4096 elements takes 4.9 us a call
-// instead of 6.9 with two launches; five units and more are read faster by as many compute units.
+// All of it by one workgroup, a quarter of it for a unit: tables of up to four units.  A vector of 4096 elements takes 3.8 us a call
+// (2.4 of them the kernel) instead of 6.9 with two launches; five units and more are read faster by as many compute units.
 constexpr uint32_t kSmallUnits = kFinishThreads / kNormThreads;
 
 __global__ __launch_bounds__(kFinishThreads) void norm_small_kernel(const NormArgs a)
@@ -261,6 +266,7 @@ static int norm(const NormArgs &a, hipStream_t stream)
         return launched();
     }
     hipLaunchKernelGGL(norm_units_kernel, dim3(a.units), dim3(kNormThreads), 0, stream, a);
+    if (launched() != SOLO_OK) return SOLO_E_HIP;
     const uint32_t tensors = a.tensor_norm ? (a.count + kFinishThreads / kLanes - 1) / (kFinishThreads / kLanes) : 0;
     hipLaunchKernelGGL(norm_finish_kernel, dim3(1 + (tensors < 256 ? tensors : 256)), dim3(kFinishThreads), 0, stream, a);
     return launched();

@@ -432,6 +432,7 @@ class SoloGradNorm:
         if self.count:
             solo_norm_table_build(arr, self.count, host.data_ptr(), nbytes)
         self.table = host.to(device)
+        self.device = self.table.device
         self.workspace = _torch.empty(solo_norm_workspace_bytes(self.units), dtype=_torch.uint8, device=device)
         self.results = _torch.zeros(1, device=device), _torch.ones(1, device=device), _torch.zeros(self.count, device=device)
         self.writes = clipped is not None
@@ -441,8 +442,8 @@ class SoloGradNorm:
         if unscale is not None:
             if unscale.dtype is not _torch.float32 or unscale.numel() != 1:
                 raise TypeError(f"unscale: one float32 value expected, got {unscale.numel()} of {unscale.dtype}")
-            if unscale.device != self.table.device:
-                raise ValueError(f"unscale: on {self.table.device} expected, got {unscale.device}")
+            if unscale.device != self.device:
+                raise ValueError(f"unscale: on {self.device} expected, got {unscale.device}")
         _operation(name, True, self.table, self.count, self.units, unscale, max_norm, *self.results, self.workspace, stream)
         return self.results
 
