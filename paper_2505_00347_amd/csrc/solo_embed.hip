@@ -66,30 +66,37 @@ __device__ __forceinline__ uint32_t token_at(const void *tokens, uint64_t i, uin
 }
 
 // ---- lookup ----------------------------------------------------------------------------------
-// Teams of 2^team_bits lanes take one token each; a lane copies eight elements at a time.
+// Teams of 2^team_bits lanes take one token each; a lane writes 16 bytes at a time.
 template <bool IN16, bool OUT16, bool WIDE, bool PAST>
 __global__ __launch_bounds__(kEmbedThreads) void embed_lookup_kernel(const EmbedArgs a)
 {
+    using Out = Lane16<OUT16>;
+    constexpr uint32_t kPer = Out::kPer;
     const uint32_t team = 1u << a.team_bits, lane = threadIdx.x & (team - 1);
     const uint64_t teams = (uint64_t)gridDim.x * kEmbedThreads >> a.team_bits;
-    const uint32_t whole = a.dim / 8 * 8;
+    const uint32_t whole = a.dim / kPer * kPer;
     for (uint64_t i = ((uint64_t)blockIdx.x * kEmbedThreads + threadIdx.x) >> a.team_bits; i < a.n; i += teams) {
         const uint32_t t = token_at<WIDE>(a.tokens, i, a.vocab);
         const bool known = t != 0xFFFFFFFFu;
         const char *from = static_cast<const char *>(a.in) + (known ? t : 0) * a.in_stride * Elements<IN16>::kBytes;
-        char *to = static_cast<char *>(a.out) + i * a.out_stride * Elements<OUT16>::kBytes;
-        for (uint32_t c = lane * 8; c < whole; c += team * 8) {
-            float x[8] = {};
-            if (known) Elements<IN16>::unpack(Elements<IN16>::load8(from, c), x);
+        char *to = static_cast<char *>(a.out) + i * a.out_stride * Out::kBytes;
+        for (uint32_t c = lane * kPer; c < whole; c += 2 * team * kPer) {      // two loads in front of their stores
+            const uint32_t d = c + team * kPer;
+            float x[kPer] = {}, y[kPer] = {};
+            if (known) {
+                load_floats<IN16, (int)kPer>(from, c, x);
+                if (d < whole) load_floats<IN16, (int)kPer>(from, d, y);
+            }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] *= a.scale;
-            if (PAST) Elements<OUT16>::store8_past(to, c, x);
-            else Elements<OUT16>::store8(to, c, x);
+            for (uint32_t k = 0; k < kPer; ++k) {
+                x[k] *= a.scale;
+                y[k] *= a.scale;
+            }
+            Out::template store<PAST>(to, c, x);
+            if (d < whole) Out::template store<PAST>(to, d, y);
         }
-        const uint32_t c = whole + lane;
-        if (c < a.dim) Elements<OUT16>::store1(to, c, known ? Elements<IN16>::load1(from, c) * a.scale : 0.0f);
-        if (team < 8 && lane == 0)                        // (fewer lanes than a shorter group of eight has elements)
-            for (uint32_t e = whole + team; e < a.dim; ++e) Elements<OUT16>::store1(to, e, known ? Elements<IN16>::load1(from, e) * a.scale : 0.0f);
+        for (uint32_t c = whole + lane; c < a.dim; c += team)
+            Elements<OUT16>::store1(to, c, known ? Elements<IN16>::load1(from, c) * a.scale : 0.0f);
     }
 }
 
@@ -678,11 +685,11 @@ int solo_embedding(const void *table, const void *tokens, void *rows, const solo
     a.in_stride = shape->table_stride; a.out_stride = shape->rows_stride;
     a.vocab = (uint32_t)shape->vocab; a.dim = (uint32_t)shape->dim; a.n = (uint32_t)shape->tokens;
     a.scale = shape->scale;
-    a.team_bits = bits_for((shape->dim + 7) / 8);
+    const bool in16 = shape->table_dtype == SOLO_BF16, out16 = shape->rows_dtype == SOLO_BF16, wide = shape->token_bits == 64;
+    a.team_bits = bits_for(out16 ? (shape->dim + 7) / 8 : (shape->dim + 3) / 4);
     if (a.team_bits > 8) a.team_bits = 8;
     uint64_t grid = ((shape->tokens << a.team_bits) + kEmbedThreads - 1) / kEmbedThreads;
     if (grid > (1u << 20)) grid = 1u << 20;
-    const bool in16 = shape->table_dtype == SOLO_BF16, out16 = shape->rows_dtype == SOLO_BF16, wide = shape->token_bits == 64;
     const bool past = past_caches(shape);
     if (in16) out16 ? lookup<true, true>(a, wide, past, grid, stream) : lookup<true, false>(a, wide, past, grid, stream);
     else out16 ? lookup<false, true>(a, wide, past, grid, stream) : lookup<false, false>(a, wide, past, grid, stream);
