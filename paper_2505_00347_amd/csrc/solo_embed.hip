@@ -232,73 +232,78 @@ __global__ __launch_bounds__(kSortWaves * kLanes) void embed_sort_kernel(const E
 }
 
 // ---- sums ------------------------------------------------------------------------------------
-// A team of 2^team_bits lanes owns eight columns per lane of one piece: `piece` places of the sorted list.  It adds the rows
+// A team of 2^team_bits lanes owns 16 bytes of columns per lane of one piece: `piece` places of the sorted list.  It adds the rows
 // that begin inside the piece, to their ends where they have no more than `piece` tokens.  A longer row ("hot") is added
 // piece by piece: the part in the piece where it begins goes to that piece's second row of `partial`, the part in every
 // later piece to that one's first, and embed_join_kernel adds these.
-template <bool OUT16>
-__device__ __forceinline__ void put_row(const EmbedArgs &a, uint32_t row, uint32_t c, const float sum[8])
+// N columns a lane: 16 bytes of a row of the rows' gradient.
+template <bool OUT16, int N>
+__device__ __forceinline__ void put_row(const EmbedArgs &a, uint32_t row, uint32_t c, const float sum[N])
 {
     char *to = static_cast<char *>(a.out) + (uint64_t)row * a.out_stride * Elements<OUT16>::kBytes;
-    float x[8];
+    float x[N];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = sum[k] * a.scale;
-    if (c + 8 <= a.dim) {
+    for (int k = 0; k < N; ++k) x[k] = sum[k] * a.scale;
+    if (c + N <= a.dim) {
         if (a.add) {
-            float old[8];
-            Elements<OUT16>::unpack(Elements<OUT16>::load8(to, c), old);
+            float old[N];
+            load_floats<OUT16, N>(to, c, old);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] += old[k];
+            for (int k = 0; k < N; ++k) x[k] += old[k];
         }
-        Elements<OUT16>::store8(to, c, x);
+        store_floats<OUT16, N>(to, c, x);
         return;
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
+    for (int k = 0; k < N; ++k)
         if (c + k < a.dim) Elements<OUT16>::store1(to, c + k, x[k] + (a.add ? Elements<OUT16>::load1(to, c + k) : 0.0f));
 }
 
-// Columns c .. c + 7 of a row, of the sums of columns from .. from + 7 (from < c only in the shorter last group).
-template <bool OUT16>
-__device__ __forceinline__ void put_columns(const EmbedArgs &a, uint32_t row, uint32_t c, uint32_t from, const float sum[8])
+// Columns c .. c + N - 1 of a row, of the sums of columns from .. from + N - 1 (from < c only in the shorter last group).
+template <bool OUT16, int N>
+__device__ __forceinline__ void put_columns(const EmbedArgs &a, uint32_t row, uint32_t c, uint32_t from, const float sum[N])
 {
     if (from == c) {
-        put_row<OUT16>(a, row, c, sum);
+        put_row<OUT16, N>(a, row, c, sum);
         return;
     }
     char *to = static_cast<char *>(a.out) + row * a.out_stride * Elements<OUT16>::kBytes;
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
+    for (int k = 0; k < N; ++k)
         if (from + k >= c) Elements<OUT16>::store1(to, from + k, sum[k] * a.scale + (a.add ? Elements<OUT16>::load1(to, from + k) : 0.0f));
 }
 
 // Where a piece's part of a hot row lies, columns c on: first or second row of the piece.  The parts of neighbouring pieces are
 // neighbours, for the columns of a team: join reads them one behind the other.
+template <int N>
 __device__ __forceinline__ float *partial_at(const EmbedArgs &a, uint32_t piece, bool second, uint32_t c)
 {
-    const uint32_t width = 8u << a.team_bits, tile = c / width;
+    const uint32_t width = (uint32_t)N << a.team_bits, tile = c / width;
     return a.partial + (((uint64_t)tile * 2 + second) * a.pieces + piece) * width + c % width;
 }
 
-__device__ __forceinline__ void put_partial(const EmbedArgs &a, uint32_t piece, bool second, uint32_t c, const float sum[8])
+template <int N>
+__device__ __forceinline__ void put_partial(const EmbedArgs &a, uint32_t piece, bool second, uint32_t c, const float sum[N])
 {
-    Elements<false>::store8(partial_at(a, piece, second, c), 0, sum);
+    store_floats<false, N>(partial_at<N>(a, piece, second, c), 0, sum);
 }
 
-// The lane with the shorter last group of a row takes the last eight columns instead, where there are eight.
-__device__ __forceinline__ uint32_t first_column(const EmbedArgs &a, uint32_t c) { return a.dim >= 8 ? min(c, a.dim - 8) : 0; }
+// The lane with the shorter last group of a row takes the last N columns instead, where there are that many.
+template <int N>
+__device__ __forceinline__ uint32_t first_column(const EmbedArgs &a, uint32_t c) { return a.dim >= N ? min(c, a.dim - N) : 0; }
 
-template <bool IN16>
-__device__ __forceinline__ typename Elements<IN16>::Raw load_columns(const EmbedArgs &a, uint32_t position, uint32_t from)
+template <bool IN16, bool PAST = false>
+__device__ __forceinline__ Quad load_columns(const EmbedArgs &a, uint32_t position, uint32_t from)
 {
-    const char *at = static_cast<const char *>(a.in) + ((uint64_t)position * a.in_stride + from) * Elements<IN16>::kBytes;
-    if (a.dim >= 8) return Elements<IN16>::load8(at, 0);
-    float x[8];
+    using Lane = Lane16<IN16>;
+    const char *at = static_cast<const char *>(a.in) + ((uint64_t)position * a.in_stride + from) * Lane::kBytes;
+    if (a.dim >= (uint32_t)Lane::kPer) return Lane::template load<PAST>(at, 0);
+    float x[Lane::kPer];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = k < (int)a.dim ? Elements<IN16>::load1(at, k) : 0.0f;
-    typename Elements<IN16>::Raw r;
-    Elements<IN16>::store8(&r, 0, x);
-    return r;
+    for (int k = 0; k < Lane::kPer; ++k) x[k] = k < (int)a.dim ? Elements<IN16>::load1(at, k) : 0.0f;
+    Quad q;
+    Lane::template store<false>(&q, 0, x);
+    return q;
 }
 
 template <bool IN16, bool OUT16>
@@ -306,6 +311,7 @@ __device__ __forceinline__ void sum_piece(const EmbedArgs &a, uint32_t piece, ui
 {
     const uint32_t begin = piece * a.piece, edge = min(begin + a.piece, total);
     if (begin >= edge) return;
+    constexpr int N = Lane16<IN16>::kPer;
     uint32_t lo = begin, hi = edge;
     bool head = false, tail = false;                       // the first row is the rest of a hot one; the last row is the beginning of one
     uint32_t row = a.sorted[begin];
@@ -320,15 +326,15 @@ __device__ __forceinline__ void sum_piece(const EmbedArgs &a, uint32_t piece, ui
         else hi = last_span.y;
     }
     if (lo >= hi) return;
-    const uint32_t from = first_column(a, c);
-    float sum[8] = {};
+    const uint32_t from = first_column<N>(a, c);
+    float sum[N] = {};
     auto put = [&](bool to_head, bool to_tail) {
-        if (to_head || to_tail) put_partial(a, piece, to_tail, c, sum);
-        else put_columns<OUT16>(a, row, c, from, sum);
+        if (to_head || to_tail) put_partial<N>(a, piece, to_tail, c, sum);
+        else put_columns<OUT16, N>(a, row, c, from, sum);
     };
     row = a.sorted[lo];
     for (uint32_t s = lo; s < hi; s += kAheadRows) {
-        typename Elements<IN16>::Raw raw[kAheadRows];
+        Quad raw[kAheadRows];
         uint32_t next[kAheadRows];
 #pragma unroll
         for (int k = 0; k < kAheadRows; ++k) {
@@ -344,24 +350,24 @@ __device__ __forceinline__ void sum_piece(const EmbedArgs &a, uint32_t piece, ui
                 head = false;
                 row = next[k];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+                for (int e = 0; e < N; ++e) sum[e] = 0.0f;
             }
-            float x[8];
-            Elements<IN16>::unpack(raw[k], x);
+            float x[N];
+            Lane16<IN16>::unpack(raw[k], x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += x[e];
+            for (int e = 0; e < N; ++e) sum[e] += x[e];
         }
     }
     put(head, tail);
 }
 
-// The same by a whole wavefront, for rows of more than 256 columns: the places of the list are a lane each, so that rows and
+// The same by a whole wavefront, for rows of more than 256 columns (fp32: 128): the places of the list are a lane each, so that rows and
 // positions are scalars, and a batch of rows is under way while the one before is added and written.  (A wait for loads also waits
 // for the stores in front of them: stores of a batch come behind the loads of the next.)
 template <bool IN16, bool OUT16, bool PAST>
 __device__ __forceinline__ void sum_piece_wave(const EmbedArgs &a, uint32_t piece, uint32_t c)
 {
-    constexpr int kBatch = IN16 ? 8 : 4;
+    constexpr int N = Lane16<IN16>::kPer, kBatch = 8;
     const uint32_t begin = piece * a.piece, lane = threadIdx.x % kLanes, total = a.span[a.vocab].x;
     const uint32_t at = min(begin + lane, a.n - 1);
     const uint32_t token = a.sorted[at], position = a.order[at];               // (behind `total`: not set, and not used)
@@ -375,28 +381,28 @@ __device__ __forceinline__ void sum_piece_wave(const EmbedArgs &a, uint32_t piec
     const uint32_t lo = first_start < begin && !head ? first_end : begin;
     const uint32_t hi = last_end > edge && last_end - last_start <= a.piece && last_start >= begin ? last_end : edge;
     if (lo >= hi) return;
-    const uint32_t from = first_column(a, c);
+    const uint32_t from = first_column<N>(a, c);
     const bool writes = c < a.dim;                          // (the last team's lanes behind the row take part, and write nothing)
     const char *const in = static_cast<const char *>(a.in) + (uint64_t)from * Elements<IN16>::kBytes;
     const uint32_t k0 = lo - begin, k1 = hi - begin;        // at most 64 places: `piece`, and one less of the last row
-    float sum[8] = {};
+    float sum[N] = {};
     uint32_t row = __builtin_amdgcn_readlane(token, k0);
     bool in_head = head;
-    typename Elements<IN16>::Raw raw[2][kBatch];
-    auto load = [&](typename Elements<IN16>::Raw *r, uint32_t k) {
+    Quad raw[2][kBatch];
+    auto load = [&](Quad *r, uint32_t k) {
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
             const uint64_t at_row = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(position, min(k + j, k1 - 1)) * a.in_stride;
             const char *const at = in + at_row * Elements<IN16>::kBytes;
-            r[j] = PAST ? Elements<IN16>::load8_past(at, 0) : Elements<IN16>::load8(at, 0);
+            r[j] = Lane16<IN16>::template load<PAST>(at, 0);
         }
     };
     auto put = [&](uint32_t row, bool head, bool tail) {
         if (!writes) return;
-        if (head || tail) put_partial(a, piece, tail && !head, c, sum);
-        else put_columns<OUT16>(a, row, c, from, sum);
+        if (head || tail) put_partial<N>(a, piece, tail && !head, c, sum);
+        else put_columns<OUT16, N>(a, row, c, from, sum);
     };
-    auto add = [&](const typename Elements<IN16>::Raw *r, uint32_t k) {
+    auto add = [&](const Quad *r, uint32_t k) {
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
             if (k + j >= k1) break;
@@ -406,12 +412,12 @@ __device__ __forceinline__ void sum_piece_wave(const EmbedArgs &a, uint32_t piec
                 in_head = false;
                 row = next;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+                for (int e = 0; e < N; ++e) sum[e] = 0.0f;
             }
-            float x[8];
-            Elements<IN16>::unpack(r[j], x);
+            float x[N];
+            Lane16<IN16>::unpack(r[j], x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += x[e];
+            for (int e = 0; e < N; ++e) sum[e] += x[e];
         }
     };
     load(raw[0], k0);
@@ -460,12 +466,12 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(const EmbedArg
     const uint64_t team = ((uint64_t)blockIdx.x * kEmbedThreads + threadIdx.x) >> a.team_bits;
     if (WAVE) {
         for (uint64_t item = __builtin_amdgcn_readfirstlane((uint32_t)team); item < items; item += teams) {
-            const uint32_t piece = (uint32_t)(item / a.tiles), c = ((uint32_t)(item % a.tiles) << 6 | lane) * 8;
+            const uint32_t piece = (uint32_t)(item / a.tiles), c = ((uint32_t)(item % a.tiles) << 6 | lane) * Lane16<IN16>::kPer;
             sum_piece_wave<IN16, OUT16, PAST>(a, piece, c);
         }
         return;
     }
-    const uint32_t total = a.span[a.vocab].x, c = (threadIdx.x & ((1u << a.team_bits) - 1)) * 8;        // (one tile)
+    const uint32_t total = a.span[a.vocab].x, c = (threadIdx.x & ((1u << a.team_bits) - 1)) * Lane16<IN16>::kPer;        // (one tile)
     for (uint64_t item = team; item < items; item += teams)
         if (c < a.dim) sum_piece<IN16, OUT16>(a, (uint32_t)item, c, total);
 }
@@ -481,6 +487,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_few_kernel(const EmbedArg
 {
     __shared__ uint32_t tokens[kFewTokens];
     __shared__ uint32_t named[kEmbedThreads / kLanes][2];
+    constexpr int N = Lane16<IN16>::kPer;
     const uint32_t lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
     tokens[threadIdx.x] = threadIdx.x < a.n ? token_at<WIDE>(a.tokens, threadIdx.x, a.vocab) : 0xFFFFFFFFu;
     if (lane < 2) named[wave][lane] = 0;
@@ -499,7 +506,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_few_kernel(const EmbedArg
     }
     const uint32_t item = __builtin_amdgcn_readfirstlane(blockIdx.x * (kEmbedThreads / kLanes) + wave), i = item / a.tiles;
     if (i >= a.n) return;
-    const uint32_t row = __builtin_amdgcn_readfirstlane(tokens[i]), c = (item % a.tiles * kLanes + lane) * 8;
+    const uint32_t row = __builtin_amdgcn_readfirstlane(tokens[i]), c = (item % a.tiles * kLanes + lane) * N;
     if (row == 0xFFFFFFFFu) return;
     uint64_t same[kFewTokens / kLanes];
 #pragma unroll
@@ -509,14 +516,14 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_few_kernel(const EmbedArg
         const uint64_t before = k < i / kLanes ? ~0ull : k == i / kLanes ? (1ull << i % kLanes) - 1 : 0;
         if (same[k] & before) return;
     }
-    const uint32_t from = first_column(a, c);
-    float sum[8] = {};
+    const uint32_t from = first_column<N>(a, c);
+    float sum[N] = {};
 #pragma unroll
     for (uint32_t k = 0; k < kFewTokens / kLanes; ++k) {
         uint64_t left = same[k];
         while (left) {
             constexpr int kBatch = 4;
-            typename Elements<IN16>::Raw raw[kBatch];
+            Quad raw[kBatch];
             int count = 0;
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
@@ -529,14 +536,14 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_few_kernel(const EmbedArg
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
                 if (j >= count) break;
-                float x[8];
-                Elements<IN16>::unpack(raw[j], x);
+                float x[N];
+                Lane16<IN16>::unpack(raw[j], x);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] += x[e];
+                for (int e = 0; e < N; ++e) sum[e] += x[e];
             }
         }
     }
-    if (c < a.dim) put_columns<OUT16>(a, row, c, from, sum);
+    if (c < a.dim) put_columns<OUT16, N>(a, row, c, from, sum);
 }
 
 // The rows with more than `piece` tokens: the piece where such a row begins adds its parts, each wavefront of the workgroup a
@@ -546,7 +553,8 @@ constexpr uint32_t kJoinPieces = 4;                        // pieces of a workgr
 template <bool IN16, bool OUT16>
 __global__ __launch_bounds__(kJoinWaves * kLanes) void embed_join_kernel(const EmbedArgs a)
 {
-    __shared__ float lds[kJoinWaves][8][kLanes];
+    constexpr int N = Lane16<IN16>::kPer;
+    __shared__ float lds[kJoinWaves][N][kLanes];
     const uint32_t lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes, total = a.span[a.vocab].x;
     // a lane looks at a piece
     const uint64_t at = (uint64_t)blockIdx.x * kJoinPieces + lane, at_edge = (at + 1) * a.piece;
@@ -564,33 +572,31 @@ __global__ __launch_bounds__(kJoinWaves * kLanes) void embed_join_kernel(const E
         const uint32_t row = __builtin_amdgcn_readlane(its_row, which), to = __builtin_amdgcn_readlane(its_end, which);
         const uint32_t parts = (to - 1) / a.piece - piece + 1;                 // the first is the second row of its piece
         const uint32_t run = (parts + kJoinWaves - 1) / kJoinWaves, begin = wave * run, end = min(begin + run, parts);
-        for (uint32_t c0 = blockIdx.y * kLanes * 8; c0 < a.dim; c0 += gridDim.y * kLanes * 8) {
-            const uint32_t c = min(c0 + lane * 8, (a.dim - 1) / 8 * 8), from = first_column(a, c);
-            float sum[8] = {};
+        for (uint32_t c0 = blockIdx.y * kLanes * N; c0 < a.dim; c0 += gridDim.y * kLanes * N) {
+            const uint32_t c = min(c0 + lane * N, (a.dim - 1) / N * N), from = first_column<N>(a, c);
+            float sum[N] = {};
             for (uint32_t p = begin; p < end; p += kAheadRows) {
-                Elements<false>::Raw raw[kAheadRows];
+                float raw[kAheadRows][N];
 #pragma unroll
                 for (int k = 0; k < kAheadRows; ++k) {
                     const uint32_t part = min(p + k, end - 1);
-                    raw[k] = Elements<false>::load8(partial_at(a, piece + part, part == 0, c), 0);
+                    load_floats<false, N>(partial_at<N>(a, piece + part, part == 0, c), 0, raw[k]);
                 }
 #pragma unroll
                 for (int k = 0; k < kAheadRows; ++k) {
-                    float x[8];
-                    Elements<false>::unpack(raw[k], x);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) sum[e] += p + k < end ? x[e] : 0.0f;       // (no branch: behind one a load would be moved)
+                    for (int e = 0; e < N; ++e) sum[e] += p + k < end ? raw[k][e] : 0.0f;       // (no branch: behind one a load would be moved)
                 }
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) lds[wave][e][lane] = sum[e];
+            for (int e = 0; e < N; ++e) lds[wave][e][lane] = sum[e];
             __syncthreads();
             if (wave == 0) {
                 const uint32_t waves = (parts + run - 1) / run;
                 for (uint32_t w = 1; w < waves; ++w)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) sum[e] += lds[w][e][lane];
-                if (c0 + lane * 8 < a.dim) put_columns<OUT16>(a, row, c, from, sum);
+                    for (int e = 0; e < N; ++e) sum[e] += lds[w][e][lane];
+                if (c0 + lane * N < a.dim) put_columns<OUT16, N>(a, row, c, from, sum);
             }
             __syncthreads();
         }
@@ -617,7 +623,7 @@ struct EmbedPlan { uint32_t bucket_bits, row_bits, piece, pieces, team_bits, til
 static EmbedPlan embed_plan(const solo_embedding_shape *s)
 {
     EmbedPlan p;
-    const uint64_t n = s->tokens, groups = (s->dim + 7) / 8;
+    const uint64_t n = s->tokens, per = s->rows_dtype == SOLO_BF16 ? 8 : 4, groups = (s->dim + per - 1) / per;      // (columns of a lane)
     const uint64_t rows = s->vocab ? s->vocab : 1;
     p.bucket_bits = bits_for(kMinBuckets);
     while (((rows - 1) >> p.bucket_bits) >> kMaxRowBits) ++p.bucket_bits;
@@ -634,7 +640,7 @@ static EmbedPlan embed_plan(const solo_embedding_shape *s)
     p.order = take(4 * n);
     p.sorted = take(4 * n);
     p.span = take(8 * (s->vocab + 1));
-    p.partial = take(n > p.piece ? 2ull * p.pieces * p.tiles * (8ull << p.team_bits) * sizeof(float) : 0);
+    p.partial = take(n > p.piece ? 2ull * p.pieces * p.tiles * (per << p.team_bits) * sizeof(float) : 0);
     p.bytes = at;
     return p;
 }
@@ -662,7 +668,8 @@ static void sum_rows(const EmbedArgs &a, const EmbedPlan &p, uint32_t sum_groups
     const uint32_t grid = sum_groups + a.zero_groups;
     if (grid) hipLaunchKernelGGL((p.team_bits < 6 ? embed_sum_kernel<IN16, OUT16, false, false>
                                      : past ? embed_sum_kernel<IN16, OUT16, true, true> : embed_sum_kernel<IN16, OUT16, true, false>), dim3(grid), dim3(kEmbedThreads), 0, stream, a);
-    const uint32_t tiles = (a.dim + kLanes * 8 - 1) / (kLanes * 8);
+    constexpr uint32_t kColumns = kLanes * Lane16<IN16>::kPer;
+    const uint32_t tiles = (a.dim + kColumns - 1) / kColumns;
     if (p.pieces > 1)
         hipLaunchKernelGGL((embed_join_kernel<IN16, OUT16>), dim3((p.pieces + kJoinPieces - 1) / kJoinPieces, tiles < 16 ? tiles : 16), dim3(kJoinWaves * kLanes), 0, stream, a);
 }
@@ -738,7 +745,8 @@ int solo_embedding_grad(const void *grad_rows, const void *tokens, void *grad_ta
     hipStream_t s = (hipStream_t)stream;
     const bool in16 = shape->rows_dtype == SOLO_BF16, out16 = shape->table_dtype == SOLO_BF16, wide = shape->token_bits == 64;
     if (a.n != 0 && a.n <= kFewTokens) {
-        a.tiles = (a.dim + kLanes * 8 - 1) / (kLanes * 8);
+        const uint32_t columns = kLanes * (in16 ? 8 : 4);
+        a.tiles = (a.dim + columns - 1) / columns;
         if (in16) out16 ? few_tokens<true, true>(a, wide, s) : few_tokens<true, false>(a, wide, s);
         else out16 ? few_tokens<false, true>(a, wide, s) : few_tokens<false, false>(a, wide, s);
         return launched();

@@ -1,5 +1,5 @@
-// What the operators around the step have in common: loads and stores of eight consecutive elements, reductions over a
-// wavefront and a workgroup, host-side checks.
+// What the operators around the step have in common: loads and stores of consecutive elements, reductions over a wavefront and a
+// workgroup, host-side checks.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -44,68 +44,9 @@ struct Elements {
         if (BF16) static_cast<uint16_t *>(base)[i] = (uint16_t)to_bf16(x, x);
         else static_cast<float *>(base)[i] = x;
     }
-    // Elements i .. i + 7.
-    struct Raw { Quad q[BF16 ? 1 : 2]; };
-    __device__ __forceinline__ static Raw load8(const void *base, uint64_t i)
-    {
-        Raw r;
-        const char *at = static_cast<const char *>(base) + i * kBytes;
-#pragma unroll
-        for (int k = 0; k < (BF16 ? 1 : 2); ++k) r.q[k] = *reinterpret_cast<const Quad *>(at + 16 * k);
-        return r;
-    }
-    __device__ __forceinline__ static void unpack(const Raw &r, float x[8])
-    {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (BF16) {
-                x[2 * k] = bf16_low(r.q[0][k]);
-                x[2 * k + 1] = bf16_high(r.q[0][k]);
-            } else {
-                x[k] = __uint_as_float(r.q[0][k]);
-                x[4 + k] = __uint_as_float(r.q[BF16 ? 0 : 1][k]);
-            }
-        }
-    }
-    __device__ __forceinline__ static void store8(void *base, uint64_t i, const float x[8])
-    {
-        char *at = static_cast<char *>(base) + i * kBytes;
-        Quad a, b;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            a[k] = BF16 ? to_bf16(x[2 * k], x[2 * k + 1]) : __float_as_uint(x[k]);
-            b[k] = __float_as_uint(x[4 + k]);
-        }
-        *reinterpret_cast<Quad *>(at) = a;
-        if (!BF16) *reinterpret_cast<Quad *>(at + 16) = b;
-    }
-    // Past the caches: what is written once and not read soon.
-    __device__ __forceinline__ static void store8_past(void *base, uint64_t i, const float x[8])
-    {
-        char *at = static_cast<char *>(base) + i * kBytes;
-        Quad a, b;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            a[k] = BF16 ? to_bf16(x[2 * k], x[2 * k + 1]) : __float_as_uint(x[k]);
-            b[k] = __float_as_uint(x[4 + k]);
-        }
-        __builtin_nontemporal_store(a, reinterpret_cast<Quad *>(at));
-        if (!BF16) __builtin_nontemporal_store(b, reinterpret_cast<Quad *>(at + 16));
-    }
-    __device__ __forceinline__ static Raw load8_past(const void *base, uint64_t i)
-    {
-        Raw r;
-        const char *at = static_cast<const char *>(base) + i * kBytes;
-#pragma unroll
-        for (int k = 0; k < (BF16 ? 1 : 2); ++k) r.q[k] = __builtin_nontemporal_load(reinterpret_cast<const Quad *>(at + 16 * k));
-        return r;
-    }
 };
 
-// 16 bytes a lane: eight bf16 or four fp32 elements, so that an instruction of a wavefront reads or writes 1 KB without gaps.
-// (Eight fp32 elements a lane, as two halves, leave gaps of 16 bytes: a gradient of 201 MB, stored past the caches, then took 109 us instead of 91.)
-// `i` is an element; `near`: less than 4 GiB behind a base that is the same for the wavefront, which saves registers of address.
-// `n` elements from element i on, 4 or 8 of them, to floats.
+// N elements from element i on, 4 or 8 of them, to floats.
 template <bool BF16, int N>
 __device__ __forceinline__ void load_floats(const void *base, uint64_t i, float x[N])
 {
@@ -125,6 +66,26 @@ __device__ __forceinline__ void load_floats(const void *base, uint64_t i, float 
     }
 }
 
+// The same to memory.
+template <bool BF16, int N>
+__device__ __forceinline__ void store_floats(void *base, uint64_t i, const float x[N])
+{
+    typedef uint32_t Half __attribute__((ext_vector_type(2), aligned(2)));
+    char *at = static_cast<char *>(base) + i * (BF16 ? 2 : 4);
+#pragma unroll
+    for (int k = 0; k < N; k += 4) {
+        if (BF16) {
+            *reinterpret_cast<Half *>(at + 2 * k) = Half{to_bf16(x[k], x[k + 1]), to_bf16(x[k + 2], x[k + 3])};
+        } else {
+            *reinterpret_cast<Quad *>(at + 4 * k) =
+                Quad{__float_as_uint(x[k]), __float_as_uint(x[k + 1]), __float_as_uint(x[k + 2]), __float_as_uint(x[k + 3])};
+        }
+    }
+}
+
+// 16 bytes a lane: eight bf16 or four fp32 elements, so that an instruction of a wavefront reads or writes 1 KB without gaps.
+// (Eight fp32 elements a lane, as two halves, leave gaps of 16 bytes: a gradient of 201 MB, stored past the caches, then took 109 us instead of 91.)
+// `i` is an element; `near`: less than 4 GiB behind a base that is the same for the wavefront, which saves registers of address.
 template <bool BF16>
 struct Lane16 {
     static constexpr int kBytes = BF16 ? 2 : 4, kPer = 16 / kBytes;

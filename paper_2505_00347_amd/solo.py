@@ -465,8 +465,9 @@ class SoloEmbedding:
         lib()
         self.vocab, self.dim, self.tokens, self.scale, self.device = vocab, dim, tokens, scale, _torch.device(device)
         self._seen = self._made = None
-        shape = solo_embedding_shape(vocab, dim, tokens, dim, dim, SOLO_FP32, SOLO_FP32, 64, 0, scale, 0)
-        self.workspace_bytes = solo_embedding_workspace_bytes(shape)
+        # (of the rows' type that needs more: a call says which it has)
+        self.workspace_bytes = max(solo_embedding_workspace_bytes(solo_embedding_shape(vocab, dim, tokens, dim, dim, SOLO_FP32, rows, 64, 0, scale, 0))
+                                   for rows in (SOLO_FP32, SOLO_BF16))
         if not self.workspace_bytes:
             raise SoloError(SOLO_E_INVALID)
         self.workspace = None                      # of the first gradient

@@ -202,7 +202,7 @@ def test_lookup(dtype, out_dtype, n, vocab, dim, extra, ids_dtype):
 GRADS = [(1, 1, 1, 0, "any"), (3, 50, 7, 0, "any"), (31, 5, 8, 0, "few"), (32, 40, 24, 0, "same"), (33, 40, 24, 1, "same"), (64, 70, 65, 0, "same"),
          (500, 40, 9, 0, "padded"), (1000, 3, 64, 2, "any"), (1025, 2000, 130, 0, "few"), (3000, 700, 515, 5, "few"),
          (4097, 17, 40, 0, "padded"), (5000, 1, 16, 0, "same"), (2049, 9000, 33, 0, "any"), (700, 600, 1000, 8, "few"), (96, 3000, 768, 0, "any"),
-         (256, 300, 64, 0, "few"), (257, 300, 64, 0, "few"), (2000, 600, 4099, 0, "few"), (40_000, 50, 8, 0, "few"), (300_000, 70_000, 1, 0, "any")]
+         (256, 300, 64, 0, "few"), (257, 300, 64, 0, "few"), (2000, 600, 4099, 0, "few"), (3000, 40, 129, 0, "few"), (3000, 40, 255, 1, "same"), (3000, 40, 257, 0, "few"), (900, 30, 515, 0, "same"), (40_000, 50, 8, 0, "few"), (300_000, 70_000, 1, 0, "any")]
 
 
 @pytest.mark.parametrize("ids_dtype", [torch.int64, torch.int32])
