@@ -11,7 +11,7 @@
 // others.  It counts the tokens of the buckets before its own, which is where its part of the sorted list begins, and its own by row
 // and wavefront; then it places them.
 //
-// Bound by memory.  16384 tokens of a bf16 table of 32000 x 4096: lookup 31 us (178 MB with every row that occurs once), gradient 83 us
+// Bound by memory.  16384 tokens of a bf16 table of 32000 x 4096: lookup 31 us (178 MB with every row that occurs once), gradient 84 us
 // (396 MB; the sort 8.8, the sums and zeros 67, the parts of frequent tokens 7.6 us); 396 MB take 72 us at the rate of a large copy.
 #include "solo_ops.h"
 
@@ -631,8 +631,9 @@ static EmbedPlan embed_plan(const solo_embedding_shape *s)
     p.team_bits = bits_for(groups);
     if (p.team_bits > 6) p.team_bits = 6;
     p.tiles = (uint32_t)((groups + (1u << p.team_bits) - 1) >> p.team_bits);
-    // (wide rows: pieces of 16 write twice as many parts of frequent tokens, 111 instead of 106 us for 16384 x 4096, and 64 are too few
-    // wavefronts; narrow ones have few lanes a piece: 40000 tokens of 5000 x 100 85 us with 32, 66 us with 8)
+    // (wide rows: pieces of 16 write twice as many parts of frequent tokens, bf16 16384 x 4096 takes 90 us with 16 and 84 us with 32, and
+    // pieces of 64 are too few wavefronts; narrow ones have few lanes a piece: 40000 tokens of a bf16 table of 5000 x 100 take 54 us
+    // with 32, 41 us with 16 and 37 us with 8)
     p.piece = p.team_bits == 6 ? 32 : 8;
     p.pieces = (uint32_t)((n + p.piece - 1) / p.piece);
     size_t at = 0;

@@ -13,7 +13,7 @@
 // few others reach (row_top()); only the groups that can hold one are looked at again, one for most threads that have any.
 //
 // Bound by memory where there are many rows: sums of 4096 x 50304 bf16 67 us (6.1 TB/s), with rank and twenty alternatives 81 us; loss and
-// gradient of 8192 x 32000 in one call 166 us (the row stays in registers: 1 GB, 6 TB/s), of 1000 x 50257 fp32 in two calls 98 us.
+// gradient of 8192 x 32000 in one call 167 us (the row stays in registers: 1 GB, 6 TB/s), of 1000 x 50257 fp32 in two calls 98 us.
 // A logit costs some twelve instructions and an exponential, 36 us of vector issue for 4096 x 50304; the alternatives add what a row costs once.
 // A single row of 50257 takes 9.8 us: one compute unit's exponentials, and loads of 4 us.
 #include "solo_ops.h"
