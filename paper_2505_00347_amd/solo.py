@@ -464,7 +464,7 @@ class SoloEmbedding:
     def __init__(self, vocab, dim, tokens, scale=1.0, device="cuda"):
         lib()
         self.vocab, self.dim, self.tokens, self.scale, self.device = vocab, dim, tokens, scale, _torch.device(device)
-        self._seen = self._made = None
+        self._last = None, None
         # (of the rows' type that needs more: a call says which it has)
         self.workspace_bytes = max(solo_embedding_workspace_bytes(solo_embedding_shape(vocab, dim, tokens, dim, dim, SOLO_FP32, rows, 64, 0, scale, 0))
                                    for rows in (SOLO_FP32, SOLO_BF16))
@@ -474,9 +474,11 @@ class SoloEmbedding:
 
     def _shape(self, table, rows, ids, flags):
         """The C struct of these tensors.  The checks and the struct are made when the tensors' layout is another than in the
-        call before: 3.6 us of the 5.9 that a lookup of a few tokens took."""
-        seen = _layout(table), _layout(rows), _layout(ids), flags, self.scale
-        if seen != self._seen:
+        call before: 3.6 us of the 5.9 that a lookup of a few tokens took.  (Layout and struct are read and stored as one: another thread's
+        call may come in between, and a struct of other tensors would send the kernel out of these.)"""
+        layout = _layout(table), _layout(rows), _layout(ids), flags, self.scale
+        seen, made = self._last
+        if layout != seen:
             n = ids.numel()
             if n > self.tokens:
                 raise ValueError(f"at most {self.tokens} tokens expected, got {n}")
@@ -484,8 +486,8 @@ class SoloEmbedding:
                                         _row_stride(rows, n, self.dim, "rows"), _dtype(table), _dtype(rows), _token_bits(ids, n),
                                         flags, self.scale, 0)
             _on(self.device.type, table, rows, ids)
-            self._made, self._seen = made, seen
-        return self._made
+            self._last = layout, made
+        return made
 
     def lookup(self, table, ids, out, stream=None):
         """out[i] = scale * table[ids[i]]"""
@@ -512,7 +514,7 @@ class SoloLogprob:
         if not 0 <= top <= SOLO_TOP_MAX:
             raise ValueError(f"0 to {SOLO_TOP_MAX} alternatives expected, got {top}")
         self.rows, self.cols, self.top, self.scale, self.device = rows, cols, top, scale, _torch.device(device).type
-        self._seen = self._made = None
+        self._last = None, None
         f32, i32 = dict(dtype=_torch.float32, device=device), dict(dtype=_torch.int32, device=device)
         self.logprob, self.entropy = _torch.empty(rows, **f32), _torch.empty(rows, **f32)
         self.stats = _torch.empty((rows, 2), **f32)
@@ -521,9 +523,10 @@ class SoloLogprob:
         self.top_token = _torch.empty((rows, top), **i32) if top else None
 
     def _shape(self, logits, targets, out=None):
-        """The C struct of these tensors, made when their layout is another than in the call before."""
-        seen = _layout(logits), _layout(targets), _layout(out), self.scale
-        if seen != self._seen:
+        """The C struct of these tensors, made when their layout is another than in the call before (as in SoloEmbedding)."""
+        layout = _layout(logits), _layout(targets), _layout(out), self.scale
+        seen, made = self._last
+        if layout != seen:
             r = logits.shape[0]
             if r > self.rows:
                 raise ValueError(f"at most {self.rows} rows expected, got {r}")
@@ -536,8 +539,8 @@ class SoloLogprob:
             made = solo_logits(r, self.cols, stride, grad_stride, _dtype(logits), 64 if targets is None else _token_bits(targets, r),
                                self.top, 0, self.scale, 0)
             _on(self.device, logits, targets, out)
-            self._made, self._seen = made, seen
-        return self._made
+            self._last = layout, made
+        return made
 
     def forward(self, logits, targets, stream=None):
         """(logprob, entropy[, rank][, top_logprob, top_token]); without targets, logprob and rank are None."""
