@@ -436,7 +436,8 @@ class SoloGradNorm:
         self.workspace = _torch.empty(solo_norm_workspace_bytes(self.units), dtype=_torch.uint8, device=device)
         self.results = _torch.zeros(1, device=device), _torch.ones(1, device=device), _torch.zeros(self.count, device=device)
         self.writes = clipped is not None
-        self._keep = grads, clipped                # the buffers the table points to
+        # the buffers the table points to: the caller's lists may change, and so may the storage that a tensor of theirs names
+        self._keep = [t.detach() for t in (*grads, *(clipped or ())) if t is not None]
 
     def _run(self, name, max_norm, unscale, stream):
         if unscale is not None:

@@ -1,7 +1,10 @@
 """The handles of the operators around the step: what they keep between calls (no GPU: nothing is launched)."""
+import gc
 import sys
 import threading
+import weakref
 
+import numpy
 import pytest
 import torch
 
@@ -49,3 +52,34 @@ def test_threads_that_share_log_probabilities_get_the_struct_of_their_own_tensor
         return lambda: plan._shape(x, t).rows == n
 
     assert interleaved([call(3), call(5000)]) == 0
+
+
+class Memory:
+    """Tensors and references to the memory behind them that do not keep it."""
+
+    def __init__(self):
+        self.alive = []
+
+    def tensor(self, n=100):
+        array = numpy.zeros(n, dtype=numpy.float32)
+        self.alive.append(weakref.ref(array))
+        return torch.from_numpy(array)
+
+    def count(self):
+        gc.collect()
+        return sum(r() is not None for r in self.alive)
+
+
+@pytest.mark.parametrize("clips", [False, True])
+def test_the_norms_table_keeps_the_memory_that_it_points_to(clips):
+    memory = Memory()
+    grads = [memory.tensor() for _ in range(3)]
+    clipped = [memory.tensor() for _ in range(3)] if clips else None
+    plan = solo.SoloGradNorm(grads, clipped, device="cpu")
+    grads[0].data = torch.zeros(100)                       # (another memory of the same tensor)
+    grads.clear()
+    if clips:
+        clipped[:] = [torch.zeros(100)] * 3
+    assert memory.count() == (6 if clips else 3)
+    del plan
+    assert memory.count() == 0
