@@ -287,17 +287,18 @@ class SoloMultiTable:
         import torch
         self.cfg, self.count = cfg, len(items)
         arr = (solo_tensor * self.count)()
+        self._keep = []                            # the memory the table points to (behind an address it is the caller's to keep)
         for k, it in enumerate(items):
             p, g, st = it[0], it[1], it[2]
             h = it[3] if len(it) > 3 else None
-            arr[k] = solo_tensor(_ptr(p), _ptr(h), _ptr(g), _ptr(st.m_codes), _ptr(st.m_scale),
-                                 _ptr(st.v_codes), _ptr(st.v_scale), _ptr(st.v_base), st.n)
+            buffers = p, h, g, st.m_codes, st.m_scale, st.v_codes, st.v_scale, st.v_base
+            arr[k] = solo_tensor(*map(_ptr, buffers), st.n)
+            self._keep += [t.detach() for t in buffers if hasattr(t, "detach")]
         self.units = solo_multi_units(arr, self.count, cfg)
         nbytes = solo_multi_table_bytes(self.count, self.units)
         host = torch.empty((nbytes + 15) // 16 * 16, dtype=torch.uint8)
         _, self.flags = solo_multi_table_build(arr, self.count, cfg, host.data_ptr(), nbytes)
         self.table = host.to(device)
-        self._keep = items                         # the buffers the table points to
 
     def step(self, step, grad_scale=None, stream=None):
         return solo_adamw_step_multi(self.table, self.count, self.units, self.flags, grad_scale, step,

@@ -83,3 +83,19 @@ def test_the_norms_table_keeps_the_memory_that_it_points_to(clips):
     assert memory.count() == (6 if clips else 3)
     del plan
     assert memory.count() == 0
+
+
+def test_the_steps_table_keeps_the_memory_that_it_points_to():
+    memory, cfg = Memory(), solo.make_config(4, 4, 128)
+    items = [[memory.tensor(256), memory.tensor(256), solo.SoloState(256, cfg, device="cpu", init=False)] for _ in range(2)]
+    for item in items:
+        for name in ("m_scale", "v_scale", "v_base"):
+            setattr(item[2], name, memory.tensor(2))
+    table = solo.SoloMultiTable(items, cfg, device="cpu")
+    items[0][1].data = torch.zeros(256)
+    items[1].clear()
+    items.clear()
+    del item
+    assert memory.count() == 10
+    del table
+    assert memory.count() == 0
