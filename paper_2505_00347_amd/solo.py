@@ -82,12 +82,13 @@ _lib = None
 _step = _multi = None            # the calls of a step: native, or through ctypes
 _calls = None                    # those of the operators around the step, by name
 _torch = None
+_device_now = _stream_now = None    # torch's current device, and the handle of the current stream of a device
 _loading = threading.RLock()
 
 
 def lib():
     """Load libsolo.so (built by ``python -m paper_2505_00347_amd.build``)."""
-    global _lib, _step, _multi, _calls, _torch
+    global _lib, _step, _multi, _calls, _torch, _device_now, _stream_now
     if _lib is not None:
         return _lib
     with _loading:
@@ -109,6 +110,8 @@ def lib():
                 native.bind_operations({name: (C.cast(getattr(L, name), C.c_void_p).value, call) for name, call in calls.items()})
                 calls = {name: getattr(native, name) for name in _OPERATIONS}
             _step, _multi, _calls, _torch = step, multi, calls, torch
+            _device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+            _stream_now = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
             _lib = L                 # last: a thread that finds it set finds the others set
     return _lib
 
@@ -406,7 +409,54 @@ def _on(device, *tensors):
             raise ValueError(f"tensors on {device} expected, got {t.device}")
 
 
-class SoloGradNorm:
+def _number_of(stream):
+    number = stream.cuda_stream
+    return getattr(number, "value", number) or 0           # (one of ctypes; None: the default stream)
+
+
+class _Handle:
+    """The streams of a handle.  Its buffers are made on torch's current stream, and a call may run on another one (`stream`, or what is
+    current then).  The first call on such a stream waits for what was enqueued on the current stream when the buffers were made (a
+    new buffer may be memory that earlier work still uses), and the allocator learns that this stream uses them.  The calls of
+    a handle follow each other, each with the buffers that the one before has left: on several streams the caller orders them, and of
+    calls under a stream's bare number it keeps the handle until they are done."""
+
+    _buffers, _home = (), None
+
+    def _hold(self, *buffers):
+        self._buffers, self._others, self._home, self._ready = [b for b in buffers if b is not None], {}, None, None
+        if self._buffers[0].is_cuda:
+            stream = _torch.cuda.current_stream(self._buffers[0].device)
+            self._home = stream.cuda_stream
+            if not _torch.cuda.is_current_stream_capturing():
+                self._ready = stream.record_event()
+
+    def _on_stream(self, stream):
+        """The number of the stream that a call runs on, ready for the buffers."""
+        number = _stream_now(_device_now()) if stream is None else stream if isinstance(stream, int) else _number_of(stream)
+        if number != self._home and self._buffers and number not in self._others:
+            self._visit(stream, number)
+        return number
+
+    def _visit(self, stream, number):
+        bare = isinstance(stream, int)
+        if stream is None:
+            stream = _torch.cuda.current_stream()
+        elif not isinstance(stream, _torch.cuda.Stream):
+            stream = _torch.cuda.ExternalStream(number)
+        with _torch.cuda.stream(stream):
+            if _torch.cuda.is_current_stream_capturing():  # (a graph's nodes wait for nothing outside; capturing begins on an idle GPU)
+                return
+        if self._ready is not None:
+            stream.wait_event(self._ready)
+        if bare:                                           # (there may be another stream of this number later, or none)
+            return
+        for b in self._buffers:
+            b.record_stream(stream)
+        self._others[number] = stream
+
+
+class SoloGradNorm(_Handle):
     """Global norm of a set of gradient tensors, and clipping: the device table of the tensors (of any shape, contiguous,
     float32 or bfloat16) with its workspace and results.  `clipped`: tensors of the same shapes and types that clip()
     writes; they may be the gradients themselves (clipping in place).
@@ -437,6 +487,7 @@ class SoloGradNorm:
         self.workspace = _torch.empty(solo_norm_workspace_bytes(self.units), dtype=_torch.uint8, device=device)
         self.results = _torch.zeros(1, device=device), _torch.ones(1, device=device), _torch.zeros(self.count, device=device)
         self.writes = clipped is not None
+        self._hold(self.table, self.workspace, *self.results)
         # the buffers the table points to: the caller's lists may change, and so may the storage that a tensor of theirs names
         self._keep = [t.detach() for t in (*grads, *(clipped or ())) if t is not None]
 
@@ -446,7 +497,7 @@ class SoloGradNorm:
                 raise TypeError(f"unscale: one float32 value expected, got {unscale.numel()} of {unscale.dtype}")
             if unscale.device != self.device:
                 raise ValueError(f"unscale: on {self.device} expected, got {unscale.device}")
-        _operation(name, True, self.table, self.count, self.units, unscale, max_norm, *self.results, self.workspace, stream)
+        _operation(name, True, self.table, self.count, self.units, unscale, max_norm, *self.results, self.workspace, self._on_stream(stream))
         return self.results
 
     def norm(self, max_norm=float("inf"), unscale=None, stream=None):
@@ -458,7 +509,7 @@ class SoloGradNorm:
         return self._run("solo_grad_clip", max_norm, unscale, stream)
 
 
-class SoloEmbedding:
+class SoloEmbedding(_Handle):
     """Lookup in an embedding table [vocab, dim] and the table's gradient, for up to `tokens` tokens a call: the workspace
     that the gradient needs.  Tables and rows may be float32 or bfloat16, each on its own; their rows contiguous, at any
     distance; tokens int64 or int32, those outside the table are padding."""
@@ -494,7 +545,7 @@ class SoloEmbedding:
     def lookup(self, table, ids, out, stream=None):
         """out[i] = scale * table[ids[i]]"""
         shape = self._shape(table, out, ids, 0)
-        _operation("solo_embedding", True, table, ids, out, C.addressof(shape), stream)
+        _operation("solo_embedding", True, table, ids, out, C.addressof(shape), self._on_stream(stream))
         return out
 
     def grad(self, grad_rows, ids, out, accumulate=False, stream=None):
@@ -502,11 +553,12 @@ class SoloEmbedding:
         shape = self._shape(out, grad_rows, ids, SOLO_EMBEDDING_ACCUMULATE if accumulate else 0)
         if self.workspace is None:
             self.workspace = _torch.empty(self.workspace_bytes, dtype=_torch.uint8, device=self.device)
-        _operation("solo_embedding_grad", True, grad_rows, ids, out, self.workspace, self.workspace_bytes, C.addressof(shape), stream)
+            self._hold(self.workspace)
+        _operation("solo_embedding_grad", True, grad_rows, ids, out, self.workspace, self.workspace_bytes, C.addressof(shape), self._on_stream(stream))
         return out
 
 
-class SoloLogprob:
+class SoloLogprob(_Handle):
     """Log probabilities, entropies, ranks and `top` alternatives of up to `rows` rows of `cols` logits (float32 or
     bfloat16, rows contiguous, at any distance), and the gradient: the buffers of the results, which the next call overwrites.
     Targets are int64 or int32; one outside the columns is a padding position."""
@@ -523,6 +575,7 @@ class SoloLogprob:
         self.rank = _torch.empty(rows, **i32) if rank else None
         self.top_logprob = _torch.empty((rows, top), **f32) if top else None
         self.top_token = _torch.empty((rows, top), **i32) if top else None
+        self._hold(self.logprob, self.entropy, self.stats, self.rank, self.top_logprob, self.top_token)
 
     def _shape(self, logits, targets, out=None):
         """The C struct of these tensors, made when their layout is another than in the call before (as in SoloEmbedding)."""
@@ -550,7 +603,7 @@ class SoloLogprob:
         none = targets is None
         logprob, rank = (None, None) if none else (self.logprob, self.rank)
         _operation("solo_logprob", True, logits, targets, logprob, self.entropy, rank, self.top_logprob, self.top_token, self.stats,
-                   C.addressof(shape), stream)
+                   C.addressof(shape), self._on_stream(stream))
         results = [logprob, self.entropy]
         if self.rank is not None:
             results.append(rank)
@@ -564,7 +617,7 @@ class SoloLogprob:
         _row_weights(grad_logprob, shape.rows, "grad_logprob", self.device)
         _row_weights(grad_entropy, shape.rows, "grad_entropy", self.device)
         _operation("solo_logprob_grad", True, logits, targets, self.entropy, self.stats, grad_logprob, grad_entropy, out,
-                   C.addressof(shape), stream)
+                   C.addressof(shape), self._on_stream(stream))
         return out
 
     def forward_grad(self, logits, targets, grad_logprob, grad_entropy, out, stream=None):
@@ -574,7 +627,7 @@ class SoloLogprob:
         _row_weights(grad_entropy, shape.rows, "grad_entropy", self.device)
         logprob = None if targets is None else self.logprob
         _operation("solo_logprob_with_grad", True, logits, targets, grad_logprob, grad_entropy, logprob, self.entropy, out,
-                   C.addressof(shape), stream)
+                   C.addressof(shape), self._on_stream(stream))
         if shape.rows != self.rows:
             return None if logprob is None else logprob[:shape.rows], self.entropy[:shape.rows], out
         return logprob, self.entropy, out

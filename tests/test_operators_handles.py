@@ -1,8 +1,10 @@
 """The handles of the operators around the step: what they keep between calls (no GPU: nothing is launched)."""
+import ctypes
 import gc
 import sys
 import threading
 import weakref
+from types import SimpleNamespace
 
 import numpy
 import pytest
@@ -99,3 +101,101 @@ def test_the_steps_table_keeps_the_memory_that_it_points_to():
     assert memory.count() == 10
     del table
     assert memory.count() == 0
+
+
+class Streams:
+    """As much of torch as a handle needs to see which stream its buffers are used on; nothing is launched."""
+
+    def __init__(self):
+        outer = self
+
+        class Stream:
+            def __init__(self, number):
+                self.cuda_stream, self.waits, self.capturing = number, [], False
+
+            def record_event(self):
+                return "event of %d" % self.cuda_stream
+
+            def wait_event(self, event):
+                self.waits.append(event)
+
+            def __enter__(self):
+                self.before, outer.current = outer.current, self
+
+            def __exit__(self, *_):
+                outer.current = self.before
+
+        self.Stream, self.current, self.external = Stream, Stream(7), []
+        self.cuda = SimpleNamespace(Stream=Stream, stream=lambda s: s, current_stream=lambda device=None: self.current, ExternalStream=self.bare,
+                                    is_current_stream_capturing=lambda: self.current.capturing)
+
+    def bare(self, number):
+        self.external.append(self.Stream(number))
+        return self.external[-1]
+
+    def buffer(self):
+        users = []
+        return SimpleNamespace(is_cuda=True, device="cuda:0", users=users, record_stream=users.append)
+
+
+@pytest.fixture
+def streams(monkeypatch):
+    solo.lib()
+    fake = Streams()
+    monkeypatch.setattr(solo, "_torch", fake)
+    monkeypatch.setattr(solo, "_device_now", lambda: 0)
+    monkeypatch.setattr(solo, "_stream_now", lambda device: fake.current.cuda_stream)
+    return fake
+
+
+def held(streams):
+    handle, buffers = solo._Handle(), [streams.buffer(), streams.buffer()]
+    handle._hold(buffers[0], None, buffers[1])
+    return handle, buffers
+
+
+def test_calls_on_the_stream_that_made_the_buffers(streams):
+    handle, buffers = held(streams)
+    assert handle._on_stream(None) == handle._on_stream(7) == handle._on_stream(streams.current) == 7
+    assert not streams.current.waits and not streams.external and not any(b.users for b in buffers)
+
+
+@pytest.mark.parametrize("current", [False, True])
+def test_the_first_call_on_another_stream_waits_for_the_buffers(streams, current):
+    """Their memory may be a block that work enqueued before still uses; and the allocator must not give it away under this stream's work."""
+    handle, buffers = held(streams)
+    side = streams.Stream(8)
+    if current:
+        streams.current = side
+    for _ in range(2):
+        assert handle._on_stream(None if current else side) == 8
+        assert side.waits == ["event of 7"] and all(b.users == [side] for b in buffers)
+    handle._hold(buffers[0])                               # (made anew)
+    assert handle._on_stream(side) == 8
+    assert side.waits == (["event of 7"] if current else ["event of 7"] * 2)
+
+
+def test_a_streams_bare_number_is_not_remembered(streams):
+    handle, buffers = held(streams)
+    for k in (1, 2):
+        assert handle._on_stream(9) == 9
+        assert len(streams.external) == k and streams.external[-1].cuda_stream == 9 and streams.external[-1].waits == ["event of 7"]
+    assert not any(b.users for b in buffers)
+    for none in (SimpleNamespace(cuda_stream=None), SimpleNamespace(cuda_stream=ctypes.c_void_p(0)), 0):
+        assert handle._on_stream(none) == 0
+
+
+def test_a_captured_call_waits_for_nothing_outside_of_the_graph(streams):
+    handle, buffers = held(streams)
+    side = streams.Stream(8)
+    side.capturing = True
+    assert handle._on_stream(side) == 8
+    assert not side.waits and not any(b.users for b in buffers)
+    side.capturing = False
+    assert handle._on_stream(side) == 8
+    assert side.waits == ["event of 7"] and all(b.users == [side] for b in buffers)
+
+
+def test_a_handle_without_buffers_takes_any_stream(streams):
+    handle = solo._Handle()
+    assert handle._on_stream(None) == 7 and handle._on_stream(9) == 9 and handle._on_stream(streams.Stream(8)) == 8
