@@ -394,7 +394,7 @@ def _row_weights(tensor, rows, name, device):
         return
     if tensor.dtype is not _torch.float32 or tensor.dim() != 1 or tensor.numel() != rows or not tensor.is_contiguous():
         raise ValueError(f"{name}: {rows} contiguous float32 values expected")
-    if tensor.device.type != device:
+    if tensor.device != device:
         raise ValueError(f"{name}: on {device} expected, got {tensor.device}")
 
 
@@ -405,17 +405,14 @@ def _layout(tensor):
 
 def _on(device, *tensors):
     for t in tensors:
-        if t is not None and t.device.type != device:
+        if t is not None and t.device != device:
             raise ValueError(f"tensors on {device} expected, got {t.device}")
 
 
-def _number_of(stream):
-    number = stream.cuda_stream
-    return getattr(number, "value", number) or 0           # (one of ctypes; None: the default stream)
-
-
 class _Handle:
-    """The streams of a handle.  Its buffers are made on torch's current stream, and a call may run on another one (`stream`, or what is
+    """Device and streams of a handle.  A call takes tensors of the handle's device, which has to be torch's current one.
+
+    Its buffers are made on torch's current stream, and a call may run on another one (`stream`, or what is
     current then).  The first call on such a stream waits for what was enqueued on the current stream when the buffers were made (a
     new buffer may be memory that earlier work still uses), and the allocator learns that this stream uses them.  The calls of
     a handle follow each other, each with the buffers that the one before has left: on several streams the caller orders them, and of
@@ -423,20 +420,35 @@ class _Handle:
 
     _buffers, _home = (), None
 
+    def __init__(self, device):
+        lib()
+        self.device = _torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = _torch.device("cuda", _torch.cuda.current_device())
+        self._index = self.device.index if self.device.type == "cuda" else None
+
     def _hold(self, *buffers):
         self._buffers, self._others, self._home, self._ready = [b for b in buffers if b is not None], {}, None, None
-        if self._buffers[0].is_cuda:
-            stream = _torch.cuda.current_stream(self._buffers[0].device)
+        if self._index is not None:
+            stream = _torch.cuda.current_stream(self.device)
             self._home = stream.cuda_stream
             if not _torch.cuda.is_current_stream_capturing():
                 self._ready = stream.record_event()
 
     def _on_stream(self, stream):
         """The number of the stream that a call runs on, ready for the buffers."""
-        number = _stream_now(_device_now()) if stream is None else stream if isinstance(stream, int) else _number_of(stream)
+        if self._index is None or _device_now() != self._index:
+            raise ValueError(f"a call runs on the GPU that is torch's current device, this handle is on {self.device}")
+        number = _stream_now(self._index) if stream is None else stream if isinstance(stream, int) else self._number_of(stream)
         if number != self._home and self._buffers and number not in self._others:
             self._visit(stream, number)
         return number
+
+    def _number_of(self, stream):
+        if getattr(stream, "device_index", self._index) != self._index:
+            raise ValueError(f"a stream on {self.device} expected, got {stream}")
+        number = stream.cuda_stream
+        return getattr(number, "value", number) or 0       # (one of ctypes; None: the default stream)
 
     def _visit(self, stream, number):
         bare = isinstance(stream, int)
@@ -465,25 +477,24 @@ class SoloGradNorm(_Handle):
     call overwrites.  grad_scale is what SoloState.step and SoloMultiTable.step take."""
 
     def __init__(self, grads, clipped=None, device="cuda"):
-        lib()
+        super().__init__(device)
         self.count = len(grads)
         if clipped is not None and len(clipped) != self.count:
             raise ValueError(f"{self.count} clipped tensors expected, got {len(clipped)}")
-        where = _torch.device(device).type
         arr = (solo_grad * self.count)()
         for k, g in enumerate(grads):
             c = clipped[k] if clipped is not None else None
             if not g.is_contiguous() or (c is not None and (not c.is_contiguous() or c.dtype is not g.dtype or c.shape != g.shape)):
                 raise ValueError(f"tensor {k}: contiguous gradients, and clipped ones of the same shapes and types, expected")
-            _on(where, g, c)
+            _on(self.device, g, c)
             arr[k] = solo_grad(_ptr(g), _ptr(c), g.numel(), _dtype(g), 0)
         self.units = solo_norm_units(arr, self.count)
         nbytes = solo_norm_table_bytes(self.count, self.units)
         host = _torch.empty((nbytes + 15) // 16 * 16, dtype=_torch.uint8)
         if self.count:
             solo_norm_table_build(arr, self.count, host.data_ptr(), nbytes)
+        device = self.device
         self.table = host.to(device)
-        self.device = self.table.device
         self.workspace = _torch.empty(solo_norm_workspace_bytes(self.units), dtype=_torch.uint8, device=device)
         self.results = _torch.zeros(1, device=device), _torch.ones(1, device=device), _torch.zeros(self.count, device=device)
         self.writes = clipped is not None
@@ -515,8 +526,8 @@ class SoloEmbedding(_Handle):
     distance; tokens int64 or int32, those outside the table are padding."""
 
     def __init__(self, vocab, dim, tokens, scale=1.0, device="cuda"):
-        lib()
-        self.vocab, self.dim, self.tokens, self.scale, self.device = vocab, dim, tokens, scale, _torch.device(device)
+        super().__init__(device)
+        self.vocab, self.dim, self.tokens, self.scale = vocab, dim, tokens, scale
         self._last = None, None
         # (of the rows' type that needs more: a call says which it has)
         self.workspace_bytes = max(solo_embedding_workspace_bytes(solo_embedding_shape(vocab, dim, tokens, dim, dim, SOLO_FP32, rows, 64, 0, scale, 0))
@@ -538,7 +549,7 @@ class SoloEmbedding(_Handle):
             made = solo_embedding_shape(self.vocab, self.dim, n, _row_stride(table, self.vocab, self.dim, "table"),
                                         _row_stride(rows, n, self.dim, "rows"), _dtype(table), _dtype(rows), _token_bits(ids, n),
                                         flags, self.scale, 0)
-            _on(self.device.type, table, rows, ids)
+            _on(self.device, table, rows, ids)
             self._last = layout, made
         return made
 
@@ -564,12 +575,12 @@ class SoloLogprob(_Handle):
     Targets are int64 or int32; one outside the columns is a padding position."""
 
     def __init__(self, rows, cols, top=0, rank=False, scale=1.0, device="cuda"):
-        lib()
+        super().__init__(device)
         if not 0 <= top <= SOLO_TOP_MAX:
             raise ValueError(f"0 to {SOLO_TOP_MAX} alternatives expected, got {top}")
-        self.rows, self.cols, self.top, self.scale, self.device = rows, cols, top, scale, _torch.device(device).type
+        self.rows, self.cols, self.top, self.scale = rows, cols, top, scale
         self._last = None, None
-        f32, i32 = dict(dtype=_torch.float32, device=device), dict(dtype=_torch.int32, device=device)
+        f32, i32 = dict(dtype=_torch.float32, device=self.device), dict(dtype=_torch.int32, device=self.device)
         self.logprob, self.entropy = _torch.empty(rows, **f32), _torch.empty(rows, **f32)
         self.stats = _torch.empty((rows, 2), **f32)
         self.rank = _torch.empty(rows, **i32) if rank else None

@@ -125,7 +125,7 @@ class Streams:
             def __exit__(self, *_):
                 outer.current = self.before
 
-        self.Stream, self.current, self.external = Stream, Stream(7), []
+        self.Stream, self.current, self.external, self.device = Stream, Stream(7), [], torch.device
         self.cuda = SimpleNamespace(Stream=Stream, stream=lambda s: s, current_stream=lambda device=None: self.current, ExternalStream=self.bare,
                                     is_current_stream_capturing=lambda: self.current.capturing)
 
@@ -135,7 +135,7 @@ class Streams:
 
     def buffer(self):
         users = []
-        return SimpleNamespace(is_cuda=True, device="cuda:0", users=users, record_stream=users.append)
+        return SimpleNamespace(users=users, record_stream=users.append)
 
 
 @pytest.fixture
@@ -149,7 +149,7 @@ def streams(monkeypatch):
 
 
 def held(streams):
-    handle, buffers = solo._Handle(), [streams.buffer(), streams.buffer()]
+    handle, buffers = solo._Handle("cuda:0"), [streams.buffer(), streams.buffer()]
     handle._hold(buffers[0], None, buffers[1])
     return handle, buffers
 
@@ -197,5 +197,54 @@ def test_a_captured_call_waits_for_nothing_outside_of_the_graph(streams):
 
 
 def test_a_handle_without_buffers_takes_any_stream(streams):
-    handle = solo._Handle()
+    handle = solo._Handle("cuda:0")
     assert handle._on_stream(None) == 7 and handle._on_stream(9) == 9 and handle._on_stream(streams.Stream(8)) == 8
+
+
+def test_a_handle_runs_on_its_own_device(streams, monkeypatch):
+    handle, _ = held(streams)
+    monkeypatch.setattr(solo, "_device_now", lambda: 1)
+    for stream in (None, 7, streams.current):
+        with pytest.raises(ValueError, match="cuda:0"):
+            handle._on_stream(stream)
+    monkeypatch.setattr(solo, "_device_now", lambda: 0)
+    other = streams.Stream(7)
+    other.device_index = 1
+    with pytest.raises(ValueError, match="stream on cuda:0"):
+        handle._on_stream(other)
+    other.device_index = 0
+    assert handle._on_stream(other) == 7
+
+
+def on(device, tensor):
+    class There(torch.Tensor):
+        pass
+
+    There.device = property(lambda self: torch.device(device))
+    return tensor.as_subclass(There)
+
+
+def test_tensors_of_another_device_are_refused():
+    """Of another GPU, too: the call runs on the handle's."""
+    embed = solo.SoloEmbedding(10, 8, 4, device="cuda:0")
+    table, ids, rows = torch.zeros(10, 8), torch.zeros(4, dtype=torch.int64), torch.zeros(4, 8)
+    here = [on("cuda:0", t) for t in (table, rows, ids)]
+    assert embed._shape(*here, 0).tokens == 4
+    for k, t in enumerate((table, rows, ids)):
+        for other in (t, on("cuda:1", t)):
+            with pytest.raises(ValueError, match="cuda:0"):
+                embed._shape(*here[:k], other, *here[k + 1:], 0)
+    with pytest.raises(ValueError, match="cuda:0"):
+        solo._row_weights(on("cuda:1", torch.zeros(4)), 4, "grad_logprob", torch.device("cuda:0"))
+
+
+def test_a_handle_on_the_host_runs_nothing():
+    """Host addresses are nothing for a kernel: every call is refused, also one that fits."""
+    table, ids, rows = torch.zeros(10, 8), torch.zeros(4, dtype=torch.int64), torch.zeros(4, 8)
+    embed, plan = solo.SoloEmbedding(10, 8, 4, device="cpu"), solo.SoloLogprob(4, 8, device="cpu")
+    norm, w = solo.SoloGradNorm([table], [table.clone()], device="cpu"), torch.zeros(4)
+    for call in (lambda: embed.lookup(table, ids, rows, stream=0), lambda: embed.grad(rows, ids, table, stream=0),
+                 lambda: plan.forward(rows, ids, stream=0), lambda: plan.grad(rows, ids, w, None, rows, stream=0),
+                 lambda: plan.forward_grad(rows, ids, w, None, rows, stream=0), lambda: norm.norm(stream=0), lambda: norm.clip(1.0, stream=0)):
+        with pytest.raises(ValueError):
+            call()
