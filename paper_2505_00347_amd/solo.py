@@ -583,10 +583,12 @@ class SoloLogprob(_Handle):
         f32, i32 = dict(dtype=_torch.float32, device=self.device), dict(dtype=_torch.int32, device=self.device)
         self.logprob, self.entropy = _torch.empty(rows, **f32), _torch.empty(rows, **f32)
         self.stats = _torch.empty((rows, 2), **f32)
+        self._entropy_with_grad = _torch.empty(rows, **f32)            # (entropy and stats are a pair: forward_grad() leaves both as they are)
+        self._summed = 0, None                     # rows and scale of what they are of
         self.rank = _torch.empty(rows, **i32) if rank else None
         self.top_logprob = _torch.empty((rows, top), **f32) if top else None
         self.top_token = _torch.empty((rows, top), **i32) if top else None
-        self._hold(self.logprob, self.entropy, self.stats, self.rank, self.top_logprob, self.top_token)
+        self._hold(self.logprob, self.entropy, self.stats, self._entropy_with_grad, self.rank, self.top_logprob, self.top_token)
 
     def _shape(self, logits, targets, out=None):
         """The C struct of these tensors, made when their layout is another than in the call before (as in SoloEmbedding)."""
@@ -615,6 +617,7 @@ class SoloLogprob(_Handle):
         logprob, rank = (None, None) if none else (self.logprob, self.rank)
         _operation("solo_logprob", True, logits, targets, logprob, self.entropy, rank, self.top_logprob, self.top_token, self.stats,
                    C.addressof(shape), self._on_stream(stream))
+        self._summed = shape.rows, shape.scale
         results = [logprob, self.entropy]
         if self.rank is not None:
             results.append(rank)
@@ -623,10 +626,14 @@ class SoloLogprob(_Handle):
         return tuple(results) if shape.rows == self.rows else tuple(t if t is None else t[:shape.rows] for t in results)
 
     def grad(self, logits, targets, grad_logprob, grad_entropy, out, stream=None):
-        """Gradient of the logits behind forward() on the same ones, for the gradients of logprob and entropy (or None)."""
+        """Gradient of the logits behind forward() on the same ones, for the gradients of logprob and entropy (or None).  forward_grad() in
+        between, on whatever logits, changes nothing."""
         shape = self._shape(logits, targets, out)
         _row_weights(grad_logprob, shape.rows, "grad_logprob", self.device)
         _row_weights(grad_entropy, shape.rows, "grad_entropy", self.device)
+        rows, scale = self._summed
+        if rows < shape.rows or scale != shape.scale:
+            raise ValueError(f"grad() takes what forward() left on the same rows: {shape.rows} with scale {shape.scale} expected, got {rows} with {scale}")
         _operation("solo_logprob_grad", True, logits, targets, self.entropy, self.stats, grad_logprob, grad_entropy, out,
                    C.addressof(shape), self._on_stream(stream))
         return out
@@ -637,11 +644,11 @@ class SoloLogprob(_Handle):
         _row_weights(grad_logprob, shape.rows, "grad_logprob", self.device)
         _row_weights(grad_entropy, shape.rows, "grad_entropy", self.device)
         logprob = None if targets is None else self.logprob
-        _operation("solo_logprob_with_grad", True, logits, targets, grad_logprob, grad_entropy, logprob, self.entropy, out,
+        _operation("solo_logprob_with_grad", True, logits, targets, grad_logprob, grad_entropy, logprob, self._entropy_with_grad, out,
                    C.addressof(shape), self._on_stream(stream))
         if shape.rows != self.rows:
-            return None if logprob is None else logprob[:shape.rows], self.entropy[:shape.rows], out
-        return logprob, self.entropy, out
+            return None if logprob is None else logprob[:shape.rows], self._entropy_with_grad[:shape.rows], out
+        return logprob, self._entropy_with_grad, out
 
 
 HBM_REGION_BYTES = 96 << 30      # an MI355X behaves as three such regions of physical memory

@@ -91,3 +91,16 @@ def test_buffers_under_work_of_another_stream_are_not_given_away():
     other = torch.empty(size, dtype=torch.uint8, device="cuda")
     assert other.data_ptr() != place
     side.synchronize()
+
+
+def test_both_gradient_calls_on_one_handle():
+    """forward_grad() on other rows between forward() and grad() does not change what grad() gives."""
+    x, other = torch.randn((40, 300), device="cuda"), torch.randn((40, 300), device="cuda") * 5
+    t, a = torch.randint(0, 300, (40,), device="cuda"), torch.rand(40, device="cuda")
+    plan = solo.SoloLogprob(40, 300)
+    plan.forward(x, t)
+    want = plan.grad(x, t, a, a, torch.empty_like(x)).clone()
+    plan.forward(x, t)
+    _, entropy, _ = plan.forward_grad(other, t, a, a, torch.empty_like(x))
+    assert torch.equal(plan.grad(x, t, a, a, torch.empty_like(x)), want)
+    assert not torch.equal(entropy, plan.entropy)

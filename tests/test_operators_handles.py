@@ -248,3 +248,33 @@ def test_a_handle_on_the_host_runs_nothing():
                  lambda: plan.forward_grad(rows, ids, w, None, rows, stream=0), lambda: norm.norm(stream=0), lambda: norm.clip(1.0, stream=0)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_a_gradient_needs_the_sums_of_its_rows(monkeypatch):
+    """grad() reads entropy and stats of forward(): of as many rows, with the same scale, and never of forward_grad()."""
+    calls = []
+    monkeypatch.setattr(solo, "_operation", lambda name, check, *args: calls.append((name, args)))
+    plan, w = solo.SoloLogprob(4, 8, device="cpu"), torch.zeros(4)
+    monkeypatch.setattr(plan, "_on_stream", lambda stream: 0)
+    x, t = torch.zeros(4, 8), torch.zeros(4, dtype=torch.int64)
+
+    def refused(n):
+        with pytest.raises(ValueError, match="forward"):
+            plan.grad(x[:n], t[:n], w[:n], None, x[:n])
+
+    refused(1)
+    plan.forward_grad(x, t, w, None, x)
+    refused(1)
+    plan.forward(x[:3], t[:3])
+    refused(4)
+    plan.grad(x[:3], t[:3], w[:3], None, x[:3])
+    plan.scale = 2.0
+    refused(3)
+    plan.forward(x, t)
+    plan.forward_grad(x[:2], t[:2], w[:2], None, x[:2])
+    plan.grad(x, t, w, None, x)
+    assert [name for name, _ in calls] == ["solo_logprob_with_grad", "solo_logprob", "solo_logprob_grad", "solo_logprob", "solo_logprob_with_grad", "solo_logprob_grad"]
+    for name, args in calls:
+        read = args[2:4] if name == "solo_logprob_grad" else (args[3], args[7]) if name == "solo_logprob" else ()
+        assert all(a is b for a, b in zip(read, (plan.entropy, plan.stats)))
+        assert name != "solo_logprob_with_grad" or not any(a is b for a in args for b in (plan.entropy, plan.stats))
