@@ -441,6 +441,10 @@ __device__ __forceinline__ void zero_row(char *to, uint32_t bytes, uint32_t lane
     for (; i < bytes; i += 2) *reinterpret_cast<uint16_t *>(to + i) = 0;       // (one lane's: what is left is less than 16 bytes)
 }
 
+// A launch has fewer than 2^32 threads, 2^30 at most for the sums: tables of more than 2^25 rows of 2 KB and more have more rows a wavefront.
+// (2^30 rows, 64 for each wavefront, are 2^24 wavefronts.)
+constexpr uint32_t kZeroWaves = 1u << 25;
+
 // `empty`: bit r is set where row first + r has no token.
 template <bool OUT16>
 __device__ __forceinline__ void zero_rows(const EmbedArgs &a, uint32_t first, uint64_t empty)
@@ -556,49 +560,51 @@ __global__ __launch_bounds__(kJoinWaves * kLanes) void embed_join_kernel(const E
     constexpr int N = Lane16<IN16>::kPer;
     __shared__ float lds[kJoinWaves][N][kLanes];
     const uint32_t lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes, total = a.span[a.vocab].x;
-    // a lane looks at a piece
-    const uint64_t at = (uint64_t)blockIdx.x * kJoinPieces + lane, at_edge = (at + 1) * a.piece;
-    uint32_t its_row = 0, its_start = 0, its_end = 0;
-    bool begins = lane < kJoinPieces && at_edge < total;
-    if (begins) {
-        its_row = a.sorted[at_edge - 1];
-        const uint2 span = a.span[its_row];
-        its_start = span.x;
-        its_end = span.y;
-        begins = its_end > at_edge && its_end - its_start > a.piece && its_start >= at * a.piece;
-    }
-    for (uint64_t left = __ballot(begins); left != 0; left &= left - 1) {
-        const uint32_t which = __builtin_ctzll(left), piece = blockIdx.x * kJoinPieces + which;
-        const uint32_t row = __builtin_amdgcn_readlane(its_row, which), to = __builtin_amdgcn_readlane(its_end, which);
-        const uint32_t parts = (to - 1) / a.piece - piece + 1;                 // the first is the second row of its piece
-        const uint32_t run = (parts + kJoinWaves - 1) / kJoinWaves, begin = wave * run, end = min(begin + run, parts);
-        for (uint32_t c0 = blockIdx.y * kLanes * N; c0 < a.dim; c0 += gridDim.y * kLanes * N) {
-            const uint32_t c = min(c0 + lane * N, (a.dim - 1) / N * N), from = first_column<N>(a, c);
-            float sum[N] = {};
-            for (uint32_t p = begin; p < end; p += kAheadRows) {
-                float raw[kAheadRows][N];
+    for (uint32_t group = blockIdx.x; group < (a.pieces + kJoinPieces - 1) / kJoinPieces; group += gridDim.x) {
+        // a lane looks at a piece
+        const uint64_t at = (uint64_t)group * kJoinPieces + lane, at_edge = (at + 1) * a.piece;
+        uint32_t its_row = 0, its_start = 0, its_end = 0;
+        bool begins = lane < kJoinPieces && at_edge < total;
+        if (begins) {
+            its_row = a.sorted[at_edge - 1];
+            const uint2 span = a.span[its_row];
+            its_start = span.x;
+            its_end = span.y;
+            begins = its_end > at_edge && its_end - its_start > a.piece && its_start >= at * a.piece;
+        }
+        for (uint64_t left = __ballot(begins); left != 0; left &= left - 1) {
+            const uint32_t which = __builtin_ctzll(left), piece = group * kJoinPieces + which;
+            const uint32_t row = __builtin_amdgcn_readlane(its_row, which), to = __builtin_amdgcn_readlane(its_end, which);
+            const uint32_t parts = (to - 1) / a.piece - piece + 1;                 // the first is the second row of its piece
+            const uint32_t run = (parts + kJoinWaves - 1) / kJoinWaves, begin = wave * run, end = min(begin + run, parts);
+            for (uint32_t c0 = blockIdx.y * kLanes * N; c0 < a.dim; c0 += gridDim.y * kLanes * N) {
+                const uint32_t c = min(c0 + lane * N, (a.dim - 1) / N * N), from = first_column<N>(a, c);
+                float sum[N] = {};
+                for (uint32_t p = begin; p < end; p += kAheadRows) {
+                    float raw[kAheadRows][N];
 #pragma unroll
-                for (int k = 0; k < kAheadRows; ++k) {
-                    const uint32_t part = min(p + k, end - 1);
-                    load_floats<false, N>(partial_at<N>(a, piece + part, part == 0, c), 0, raw[k]);
+                    for (int k = 0; k < kAheadRows; ++k) {
+                        const uint32_t part = min(p + k, end - 1);
+                        load_floats<false, N>(partial_at<N>(a, piece + part, part == 0, c), 0, raw[k]);
+                    }
+#pragma unroll
+                    for (int k = 0; k < kAheadRows; ++k) {
+#pragma unroll
+                        for (int e = 0; e < N; ++e) sum[e] += p + k < end ? raw[k][e] : 0.0f;       // (no branch: behind one a load would be moved)
+                    }
                 }
 #pragma unroll
-                for (int k = 0; k < kAheadRows; ++k) {
+                for (int e = 0; e < N; ++e) lds[wave][e][lane] = sum[e];
+                __syncthreads();
+                if (wave == 0) {
+                    const uint32_t waves = (parts + run - 1) / run;
+                    for (uint32_t w = 1; w < waves; ++w)
 #pragma unroll
-                    for (int e = 0; e < N; ++e) sum[e] += p + k < end ? raw[k][e] : 0.0f;       // (no branch: behind one a load would be moved)
+                        for (int e = 0; e < N; ++e) sum[e] += lds[w][e][lane];
+                    if (c0 + lane * N < a.dim) put_columns<OUT16, N>(a, row, c, from, sum);
                 }
+                __syncthreads();
             }
-#pragma unroll
-            for (int e = 0; e < N; ++e) lds[wave][e][lane] = sum[e];
-            __syncthreads();
-            if (wave == 0) {
-                const uint32_t waves = (parts + run - 1) / run;
-                for (uint32_t w = 1; w < waves; ++w)
-#pragma unroll
-                    for (int e = 0; e < N; ++e) sum[e] += lds[w][e][lane];
-                if (c0 + lane * N < a.dim) put_columns<OUT16, N>(a, row, c, from, sum);
-            }
-            __syncthreads();
         }
     }
 }
@@ -671,8 +677,9 @@ static void sum_rows(const EmbedArgs &a, const EmbedPlan &p, uint32_t sum_groups
                                      : past ? embed_sum_kernel<IN16, OUT16, true, true> : embed_sum_kernel<IN16, OUT16, true, false>), dim3(grid), dim3(kEmbedThreads), 0, stream, a);
     constexpr uint32_t kColumns = kLanes * Lane16<IN16>::kPer;
     const uint32_t tiles = (a.dim + kColumns - 1) / kColumns;
+    const uint32_t join_groups = (p.pieces + kJoinPieces - 1) / kJoinPieces;
     if (p.pieces > 1)
-        hipLaunchKernelGGL((embed_join_kernel<IN16, OUT16>), dim3((p.pieces + kJoinPieces - 1) / kJoinPieces, tiles < 16 ? tiles : 16), dim3(kJoinWaves * kLanes), 0, stream, a);
+        hipLaunchKernelGGL((embed_join_kernel<IN16, OUT16>), dim3(join_groups < (1u << 22) ? join_groups : 1u << 22, tiles < 16 ? tiles : 16), dim3(kJoinWaves * kLanes), 0, stream, a);
 }
 
 }  // namespace solo
@@ -740,6 +747,7 @@ int solo_embedding_grad(const void *grad_rows, const void *tokens, void *grad_ta
         a.zero_team_bits = bits_for((row_bytes + 15) / 16);
         if (a.zero_team_bits > 6) a.zero_team_bits = 6;
         a.zero_rows = row_bytes >= 4096 ? 1 : 4096 / row_bytes < kLanes ? 4096 / row_bytes : kLanes;
+        while ((a.vocab + a.zero_rows - 1) / a.zero_rows > kZeroWaves) a.zero_rows *= 2;
         const uint32_t waves = (a.vocab + a.zero_rows - 1) / a.zero_rows;
         a.zero_groups = (waves + kEmbedThreads / kLanes - 1) / (kEmbedThreads / kLanes);
     }
