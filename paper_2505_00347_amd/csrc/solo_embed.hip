@@ -655,31 +655,32 @@ static EmbedPlan embed_plan(const solo_embedding_shape *s)
 static bool past_caches(const solo_embedding_shape *s) { return s->tokens * s->dim * element_bytes(s->rows_dtype) > kPastBytes; }
 
 template <bool IN16, bool OUT16>
-static void lookup(const EmbedArgs &a, bool wide, bool past, uint64_t grid, void *stream)
+static int lookup(const EmbedArgs &a, bool wide, bool past, uint64_t grid, void *stream)
 {
     void (*kernel)(EmbedArgs) = wide ? (past ? embed_lookup_kernel<IN16, OUT16, true, true> : embed_lookup_kernel<IN16, OUT16, true, false>)
                                      : (past ? embed_lookup_kernel<IN16, OUT16, false, true> : embed_lookup_kernel<IN16, OUT16, false, false>);
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)grid), dim3(kEmbedThreads), 0, (hipStream_t)stream, a);
+    return launch(kernel, dim3((uint32_t)grid), kEmbedThreads, (hipStream_t)stream, a);
 }
 
 template <bool IN16, bool OUT16>
-static void few_tokens(const EmbedArgs &a, bool wide, hipStream_t stream)
+static int few_tokens(const EmbedArgs &a, bool wide, hipStream_t stream)
 {
     const uint32_t waves = kEmbedThreads / kLanes, grid = (a.n * a.tiles + waves - 1) / waves + a.zero_groups;
-    hipLaunchKernelGGL((wide ? embed_few_kernel<IN16, OUT16, true> : embed_few_kernel<IN16, OUT16, false>), dim3(grid), dim3(kEmbedThreads), 0, stream, a);
+    return launch(wide ? embed_few_kernel<IN16, OUT16, true> : embed_few_kernel<IN16, OUT16, false>, dim3(grid), kEmbedThreads, stream, a);
 }
 
 template <bool IN16, bool OUT16>
-static void sum_rows(const EmbedArgs &a, const EmbedPlan &p, uint32_t sum_groups, bool past, hipStream_t stream)
+static int sum_rows(const EmbedArgs &a, const EmbedPlan &p, uint32_t sum_groups, bool past, hipStream_t stream)
 {
     const uint32_t grid = sum_groups + a.zero_groups;
-    if (grid) hipLaunchKernelGGL((p.team_bits < 6 ? embed_sum_kernel<IN16, OUT16, false, false>
-                                     : past ? embed_sum_kernel<IN16, OUT16, true, true> : embed_sum_kernel<IN16, OUT16, true, false>), dim3(grid), dim3(kEmbedThreads), 0, stream, a);
+    void (*const sum)(EmbedArgs) = p.team_bits < 6 ? embed_sum_kernel<IN16, OUT16, false, false>
+                                   : past          ? embed_sum_kernel<IN16, OUT16, true, true>
+                                                   : embed_sum_kernel<IN16, OUT16, true, false>;
+    const int rc = grid ? launch(sum, dim3(grid), kEmbedThreads, stream, a) : SOLO_OK;
+    if (rc != SOLO_OK || p.pieces <= 1) return rc;
     constexpr uint32_t kColumns = kLanes * Lane16<IN16>::kPer;
-    const uint32_t tiles = (a.dim + kColumns - 1) / kColumns;
-    const uint32_t join_groups = (p.pieces + kJoinPieces - 1) / kJoinPieces;
-    if (p.pieces > 1)
-        hipLaunchKernelGGL((embed_join_kernel<IN16, OUT16>), dim3(join_groups < (1u << 22) ? join_groups : 1u << 22, tiles < 16 ? tiles : 16), dim3(kJoinWaves * kLanes), 0, stream, a);
+    const uint32_t tiles = (a.dim + kColumns - 1) / kColumns, join_groups = (p.pieces + kJoinPieces - 1) / kJoinPieces;
+    return launch(embed_join_kernel<IN16, OUT16>, dim3(join_groups < (1u << 22) ? join_groups : 1u << 22, tiles < 16 ? tiles : 16), kJoinWaves * kLanes, stream, a);
 }
 
 }  // namespace solo
@@ -706,9 +707,8 @@ int solo_embedding(const void *table, const void *tokens, void *rows, const solo
     uint64_t grid = ((shape->tokens << a.team_bits) + kEmbedThreads - 1) / kEmbedThreads;
     if (grid > (1u << 20)) grid = 1u << 20;
     const bool past = past_caches(shape);
-    if (in16) out16 ? lookup<true, true>(a, wide, past, grid, stream) : lookup<true, false>(a, wide, past, grid, stream);
-    else out16 ? lookup<false, true>(a, wide, past, grid, stream) : lookup<false, false>(a, wide, past, grid, stream);
-    return launched();
+    if (in16) return out16 ? lookup<true, true>(a, wide, past, grid, stream) : lookup<true, false>(a, wide, past, grid, stream);
+    return out16 ? lookup<false, true>(a, wide, past, grid, stream) : lookup<false, false>(a, wide, past, grid, stream);
 }
 
 size_t solo_embedding_workspace_bytes(const solo_embedding_shape *shape)
@@ -756,21 +756,19 @@ int solo_embedding_grad(const void *grad_rows, const void *tokens, void *grad_ta
     if (a.n != 0 && a.n <= kFewTokens) {
         const uint32_t columns = kLanes * (in16 ? 8 : 4);
         a.tiles = (a.dim + columns - 1) / columns;
-        if (in16) out16 ? few_tokens<true, true>(a, wide, s) : few_tokens<true, false>(a, wide, s);
-        else out16 ? few_tokens<false, true>(a, wide, s) : few_tokens<false, false>(a, wide, s);
-        return launched();
+        if (in16) return out16 ? few_tokens<true, true>(a, wide, s) : few_tokens<true, false>(a, wide, s);
+        return out16 ? few_tokens<false, true>(a, wide, s) : few_tokens<false, false>(a, wide, s);
     }
     if (a.n != 0) {
         const uint32_t lds = kSortWaves * (1u << p.row_bits) * (uint32_t)sizeof(uint32_t);
-        if (wide) hipLaunchKernelGGL(embed_sort_kernel<true>, dim3(1u << p.bucket_bits), dim3(kSortWaves * kLanes), lds, s, a);
-        else hipLaunchKernelGGL(embed_sort_kernel<false>, dim3(1u << p.bucket_bits), dim3(kSortWaves * kLanes), lds, s, a);
-        if (launched() != SOLO_OK) return SOLO_E_HIP;      // (what follows reads what the sort writes)
+        const int rc = launch(wide ? embed_sort_kernel<true> : embed_sort_kernel<false>, dim3(1u << p.bucket_bits), kSortWaves * kLanes, s, a, lds);
+        if (rc != SOLO_OK) return rc;                      // (what follows reads what the sort writes)
     }
     uint64_t items = (uint64_t)p.pieces * p.tiles, groups = ((items << p.team_bits) + kEmbedThreads - 1) / kEmbedThreads;
     if (groups > (1u << 22)) groups = 1u << 22;
-    if (in16) out16 ? sum_rows<true, true>(a, p, (uint32_t)groups, past_caches(shape), s) : sum_rows<true, false>(a, p, (uint32_t)groups, past_caches(shape), s);
-    else out16 ? sum_rows<false, true>(a, p, (uint32_t)groups, past_caches(shape), s) : sum_rows<false, false>(a, p, (uint32_t)groups, past_caches(shape), s);
-    return launched();
+    const bool past = past_caches(shape);
+    if (in16) return out16 ? sum_rows<true, true>(a, p, (uint32_t)groups, past, s) : sum_rows<true, false>(a, p, (uint32_t)groups, past, s);
+    return out16 ? sum_rows<false, true>(a, p, (uint32_t)groups, past, s) : sum_rows<false, false>(a, p, (uint32_t)groups, past, s);
 }
 
 }  // extern "C"

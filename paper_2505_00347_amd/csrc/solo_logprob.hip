@@ -581,7 +581,7 @@ constexpr uint64_t kPastLoads = 256ull << 20, kPastStores = 32ull << 20;
 static uint64_t logits_bytes(const RowArgs &a, bool bf16) { return a.rows * a.cols * (bf16 ? 2 : 4); }
 
 template <bool BF16, bool TOP, int THREADS, int DEPTH>
-static void logprob_launch(const RowArgs &a, hipStream_t stream)
+static int logprob_launch(const RowArgs &a, hipStream_t stream)
 {
     const bool rank = a.rank != nullptr;
     void (*kernel)(RowArgs);
@@ -589,11 +589,11 @@ static void logprob_launch(const RowArgs &a, hipStream_t stream)
         kernel = rank ? logprob_kernel<BF16, TOP, true, true, THREADS, DEPTH> : logprob_kernel<BF16, TOP, false, true, THREADS, DEPTH>;
     else
         kernel = rank ? logprob_kernel<BF16, TOP, true, false, THREADS, DEPTH> : logprob_kernel<BF16, TOP, false, false, THREADS, DEPTH>;
-    hipLaunchKernelGGL(kernel, dim3(row_grid(a.rows)), dim3(THREADS), 0, stream, a);
+    return launch(kernel, dim3(row_grid(a.rows)), THREADS, stream, a);
 }
 
 template <bool BF16, bool FORWARD, bool RESIDENT, int THREADS, int DEPTH>
-static void grad_launch(const RowArgs &a, hipStream_t stream)
+static int grad_launch(const RowArgs &a, hipStream_t stream)
 {
     constexpr int kDepth = BF16 ? DEPTH : 2 * DEPTH;
     const uint64_t bytes = logits_bytes(a, BF16);
@@ -605,7 +605,7 @@ static void grad_launch(const RowArgs &a, hipStream_t stream)
     else kernel = bytes > kPastLoads    ? logprob_grad_kernel<BF16, FORWARD, RESIDENT, false, kBoth, THREADS, kDepth>
                   : bytes > kPastStores ? logprob_grad_kernel<BF16, FORWARD, RESIDENT, false, 1, THREADS, kDepth>
                                         : logprob_grad_kernel<BF16, FORWARD, RESIDENT, false, 0, THREADS, kDepth>;
-    hipLaunchKernelGGL(kernel, dim3(row_grid(a.rows)), dim3(THREADS), 0, stream, a);
+    return launch(kernel, dim3(row_grid(a.rows)), THREADS, stream, a);
 }
 
 // A wavefront takes a row by itself where rows are short, or where there are enough of them that no compute unit waits and they
@@ -614,13 +614,13 @@ static void grad_launch(const RowArgs &a, hipStream_t stream)
 // one row of 50257: 26 us, with 512 threads 10.)  With alternatives, 256 threads have one load of bf16 ahead instead of two: the
 // registers leave room for another wavefront, 83 instead of 86 us.  (groups: of eight columns)
 template <bool BF16, bool TOP>
-static void logprob_rows(const RowArgs &a, hipStream_t stream)
+static int logprob_rows(const RowArgs &a, hipStream_t stream)
 {
     const uint32_t groups = a.cols / 8;
     constexpr int kDepth = BF16 ? 2 : 4;
-    if (groups <= 256 || (a.rows >= 4096 && groups <= 2048)) logprob_launch<BF16, TOP, 64, kDepth>(a, stream);
-    else if (a.rows >= 128 || groups <= 1024) logprob_launch<BF16, TOP, 256, BF16 && TOP ? 1 : kDepth>(a, stream);
-    else logprob_launch<BF16, TOP, 512, kDepth>(a, stream);
+    if (groups <= 256 || (a.rows >= 4096 && groups <= 2048)) return logprob_launch<BF16, TOP, 64, kDepth>(a, stream);
+    if (a.rows >= 128 || groups <= 1024) return logprob_launch<BF16, TOP, 256, BF16 && TOP ? 1 : kDepth>(a, stream);
+    return logprob_launch<BF16, TOP, 512, kDepth>(a, stream);
 }
 
 // The fewest threads that hold the row with four groups of eight columns each, so that two workgroups share a compute unit and one
@@ -628,28 +628,28 @@ static void logprob_rows(const RowArgs &a, hipStream_t stream)
 // eight 187, 256 with sixteen 229, reading the row twice 230; 20000 x 8000: 256 with four 114, twice 131; 4096 x 50304: 1024 with eight 172,
 // 512 with sixteen 196.)  Longer rows are read twice, 1024 threads: 2000 x 100000 196 us, with 512 226.
 template <bool BF16>
-static void with_grad_launch(const RowArgs &a, hipStream_t stream)
+static int with_grad_launch(const RowArgs &a, hipStream_t stream)
 {
     const uint32_t groups = (a.cols + 7) / 8;              // (all of them have to fit)
-    if (groups <= 64 * 4) grad_launch<BF16, true, true, 64, 4>(a, stream);
-    else if (groups <= 256 * 4) grad_launch<BF16, true, true, 256, 4>(a, stream);
-    else if (groups <= 512 * 4) grad_launch<BF16, true, true, 512, 4>(a, stream);
-    else if (groups <= 1024 * 4) grad_launch<BF16, true, true, 1024, 4>(a, stream);
-    else if (groups <= 1024 * 8) grad_launch<BF16, true, true, 1024, 8>(a, stream);
-    else grad_launch<BF16, true, false, 1024, 2>(a, stream);
+    if (groups <= 64 * 4) return grad_launch<BF16, true, true, 64, 4>(a, stream);
+    if (groups <= 256 * 4) return grad_launch<BF16, true, true, 256, 4>(a, stream);
+    if (groups <= 512 * 4) return grad_launch<BF16, true, true, 512, 4>(a, stream);
+    if (groups <= 1024 * 4) return grad_launch<BF16, true, true, 1024, 4>(a, stream);
+    if (groups <= 1024 * 8) return grad_launch<BF16, true, true, 1024, 8>(a, stream);
+    return grad_launch<BF16, true, false, 1024, 2>(a, stream);
 }
 
 // Two or three groups of a row for each thread.  (8192 x 32000 bf16: 1024 threads 184 us, 512 197, 256 205; 20000 x 3000: 256 47, 1024 108;
 // 40000 x 500: 64 17, 256 23.)
 template <bool BF16>
-static void only_grad_launch(const RowArgs &a, hipStream_t stream)
+static int only_grad_launch(const RowArgs &a, hipStream_t stream)
 {
     const uint32_t groups = a.cols / 8;
-    if (groups <= 128) grad_launch<BF16, false, false, 64, 2>(a, stream);
-    else if (groups <= 256) grad_launch<BF16, false, false, 128, 2>(a, stream);
-    else if (groups <= 640) grad_launch<BF16, false, false, 256, 2>(a, stream);
-    else if (groups <= 1536) grad_launch<BF16, false, false, 512, 2>(a, stream);
-    else grad_launch<BF16, false, false, 1024, 2>(a, stream);
+    if (groups <= 128) return grad_launch<BF16, false, false, 64, 2>(a, stream);
+    if (groups <= 256) return grad_launch<BF16, false, false, 128, 2>(a, stream);
+    if (groups <= 640) return grad_launch<BF16, false, false, 256, 2>(a, stream);
+    if (groups <= 1536) return grad_launch<BF16, false, false, 512, 2>(a, stream);
+    return grad_launch<BF16, false, false, 1024, 2>(a, stream);
 }
 
 }  // namespace solo
@@ -669,9 +669,8 @@ int solo_logprob(const void *logits, const void *targets, float *logprob, float 
         return SOLO_E_INVALID;
     a.logprob = logprob; a.entropy = entropy; a.rank = rank; a.top_logprob = top_logprob; a.top_token = top_token; a.stats = stats;
     const hipStream_t s = (hipStream_t)stream;
-    if (shape->dtype == SOLO_BF16) a.top ? logprob_rows<true, true>(a, s) : logprob_rows<true, false>(a, s);
-    else a.top ? logprob_rows<false, true>(a, s) : logprob_rows<false, false>(a, s);
-    return launched();
+    if (shape->dtype == SOLO_BF16) return a.top ? logprob_rows<true, true>(a, s) : logprob_rows<true, false>(a, s);
+    return a.top ? logprob_rows<false, true>(a, s) : logprob_rows<false, false>(a, s);
 }
 
 int solo_logprob_grad(const void *logits, const void *targets, const float *entropy, const float *stats, const float *grad_logprob,
@@ -688,9 +687,7 @@ int solo_logprob_grad(const void *logits, const void *targets, const float *entr
         return SOLO_E_INVALID;
     a.entropy = const_cast<float *>(entropy); a.stats = const_cast<float *>(stats);
     a.grad_logprob = grad_logprob; a.grad_entropy = grad_entropy; a.grad = grad_logits;
-    if (shape->dtype == SOLO_BF16) only_grad_launch<true>(a, (hipStream_t)stream);
-    else only_grad_launch<false>(a, (hipStream_t)stream);
-    return launched();
+    return shape->dtype == SOLO_BF16 ? only_grad_launch<true>(a, (hipStream_t)stream) : only_grad_launch<false>(a, (hipStream_t)stream);
 }
 
 int solo_logprob_with_grad(const void *logits, const void *targets, const float *grad_logprob, const float *grad_entropy, float *logprob,
@@ -708,9 +705,7 @@ int solo_logprob_with_grad(const void *logits, const void *targets, const float 
         return SOLO_E_INVALID;
     a.logprob = logprob; a.entropy = entropy;
     a.grad_logprob = grad_logprob; a.grad_entropy = grad_entropy; a.grad = grad_logits;
-    if (shape->dtype == SOLO_BF16) with_grad_launch<true>(a, (hipStream_t)stream);
-    else with_grad_launch<false>(a, (hipStream_t)stream);
-    return launched();
+    return shape->dtype == SOLO_BF16 ? with_grad_launch<true>(a, (hipStream_t)stream) : with_grad_launch<false>(a, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -261,15 +261,11 @@ static int norm_args(NormArgs &a, const void *table, uint32_t count, uint64_t un
 
 static int norm(const NormArgs &a, hipStream_t stream)
 {
-    if (a.units <= kSmallUnits) {
-        hipLaunchKernelGGL(norm_small_kernel, dim3(1), dim3(kFinishThreads), 0, stream, a);
-        return launched();
-    }
-    hipLaunchKernelGGL(norm_units_kernel, dim3(a.units), dim3(kNormThreads), 0, stream, a);
-    if (launched() != SOLO_OK) return SOLO_E_HIP;
+    if (a.units <= kSmallUnits) return launch(norm_small_kernel, dim3(1), kFinishThreads, stream, a);
+    const int rc = launch(norm_units_kernel, dim3(a.units), kNormThreads, stream, a);
+    if (rc != SOLO_OK) return rc;
     const uint32_t tensors = a.tensor_norm ? (a.count + kFinishThreads / kLanes - 1) / (kFinishThreads / kLanes) : 0;
-    hipLaunchKernelGGL(norm_finish_kernel, dim3(1 + (tensors < 256 ? tensors : 256)), dim3(kFinishThreads), 0, stream, a);
-    return launched();
+    return launch(norm_finish_kernel, dim3(1 + (tensors < 256 ? tensors : 256)), kFinishThreads, stream, a);
 }
 
 }  // namespace solo
@@ -329,8 +325,7 @@ int solo_grad_clip(const void *table_device, uint32_t count, uint64_t units, con
     int rc = solo::norm_args(a, table_device, count, units, unscale, max_norm, norm, grad_scale, tensor_norm, workspace);
     if (rc == SOLO_OK) rc = solo::norm(a, (hipStream_t)stream);
     if (rc != SOLO_OK || units == 0) return rc;
-    hipLaunchKernelGGL(solo::clip_units_kernel, dim3(a.units), dim3(solo::kNormThreads), 0, (hipStream_t)stream, a);
-    return solo::launched();
+    return solo::launch(solo::clip_units_kernel, dim3(a.units), solo::kNormThreads, (hipStream_t)stream, a);
 }
 
 }  // extern "C"

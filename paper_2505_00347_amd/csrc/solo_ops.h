@@ -197,6 +197,15 @@ __device__ __forceinline__ T group_sum(T x, T *lds, int waves)
 inline bool at_multiple(const void *p, uintptr_t a) { return p && reinterpret_cast<uintptr_t>(p) % a == 0; }
 inline uintptr_t element_bytes(uint32_t dtype) { return dtype == SOLO_BF16 ? 2 : 4; }
 inline bool dtype_ok(uint32_t dtype) { return dtype == SOLO_FP32 || dtype == SOLO_BF16; }
-inline int launched() { return hipGetLastError() == hipSuccess ? SOLO_OK : SOLO_E_HIP; }
+
+// A launch by its own result: the runtime's last error may be another call's.
+template <typename Args>
+inline int launch(void (*kernel)(Args), dim3 grid, uint32_t threads, hipStream_t stream, const Args &args, uint32_t lds = 0)
+{
+    void *at[] = {const_cast<Args *>(&args)};
+    if (hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3(threads), at, lds, stream) == hipSuccess) return SOLO_OK;
+    (void)hipGetLastError();                               // (reported here, not by the caller's next call)
+    return SOLO_E_HIP;
+}
 
 }  // namespace solo

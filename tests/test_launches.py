@@ -8,6 +8,8 @@ import sys
 
 import pytest
 
+from paper_2505_00347_amd import solo
+
 HERE = os.path.dirname(os.path.abspath(__file__))
 RUNTIME = r"""
 #include <hip/hip_runtime_api.h>
@@ -118,3 +120,30 @@ def test_the_largest_shapes_that_are_taken_can_be_launched(run):
         assert code == 0, (shape, launches)
         assert launches or shape[0] in ("gradient", "lookup") and shape[3] == 0, shape
         assert all(stream == 5 for *_, stream in launches)
+
+
+EACH = r"""
+embed = lambda n: solo.solo_embedding_shape(1000, 520, n, 520, 520, 1, 1, 64, 0, 1.0, 0)
+x = solo.solo_logits(700, 3000, 3000, 3000, 1, 64, 5, 0, 1.0, 0)
+calls = [("solo_grad_norm", 16, 2, 3, None, 1.0, 16, 16, 16, 16), ("solo_grad_norm", 16, 2, 9, None, 1.0, 16, 16, 16, 16),
+         ("solo_grad_clip", 16, 2, 3, None, 1.0, 16, 16, 16, 16), ("solo_grad_clip", 16, 2, 9, None, 1.0, 16, 16, 16, 16),
+         ("solo_embedding", 16, 16, 16, embed(700)), ("solo_embedding_grad", 16, 16, 16, 16, 1 << 40, embed(70)),
+         ("solo_embedding_grad", 16, 16, 16, 16, 1 << 40, embed(0)), ("solo_embedding_grad", 16, 16, 16, 16, 1 << 40, embed(700)),
+         ("solo_logprob", 16, 16, 16, 16, 16, 16, 16, 16, x), ("solo_logprob_grad", 16, 16, 16, 16, 16, 16, 16, x),
+         ("solo_logprob_with_grad", 16, 16, 16, 16, 16, 16, 16, x)]
+"""
+
+
+def test_an_error_of_another_call_is_not_one_of_these(run):
+    """HIP keeps the last error until someone asks: the launches have succeeded all the same."""
+    for name, code, launches, left in run(EACH + "for c in calls: results.append([c[0], *call(*c, left=1), runtime.hipGetLastError()])"):
+        assert code == 0 and launches, name
+        assert left == 1, name                             # (whose it is finds it)
+
+
+def test_a_launch_that_fails_is_reported_and_nothing_follows_it(run):
+    results = run(EACH + "for c in calls:\n for k in range(len(call(*c)[1])): results.append([c[0], k, *call(*c, refuse=k), runtime.hipGetLastError()])")
+    assert len(results) > 11
+    for name, k, code, launches, left in results:
+        assert code == solo.SOLO_E_HIP and len(launches) == k + 1, (name, k)
+        assert left == 0, name                             # (reported here, not by the caller's next call)
