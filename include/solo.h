@@ -321,7 +321,7 @@ int solo_embedding_grad(const void *grad_rows, const void *tokens, void *grad_ta
  *   rank = number of columns whose logit is larger than the target's
  *   top_logprob, top_token [rows, top]: z - L of the `top` largest logits and their columns, larger ones
  *            first, ties by the lower column; places behind the last column are -inf and -1
- *   stats [rows, 2]: what solo_logprob_grad takes: a logit near the row's largest, and the sum of e^z relative to it
+ *   stats [rows, 2]: what solo_logprob_grad takes: the row's largest logit, and the sum of e^z relative to it
  *
  * and for a loss with d loss / d logprob = a, d loss / d entropy = b (one float per row each):
  *

@@ -4,8 +4,10 @@
 //   logprob = d_t - ln S        entropy = ln S - W / S        log p_j = d_j - ln S
 //   dx_j = s (a (delta_jt - p_j) - b p_j (log p_j + entropy))        a, b: gradients of logprob and entropy
 //
-// One workgroup takes a row, and one pass over it: every thread keeps a reference (a value near the largest one that it has
-// seen) and its sums relative to that; the sums of the threads are brought to the row's maximum at the end.  Differences
+// One workgroup takes a row, and one pass over it: every thread keeps the largest logit that it has seen and its sums relative
+// to that; the sums of the threads are brought to the row's maximum at the end.  S is then 1 or more, and d_t - ln S of a target with nearly all
+// of the probability loses no digits.  (A reference that may lie up to 8 binary orders below the maximum saves few exponentials, sums of
+// 4096 x 50304 bf16 67.1 us instead of 68.2, and costs up to 1e-6 of such a log probability.)  Differences
 // are taken before they are scaled, so a row of the type's lowest value is as good as any other.
 //
 // The alternatives come out of the same pass: a thread also remembers its largest logit, the group that holds it and the largest
@@ -25,7 +27,6 @@
 namespace solo {
 
 constexpr int kCandidates = 512;       // logits that are collected for the alternatives, before a slower selection takes over
-constexpr float kSlack = 8.0f;         // binary orders that a logit may lie above a thread's reference
 constexpr float kFloor = -1000.0f;     // e^d is 0 far above this; below it d is -inf or would be no number times 0
 
 struct RowArgs {
@@ -40,7 +41,7 @@ struct RowArgs {
     uint32_t wide;          // targets of 64 bits
 };
 
-// Sums of a part of a row: relative to a reference `at` in units of the logits; exponentials of base 2.
+// Sums of a part of a row: relative to its largest logit, `at`; exponentials of base 2.
 struct Sums { float at, s, w; };
 
 __device__ __forceinline__ void rebase(Sums &a, float at, float k)
@@ -158,7 +159,7 @@ __device__ __forceinline__ Sums row_sums(const Row<BF16> &row, float k, float ta
         float x[kPer];
         Lane16<BF16>::unpack(quad, x);
         const float m = max_of<kPer>(x);
-        if ((m - a.at) * k > kSlack) rebase(a, m, k);
+        if (m > a.at) rebase(a, m, k);
         if (TOP) largest.see(m, g);
         if (RANK) {
 #pragma unroll
@@ -183,7 +184,7 @@ __device__ __forceinline__ Sums row_sums(const Row<BF16> &row, float k, float ta
     for (int j = 0; j < DEPTH; ++j)
         if (g0 + j * THREADS + threadIdx.x < row.groups) add(q[j], g0 + j * THREADS + threadIdx.x);
     if (threadIdx.x < row.rest) {
-        if ((last - a.at) * k > kSlack) rebase(a, last, k);
+        if (last > a.at) rebase(a, last, k);
         if (TOP) largest.see(last, row.groups);
         if (RANK) count += last > target;
         add1(a, last, k);
