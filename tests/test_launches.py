@@ -13,19 +13,36 @@ from paper_2505_00347_amd import solo
 HERE = os.path.dirname(os.path.abspath(__file__))
 RUNTIME = r"""
 #include <hip/hip_runtime_api.h>
+#include <cstring>
+
+// The kernels of libsolo, as it registers them when it is loaded.
+static const void *handles[8192];
+static char names[8192][256];
+static int known;
 
 static unsigned long long launches[64][4];      // workgroups, threads of one, bytes of LDS, stream
+static const char *launched_names[64];
 static int count, refused = -1;
 static hipError_t error;
 
 extern "C" {
-hipError_t hipLaunchKernel(const void *, dim3 grid, dim3 block, void **, size_t lds, hipStream_t stream)
+void __hipRegisterFunction(void **, const void *handle, char *name, const char *, unsigned, void *, void *, dim3 *, dim3 *, int *)
+{
+    if (known == 8192 || !strstr(name, "4solo")) return;
+    handles[known] = handle;
+    strncpy(names[known++], name, 255);
+}
+const char *kernel(int i) { return i < known ? names[i] : nullptr; }
+
+hipError_t hipLaunchKernel(const void *handle, dim3 grid, dim3 block, void **, size_t lds, hipStream_t stream)
 {
     const unsigned long long groups = 1ull * grid.x * grid.y * grid.z, threads = 1ull * block.x * block.y * block.z;
     const bool fits = count != refused && 1ull * grid.x * block.x <= 0xFFFFFFFFu && grid.y * block.y < 65536 && threads <= 1024 && groups != 0 && lds <= 65536;
     if (count < 64) {
         const unsigned long long row[4] = {groups, threads, lds, (unsigned long long)stream};
         for (int k = 0; k < 4; ++k) launches[count][k] = row[k];
+        for (int k = 0; k < known; ++k)
+            if (handles[k] == handle) launched_names[count] = names[k];
     }
     ++count;
     if (!fits) error = hipErrorInvalidConfiguration;
@@ -52,12 +69,14 @@ hipError_t hipPeekAtLastError(void) { return error; }
 void expect(int refuse, int left) { count = 0; refused = refuse; error = (hipError_t)left; }
 int launched(void) { return count; }
 unsigned long long launch(int i, int what) { return launches[i][what]; }
+const char *launched_name(int i) { return launched_names[i]; }
 }
 """
 PROLOGUE = r"""
 import ctypes as C, json, sys
 runtime = C.CDLL(sys.argv[1], C.RTLD_GLOBAL)               # (in front of the real one)
 runtime.launch.restype = C.c_ulonglong
+runtime.kernel.restype = runtime.launched_name.restype = C.c_char_p
 from paper_2505_00347_amd import solo
 solo.lib()
 
