@@ -211,9 +211,9 @@ int solo_state_init(uint32_t *m_codes, float *m_scale, uint32_t *v_codes, float 
     const uint32_t last = solo::zero_level_word(cfg->bits_m, rem ? rem : cm);
     uint64_t blocks = (m_total + 255) / 256;
     if (blocks > 65536) blocks = 65536;
-    hipLaunchKernelGGL(solo::init_kernel, dim3((uint32_t)blocks), dim3(256), 0, (hipStream_t)stream,
-                       m_codes, m_scale, v_codes, v_scale, v_base, m_total, v_total, nblk, full, last);
-    return hipGetLastError() == hipSuccess ? SOLO_OK : SOLO_E_HIP;
+    const hipError_t e = solo::launch(solo::init_kernel, (uint32_t)blocks, 256, (hipStream_t)stream,
+                                      m_codes, m_scale, v_codes, v_scale, v_base, m_total, v_total, nblk, full, last);
+    return e == hipSuccess ? SOLO_OK : SOLO_E_HIP;
 }
 
 int solo_adamw_step(float *param, const void *grad, uint32_t *m_codes, float *m_scale,

@@ -1,4 +1,4 @@
-"""What the operators around the step ask the HIP runtime for, and what they make of its answers: the library on a runtime whose launches are
+"""What the operators around the step (and the state's initialisation) ask the HIP runtime for, and what they make of its answers: the library on a runtime whose launches are
 only written down (no GPU; the calls are made in a process of their own, with addresses that nothing reads)."""
 import json
 import os
@@ -144,7 +144,7 @@ def test_the_largest_shapes_that_are_taken_can_be_launched(run):
 EACH = r"""
 embed = lambda n: solo.solo_embedding_shape(1000, 520, n, 520, 520, 1, 1, 64, 0, 1.0, 0)
 x = solo.solo_logits(700, 3000, 3000, 3000, 1, 64, 5, 0, 1.0, 0)
-calls = [("solo_grad_norm", 16, 2, 3, None, 1.0, 16, 16, 16, 16), ("solo_grad_norm", 16, 2, 9, None, 1.0, 16, 16, 16, 16),
+calls = [("solo_state_init", 16, 16, 16, 16, 16, 1000, solo.make_config()), ("solo_grad_norm", 16, 2, 3, None, 1.0, 16, 16, 16, 16), ("solo_grad_norm", 16, 2, 9, None, 1.0, 16, 16, 16, 16),
          ("solo_grad_clip", 16, 2, 3, None, 1.0, 16, 16, 16, 16), ("solo_grad_clip", 16, 2, 9, None, 1.0, 16, 16, 16, 16),
          ("solo_embedding", 16, 16, 16, embed(700)), ("solo_embedding_grad", 16, 16, 16, 16, 1 << 40, embed(70)),
          ("solo_embedding_grad", 16, 16, 16, 16, 1 << 40, embed(0)), ("solo_embedding_grad", 16, 16, 16, 16, 1 << 40, embed(700)),
