@@ -241,7 +241,8 @@ int solo_adamw_step_multi(const void *table_device, uint32_t count, uint64_t uni
  * and clipping, the embedding and its gradient, the log probabilities of given tokens and their
  * gradient.  The conventions of the step hold: device pointers owned by the caller, a host struct
  * read during the call, work enqueued on `stream`, no allocation, no synchronisation, SOLO_OK or a
- * negative code with nothing enqueued.  A workspace needs no initialisation, holds nothing between
+ * negative code with nothing enqueued (but SOLO_E_HIP of a call of several launches: those before the
+ * one that the runtime refused are enqueued, and the outputs are then not specified).  A workspace needs no initialisation, holds nothing between
  * calls and serves one call at a time (calls on one stream follow each other).  Tensors need the
  * alignment of their elements only.  Every call gives the same bits for the same inputs: no sum is
  * made by atomic additions.  All calls can be captured into a HIP graph. */
@@ -254,8 +255,8 @@ int solo_adamw_step_multi(const void *table_device, uint32_t count, uint64_t uni
  * *norm = N, *grad_scale = c (what solo_adamw_step_mp and _multi take as grad_scale), tensor_norm[k] =
  * N_k.  Squares and sums are binary64, so N is that of the exact sum to about one rounding, for every
  * finite gradient.  Where N is not finite (a gradient is not, or N exceeds binary32), c is 0.
- * solo_grad_clip also writes clipped_k = c * g_k, rounded once; where c is 0, zeros, whatever the
- * gradient holds.  The table is built like that of the multi-tensor step:
+ * solo_grad_clip also writes clipped_k = c * g_k, the binary32 product rounded to the gradient's type;
+ * where c is 0, zeros, whatever the gradient holds.  The table is built like that of the multi-tensor step:
  *
  *   units = solo_norm_units(grads, count);
  *   solo_norm_table_build(grads, count, host_buffer, solo_norm_table_bytes(count, units));
@@ -330,7 +331,8 @@ int solo_embedding_grad(const void *grad_rows, const void *tokens, void *grad_ta
  * (the alternatives carry no gradient).  Logits of -inf have probability 0; in a row that has no other,
  * logprob is -inf, entropy and gradient are 0.  A target outside [0, cols) means none (a padding
  * position): the row is not read, logprob and entropy are 0, rank is -1, the alternatives are -inf and -1,
- * the gradient is 0.  A NaN or +inf in a row makes its logprob, entropy and gradient NaN and its alternatives
+ * the gradient is 0.  Sums are binary32 and relative to the row's largest logit: logprob <= 0, with an error of some 1e-7 of
+ * 1 + the distance of the target's z from the largest.  A NaN or +inf in a row makes its logprob, entropy and gradient NaN and its alternatives
  * and rank unspecified.  solo_logprob_with_grad does both for weights that are known beforehand (a mean over
  * tokens), reading the logits from HBM once. */
 #define SOLO_TOP_MAX 32

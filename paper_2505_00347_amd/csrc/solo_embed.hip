@@ -12,7 +12,7 @@
 // and wavefront; then it places them.
 //
 // Bound by memory.  16384 tokens of a bf16 table of 32000 x 4096: lookup 31 us (178 MB with every row that occurs once), gradient 84 us
-// (396 MB; the sort 8.8, the sums and zeros 67, the parts of frequent tokens 7.6 us); 396 MB take 72 us at the rate of a large copy.
+// (396 MB; the sort 8.9, the sums and zeros 67, the parts of frequent tokens 8 us); 396 MB take 72 us at the rate of a large copy.
 #include "solo_ops.h"
 
 #include <math.h>
@@ -26,7 +26,8 @@ constexpr uint32_t kMinBuckets = 256;                      // workgroups that so
 constexpr uint32_t kMaxRowBits = 9;                        // rows of a bucket: 512 at most (counters by wavefront: 32 KB of LDS)
 constexpr int kEmbedThreads = 256;
 // Looked-up rows of more bytes than this are written past the caches, and gradients of more are read past them: a quarter of the
-// last-level cache.  Lookup of 134 MB 43 us through the caches, 32 us past them, of 16 MB no difference; gradient of 134 MB 94 and 84 us,
+// last-level cache.  Lookup of 134 MB of a text's tokens 43 us through the caches, 32 us past them, of evenly drawn tokens 50 and 42 (with
+// the product that reads the rows next, 4096 columns, 445 and 451), of 16 MB no difference; gradient of 134 MB 94 and 84 us,
 // but of 40 MB, which the backward pass has left in the caches, 38 and 51 us.
 constexpr uint64_t kPastBytes = 64ull << 20;
 constexpr int kAheadRows = 8;                              // rows of dy that a team has under way

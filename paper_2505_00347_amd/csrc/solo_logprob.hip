@@ -14,8 +14,9 @@
 // one of its other groups.  From the threads' largest follows a value that the k largest logits of the row are not below, and that
 // few others reach (row_top()); only the groups that can hold one are looked at again, one for most threads that have any.
 //
-// Bound by memory where there are many rows: sums of 4096 x 50304 bf16 67 us (6.1 TB/s), with rank and twenty alternatives 81 us; loss and
-// gradient of 8192 x 32000 in one call 167 us (the row stays in registers: 1 GB, 6 TB/s), of 1000 x 50257 fp32 in two calls 98 us.
+// Bound by memory where there are many rows: sums of 4096 x 50304 bf16 68 us (6.0 TB/s), with rank and twenty alternatives 82 us; loss and
+// gradient of 8192 x 32000 in one call 172 us (the row stays in registers: 1.05 GB, 6.1 TB/s), 168 us where a tenth of the rows has no target;
+// of 1000 x 50257 fp32 in two calls 98 us.
 // A logit costs some twelve instructions and an exponential, 36 us of vector issue for 4096 x 50304; the alternatives add what a row costs once.
 // A single row of 50257 takes 9.8 us: one compute unit's exponentials, and loads of 4 us.
 #include "solo_ops.h"
@@ -576,7 +577,9 @@ static uint32_t row_grid(uint64_t rows) { return (uint32_t)(rows < (1u << 20) ? 
 
 // Logits of more bytes than the last-level cache (256 MiB) keeps are read past the caches (412 MB: 75 and 67 us; 80 MB that the head has
 // just written: 25 and 27), and gradients that are not small are written past them (64 MB: 25.6 and 20.7 us; 524 MB, with the
-// loads, 185 and 171).
+// loads, 185 and 171).  The product that reads the gradient next finds less of it in the caches: call and product together are
+// between 3.5 % faster and 3.5 % slower for it at 41 to 256 MB, by the product (bf16 1024 x 32000 with 768 columns 216.5 us past the caches, 216.3
+// through them; 1000 x 50257 417 and 403; 1000 x 50304 323 and 327; fp32 512 x 32000 with 256 columns, the worst, 215 and 199).
 constexpr uint64_t kPastLoads = 256ull << 20, kPastStores = 32ull << 20;
 
 static uint64_t logits_bytes(const RowArgs &a, bool bf16) { return a.rows * a.cols * (bf16 ? 2 : 4); }
@@ -611,9 +614,9 @@ static int grad_launch(const RowArgs &a, hipStream_t stream)
 
 // A wavefront takes a row by itself where rows are short, or where there are enough of them that no compute unit waits and they
 // are not so long that all wavefronts look for their alternatives at the same time; few rows get more threads each.  (16384 rows of
-// 4096 columns, bf16, five alternatives: 40 us, with 256 threads 78; 4096 rows of 50304, twenty: 105 us, with 256 threads 83;
-// one row of 50257: 26 us, with 512 threads 10.)  With alternatives, 256 threads have one load of bf16 ahead instead of two: the
-// registers leave room for another wavefront, 83 instead of 86 us.  (groups: of eight columns)
+// 4096 columns, bf16, five alternatives: 40 us, with 256 threads 69; 4096 rows of 50304, twenty: 108 us, with 256 threads 82;
+// one row of 50257: 31 us, with 256 threads 12, with 512 threads 10.)  With alternatives, 256 threads have one load of bf16 ahead instead of two: the
+// registers leave room for another wavefront, 82 instead of 84 us.  (groups: of eight columns)
 template <bool BF16, bool TOP>
 static int logprob_rows(const RowArgs &a, hipStream_t stream)
 {
@@ -625,9 +628,9 @@ static int logprob_rows(const RowArgs &a, hipStream_t stream)
 }
 
 // The fewest threads that hold the row with four groups of eight columns each, so that two workgroups share a compute unit and one
-// loads while the other computes; up to 65536 columns eight each, one workgroup.  (8192 x 32000 bf16: 1024 threads with four 183 us, 512 with
-// eight 187, 256 with sixteen 229, reading the row twice 230; 20000 x 8000: 256 with four 114, twice 131; 4096 x 50304: 1024 with eight 172,
-// 512 with sixteen 196.)  Longer rows are read twice, 1024 threads: 2000 x 100000 196 us, with 512 226.
+// loads while the other computes; up to 65536 columns eight each, one workgroup.  (8192 x 32000 bf16: 1024 threads with four 172 us, 512 with
+// eight 174, 256 with sixteen 219, reading the row twice 200; 20000 x 8000: 256 with four 107, twice 208; 4096 x 50304: 1024 with eight 165,
+// 512 with sixteen 189.)  Longer rows are read twice, 1024 threads: 2000 x 100000 182 us, with 512 197.
 template <bool BF16>
 static int with_grad_launch(const RowArgs &a, hipStream_t stream)
 {

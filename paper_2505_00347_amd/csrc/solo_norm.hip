@@ -6,10 +6,10 @@
 // norm_units_kernel writes one partial sum per unit, norm_finish_kernel adds them in the order of the units, per tensor
 // and over all, so the result does not depend on the order in which workgroups run.
 //
-// Bound by memory: two operations per element beside 2 or 4 bytes.  The 291 tensors of the 7B shapes in bf16, 13.5 GB: 1.90 ms, 7.1 TB/s
+// Bound by memory: two operations per element beside 2 or 4 bytes.  The 291 tensors of the 7B shapes in bf16, 13.5 GB: 1.91 ms, 7.1 TB/s
 // (a large copy reaches 5.4, reads alone through the caches 6.1), 9 us of them the sums of 51000 units.  Clipping reads twice,
 // since no element can be scaled before the last one is known, and writes once: 1.31e9 bf16 elements 1.39 ms (7.9 GB), 1.24e8 fp32 elements
-// 266 us (1.5 GB).
+// 266 us (1.5 GB: the norm 75 us, the rest at the rate of a copy).
 #include "solo_ops.h"
 
 #include <math.h>
@@ -22,9 +22,10 @@ constexpr uint64_t kNormUnits = 1 << 16;                   // a larger table has
 constexpr int kFinishThreads = 1024;
 // Gradients of up to so many bytes are partly in the last-level cache (256 MiB) when the norm is known: the norm loads them
 // through the caches, and clipping, which is the last to look at them, loads and writes past them.  Of more nothing is left by
-// then: the norm loads past the caches.  Clipping 1.2e8 elements: bf16, 249 MB, 148 us with plain accesses throughout, 122 us;
+// then: the norm loads past the caches, and clipping loads and writes through them.  Clipping 1.2e8 elements: bf16, 249 MB, 148 us with plain accesses throughout, 122 us;
 // fp32, 498 MB, 296 and 276 us.  Norm of 4e9 bf16 elements: 1.33 ms, past the caches 1.24 ms (6.45 TB/s).  The two sides
-// cross between 360 and 500 MB.
+// cross between 360 and 500 MB.  What reads the clipped gradients next loses nothing: clipping and a step of 1.05e8 bf16 elements 285 us,
+// 295 us where clipping writes through the caches.
 constexpr uint64_t kLargeBytes = 384ull << 20;
 
 struct NormEntry {

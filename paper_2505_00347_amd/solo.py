@@ -474,7 +474,10 @@ class SoloGradNorm(_Handle):
     writes; they may be the gradients themselves (clipping in place).
 
     norm() and clip() return (norm [1], grad_scale [1], tensor_norm [count]): buffers of this object that the next
-    call overwrites.  grad_scale is what SoloState.step and SoloMultiTable.step take."""
+    call overwrites.  grad_scale is what SoloState.step and SoloMultiTable.step take.
+
+    The table names the memory of the tensors as it is when the object is made, and the object keeps it.  Gradients that a training loop
+    sets to None or replaces are other tensors: keep them (zero_grad(set_to_none=False)) or make another object."""
 
     def __init__(self, grads, clipped=None, device="cuda"):
         super().__init__(device)
