@@ -416,7 +416,7 @@ class _Handle:
     current then).  The first call on such a stream waits for what was enqueued on the current stream when the buffers were made (a
     new buffer may be memory that earlier work still uses), and the allocator learns that this stream uses them.  The calls of
     a handle follow each other, each with the buffers that the one before has left: on several streams the caller orders them, and of
-    calls under a stream's bare number it keeps the handle until they are done."""
+    calls on a stream that is not torch's (a bare number, another library's object) it keeps the handle until they are done."""
 
     _buffers, _home = (), None
 
@@ -428,12 +428,13 @@ class _Handle:
         self._index = self.device.index if self.device.type == "cuda" else None
 
     def _hold(self, *buffers):
-        self._buffers, self._others, self._home, self._ready = [b for b in buffers if b is not None], {}, None, None
+        self._others, self._home, self._ready = {}, None, None
         if self._index is not None:
             stream = _torch.cuda.current_stream(self.device)
             self._home = stream.cuda_stream
             if not _torch.cuda.is_current_stream_capturing():
                 self._ready = stream.record_event()
+        self._buffers = [b for b in buffers if b is not None]          # (last: a lookup of another thread finds all of it or none)
 
     def _on_stream(self, stream):
         """The number of the stream that a call runs on, ready for the buffers."""
@@ -451,17 +452,17 @@ class _Handle:
         return getattr(number, "value", number) or 0       # (one of ctypes; None: the default stream)
 
     def _visit(self, stream, number):
-        bare = isinstance(stream, int)
-        if stream is None:
-            stream = _torch.cuda.current_stream()
-        elif not isinstance(stream, _torch.cuda.Stream):
+        foreign = not (stream is None or isinstance(stream, _torch.cuda.Stream))
+        if foreign:
             stream = _torch.cuda.ExternalStream(number)
+        elif stream is None:
+            stream = _torch.cuda.current_stream()
         with _torch.cuda.stream(stream):
             if _torch.cuda.is_current_stream_capturing():  # (a graph's nodes wait for nothing outside; capturing begins on an idle GPU)
                 return
         if self._ready is not None:
             stream.wait_event(self._ready)
-        if bare:                                           # (there may be another stream of this number later, or none)
+        if foreign:                                        # (there may be another stream of this number later, or none)
             return
         for b in self._buffers:
             b.record_stream(stream)
@@ -526,7 +527,8 @@ class SoloGradNorm(_Handle):
 class SoloEmbedding(_Handle):
     """Lookup in an embedding table [vocab, dim] and the table's gradient, for up to `tokens` tokens a call: the workspace
     that the gradient needs.  Tables and rows may be float32 or bfloat16, each on its own; their rows contiguous, at any
-    distance; tokens int64 or int32, those outside the table are padding."""
+    distance; tokens int64 or int32, those outside the table are padding.  Lookups may run beside each other; gradients share the
+    workspace and follow each other."""
 
     def __init__(self, vocab, dim, tokens, scale=1.0, device="cuda"):
         super().__init__(device)

@@ -38,7 +38,7 @@ def norm_of(x, t, stream):
     return plan, (*plan.clip(1.0, stream=stream), plan._keep[1])
 
 
-@pytest.mark.parametrize("way", ["argument", "current"])
+@pytest.mark.parametrize("way", ["argument", "number", "current"])
 @pytest.mark.parametrize("call", [logprob_of, gradient_of, norm_of])
 def test_the_first_call_comes_behind_the_work_that_its_buffers_memory_may_still_have(call, way):
     """A stream's first call waits for the stream that made the buffers, and leaves them to no one else before it is done."""
@@ -50,8 +50,8 @@ def test_the_first_call_comes_behind_the_work_that_its_buffers_memory_may_still_
     torch.cuda._sleep(ticks())
     busy = torch.cuda.Event()
     busy.record()
-    if way == "argument":
-        plan, got = call(x, t, side)
+    if way != "current":
+        plan, got = call(x, t, side if way == "argument" else side.cuda_stream)
     else:                                                  # the buffers are made on the one, the call comes on the other
         real = solo._operation
         with pytest.MonkeyPatch.context() as patch:

@@ -175,10 +175,12 @@ def test_the_first_call_on_another_stream_waits_for_the_buffers(streams, current
     assert side.waits == (["event of 7"] if current else ["event of 7"] * 2)
 
 
-def test_a_streams_bare_number_is_not_remembered(streams):
+@pytest.mark.parametrize("stream", [9, SimpleNamespace(cuda_stream=9)])
+def test_a_stream_that_is_not_torchs_is_not_remembered(streams, stream):
+    """It may be destroyed before the buffers are, and its number be another's."""
     handle, buffers = held(streams)
     for k in (1, 2):
-        assert handle._on_stream(9) == 9
+        assert handle._on_stream(stream) == 9
         assert len(streams.external) == k and streams.external[-1].cuda_stream == 9 and streams.external[-1].waits == ["event of 7"]
     assert not any(b.users for b in buffers)
     for none in (SimpleNamespace(cuda_stream=None), SimpleNamespace(cuda_stream=ctypes.c_void_p(0)), 0):
