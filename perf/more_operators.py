@@ -284,21 +284,22 @@ def _plain_sample(state):
     w = ((x - m) / torch.where(temperature > 0, temperature, 1.0)).exp()
     w = torch.where(temperature > 0, w, (x == m).double())
     top_k = torch.where(temperature > 0, torch.where(top_k > 0, top_k, c), 1)
-    # the first columns in the order of the logits, ties by the lower column
+    # the columns in the order of the logits, ties by the lower column
     order = x.sort(dim=1, descending=True, stable=True).indices
-    sorted_w = w.gather(1, order)
-    first = (torch.arange(c, device="cuda")[None, :] < top_k) & (sorted_w >= min_p)
-    sorted_w = torch.where(first, sorted_w, 0.0)
-    sums = sorted_w.cumsum(1)
+    w = w.gather(1, order)
+    first = (torch.arange(c, device="cuda")[None, :] < top_k) & (w >= min_p)
+    first[:, 0] = True
+    w = torch.where(first, w, 0.0)
+    sums = w.cumsum(1)
     # a column stays if those before it do not have the nucleus's share yet
     before = torch.cat([torch.zeros_like(m), sums[:, :-1]], 1)
     first = first & ((top_p >= 1) | (before < top_p * sums[:, -1:]))
     first[:, 0] = True
-    kept = torch.zeros_like(w).scatter_(1, order, first.double()) * w
-    sums = kept.cumsum(1)
+    w = torch.where(first, w, 0.0)
+    sums = w.cumsum(1)
     mass = sums[:, -1:]
-    token = (sums > state["uniform"].double()[:, None] * mass).int().argmax(1, keepdim=True)
-    return token.reshape(-1), (kept.gather(1, token) / mass).log().float().reshape(-1)
+    at = (sums > state["uniform"].double()[:, None] * mass).int().argmax(1, keepdim=True)
+    return order.gather(1, at).reshape(-1), (w.gather(1, at) / mass).log().float().reshape(-1)
 
 
 def work(case):
@@ -398,7 +399,7 @@ def _exact_sample(case, state):
         if t <= 0:
             found.append(torch.zeros((), dtype=torch.float64, device="cuda"))
             continue
-        v, at = x.sort(descending=True, stable=True)
+        v = x.sort(descending=True).values
         q = ((v - v[0]) / t).exp()
         q[int(k) if k > 0 else case["cols"]:] = 0
         q[1:][q[1:] < m] = 0
@@ -408,7 +409,5 @@ def _exact_sample(case, state):
             gone[0] = False
             q[gone] = 0
             q = q / q.sum()
-        by_column = torch.zeros_like(q).index_put_((at,), q)
-        token = (by_column.cumsum(0) > state["uniform"][r].double()).int().argmax()
-        found.append(by_column[token].log())
+        found.append(q[(q.cumsum(0) > state["uniform"][r].double()).int().argmax()].log())
     return [None, torch.stack(found)]
