@@ -239,7 +239,7 @@ int solo_adamw_step_multi(const void *table_device, uint32_t count, uint64_t uni
 /* ==== around the step ============================================================================
  * The operators of a training loop that lie next to the optimizer step: the gradients' global norm
  * and clipping, the embedding and its gradient, the log probabilities of given tokens and their
- * gradient.  The conventions of the step hold: device pointers owned by the caller, a host struct
+ * gradient, layer norm and its gradient.  The conventions of the step hold: device pointers owned by the caller, a host struct
  * read during the call, work enqueued on `stream`, no allocation, no synchronisation, SOLO_OK or a
  * negative code with nothing enqueued (but SOLO_E_HIP of a call of several launches: those before the
  * one that the runtime refused are enqueued, and the outputs are then not specified).  A workspace needs no initialisation, holds nothing between
@@ -358,6 +358,44 @@ int solo_logprob_grad(const void *logits, const void *targets, const float *entr
                       const solo_logits *shape, void *stream);
 int solo_logprob_with_grad(const void *logits, const void *targets, const float *grad_logprob, const float *grad_entropy,
                            float *logprob, float *entropy, void *grad_logits, const solo_logits *shape, void *stream);
+
+/* ---- layer norm -------------------------------------------------------------------------------
+ * For every row x of `cols` elements
+ *
+ *   mean = sum x / cols (SOLO_LAYERNORM_RMS: 0)      rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps)
+ *   h = (x - mean) rstd       y = h w + b
+ *
+ * weight NULL is 1, bias NULL 0.  stats [rows, 2], NULL or what solo_layernorm_grad takes: mean and rstd.  With g = grad_y w
+ *
+ *   grad_x = rstd (g - sum g / cols - h sum(g h) / cols)          (SOLO_LAYERNORM_RMS: without the term in sum g)
+ *   grad_weight = sum over the rows of grad_y h                   grad_bias = sum over the rows of grad_y
+ *
+ * grad_weight and grad_bias have the weights' type; with SOLO_LAYERNORM_ACCUMULATE the sums are added to what is there (a second
+ * micro-batch).  Sums are binary32, over the rows in an order that the shape alone determines; one rounding at the end.  The squares
+ * are those of the differences from the mean.  A row with a NaN or an infinity, or whose squares overflow binary32, has unspecified
+ * results in that row (and in the sums over the rows), no others.  y may be x, grad_x may be x or grad_y, where types and
+ * strides are the same; otherwise outputs must not overlap inputs. */
+#define SOLO_LAYERNORM_RMS 1u
+#define SOLO_LAYERNORM_ACCUMULATE 2u
+typedef struct solo_layernorm_shape {
+    uint64_t rows, cols;        /* below 2^31 and 2^24                                           */
+    uint64_t x_stride;          /* elements from row to row of x, >= cols, below 2^31            */
+    uint64_t y_stride;          /* the same of y / grad_y                                        */
+    uint64_t grad_stride;       /* the same of grad_x                                            */
+    uint32_t x_dtype;           /* of x and grad_x                                               */
+    uint32_t y_dtype;           /* of y and grad_y                                               */
+    uint32_t weight_dtype;      /* of weight, bias and their gradients                           */
+    uint32_t flags;             /* SOLO_LAYERNORM_*; ACCUMULATE for the gradient only            */
+    float eps;                  /* > 0, finite                                                   */
+    uint32_t reserved;          /* must be 0                                                     */
+} solo_layernorm_shape;
+
+int solo_layernorm(const void *x, const void *weight, const void *bias, void *y, float *stats, const solo_layernorm_shape *shape, void *stream);
+/* Bytes of workspace of solo_layernorm_grad (16-byte aligned), no fewer for more rows; 0 if the shape is invalid. */
+size_t solo_layernorm_workspace_bytes(const solo_layernorm_shape *shape);
+/* stats: of solo_layernorm on the same x.  grad_x may be NULL, and grad_weight or grad_bias or both (no workspace is needed then), not all three. */
+int solo_layernorm_grad(const void *grad_y, const void *x, const void *weight, const float *stats, void *grad_x, void *grad_weight, void *grad_bias,
+                        void *workspace, size_t workspace_bytes, const solo_layernorm_shape *shape, void *stream);
 
 /* Static, human-readable text for a return code. */
 const char *solo_strerror(int code);

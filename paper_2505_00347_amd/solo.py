@@ -30,6 +30,7 @@ SOLO_TABLE_BF16_COPY, SOLO_TABLE_SHORT_BLOCK = 1, 2
 SOLO_FP32, SOLO_BF16 = 0, 1
 SOLO_EMBEDDING_ACCUMULATE = 1
 SOLO_TOP_MAX = 32
+SOLO_LAYERNORM_RMS, SOLO_LAYERNORM_ACCUMULATE = 1, 2
 
 
 class solo_config(C.Structure):
@@ -70,6 +71,12 @@ class solo_logits(C.Structure):
     _fields_ = [("rows", C.c_uint64), ("cols", C.c_uint64), ("stride", C.c_uint64), ("grad_stride", C.c_uint64),
                 ("dtype", C.c_uint32), ("target_bits", C.c_uint32), ("top", C.c_uint32), ("reserved", C.c_uint32),
                 ("scale", C.c_float), ("reserved2", C.c_uint32)]
+
+
+class solo_layernorm_shape(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("cols", C.c_uint64), ("x_stride", C.c_uint64), ("y_stride", C.c_uint64), ("grad_stride", C.c_uint64),
+                ("x_dtype", C.c_uint32), ("y_dtype", C.c_uint32), ("weight_dtype", C.c_uint32), ("flags", C.c_uint32),
+                ("eps", C.c_float), ("reserved", C.c_uint32)]
 
 
 class SoloError(RuntimeError):
@@ -145,16 +152,19 @@ def _declared(L):
     L.solo_norm_table_build.restype = C.c_int; L.solo_norm_table_build.argtypes = [gp, u32, vp, size]
     L.solo_embedding_workspace_bytes.restype = size
     L.solo_embedding_workspace_bytes.argtypes = [C.POINTER(solo_embedding_shape)]
+    L.solo_layernorm_workspace_bytes.restype = size
+    L.solo_layernorm_workspace_bytes.argtypes = [C.POINTER(solo_layernorm_shape)]
     norm = [vp, u32, u64, vp, C.c_float, vp, vp, vp, vp, vp]
     for name, types in {"solo_grad_norm": norm, "solo_grad_clip": norm, "solo_embedding": [vp] * 5,
                         "solo_embedding_grad": [vp, vp, vp, vp, size, vp, vp], "solo_logprob": [vp] * 10,
-                        "solo_logprob_grad": [vp] * 9, "solo_logprob_with_grad": [vp] * 9}.items():
+                        "solo_logprob_grad": [vp] * 9, "solo_logprob_with_grad": [vp] * 9, "solo_layernorm": [vp] * 7,
+                        "solo_layernorm_grad": [vp] * 8 + [size, vp, vp]}.items():
         getattr(L, name).restype, getattr(L, name).argtypes = C.c_int, types
     return L
 
 
 _OPERATIONS = ("solo_grad_norm", "solo_grad_clip", "solo_embedding", "solo_embedding_grad", "solo_logprob",
-               "solo_logprob_grad", "solo_logprob_with_grad")
+               "solo_logprob_grad", "solo_logprob_with_grad", "solo_layernorm", "solo_layernorm_grad")
 
 
 def _by_ctypes(function, *args):
@@ -355,6 +365,18 @@ def solo_logprob_grad(logits, targets, entropy, stats, grad_logprob, grad_entrop
 def solo_logprob_with_grad(logits, targets, grad_logprob, grad_entropy, logprob, entropy, grad_logits, shape, stream=None, check=True):
     return _operation("solo_logprob_with_grad", check, logits, targets, grad_logprob, grad_entropy, logprob, entropy, grad_logits,
                       _address(shape, solo_logits), stream)
+
+
+def solo_layernorm(x, weight, bias, y, stats, shape, stream=None, check=True):
+    return _operation("solo_layernorm", check, x, weight, bias, y, stats, _address(shape, solo_layernorm_shape), stream)
+
+
+def solo_layernorm_workspace_bytes(shape): return lib().solo_layernorm_workspace_bytes(C.byref(shape))
+
+
+def solo_layernorm_grad(grad_y, x, weight, stats, grad_x, grad_weight, grad_bias, workspace, workspace_bytes, shape, stream=None, check=True):
+    return _operation("solo_layernorm_grad", check, grad_y, x, weight, stats, grad_x, grad_weight, grad_bias, workspace, workspace_bytes,
+                      _address(shape, solo_layernorm_shape), stream)
 
 
 def _dtype(tensor):
@@ -654,6 +676,85 @@ class SoloLogprob(_Handle):
         if shape.rows != self.rows:
             return None if logprob is None else logprob[:shape.rows], self._entropy_with_grad[:shape.rows], out
         return logprob, self._entropy_with_grad, out
+
+
+class SoloLayerNorm(_Handle):
+    """Layer norm of up to `rows` rows of `cols` elements (with `rms` by their root mean square alone), and its gradients: the rows' means and
+    reciprocal deviations, which the next forward() overwrites, and the gradient's workspace.  Input and output may be
+    float32 or bfloat16, each on its own, rows contiguous, at any distance; weight and bias [cols] are of one type; either or both may be None.
+    One object for each layer of a model: its gradient takes what its forward() has left."""
+
+    def __init__(self, rows, cols, eps=1e-5, rms=False, device="cuda"):
+        super().__init__(device)
+        self.rows, self.cols, self.eps, self.flags = rows, cols, eps, SOLO_LAYERNORM_RMS if rms else 0
+        self._last, self._last_grad = (None, None), (None, None)
+        shape = solo_layernorm_shape(rows, cols, cols, cols, cols, SOLO_FP32, SOLO_FP32, SOLO_FP32, self.flags, eps, 0)
+        self.workspace_bytes = solo_layernorm_workspace_bytes(shape)
+        if not self.workspace_bytes:
+            raise SoloError(SOLO_E_INVALID)
+        self.stats = _torch.empty((rows, 2), dtype=_torch.float32, device=self.device)
+        self.workspace = None                      # of the first gradient
+        self._summed = 0, None                     # rows and eps of what stats are of
+        self._hold(self.stats)
+
+    def _weights(self, tensors):
+        """The type of the weights and their gradients."""
+        kinds = {_dtype(t) for t in tensors if t is not None}
+        for t in tensors:
+            if t is not None and (t.dim() != 1 or t.numel() != self.cols or not t.is_contiguous()):
+                raise ValueError(f"{self.cols} contiguous weights expected, got {tuple(t.shape)}")
+        if len(kinds) > 1:
+            raise TypeError("weight, bias and their gradients of one type expected")
+        return kinds.pop() if kinds else SOLO_FP32
+
+    def _rows(self, x):
+        if x.dim() != 2:
+            raise ValueError(f"rows of {self.cols} expected, got {tuple(x.shape)}")
+        n = x.shape[0]
+        if n > self.rows:
+            raise ValueError(f"at most {self.rows} rows expected, got {n}")
+        return n
+
+    def forward(self, x, weight, bias, out, stream=None):
+        """out = (x - mean) * rstd * weight + bias, row by row"""
+        layout = _layout(x), _layout(weight), _layout(bias), _layout(out), self.eps
+        seen, shape = self._last                   # (read and stored as one, as in SoloEmbedding)
+        if layout != seen:
+            n = self._rows(x)
+            shape = solo_layernorm_shape(n, self.cols, _row_stride(x, n, self.cols, "input"), _row_stride(out, n, self.cols, "output"), self.cols,
+                                         _dtype(x), _dtype(out), self._weights((weight, bias)), self.flags, self.eps, 0)
+            _on(self.device, x, weight, bias, out)
+            self._last = layout, shape
+        _operation("solo_layernorm", True, x, weight, bias, out, self.stats, C.addressof(shape), self._on_stream(stream))
+        self._summed = shape.rows, shape.eps
+        return out
+
+    def grad(self, grad_out, x, weight, grad_x, grad_weight, grad_bias, accumulate=False, stream=None):
+        """Gradients behind forward() on the same x: of the input, and of weight and bias, added to what they hold if `accumulate`.  Each of the
+        three may be None, not all."""
+        layout = _layout(grad_out), _layout(x), _layout(weight), _layout(grad_x), _layout(grad_weight), _layout(grad_bias), accumulate, self.eps
+        seen, shape = self._last_grad
+        if layout != seen:
+            n = self._rows(x)
+            grad_stride = self.cols
+            if grad_x is not None:
+                grad_stride = _row_stride(grad_x, n, self.cols, "gradient")
+                if grad_x.dtype is not x.dtype:
+                    raise TypeError(f"gradient: {x.dtype} expected, got {grad_x.dtype}")
+            shape = solo_layernorm_shape(n, self.cols, _row_stride(x, n, self.cols, "input"), _row_stride(grad_out, n, self.cols, "output's gradient"),
+                                         grad_stride, _dtype(x), _dtype(grad_out), self._weights((weight, grad_weight, grad_bias)),
+                                         self.flags | (SOLO_LAYERNORM_ACCUMULATE if accumulate else 0), self.eps, 0)
+            _on(self.device, grad_out, x, weight, grad_x, grad_weight, grad_bias)
+            self._last_grad = layout, shape
+        rows, eps = self._summed
+        if rows < shape.rows or (shape.rows and eps != shape.eps):
+            raise ValueError(f"grad() takes what forward() left on the same rows: {shape.rows} expected, got {rows}")
+        if self.workspace is None:
+            self.workspace = _torch.empty(self.workspace_bytes, dtype=_torch.uint8, device=self.device)
+            self._hold(self.stats, self.workspace)
+        _operation("solo_layernorm_grad", True, grad_out, x, weight, self.stats, grad_x, grad_weight, grad_bias, self.workspace, self.workspace_bytes,
+                   C.addressof(shape), self._on_stream(stream))
+        return grad_x, grad_weight, grad_bias
 
 
 HBM_REGION_BYTES = 96 << 30      # an MI355X behaves as three such regions of physical memory
