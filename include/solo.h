@@ -239,7 +239,7 @@ int solo_adamw_step_multi(const void *table_device, uint32_t count, uint64_t uni
 /* ==== around the step ============================================================================
  * The operators of a training loop that lie next to the optimizer step: the gradients' global norm
  * and clipping, the embedding and its gradient, the log probabilities of given tokens and their
- * gradient, layer norm and its gradient.  The conventions of the step hold: device pointers owned by the caller, a host struct
+ * gradient, layer norm and its gradient, distillation from a teacher's alternatives and its gradient.  The conventions of the step hold: device pointers owned by the caller, a host struct
  * read during the call, work enqueued on `stream`, no allocation, no synchronisation, SOLO_OK or a
  * negative code with nothing enqueued (but SOLO_E_HIP of a call of several launches: those before the
  * one that the runtime refused are enqueued, and the outputs are then not specified).  A workspace needs no initialisation, holds nothing between
@@ -396,6 +396,56 @@ size_t solo_layernorm_workspace_bytes(const solo_layernorm_shape *shape);
 /* stats: of solo_layernorm on the same x.  grad_x may be NULL, and grad_weight or grad_bias or both (no workspace is needed then), not all three. */
 int solo_layernorm_grad(const void *grad_y, const void *x, const void *weight, const float *stats, void *grad_x, void *grad_weight, void *grad_bias,
                         void *workspace, size_t workspace_bytes, const solo_layernorm_shape *shape, void *stream);
+
+/* ---- distillation -----------------------------------------------------------------------------
+ * For every row x of a student's logits, with z = scale * x and q = softmax of z, and `top` alternatives of a teacher, values v_k at
+ * columns t_k (what solo_logprob writes as top_logprob and top_token, or stored logits):
+ *
+ *   p_k = softmax of teacher_scale * v over the row's alternatives, r = 0
+ *   SOLO_DISTILL_REST: p_k = e^(v_k), and what they leave of 1 is one more alternative, r = 1 - sum p_k (0 where that is below 2^-20:
+ *            the values' rounding), against the student's q_r = sum of q_j over the columns that are not among the t_k
+ *
+ *   loss = sum p_k (ln p_k - ln q_(t_k)) + r (ln r - ln q_r)            (terms with p_k = 0 or r = 0 are 0)
+ *   stats [rows, 3]: what solo_distill_grad takes: the row's largest logit, and the sums of e^z relative to it, of all columns and of
+ *            those that are not among the t_k
+ *
+ * and with d loss / d z times scale, for a = grad_loss of the row and T = sum p_k + r:
+ *
+ *   grad_logits_j = scale * a * (T q_j - sum over the k with t_k = j of p_k)        j among the t_k
+ *   grad_logits_j = scale * a * q_j (T - r / q_r)                                   elsewhere (0 where q_r is)
+ *
+ * A place whose token lies outside [0, cols) or whose value is -inf is none (solo_logprob writes -1 and -inf behind the last column); a
+ * column may occur more than once.  A row without alternatives is not read (a padding position): loss and gradient are 0.  Where the student
+ * gives no probability to an alternative that has some (-inf), the loss is +inf and the gradient the formula's; in a row of -inf alone the loss is +inf, the gradient 0.  A NaN or
+ * +inf among the logits or values of a row makes its results NaN or unspecified, no other row's.  q_r is summed by itself, not taken from 1.  Sums
+ * are binary32 and relative to the row's largest logit (1 - sum p_k: binary64).  solo_distill_with_grad does both for weights that are known beforehand,
+ * reading the logits from HBM once. */
+#define SOLO_DISTILL_REST 1u
+#define SOLO_DISTILL_MAX 128
+typedef struct solo_distill_shape {
+    uint64_t rows, cols;        /* cols below 2^29                                               */
+    uint64_t stride;            /* elements from row to row of logits, >= cols                   */
+    uint64_t grad_stride;       /* the same of grad_logits                                       */
+    uint64_t value_stride;      /* the same of teacher_value, >= top                             */
+    uint64_t token_stride;      /* the same of teacher_token, >= top                             */
+    uint32_t top;               /* alternatives, 1 .. SOLO_DISTILL_MAX                           */
+    uint32_t dtype;             /* of logits and grad_logits                                     */
+    uint32_t value_dtype;       /* of teacher_value                                              */
+    uint32_t token_bits;        /* 32 or 64: signed whole numbers                                */
+    uint32_t flags;             /* 0 or SOLO_DISTILL_REST                                        */
+    uint32_t reserved;          /* must be 0                                                     */
+    float scale;                /* > 0, finite                                                   */
+    float teacher_scale;        /* > 0, finite; 1 with SOLO_DISTILL_REST                         */
+} solo_distill_shape;
+
+/* loss and stats may be NULL. */
+int solo_distill(const void *logits, const void *teacher_value, const void *teacher_token, float *loss, float *stats,
+                 const solo_distill_shape *shape, void *stream);
+/* stats: of solo_distill on the same logits, teacher and scales.  grad_logits may be the logits themselves (same stride); it must not overlap them in another way. */
+int solo_distill_grad(const void *logits, const void *teacher_value, const void *teacher_token, const float *stats, const float *grad_loss,
+                      void *grad_logits, const solo_distill_shape *shape, void *stream);
+int solo_distill_with_grad(const void *logits, const void *teacher_value, const void *teacher_token, const float *grad_loss, float *loss,
+                           void *grad_logits, const solo_distill_shape *shape, void *stream);
 
 /* Static, human-readable text for a return code. */
 const char *solo_strerror(int code);

@@ -1,0 +1,496 @@
+// Distillation: the divergence of every row of a student's logits from a teacher of which a few alternatives are known, and the gradient.
+//
+//   e_j = e^(s (x_j - max x)),  S = sum_j e_j,  q_j = e_j / S;   the teacher's p_k at columns c_k, and what they leave of 1, r
+//   R = sum of e_j over the columns that are not among the c_k
+//   loss = sum_k p_k (ln p_k - ln q_(c_k)) + r (ln r - ln (R / S))
+//   dx_j = s a (e_j T / S - sum over k with c_k = j of p_k)  among the c_k,   s a e_j (T / S - r / R)  elsewhere,   T = sum_k p_k + r
+//
+// (r is 0 where the p_k are brought to a sum of 1.)  R is summed by itself: as 1 minus the rest of the q it would have no digits left in a
+// student that is sure of an alternative.  So the columns c_k have to be told apart in the sums already.  One wavefront reads the
+// teacher's row while the logits are on their way and hangs every alternative into a list of the thread that has its column; a thread
+// knows by one bit for each of its groups whether to look at its list.  It takes the alternatives' logits out of the sums and leaves
+// them in LDS, where the loss finds them.
+//
+// Otherwise as the log probabilities: a workgroup takes a row, one pass for the sums, the row stays in registers for the gradient.
+#include "solo_rows.h"
+
+#include <float.h>
+#include <math.h>
+
+namespace solo {
+
+constexpr int kMostTop = SOLO_DISTILL_MAX;
+constexpr uint32_t kNone = 0xFFFFFFFFu;
+constexpr double kNoRest = 1.0 / (1 << 20);    // what is left of 1 below this is the probabilities' rounding
+
+struct DistillArgs {
+    const void *logits, *value, *token;
+    void *grad;
+    float *loss, *stats;
+    const float *grad_loss;
+    uint64_t rows, stride, grad_stride, value_stride, token_stride;
+    uint32_t cols, top;
+    float scale, teacher_scale;
+    uint32_t wide, value_bf16, rest;
+};
+
+template <int THREADS>
+struct TeacherLds {
+    uint32_t head[THREADS];            // a thread's first alternative; kNone: it has none
+    uint32_t column[kMostTop];         // of an alternative; kNone: none, or an earlier one has the same
+    uint32_t next[kMostTop];
+    float p[kMostTop];                 // of all alternatives of the column
+    float logit[kMostTop];
+    float total, left;                 // T and r
+    uint32_t any;
+    float at[THREADS / kLanes], s[THREADS / kLanes];
+};
+
+// What a lane of the first wavefront keeps of its alternatives (lane, lane + 64).
+struct Alternatives {
+    static constexpr int kPer = kMostTop / kLanes;
+    float p[kPer], log_p[kPer];
+    uint32_t same[kPer];               // the first alternative with the column
+};
+
+__device__ __forceinline__ void lds_in_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
+
+// By the first wavefront: the teacher's row, and the lists.  A barrier has to follow.
+template <bool BF16, int THREADS>
+__device__ __forceinline__ void read_teacher(const DistillArgs &a, const Row<BF16> &row, uint64_t r, TeacherLds<THREADS> &lds, Alternatives &own)
+{
+    constexpr int kPer = Alternatives::kPer;
+    const uint32_t lane = threadIdx.x;
+    uint32_t column[kPer];
+    float value[kPer];
+    bool live[kPer];
+    for (uint32_t t = lane; t < THREADS; t += kLanes) lds.head[t] = kNone;
+    float most = -INFINITY;
+    bool some = false;
+#pragma unroll
+    for (int h = 0; h < kPer; ++h) {
+        const uint32_t i = lane + h * kLanes;
+        int64_t id = -1;
+        value[h] = -INFINITY;
+        if (i < a.top) {
+            id = a.wide ? static_cast<const int64_t *>(a.token)[r * a.token_stride + i] : (int64_t)static_cast<const int32_t *>(a.token)[r * a.token_stride + i];
+            value[h] = a.value_bf16 ? Elements<true>::load1(a.value, r * a.value_stride + i) : Elements<false>::load1(a.value, r * a.value_stride + i);
+        }
+        live[h] = id >= 0 && id < (int64_t)a.cols && value[h] != -INFINITY;      // (a NaN counts, and shows)
+        column[h] = live[h] ? (uint32_t)id : kNone;
+        some = some || live[h];
+        if (live[h]) most = fmaxf(most, value[h]);
+    }
+    const bool any = __ballot(some) != 0;
+    float total, left = 0.0f;
+    if (a.rest) {
+        double sum = 0.0;
+#pragma unroll
+        for (int h = 0; h < kPer; ++h) {
+            const double p = live[h] ? exp((double)value[h]) : 0.0;
+            own.p[h] = (float)p;
+            own.log_p[h] = value[h];
+            sum += p;
+        }
+        sum = wave_sum(sum);
+        if (!(1.0 - sum < kNoRest)) left = (float)(1.0 - sum);
+        total = (float)sum + left;
+    } else {
+        most = wave_max(most);
+        float sum = 0.0f;
+#pragma unroll
+        for (int h = 0; h < kPer; ++h) {
+            own.log_p[h] = (value[h] - most) * a.teacher_scale;
+            own.p[h] = live[h] ? __builtin_amdgcn_exp2f(own.log_p[h] * kLog2E) : 0.0f;
+            sum += own.p[h];
+        }
+        sum = wave_sum(sum);
+        const float log_sum = __builtin_amdgcn_logf(sum) * kLn2;
+#pragma unroll
+        for (int h = 0; h < kPer; ++h) {
+            own.p[h] /= any ? sum : 1.0f;
+            own.log_p[h] -= log_sum;
+        }
+        total = any ? 1.0f : 0.0f;
+    }
+#pragma unroll
+    for (int h = 0; h < kPer; ++h) {
+        lds.column[lane + h * kLanes] = column[h];
+        lds.p[lane + h * kLanes] = own.p[h];
+        own.same[h] = lane + h * kLanes;
+    }
+    if (lane == 0) {
+        lds.total = total;
+        lds.left = left;
+        lds.any = any;
+    }
+    lds_in_order();
+    float p[kPer] = {};
+    for (uint32_t i = 0; i < a.top; ++i) {                 // (the alternatives of one column in their order)
+        const uint32_t c = lds.column[i];
+        const float pi = lds.p[i];
+#pragma unroll
+        for (int h = 0; h < kPer; ++h)
+            if (c == column[h]) {
+                p[h] += pi;
+                own.same[h] = min(own.same[h], i);
+            }
+    }
+    lds_in_order();
+#pragma unroll
+    for (int h = 0; h < kPer; ++h) {
+        const uint32_t i = lane + h * kLanes;
+        lds.p[i] = p[h];
+        if (own.same[h] != i || !live[h]) {
+            lds.column[i] = kNone;
+        } else {
+            const uint32_t g = column[h] / Row<BF16>::kPer;
+            lds.next[i] = atomicExch(&lds.head[g < row.groups ? g % THREADS : column[h] - row.groups * Row<BF16>::kPer], i);
+        }
+    }
+}
+
+// The bits of a thread's groups that hold an alternative (group g has bit g / THREADS, of 32), and the one of its last column.
+template <bool BF16, int THREADS>
+__device__ __forceinline__ uint32_t own_alternatives(const Row<BF16> &row, const TeacherLds<THREADS> &lds, uint32_t &at_last)
+{
+    uint32_t mask = 0;
+    at_last = kNone;
+    for (uint32_t k = lds.head[threadIdx.x]; k != kNone; k = lds.next[k]) {
+        const uint32_t g = lds.column[k] / Row<BF16>::kPer;
+        if (g < row.groups) mask |= 1u << (g / THREADS % 32);
+        else at_last = k;
+    }
+    return mask;
+}
+
+// use(k, element) for the alternatives in group g.
+template <bool BF16, int THREADS, typename Use>
+__device__ __forceinline__ void for_alternatives(const TeacherLds<THREADS> &lds, uint32_t g, Use &&use)
+{
+    for (uint32_t k = lds.head[threadIdx.x]; k != kNone; k = lds.next[k]) {
+        const uint32_t c = lds.column[k];
+        if (c / Row<BF16>::kPer == g) use(k, c % Row<BF16>::kPer);
+    }
+}
+
+struct RowSums { float at, all, rest; };       // the largest logit, S and R
+
+// The sums of a row, for every thread; the alternatives' logits go to lds.  `q`, `last`: as for the sums of the log probabilities.
+template <bool BF16, bool RESIDENT, bool PAST, int THREADS, int DEPTH>
+__device__ __forceinline__ RowSums student_sums(const Row<BF16> &row, float k, TeacherLds<THREADS> &lds, Quad q[DEPTH], float last, uint32_t top,
+                                                uint32_t mask, uint32_t at_last)
+{
+    constexpr int kPer = Row<BF16>::kPer;
+    float at = -FLT_MAX, s = 0.0f, most = -FLT_MAX;        // the largest logit of the rest and its sum relative to it; the alternatives' largest
+    auto rebase = [&](float to) {
+        s *= __builtin_amdgcn_exp2f((at - to) * k);        // (0 where nothing has been added)
+        at = to;
+    };
+    auto add = [&](const Quad &quad, uint32_t g) {
+        float x[kPer];
+        Lane16<BF16>::unpack(quad, x);
+        if (mask >> (g / THREADS % 32) & 1)
+            for_alternatives<BF16, THREADS>(lds, g, [&](uint32_t i, uint32_t e) {
+                float it = x[0];
+#pragma unroll
+                for (int o = 0; o < kPer; ++o)
+                    if (o == (int)e) {
+                        it = x[o];
+                        x[o] = -INFINITY;
+                    }
+                lds.logit[i] = it;
+                most = __builtin_elementwise_maximum(most, it);
+            });
+        const float m = max_of<kPer>(x);
+        if (m > at) rebase(m);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) s += __builtin_amdgcn_exp2f((x[e] - at) * k);
+    };
+    uint32_t g0 = 0;
+    if (!RESIDENT)
+        for (; g0 + THREADS * DEPTH <= row.groups; g0 += THREADS * DEPTH) {
+            Quad now[DEPTH];
+#pragma unroll
+            for (int j = 0; j < DEPTH; ++j) {
+                now[j] = q[j];
+                q[j] = row.template group<PAST>(min(g0 + THREADS * DEPTH + j * THREADS + threadIdx.x, row.groups - 1));
+            }
+#pragma unroll
+            for (int j = 0; j < DEPTH; ++j) add(now[j], g0 + j * THREADS + threadIdx.x);
+        }
+#pragma unroll
+    for (int j = 0; j < DEPTH; ++j)
+        if (g0 + j * THREADS + threadIdx.x < row.groups) add(q[j], g0 + j * THREADS + threadIdx.x);
+    if (threadIdx.x < row.rest) {
+        if (at_last != kNone) {
+            lds.logit[at_last] = last;
+            most = __builtin_elementwise_maximum(most, last);
+        } else {
+            if (last > at) rebase(last);
+            s += __builtin_amdgcn_exp2f((last - at) * k);
+        }
+    }
+    // (an alternative that is NaN shows in its own term below)
+    const float wave_at = wave_max(fmaxf(at, most));
+    rebase(wave_at);
+    s = wave_sum(s);
+    constexpr int kWaves = THREADS / kLanes;
+    RowSums sums = {wave_at, 0.0f, s};
+    if (threadIdx.x % kLanes == 0) {
+        lds.at[threadIdx.x / kLanes] = wave_at;
+        lds.s[threadIdx.x / kLanes] = s;
+    }
+    __syncthreads();
+    if (kWaves > 1) {
+        const int part = threadIdx.x % kWaves;
+        const float part_at = lds.at[part];
+        sums.at = wave_max<kWaves>(part_at);
+        sums.rest = wave_sum<kWaves>(lds.s[part] * __builtin_amdgcn_exp2f((part_at - sums.at) * k));
+    }
+    float among = 0.0f;
+    for (uint32_t i = threadIdx.x % kLanes; i < top; i += kLanes)
+        if (lds.column[i] != kNone) among += __builtin_amdgcn_exp2f((lds.logit[i] - sums.at) * k);
+    sums.all = sums.rest + wave_sum(among);
+    return sums;
+}
+
+// By the first wavefront, behind the sums: the row's loss, for each of its lanes.
+template <int THREADS>
+__device__ __forceinline__ float row_loss(const RowSums &sums, const Alternatives &own, const TeacherLds<THREADS> &lds, uint32_t top, float scale)
+{
+    const float log_s = __builtin_amdgcn_logf(sums.all) * kLn2;
+    float loss = 0.0f;
+#pragma unroll
+    for (int h = 0; h < Alternatives::kPer; ++h)
+        if (threadIdx.x + h * kLanes < top && !(own.p[h] <= 0.0f))
+            loss = fmaf(own.p[h], own.log_p[h] - fmaf(lds.logit[own.same[h]] - sums.at, scale, -log_s), loss);
+    loss = wave_sum(loss);
+    if (lds.left > 0.0f) loss = fmaf(lds.left, (__builtin_amdgcn_logf(lds.left) - __builtin_amdgcn_logf(sums.rest)) * kLn2 + log_s, loss);
+    return sums.all == 0.0f ? INFINITY : loss;
+}
+
+// What the gradient of a row needs: dx_j = (e_j rest) factor, or (e_j all - p) factor at an alternative.
+struct DistillSlope { float at, all, rest, factor; };
+
+__device__ __forceinline__ DistillSlope distill_slope(const RowSums &sums, float total, float left, float factor)
+{
+    // (no column of a student's row without probabilities has a gradient)
+    const float all = sums.all == 0.0f ? 0.0f : total / sums.all, rest = sums.rest == 0.0f ? 0.0f : all - left / sums.rest;
+    return DistillSlope{sums.at, all, rest, sums.all == 0.0f ? 0.0f : factor};
+}
+
+template <bool BF16, bool PAST, int THREADS>
+__device__ __forceinline__ void put_distilled(const Quad &q, void *out, uint32_t g, uint32_t mask, const TeacherLds<THREADS> &lds, const DistillSlope &s, float k)
+{
+    constexpr int kPer = Row<BF16>::kPer;
+    float x[kPer];
+    Lane16<BF16>::unpack(q, x);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) x[e] = __builtin_amdgcn_exp2f((x[e] - s.at) * k);
+    float among[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) among[e] = x[e] * s.rest * s.factor;
+    if (mask >> (g / THREADS % 32) & 1)
+        for_alternatives<BF16, THREADS>(lds, g, [&](uint32_t i, uint32_t e) {
+            const float p = lds.p[i];
+#pragma unroll
+            for (int o = 0; o < kPer; ++o)
+                if (o == (int)e) among[o] = fmaf(x[o], s.all, -p) * s.factor;
+        });
+    Lane16<BF16>::template store_near<PAST>(out, g * kPer, among);
+}
+
+// FORWARD: the sums and the loss; GRAD: the gradient, from the sums or, without FORWARD, from those that are given.  RESIDENT: the row has no more
+// than THREADS * DEPTH groups, which stay in registers between the two.  PAST: 1 stores past the caches, 2 loads as well.
+template <bool BF16, bool FORWARD, bool GRAD, bool RESIDENT, int PAST, int THREADS, int DEPTH>
+__global__ __launch_bounds__(THREADS) void distill_kernel(const DistillArgs a)
+{
+    __shared__ TeacherLds<THREADS> lds;
+    const float k = a.scale * kLog2E;
+    for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        const Row<BF16> row(a, r);
+        Quad raw[DEPTH];
+        if (FORWARD) first_groups<BF16, (PAST > 1), THREADS, DEPTH>(row, raw);
+        const float last = threadIdx.x < row.rest ? row.one(row.last_column(threadIdx.x)) : -INFINITY;
+        Alternatives own;
+        if (threadIdx.x < kLanes) read_teacher<BF16, THREADS>(a, row, r, lds, own);
+        __syncthreads();
+        char *out = static_cast<char *>(a.grad) + r * a.grad_stride * Elements<BF16>::kBytes;
+        if (!lds.any) {                                    // no teacher
+            if (GRAD) {
+                const float none[Row<BF16>::kPer] = {};
+                for (uint32_t g = threadIdx.x; g < row.groups; g += THREADS) Lane16<BF16>::template store_near<(PAST > 0)>(out, g * Row<BF16>::kPer, none);
+                if (threadIdx.x < row.rest) Elements<BF16>::store1(out, row.last_column(threadIdx.x), 0.0f);
+            }
+            if (FORWARD && threadIdx.x == 0) {
+                if (a.loss) a.loss[r] = 0.0f;
+                if (a.stats) { a.stats[3 * r] = 0.0f; a.stats[3 * r + 1] = 0.0f; a.stats[3 * r + 2] = 0.0f; }
+            }
+            __syncthreads();                               // (lds.any)
+            continue;
+        }
+        uint32_t at_last;
+        const uint32_t mask = own_alternatives<BF16, THREADS>(row, lds, at_last);
+        RowSums sums;
+        if (FORWARD) {
+            sums = student_sums<BF16, RESIDENT, (PAST > 1), THREADS, DEPTH>(row, k, lds, raw, last, a.top, mask, at_last);
+            if (threadIdx.x < kLanes) {
+                const float loss = row_loss<THREADS>(sums, own, lds, a.top, a.scale);
+                if (threadIdx.x == 0) {
+                    if (a.loss) a.loss[r] = loss;
+                    if (a.stats) { a.stats[3 * r] = sums.at; a.stats[3 * r + 1] = sums.all; a.stats[3 * r + 2] = sums.rest; }
+                }
+            }
+        } else {
+            sums = RowSums{a.stats[3 * r], a.stats[3 * r + 1], a.stats[3 * r + 2]};
+        }
+        if (GRAD) {
+            const DistillSlope slope = distill_slope(sums, lds.total, lds.left, a.scale * a.grad_loss[r]);
+            for (uint32_t g0 = threadIdx.x; g0 < row.groups; g0 += THREADS * DEPTH) {
+                if (!(FORWARD && RESIDENT)) {
+#pragma unroll
+                    for (int j = 0; j < DEPTH; ++j)
+                        if (g0 + j * THREADS < row.groups) raw[j] = row.template group<(PAST > 1)>(g0 + j * THREADS);
+                }
+#pragma unroll
+                for (int j = 0; j < DEPTH; ++j)
+                    if (g0 + j * THREADS < row.groups) {
+                        // (what has been unpacked for the sums is not kept: it would take twice the registers)
+                        if (FORWARD && RESIDENT) forget(raw[j]);
+                        put_distilled<BF16, (PAST > 0), THREADS>(raw[j], out, g0 + j * THREADS, mask, lds, slope, k);
+                    }
+                if (FORWARD && RESIDENT) break;
+            }
+            if (threadIdx.x < row.rest) {
+                const float e = __builtin_amdgcn_exp2f((last - slope.at) * k);
+                const float dx = at_last != kNone ? fmaf(e, slope.all, -lds.p[at_last]) * slope.factor : e * slope.rest * slope.factor;
+                Elements<BF16>::store1(out, row.last_column(threadIdx.x), dx);
+            }
+        }
+        __syncthreads();                                   // (the lists and sums in lds)
+    }
+}
+
+// ---- host ------------------------------------------------------------------------------------
+static int distill_args(DistillArgs &a, const void *logits, const void *value, const void *token, const solo_distill_shape *s)
+{
+    if (!s || !dtype_ok(s->dtype) || !dtype_ok(s->value_dtype) || (s->token_bits != 32 && s->token_bits != 64) || (s->flags & ~SOLO_DISTILL_REST) ||
+        s->top < 1 || s->top > SOLO_DISTILL_MAX || s->reserved != 0 || !(s->scale > 0.0f) || !isfinite(s->scale) || !isfinite(s->scale * kLog2E) ||
+        !(s->teacher_scale > 0.0f) || !isfinite(s->teacher_scale) || ((s->flags & SOLO_DISTILL_REST) && s->teacher_scale != 1.0f) ||
+        s->stride < s->cols || s->value_stride < s->top || s->token_stride < s->top)
+        return SOLO_E_INVALID;
+    if (s->rows != 0 && ((s->cols != 0 && !at_multiple(logits, element_bytes(s->dtype))) || !at_multiple(value, element_bytes(s->value_dtype)) ||
+                         !at_multiple(token, s->token_bits / 8)))
+        return SOLO_E_INVALID;
+    if (s->cols >= (1ull << 29) || s->rows >= (1ull << 40) || s->stride >= (1ull << 40) || s->grad_stride >= (1ull << 40) || s->value_stride >= (1ull << 40) ||
+        s->token_stride >= (1ull << 40))
+        return SOLO_E_UNSUPPORTED;
+    a = DistillArgs{};
+    a.logits = logits; a.value = value; a.token = token;
+    a.rows = s->rows; a.cols = (uint32_t)s->cols; a.stride = s->stride; a.grad_stride = s->grad_stride;
+    a.value_stride = s->value_stride; a.token_stride = s->token_stride;
+    a.top = s->top; a.scale = s->scale; a.teacher_scale = s->teacher_scale;
+    a.wide = s->token_bits == 64; a.value_bf16 = s->value_dtype == SOLO_BF16; a.rest = (s->flags & SOLO_DISTILL_REST) != 0;
+    return SOLO_OK;
+}
+
+static bool optional_at(const void *p, uintptr_t size) { return !p || at_multiple(p, size); }
+
+// As for the log probabilities: what is larger than the last-level cache is read past it, gradients that are not small are written past it.
+constexpr uint64_t kDistillPastLoads = 256ull << 20, kDistillPastStores = 32ull << 20;
+
+template <bool BF16, bool FORWARD, bool GRAD, bool RESIDENT, int THREADS, int DEPTH>
+static int distill_launch(const DistillArgs &a, hipStream_t stream)
+{
+    constexpr int kDepth = BF16 ? DEPTH : 2 * DEPTH;
+    const uint64_t bytes = a.rows * a.cols * (BF16 ? 2 : 4);
+    const dim3 grid((uint32_t)(a.rows < (1u << 20) ? a.rows : 1u << 20));
+    if constexpr (GRAD) {
+        constexpr int kBoth = FORWARD && !RESIDENT ? 1 : 2;        // (a row that is read twice stays in the caches)
+        return launch(bytes > kDistillPastLoads    ? distill_kernel<BF16, FORWARD, GRAD, RESIDENT, kBoth, THREADS, kDepth>
+                      : bytes > kDistillPastStores ? distill_kernel<BF16, FORWARD, GRAD, RESIDENT, 1, THREADS, kDepth>
+                                                   : distill_kernel<BF16, FORWARD, GRAD, RESIDENT, 0, THREADS, kDepth>,
+                      grid, THREADS, stream, a);
+    } else {
+        return launch(bytes > kDistillPastLoads ? distill_kernel<BF16, FORWARD, GRAD, RESIDENT, 2, THREADS, kDepth>
+                                                : distill_kernel<BF16, FORWARD, GRAD, RESIDENT, 0, THREADS, kDepth>,
+                      grid, THREADS, stream, a);
+    }
+}
+
+template <bool BF16>
+static int distill_forward(const DistillArgs &a, hipStream_t stream)
+{
+    const uint32_t groups = a.cols / 8;
+    if (groups <= 256) return distill_launch<BF16, true, false, false, 64, 2>(a, stream);
+    if (a.rows >= 128 || groups <= 1024) return distill_launch<BF16, true, false, false, 256, 2>(a, stream);
+    return distill_launch<BF16, true, false, false, 512, 2>(a, stream);
+}
+
+template <bool BF16>
+static int distill_with_grad(const DistillArgs &a, hipStream_t stream)
+{
+    const uint32_t groups = (a.cols + 7) / 8;              // (all of them have to fit)
+    if (groups <= 64 * 4) return distill_launch<BF16, true, true, true, 64, 4>(a, stream);
+    if (groups <= 256 * 4) return distill_launch<BF16, true, true, true, 256, 4>(a, stream);
+    if (groups <= 512 * 4) return distill_launch<BF16, true, true, true, 512, 4>(a, stream);
+    if (groups <= 1024 * 4) return distill_launch<BF16, true, true, true, 1024, 4>(a, stream);
+    if (groups <= 1024 * 8) return distill_launch<BF16, true, true, true, 1024, 8>(a, stream);
+    return distill_launch<BF16, true, true, false, 1024, 2>(a, stream);
+}
+
+template <bool BF16>
+static int distill_only_grad(const DistillArgs &a, hipStream_t stream)
+{
+    const uint32_t groups = a.cols / 8;
+    if (groups <= 128) return distill_launch<BF16, false, true, false, 64, 2>(a, stream);
+    if (groups <= 640) return distill_launch<BF16, false, true, false, 256, 2>(a, stream);
+    return distill_launch<BF16, false, true, false, 1024, 2>(a, stream);
+}
+
+}  // namespace solo
+
+extern "C" {
+
+int solo_distill(const void *logits, const void *teacher_value, const void *teacher_token, float *loss, float *stats, const solo_distill_shape *shape, void *stream)
+{
+    using namespace solo;
+    DistillArgs a;
+    const int rc = distill_args(a, logits, teacher_value, teacher_token, shape);
+    if (rc != SOLO_OK) return rc;
+    if (shape->rows == 0) return SOLO_OK;
+    if (!optional_at(loss, 4) || !optional_at(stats, 4)) return SOLO_E_INVALID;
+    a.loss = loss; a.stats = stats;
+    return shape->dtype == SOLO_BF16 ? distill_forward<true>(a, (hipStream_t)stream) : distill_forward<false>(a, (hipStream_t)stream);
+}
+
+int solo_distill_grad(const void *logits, const void *teacher_value, const void *teacher_token, const float *stats, const float *grad_loss, void *grad_logits,
+                      const solo_distill_shape *shape, void *stream)
+{
+    using namespace solo;
+    DistillArgs a;
+    const int rc = distill_args(a, logits, teacher_value, teacher_token, shape);
+    if (rc != SOLO_OK) return rc;
+    if (shape->grad_stride < shape->cols) return SOLO_E_INVALID;
+    if (shape->rows == 0 || shape->cols == 0) return SOLO_OK;
+    if (!at_multiple(stats, 4) || !at_multiple(grad_loss, 4) || !at_multiple(grad_logits, element_bytes(shape->dtype))) return SOLO_E_INVALID;
+    a.stats = const_cast<float *>(stats); a.grad_loss = grad_loss; a.grad = grad_logits;
+    return shape->dtype == SOLO_BF16 ? distill_only_grad<true>(a, (hipStream_t)stream) : distill_only_grad<false>(a, (hipStream_t)stream);
+}
+
+int solo_distill_with_grad(const void *logits, const void *teacher_value, const void *teacher_token, const float *grad_loss, float *loss, void *grad_logits,
+                           const solo_distill_shape *shape, void *stream)
+{
+    using namespace solo;
+    DistillArgs a;
+    const int rc = distill_args(a, logits, teacher_value, teacher_token, shape);
+    if (rc != SOLO_OK) return rc;
+    if (shape->grad_stride < shape->cols) return SOLO_E_INVALID;
+    if (shape->rows == 0) return SOLO_OK;
+    if (!optional_at(loss, 4) || !at_multiple(grad_loss, 4) || (shape->cols != 0 && !at_multiple(grad_logits, element_bytes(shape->dtype)))) return SOLO_E_INVALID;
+    a.loss = loss; a.grad_loss = grad_loss; a.grad = grad_logits;
+    return shape->dtype == SOLO_BF16 ? distill_with_grad<true>(a, (hipStream_t)stream) : distill_with_grad<false>(a, (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -182,6 +182,9 @@ Entry<decltype(&solo_logprob_grad)> g_logprob_grad;
 Entry<decltype(&solo_logprob_with_grad)> g_logprob_with_grad;
 Entry<decltype(&solo_layernorm)> g_layernorm;
 Entry<decltype(&solo_layernorm_grad)> g_layernorm_grad;
+Entry<decltype(&solo_distill)> g_distill;
+Entry<decltype(&solo_distill_grad)> g_distill_grad;
+Entry<decltype(&solo_distill_with_grad)> g_distill_with_grad;
 
 template <typename T>
 bool argument(PyObject *o, T *&out) { return pointer(o, out); }
@@ -253,7 +256,8 @@ PyObject *bind_operations(PyObject *, PyObject *calls)
         {"solo_grad_norm", keep<&g_grad_norm>}, {"solo_grad_clip", keep<&g_grad_clip>}, {"solo_embedding", keep<&g_embedding>},
         {"solo_embedding_grad", keep<&g_embedding_grad>}, {"solo_logprob", keep<&g_logprob>},
         {"solo_logprob_grad", keep<&g_logprob_grad>}, {"solo_logprob_with_grad", keep<&g_logprob_with_grad>},
-        {"solo_layernorm", keep<&g_layernorm>}, {"solo_layernorm_grad", keep<&g_layernorm_grad>}};
+        {"solo_layernorm", keep<&g_layernorm>}, {"solo_layernorm_grad", keep<&g_layernorm_grad>},
+        {"solo_distill", keep<&g_distill>}, {"solo_distill_grad", keep<&g_distill_grad>}, {"solo_distill_with_grad", keep<&g_distill_with_grad>}};
     if (!PyDict_Check(calls)) {
         PyErr_SetString(PyExc_TypeError, "a dict expected");
         return nullptr;
@@ -314,6 +318,7 @@ PyMethodDef methods[] = {
     SOLO_OPERATION(grad_norm), SOLO_OPERATION(grad_clip), SOLO_OPERATION(embedding), SOLO_OPERATION(embedding_grad),
     SOLO_OPERATION(logprob), SOLO_OPERATION(logprob_grad), SOLO_OPERATION(logprob_with_grad),
     SOLO_OPERATION(layernorm), SOLO_OPERATION(layernorm_grad),
+    SOLO_OPERATION(distill), SOLO_OPERATION(distill_grad), SOLO_OPERATION(distill_with_grad),
     {"bind_operations", bind_operations, METH_O, "the entry points of the operators around the step"},
     {"bind", bind, METH_VARARGS, "the entry points and types of the binding"},
     {"forked", forked, METH_NOARGS, "called in a forked child"},

@@ -31,6 +31,7 @@ SOLO_FP32, SOLO_BF16 = 0, 1
 SOLO_EMBEDDING_ACCUMULATE = 1
 SOLO_TOP_MAX = 32
 SOLO_LAYERNORM_RMS, SOLO_LAYERNORM_ACCUMULATE = 1, 2
+SOLO_DISTILL_REST, SOLO_DISTILL_MAX = 1, 128
 
 
 class solo_config(C.Structure):
@@ -77,6 +78,12 @@ class solo_layernorm_shape(C.Structure):
     _fields_ = [("rows", C.c_uint64), ("cols", C.c_uint64), ("x_stride", C.c_uint64), ("y_stride", C.c_uint64), ("grad_stride", C.c_uint64),
                 ("x_dtype", C.c_uint32), ("y_dtype", C.c_uint32), ("weight_dtype", C.c_uint32), ("flags", C.c_uint32),
                 ("eps", C.c_float), ("reserved", C.c_uint32)]
+
+
+class solo_distill_shape(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("cols", C.c_uint64), ("stride", C.c_uint64), ("grad_stride", C.c_uint64), ("value_stride", C.c_uint64),
+                ("token_stride", C.c_uint64), ("top", C.c_uint32), ("dtype", C.c_uint32), ("value_dtype", C.c_uint32), ("token_bits", C.c_uint32),
+                ("flags", C.c_uint32), ("reserved", C.c_uint32), ("scale", C.c_float), ("teacher_scale", C.c_float)]
 
 
 class SoloError(RuntimeError):
@@ -158,13 +165,15 @@ def _declared(L):
     for name, types in {"solo_grad_norm": norm, "solo_grad_clip": norm, "solo_embedding": [vp] * 5,
                         "solo_embedding_grad": [vp, vp, vp, vp, size, vp, vp], "solo_logprob": [vp] * 10,
                         "solo_logprob_grad": [vp] * 9, "solo_logprob_with_grad": [vp] * 9, "solo_layernorm": [vp] * 7,
-                        "solo_layernorm_grad": [vp] * 8 + [size, vp, vp]}.items():
+                        "solo_layernorm_grad": [vp] * 8 + [size, vp, vp], "solo_distill": [vp] * 7, "solo_distill_grad": [vp] * 8,
+                        "solo_distill_with_grad": [vp] * 8}.items():
         getattr(L, name).restype, getattr(L, name).argtypes = C.c_int, types
     return L
 
 
 _OPERATIONS = ("solo_grad_norm", "solo_grad_clip", "solo_embedding", "solo_embedding_grad", "solo_logprob",
-               "solo_logprob_grad", "solo_logprob_with_grad", "solo_layernorm", "solo_layernorm_grad")
+               "solo_logprob_grad", "solo_logprob_with_grad", "solo_layernorm", "solo_layernorm_grad", "solo_distill", "solo_distill_grad",
+               "solo_distill_with_grad")
 
 
 def _by_ctypes(function, *args):
@@ -379,6 +388,20 @@ def solo_layernorm_grad(grad_y, x, weight, stats, grad_x, grad_weight, grad_bias
                       _address(shape, solo_layernorm_shape), stream)
 
 
+def solo_distill(logits, teacher_value, teacher_token, loss, stats, shape, stream=None, check=True):
+    return _operation("solo_distill", check, logits, teacher_value, teacher_token, loss, stats, _address(shape, solo_distill_shape), stream)
+
+
+def solo_distill_grad(logits, teacher_value, teacher_token, stats, grad_loss, grad_logits, shape, stream=None, check=True):
+    return _operation("solo_distill_grad", check, logits, teacher_value, teacher_token, stats, grad_loss, grad_logits,
+                      _address(shape, solo_distill_shape), stream)
+
+
+def solo_distill_with_grad(logits, teacher_value, teacher_token, grad_loss, loss, grad_logits, shape, stream=None, check=True):
+    return _operation("solo_distill_with_grad", check, logits, teacher_value, teacher_token, grad_loss, loss, grad_logits,
+                      _address(shape, solo_distill_shape), stream)
+
+
 def _dtype(tensor):
     if tensor.dtype is _torch.float32:
         return SOLO_FP32
@@ -392,6 +415,10 @@ def _token_bits(tensor, n):
         raise ValueError(f"{n} tokens in one dimension expected, got {tuple(tensor.shape)}")
     if n > 1 and tensor.stride(0) != 1:
         raise ValueError("tokens must be contiguous")
+    return _bits(tensor)
+
+
+def _bits(tensor):
     if tensor.dtype is _torch.int64:
         return 64
     if tensor.dtype is _torch.int32:
@@ -755,6 +782,75 @@ class SoloLayerNorm(_Handle):
         _operation("solo_layernorm_grad", True, grad_out, x, weight, self.stats, grad_x, grad_weight, grad_bias, self.workspace, self.workspace_bytes,
                    C.addressof(shape), self._on_stream(stream))
         return grad_x, grad_weight, grad_bias
+
+
+class SoloDistill(_Handle):
+    """Divergence of up to `rows` rows of a student's `cols` logits from the `top` alternatives of a teacher, and the gradient: the buffers of the
+    results, which the next call overwrites.  Logits are float32 or bfloat16, rows contiguous, at any distance; a teacher is values and
+    tokens [rows, top], such as SoloLogprob of the teacher's logits returns them (clone what the next call would overwrite) or parts of stored ones.
+    `rest`: values are log probabilities, and what they leave of 1 is one more alternative; else they are brought to a sum of 1 after a
+    multiplication by `teacher_scale`, a reciprocal temperature as `scale` is of the student."""
+
+    def __init__(self, rows, cols, top, rest=False, scale=1.0, teacher_scale=1.0, device="cuda"):
+        super().__init__(device)
+        if not 1 <= top <= SOLO_DISTILL_MAX:
+            raise ValueError(f"1 to {SOLO_DISTILL_MAX} alternatives expected, got {top}")
+        if rest and teacher_scale != 1.0:
+            raise ValueError("values whose rest counts are log probabilities: teacher_scale 1 expected")
+        self.rows, self.cols, self.top, self.flags = rows, cols, top, SOLO_DISTILL_REST if rest else 0
+        self.scale, self.teacher_scale = scale, teacher_scale
+        self._last = None, None
+        self.loss = _torch.empty(rows, dtype=_torch.float32, device=self.device)
+        self.stats = _torch.empty((rows, 3), dtype=_torch.float32, device=self.device)
+        self._summed = 0, None, None               # rows and scales of what stats are of
+        self._hold(self.loss, self.stats)
+
+    def _shape(self, logits, values, tokens, out=None):
+        layout = _layout(logits), _layout(values), _layout(tokens), _layout(out), self.scale, self.teacher_scale
+        seen, made = self._last                    # (read and stored as one, as in SoloEmbedding)
+        if layout != seen:
+            r = logits.shape[0]
+            if r > self.rows:
+                raise ValueError(f"at most {self.rows} rows expected, got {r}")
+            stride = _row_stride(logits, r, self.cols, "logits")
+            grad_stride = stride
+            if out is not None:
+                grad_stride = _row_stride(out, r, self.cols, "gradient")
+                if out.dtype is not logits.dtype:
+                    raise TypeError(f"gradient: {logits.dtype} expected, got {out.dtype}")
+            made = solo_distill_shape(r, self.cols, stride, grad_stride, _row_stride(values, r, self.top, "values"), _row_stride(tokens, r, self.top, "tokens"),
+                                      self.top, _dtype(logits), _dtype(values), _bits(tokens), self.flags, 0, self.scale, self.teacher_scale)
+            _on(self.device, logits, values, tokens, out)
+            self._last = layout, made
+        return made
+
+    def forward(self, logits, values, tokens, stream=None):
+        """The rows' losses."""
+        shape = self._shape(logits, values, tokens)
+        _operation("solo_distill", True, logits, values, tokens, self.loss, self.stats, C.addressof(shape), self._on_stream(stream))
+        self._summed = shape.rows, shape.scale, shape.teacher_scale
+        return self.loss if shape.rows == self.rows else self.loss[:shape.rows]
+
+    def grad(self, logits, values, tokens, grad_loss, out, stream=None):
+        """Gradient of the logits behind forward() on the same ones and the same teacher."""
+        shape = self._shape(logits, values, tokens, out)
+        if grad_loss is None:
+            raise ValueError(f"grad_loss: {shape.rows} contiguous float32 values expected")
+        _row_weights(grad_loss, shape.rows, "grad_loss", self.device)
+        rows, *scales = self._summed
+        if rows < shape.rows or scales != [shape.scale, shape.teacher_scale]:
+            raise ValueError(f"grad() takes what forward() left on the same rows: {shape.rows} expected, got {rows}, or other scales")
+        _operation("solo_distill_grad", True, logits, values, tokens, self.stats, grad_loss, out, C.addressof(shape), self._on_stream(stream))
+        return out
+
+    def forward_grad(self, logits, values, tokens, grad_loss, out, stream=None):
+        """(loss, gradient) in one pass, for row weights that are known beforehand.  What grad() takes stays as forward() left it."""
+        shape = self._shape(logits, values, tokens, out)
+        if grad_loss is None:
+            raise ValueError(f"grad_loss: {shape.rows} contiguous float32 values expected")
+        _row_weights(grad_loss, shape.rows, "grad_loss", self.device)
+        _operation("solo_distill_with_grad", True, logits, values, tokens, grad_loss, self.loss, out, C.addressof(shape), self._on_stream(stream))
+        return self.loss if shape.rows == self.rows else self.loss[:shape.rows], out
 
 
 HBM_REGION_BYTES = 96 << 30      # an MI355X behaves as three such regions of physical memory

@@ -94,6 +94,72 @@ def test_layer_norm_handles_refuse_what_does_not_fit():
         solo.SoloLayerNorm(4, 1 << 24, device="cpu")
 
 
+# ---- distillation ----------------------------------------------------------------------------
+
+def distill(**changes):
+    return changed(solo.solo_distill_shape(4, 8, 8, 8, 3, 3, 3, 0, 0, 64, 0, 0, 1.0, 1.0), changes)
+
+
+def distill_codes(s):
+    return {solo.solo_distill(16, 16, 16, 16, 16, s, stream=0, check=False), solo.solo_distill_grad(16, 16, 16, 16, 16, 16, s, stream=0, check=False),
+            solo.solo_distill_with_grad(16, 16, 16, 16, 16, 16, s, stream=0, check=False)}
+
+
+@pytest.mark.parametrize("changes", [dict(dtype=2), dict(value_dtype=2), dict(token_bits=16), dict(top=0), dict(top=129, value_stride=200, token_stride=200),
+                                     dict(flags=2), dict(reserved=1), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf), dict(scale=math.nan),
+                                     dict(scale=3e38), dict(teacher_scale=0.0), dict(teacher_scale=math.nan), dict(flags=1, teacher_scale=2.0),
+                                     dict(stride=7), dict(value_stride=2), dict(token_stride=2)])
+def test_distillation_shapes_that_are_refused(changes):
+    assert distill_codes(distill(**changes)) == {BAD}
+
+
+@pytest.mark.parametrize("changes", [dict(cols=1 << 29, stride=1 << 29, grad_stride=1 << 29), dict(rows=1 << 40), dict(stride=1 << 40), dict(grad_stride=1 << 40),
+                                     dict(value_stride=1 << 40), dict(token_stride=1 << 40)])
+def test_distillation_shapes_that_are_too_large(changes):
+    assert distill_codes(distill(**changes)) == {TOO_LARGE}
+
+
+def test_distillation_pointers():
+    s, good = distill(), [16] * 6
+    for at, bad in ((0, None), (0, 18), (1, None), (1, 18), (2, None), (2, 20), (3, 18), (4, 18)):
+        assert solo.solo_distill(*good[:at], bad, *good[at + 1:5], s, stream=0, check=False) == BAD, (at, bad)
+    for at, bad in ((0, None), (1, None), (2, 20), (3, None), (3, 18), (4, None), (4, 18), (5, None), (5, 18)):
+        assert solo.solo_distill_grad(*good[:at], bad, *good[at + 1:], s, stream=0, check=False) == BAD, (at, bad)
+    for at, bad in ((0, None), (1, None), (2, 20), (3, None), (3, 18), (4, 18), (5, None), (5, 18)):
+        assert solo.solo_distill_with_grad(*good[:at], bad, *good[at + 1:], s, stream=0, check=False) == BAD, (at, bad)
+    assert solo.solo_distill_grad(*good, distill(grad_stride=7), stream=0, check=False) == BAD
+    assert solo.solo_distill_with_grad(*good, distill(grad_stride=7), stream=0, check=False) == BAD
+    nothing = [None] * 6
+    assert solo.solo_distill(*nothing[:5], distill(rows=0), stream=0) == solo.SOLO_OK
+    assert solo.solo_distill_grad(*nothing, distill(rows=0), stream=0) == solo.SOLO_OK
+    assert solo.solo_distill_with_grad(*nothing, distill(rows=0), stream=0) == solo.SOLO_OK
+    for wrong in (None, 16, solo.solo_logits()):
+        with pytest.raises((C.ArgumentError, TypeError)):
+            solo.solo_distill(*good[:5], wrong, stream=0)
+
+
+def test_distillation_handles_refuse_what_does_not_fit():
+    plan = solo.SoloDistill(4, 8, 3, device="cpu")
+    x, v, t, w = torch.zeros(4, 8), torch.zeros(4, 3), torch.zeros(4, 3, dtype=torch.int64), torch.zeros(4)
+    for args in ((x[:, :7], v, t), (x, v[:3], t), (x, v, t[:, :2]), (x, v.t().contiguous().t(), t), (torch.zeros(5, 8), torch.zeros(5, 3), torch.zeros(5, 3).long())):
+        with pytest.raises(ValueError):
+            plan.forward(*args, stream=0)
+    for args in ((x.half(), v, t), (x, v.double(), t), (x, v, t.short()), (x, v, t.float())):
+        with pytest.raises(TypeError):
+            plan.forward(*args, stream=0)
+    for call in (plan.grad, plan.forward_grad):
+        for args in ((x, v, t, w[:3], x), (x, v, t, w.double(), x), (x, v, t, w, x[:3]), (x, v, t, None, x)):
+            with pytest.raises(ValueError):
+                call(*args, stream=0)
+        with pytest.raises(TypeError):
+            call(x, v, t, w, x.bfloat16(), stream=0)
+    with pytest.raises(ValueError, match="forward"):
+        plan.grad(x, v, t, w, x, stream=0)
+    for bad in (dict(top=0), dict(top=129), dict(top=3, rest=True, teacher_scale=2.0)):
+        with pytest.raises(ValueError):
+            solo.SoloDistill(4, 8, **bad, device="cpu")
+
+
 # ---- all of them -----------------------------------------------------------------------------
 
 @pytest.mark.parametrize("native", (True, False))
@@ -110,3 +176,8 @@ def test_both_ways_into_the_library_take_the_same_arguments(tmp_path, native):
     assert b.solo_layernorm_grad(*[Tensor()] * 8, C.c_size_t(3), s, stream=0, check=False) == BAD
     with pytest.raises((C.ArgumentError, TypeError)):
         b.solo_layernorm_grad(*[Tensor()] * 8, 1.5, s, stream=0)
+    s = b.solo_distill_shape(0, 8, 8, 8, 3, 3, 3, 0, 0, 64, 0, 0, 1.0, 1.0)
+    assert b.solo_distill(Tensor(), 16, C.c_void_p(16), Tensor(), None, s, stream=0) == b.SOLO_OK
+    assert b.solo_distill_grad(*[Tensor()] * 6, s, stream=0) == b.solo_distill_with_grad(*[Tensor()] * 6, s, stream=0) == b.SOLO_OK
+    s.top = 0
+    assert b.solo_distill_with_grad(*[Tensor()] * 6, s, stream=0, check=False) == BAD
