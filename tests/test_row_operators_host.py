@@ -177,7 +177,7 @@ def test_both_ways_into_the_library_take_the_same_arguments(tmp_path, native):
     with pytest.raises((C.ArgumentError, TypeError)):
         b.solo_layernorm_grad(*[Tensor()] * 8, 1.5, s, stream=0)
     s = b.solo_distill_shape(0, 8, 8, 8, 3, 3, 3, 0, 0, 64, 0, 0, 1.0, 1.0)
-    assert b.solo_distill(Tensor(), 16, C.c_void_p(16), Tensor(), None, s, stream=0) == b.SOLO_OK
+    assert b.solo_distill(Tensor(), 16, Tensor(), Tensor(), None, s, stream=0) == b.SOLO_OK
     assert b.solo_distill_grad(*[Tensor()] * 6, s, stream=0) == b.solo_distill_with_grad(*[Tensor()] * 6, s, stream=0) == b.SOLO_OK
     s.top = 0
     assert b.solo_distill_with_grad(*[Tensor()] * 6, s, stream=0, check=False) == BAD
