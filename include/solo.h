@@ -239,7 +239,8 @@ int solo_adamw_step_multi(const void *table_device, uint32_t count, uint64_t uni
 /* ==== around the step ============================================================================
  * The operators of a training loop that lie next to the optimizer step: the gradients' global norm
  * and clipping, the embedding and its gradient, the log probabilities of given tokens and their
- * gradient, layer norm and its gradient, distillation from a teacher's alternatives and its gradient.  The conventions of the step hold: device pointers owned by the caller, a host struct
+ * gradient, layer norm and its gradient, distillation from a teacher's alternatives and its
+ * gradient, sampling.  The conventions of the step hold: device pointers owned by the caller, a host struct
  * read during the call, work enqueued on `stream`, no allocation, no synchronisation, SOLO_OK or a
  * negative code with nothing enqueued (but SOLO_E_HIP of a call of several launches: those before the
  * one that the runtime refused are enqueued, and the outputs are then not specified).  A workspace needs no initialisation, holds nothing between
@@ -446,6 +447,37 @@ int solo_distill_grad(const void *logits, const void *teacher_value, const void 
                       void *grad_logits, const solo_distill_shape *shape, void *stream);
 int solo_distill_with_grad(const void *logits, const void *teacher_value, const void *teacher_token, const float *grad_loss, float *loss,
                            void *grad_logits, const solo_distill_shape *shape, void *stream);
+
+/* ---- sampling ---------------------------------------------------------------------------------
+ * For every row x of logits one column, by a given number u of [0, 1) (greater numbers count as the one next to 1, smaller ones as 0):
+ *
+ *   w_j = e^((x_j - max x) / temperature)        the columns in the order of their logits, larger ones first, ties by the lower column
+ *   kept: the first top_k of the columns with w_j >= min_p, and of these the shortest beginning whose sum of w is
+ *            at least top_p times that of them all; one column at least
+ *   token = the first column, in that order, at which the running sum of the kept w exceeds u times their sum
+ *   logprob = ln of the token's share of the kept w
+ *
+ * temperature 0: the largest logit's column (lowest of several), logprob 0.  top_k <= 0, top_p >= 1, min_p <= 0: no limit by it.  A
+ * logit of -inf is never chosen; in a row that has no other the token is -1 and logprob -inf.  A row with a NaN or +inf among its
+ * logits, or with a NaN or a negative temperature among its parameters, gives -1 and NaN.
+ * Weights are computed in binary64 and summed exactly as whole multiples of 2^-(62 - log2 cols) (2^-51 at most) of the largest, so the token is
+ * that of exact arithmetic unless u or a limit lies within some 1e-11 of a border; columns below half such a multiple are never chosen. */
+typedef struct solo_sample_shape {
+    uint64_t rows, cols;        /* cols below 2^29                                               */
+    uint64_t stride;            /* elements from row to row of logits, >= cols                   */
+    uint32_t dtype;             /* of logits                                                     */
+    uint32_t token_bits;        /* of token, 32 or 64                                            */
+    int32_t top_k;              /* where top_k is NULL                                           */
+    uint32_t reserved;          /* must be 0                                                     */
+    float temperature;          /* where temperature is NULL, >= 0                               */
+    float top_p, min_p;         /* where these are NULL, not NaN                                 */
+    uint32_t reserved2;         /* must be 0                                                     */
+} solo_sample_shape;
+
+/* uniform: float[rows]; temperature, top_k, top_p, min_p [rows]: of the rows' own, each may be NULL (all rows take the shape's); token [rows];
+ * logprob: float[rows] or NULL. */
+int solo_sample(const void *logits, const float *uniform, const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                void *token, float *logprob, const solo_sample_shape *shape, void *stream);
 
 /* Static, human-readable text for a return code. */
 const char *solo_strerror(int code);

@@ -26,7 +26,7 @@ SOURCES = ["solo_api.hip", "solo_step_m2.hip", "solo_step_m3.hip", "solo_step_m4
            "solo_step_m2_de.hip", "solo_step_m3_de.hip", "solo_step_m4_de.hip",
            "solo_step_big.hip", "solo_step_big_de.hip",
            "solo_norm.hip", "solo_embed.hip", "solo_logprob.hip", "solo_layer.hip",
-           "solo_distill.hip"]
+           "solo_distill.hip", "solo_sample.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # -ffp-contract=off and IEEE divide/sqrt: the stored codes and scales depend on the exact
 # rounding of every operation.  Packed-FP32 instructions are disabled on the test machines.

@@ -185,6 +185,7 @@ Entry<decltype(&solo_layernorm_grad)> g_layernorm_grad;
 Entry<decltype(&solo_distill)> g_distill;
 Entry<decltype(&solo_distill_grad)> g_distill_grad;
 Entry<decltype(&solo_distill_with_grad)> g_distill_with_grad;
+Entry<decltype(&solo_sample)> g_sample;
 
 template <typename T>
 bool argument(PyObject *o, T *&out) { return pointer(o, out); }
@@ -257,7 +258,8 @@ PyObject *bind_operations(PyObject *, PyObject *calls)
         {"solo_embedding_grad", keep<&g_embedding_grad>}, {"solo_logprob", keep<&g_logprob>},
         {"solo_logprob_grad", keep<&g_logprob_grad>}, {"solo_logprob_with_grad", keep<&g_logprob_with_grad>},
         {"solo_layernorm", keep<&g_layernorm>}, {"solo_layernorm_grad", keep<&g_layernorm_grad>},
-        {"solo_distill", keep<&g_distill>}, {"solo_distill_grad", keep<&g_distill_grad>}, {"solo_distill_with_grad", keep<&g_distill_with_grad>}};
+        {"solo_distill", keep<&g_distill>}, {"solo_distill_grad", keep<&g_distill_grad>}, {"solo_distill_with_grad", keep<&g_distill_with_grad>},
+        {"solo_sample", keep<&g_sample>}};
     if (!PyDict_Check(calls)) {
         PyErr_SetString(PyExc_TypeError, "a dict expected");
         return nullptr;
@@ -319,6 +321,7 @@ PyMethodDef methods[] = {
     SOLO_OPERATION(logprob), SOLO_OPERATION(logprob_grad), SOLO_OPERATION(logprob_with_grad),
     SOLO_OPERATION(layernorm), SOLO_OPERATION(layernorm_grad),
     SOLO_OPERATION(distill), SOLO_OPERATION(distill_grad), SOLO_OPERATION(distill_with_grad),
+    SOLO_OPERATION(sample),
     {"bind_operations", bind_operations, METH_O, "the entry points of the operators around the step"},
     {"bind", bind, METH_VARARGS, "the entry points and types of the binding"},
     {"forked", forked, METH_NOARGS, "called in a forked child"},

@@ -86,6 +86,12 @@ class solo_distill_shape(C.Structure):
                 ("flags", C.c_uint32), ("reserved", C.c_uint32), ("scale", C.c_float), ("teacher_scale", C.c_float)]
 
 
+class solo_sample_shape(C.Structure):
+    _fields_ = [("rows", C.c_uint64), ("cols", C.c_uint64), ("stride", C.c_uint64), ("dtype", C.c_uint32), ("token_bits", C.c_uint32),
+                ("top_k", C.c_int32), ("reserved", C.c_uint32), ("temperature", C.c_float), ("top_p", C.c_float), ("min_p", C.c_float),
+                ("reserved2", C.c_uint32)]
+
+
 class SoloError(RuntimeError):
     def __init__(self, code):
         self.code = code
@@ -166,14 +172,14 @@ def _declared(L):
                         "solo_embedding_grad": [vp, vp, vp, vp, size, vp, vp], "solo_logprob": [vp] * 10,
                         "solo_logprob_grad": [vp] * 9, "solo_logprob_with_grad": [vp] * 9, "solo_layernorm": [vp] * 7,
                         "solo_layernorm_grad": [vp] * 8 + [size, vp, vp], "solo_distill": [vp] * 7, "solo_distill_grad": [vp] * 8,
-                        "solo_distill_with_grad": [vp] * 8}.items():
+                        "solo_distill_with_grad": [vp] * 8, "solo_sample": [vp] * 10}.items():
         getattr(L, name).restype, getattr(L, name).argtypes = C.c_int, types
     return L
 
 
 _OPERATIONS = ("solo_grad_norm", "solo_grad_clip", "solo_embedding", "solo_embedding_grad", "solo_logprob",
                "solo_logprob_grad", "solo_logprob_with_grad", "solo_layernorm", "solo_layernorm_grad", "solo_distill", "solo_distill_grad",
-               "solo_distill_with_grad")
+               "solo_distill_with_grad", "solo_sample")
 
 
 def _by_ctypes(function, *args):
@@ -402,6 +408,10 @@ def solo_distill_with_grad(logits, teacher_value, teacher_token, grad_loss, loss
                       _address(shape, solo_distill_shape), stream)
 
 
+def solo_sample(logits, uniform, temperature, top_k, top_p, min_p, token, logprob, shape, stream=None, check=True):
+    return _operation("solo_sample", check, logits, uniform, temperature, top_k, top_p, min_p, token, logprob, _address(shape, solo_sample_shape), stream)
+
+
 def _dtype(tensor):
     if tensor.dtype is _torch.float32:
         return SOLO_FP32
@@ -438,11 +448,12 @@ def _row_stride(tensor, rows, cols, name):
     return stride
 
 
-def _row_weights(tensor, rows, name, device):
+def _row_weights(tensor, rows, name, device, dtype=None):
+    dtype = dtype or _torch.float32
     if tensor is None:
         return
-    if tensor.dtype is not _torch.float32 or tensor.dim() != 1 or tensor.numel() != rows or not tensor.is_contiguous():
-        raise ValueError(f"{name}: {rows} contiguous float32 values expected")
+    if tensor.dtype is not dtype or tensor.dim() != 1 or tensor.numel() != rows or not tensor.is_contiguous():
+        raise ValueError(f"{name}: {rows} contiguous {str(dtype)[6:]} values expected")
     if tensor.device != device:
         raise ValueError(f"{name}: on {device} expected, got {tensor.device}")
 
@@ -851,6 +862,43 @@ class SoloDistill(_Handle):
         _row_weights(grad_loss, shape.rows, "grad_loss", self.device)
         _operation("solo_distill_with_grad", True, logits, values, tokens, grad_loss, self.loss, out, C.addressof(shape), self._on_stream(stream))
         return self.loss if shape.rows == self.rows else self.loss[:shape.rows], out
+
+
+class SoloSampler(_Handle):
+    """A token of each of up to `rows` rows of `cols` logits (float32 or bfloat16, rows contiguous, at any distance), drawn by given uniform numbers,
+    and its log probability among what temperature, top_k, min_p and top_p keep: buffers of this object, which the next call
+    overwrites.  Rows with parameters of their own give a call tensors [rows] of them (float32; top_k: int32) in the place of the object's numbers."""
+
+    def __init__(self, rows, cols, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, device="cuda"):
+        super().__init__(device)
+        if not temperature >= 0.0 or top_p != top_p or min_p != min_p:
+            raise ValueError(f"a temperature of 0 or more, and numbers, expected, got {temperature}, top_p {top_p}, min_p {min_p}")
+        self.rows, self.cols = rows, cols
+        self.temperature, self.top_k, self.top_p, self.min_p = temperature, top_k, top_p, min_p
+        self._last = None, None
+        self.token = _torch.empty(rows, dtype=_torch.int64, device=self.device)
+        self.logprob = _torch.empty(rows, dtype=_torch.float32, device=self.device)
+        self._hold(self.token, self.logprob)
+
+    def sample(self, logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+        """(token, logprob)"""
+        own = temperature, top_k, top_p, min_p
+        layout = (_layout(logits), _layout(uniform), *map(_layout, own), self.temperature, self.top_k, self.top_p, self.min_p)
+        seen, shape = self._last                   # (read and stored as one, as in SoloEmbedding)
+        if layout != seen:
+            r = logits.shape[0]
+            if r > self.rows:
+                raise ValueError(f"at most {self.rows} rows expected, got {r}")
+            shape = solo_sample_shape(r, self.cols, _row_stride(logits, r, self.cols, "logits"), _dtype(logits), 64, min(max(self.top_k, 0), 0x7FFFFFFF), 0,
+                                      self.temperature, self.top_p, self.min_p, 0)
+            if uniform is None:
+                raise ValueError(f"uniform: {r} contiguous float32 values expected")
+            _on(self.device, logits)
+            for tensor, name in zip((uniform, *own), ("uniform", "temperature", "top_k", "top_p", "min_p")):
+                _row_weights(tensor, r, name, self.device, _torch.int32 if name == "top_k" else None)
+            self._last = layout, shape
+        _operation("solo_sample", True, logits, uniform, *own, self.token, self.logprob, C.addressof(shape), self._on_stream(stream))
+        return (self.token, self.logprob) if shape.rows == self.rows else (self.token[:shape.rows], self.logprob[:shape.rows])
 
 
 HBM_REGION_BYTES = 96 << 30      # an MI355X behaves as three such regions of physical memory

@@ -160,6 +160,47 @@ def test_distillation_handles_refuse_what_does_not_fit():
             solo.SoloDistill(4, 8, **bad, device="cpu")
 
 
+# ---- sampling --------------------------------------------------------------------------------
+
+def sample(**changes):
+    return changed(solo.solo_sample_shape(4, 8, 8, 0, 64, 0, 0, 1.0, 1.0, 0.0, 0), changes)
+
+
+@pytest.mark.parametrize("changes", [dict(dtype=2), dict(token_bits=8), dict(reserved=1), dict(reserved2=1), dict(temperature=-1.0), dict(temperature=math.nan),
+                                     dict(top_p=math.nan), dict(min_p=math.nan), dict(stride=7)])
+def test_sampling_shapes_that_are_refused(changes):
+    assert solo.solo_sample(*[16] * 8, sample(**changes), stream=0, check=False) == BAD
+
+
+@pytest.mark.parametrize("changes", [dict(cols=1 << 29, stride=1 << 29), dict(rows=1 << 40), dict(stride=1 << 40)])
+def test_sampling_shapes_that_are_too_large(changes):
+    assert solo.solo_sample(*[16] * 8, sample(**changes), stream=0, check=False) == TOO_LARGE
+
+
+def test_sampling_pointers():
+    s, good = sample(), [16] * 8
+    for at, bad in ((0, None), (0, 18), (1, None), (1, 18), (2, 18), (3, 18), (4, 18), (5, 18), (6, None), (6, 20), (7, 18)):
+        assert solo.solo_sample(*good[:at], bad, *good[at + 1:], s, stream=0, check=False) == BAD, (at, bad)
+    assert solo.solo_sample(*[None] * 8, sample(rows=0), stream=0) == solo.SOLO_OK
+    for wrong in (None, 16, solo.solo_logits()):
+        with pytest.raises((C.ArgumentError, TypeError)):
+            solo.solo_sample(*good, wrong, stream=0)
+
+
+def test_sampling_handles_refuse_what_does_not_fit():
+    plan = solo.SoloSampler(4, 8, device="cpu")
+    x, u, k = torch.zeros(4, 8), torch.zeros(4), torch.zeros(4, dtype=torch.int32)
+    for args, more in (((x[:, :7], u), {}), ((x, u[:3]), {}), ((x, u.double()), {}), ((x, None), {}), ((torch.zeros(5, 8), torch.zeros(5)), {}), ((x, u), dict(top_k=u)),
+                       ((x, u), dict(top_k=k.long())), ((x, u), dict(temperature=k)), ((x, u), dict(top_p=u[:2])), ((x, u), dict(min_p=torch.zeros(8)[::2]))):
+        with pytest.raises(ValueError):
+            plan.sample(*args, **more, stream=0)
+    with pytest.raises(TypeError):
+        plan.sample(x.half(), u, stream=0)
+    for bad in (dict(temperature=-1.0), dict(temperature=math.nan), dict(top_p=math.nan), dict(min_p=math.nan)):
+        with pytest.raises(ValueError):
+            solo.SoloSampler(4, 8, **bad, device="cpu")
+
+
 # ---- all of them -----------------------------------------------------------------------------
 
 @pytest.mark.parametrize("native", (True, False))
@@ -179,5 +220,6 @@ def test_both_ways_into_the_library_take_the_same_arguments(tmp_path, native):
     s = b.solo_distill_shape(0, 8, 8, 8, 3, 3, 3, 0, 0, 64, 0, 0, 1.0, 1.0)
     assert b.solo_distill(Tensor(), 16, Tensor(), Tensor(), None, s, stream=0) == b.SOLO_OK
     assert b.solo_distill_grad(*[Tensor()] * 6, s, stream=0) == b.solo_distill_with_grad(*[Tensor()] * 6, s, stream=0) == b.SOLO_OK
+    assert b.solo_sample(Tensor(), 16, None, Tensor(), None, None, 16, None, b.solo_sample_shape(0, 8, 8, 0, 32, 0, 0, 1.0, 1.0, 0.0, 0), stream=0) == b.SOLO_OK
     s.top = 0
     assert b.solo_distill_with_grad(*[Tensor()] * 6, s, stream=0, check=False) == BAD
