@@ -6,11 +6,12 @@
 //
 // Each of the three is a place in the order at which a running sum (of ones or of w) reaches a goal, and none needs the order itself: a
 // histogram over the distance from the maximum gives the bucket that holds the place, and only that bucket's columns are looked at
-// again, each against all others of them.  A bucket with too many (equal logits, mostly) is cut further by whole keys, value and column, until it has few.
+// again, each against all others of them.  A bucket with too many (equal logits, mostly) is cut further by whole keys, value and column, until
+// it has few.  Where top_k or min_p leave few columns, which a bound on their logits shows beforehand, only these are weighed and put in order.
 //
 // Which column it is hangs on comparisons of sums, so these are exact: w is computed in binary64 (the rate of its instructions is that of
-// binary32), to 4e-14, and rounded to a whole multiple of 2^-shift; sums of such are whole numbers below 2^63, the same in every order, and atomic additions in
-// LDS make them.
+// binary32), to 2e-13, and rounded to a whole multiple of 2^-shift; sums of such are whole numbers below 2^63, the same in every order, and atomic
+// additions in LDS make them.
 #include "solo_rows.h"
 
 #include <float.h>
@@ -18,8 +19,21 @@
 
 namespace solo {
 
-constexpr uint32_t kBuckets = 2048;    // of the distance from the maximum
-constexpr uint32_t kListed = 1024;     // columns of a bucket that are compared with each other
+constexpr uint32_t kBuckets = 2048;    // of a 32nd of a binary order of w each
+constexpr uint32_t kListed = 1024;     // columns that are kept as a list
+constexpr uint32_t kSorted = 512;      // columns that are put in order by comparing each with all others
+
+// 2^(i / 32)
+__constant__ const double kRoots[32] = {
+    0x1.0000000000000p+0, 0x1.059b0d3158574p+0, 0x1.0b5586cf9890fp+0, 0x1.11301d0125b51p+0,
+    0x1.172b83c7d517bp+0, 0x1.1d4873168b9aap+0, 0x1.2387a6e756238p+0, 0x1.29e9df51fdee1p+0,
+    0x1.306fe0a31b715p+0, 0x1.371a7373aa9cbp+0, 0x1.3dea64c123422p+0, 0x1.44e086061892dp+0,
+    0x1.4bfdad5362a27p+0, 0x1.5342b569d4f82p+0, 0x1.5ab07dd485429p+0, 0x1.6247eb03a5585p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.71f75e8ec5f74p+0, 0x1.7a11473eb0187p+0, 0x1.82589994cce13p+0,
+    0x1.8ace5422aa0dbp+0, 0x1.93737b0cdc5e5p+0, 0x1.9c49182a3f090p+0, 0x1.a5503b23e255dp+0,
+    0x1.ae89f995ad3adp+0, 0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0,
+    0x1.d5818dcfba487p+0, 0x1.dfc97337b9b5fp+0, 0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0,
+};
 
 struct SampleArgs {
     const void *logits;
@@ -38,71 +52,181 @@ template <int THREADS>
 struct SampleLds {
     uint64_t mass[kBuckets + 1];       // sums of the buckets, then of all in front of a bucket
     uint32_t count[kBuckets + 1];
-    uint64_t key[kListed], weight[kListed], before[kListed];
-    uint32_t places[kListed];
+    uint64_t key[kListed], weight[kListed];            // of the columns above a bound
+    uint64_t sub_key[kSorted], sub_weight[kSorted];        // of those in a bucket
+    uint64_t running[kSorted];         // in order: the sum of w up to and with each
+    uint32_t place[kSorted], ordered[kSorted];
+    uint64_t root[32];                 // 2^(i / 32) times 2^shift, as bits, less what i adds to the exponent below
     uint64_t wave_mass[THREADS / kLanes], lowest, highest;
     uint32_t wave_count[THREADS / kLanes];
     float at[THREADS / kLanes];
-    uint32_t listed, bucket, column;
+    uint32_t listed, bucket;
     uint64_t found_key, found_mass;
+    double inverse, below, nucleus;    // of temperature; uniform and top_p, within their ends
 };
 
-// The weights of a row.  A whole number of 2^-shift; 0 where the column does not count (w below min_p, or nothing at all).
-struct Weights {
-    float max, per_bucket;             // (max - x) * per_bucket is the bucket
-    double per_order, least;           // (x - max) * per_order is log2 w; least: min_p in whole numbers
-    uint32_t shift;
-
-    __device__ __forceinline__ float place(float x) const { return (max - x) * per_bucket; }
-    __device__ __forceinline__ static bool counts(float place) { return place <= kBuckets * 1.001f; }     // (not a NaN)
-    __device__ __forceinline__ static uint32_t bucket(float place) { return min((uint32_t)place, kBuckets - 1); }
-    __device__ __forceinline__ uint64_t operator()(float x) const
-    {
-        const double t = fmax(((double)x - (double)max) * per_order, -2000.0);
-        const double z = t + 0x1.8p52, r = t - (z - 0x1.8p52);
-        const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, z);
-        // 2^r - 1 over r, interpolated at Chebyshev's nodes of [-1/2, 1/2]
-        double p = 1.0203121063391729e-07;
-        p = fma(p, r, 1.3255224878668817e-06);
-        p = fma(p, r, 1.525268684626772e-05);
-        p = fma(p, r, 0.00015403455852453838);
-        p = fma(p, r, 0.0013333558179043112);
-        p = fma(p, r, 0.009618129159402558);
-        p = fma(p, r, 0.055504108664760424);
-        p = fma(p, r, 0.2402265069581299);
-        p = fma(p, r, 0.6931471805599453);
-        p = fma(p, r, 1.0);
-        const double w = __builtin_amdgcn_ldexp(p, n + (int)shift);
-        const uint64_t whole = __builtin_bit_cast(uint64_t, w + 0x1p52) - 0x4330000000000000ull;
-        return w >= least ? whole : 0;
-    }
-};
-
-// use(x, column) for every column of the row, each by one thread.
-template <bool BF16, int THREADS, typename Use>
-__device__ __forceinline__ void for_columns(const Row<BF16> &row, Use &&use)
+// threadIdx.x, as something that the compiler does not know: addresses made of it are made where they are used.  Made in front of the loop
+// over the places to find and kept, as they would be, they take forty registers.
+__device__ __forceinline__ uint32_t this_thread()
 {
-    constexpr int kPer = Row<BF16>::kPer, kDepth = 4;
-    for (uint32_t g0 = threadIdx.x; g0 < row.groups; g0 += THREADS * kDepth) {
-        Quad q[kDepth];
-#pragma unroll
-        for (int j = 0; j < kDepth; ++j) q[j] = row.group(min(g0 + j * THREADS, row.groups - 1));
-#pragma unroll
-        for (int j = 0; j < kDepth; ++j)
-            if (g0 + j * THREADS < row.groups) {
-                float x[kPer];
-                Lane16<BF16>::unpack(q[j], x);
-#pragma unroll
-                for (int e = 0; e < kPer; ++e) use(x[e], (g0 + j * THREADS) * kPer + e);
-            }
+    uint32_t thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));
+    return thread;
+}
+
+// A value that is the same in all lanes, in scalar registers.
+template <typename T>
+__device__ __forceinline__ T scalar(T x)
+{
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+    } else {
+        const uint64_t bits = __builtin_bit_cast(uint64_t, x);
+        const uint32_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)bits), high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(bits >> 32));
+        return __builtin_bit_cast(T, (uint64_t)high << 32 | low);
     }
-    if (threadIdx.x < row.rest) use(row.one(row.last_column(threadIdx.x)), row.last_column(threadIdx.x));
+}
+
+// The weights of a row, as whole numbers of 2^-shift.
+struct Weights {
+    double max, per_order;             // (x - max) * per_order is log2 w
+    uint64_t least;                    // what counts: min_p, or 1
+    const uint64_t *root;
+
+    // w, and its bucket (that of w = 2^-64 for all below)
+    __device__ __forceinline__ uint64_t operator()(float x, uint32_t &bucket) const
+    {
+        const double t = fmax(((double)x - max) * per_order, -64.0);
+        const double z = t + 0x1.8p47, r = t - (z - 0x1.8p47);     // (to 32nds)
+        const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, z);
+        bucket = 0 - n;
+        // (2^r - 1) / r, interpolated at Chebyshev's nodes of [-1/64, 1/64]
+        double p = 0.009618166713972776;
+        p = fma(p, r, 0.055504434191939005);
+        p = fma(p, r, 0.24022650695795306);
+        p = fma(p, r, 0.693147180550011);
+        p = fma(p, r, 1.0);
+        // n / 32 whole orders are added to the exponent: n << 47, and what n % 32 adds there has been taken from the root
+        const uint64_t root_bits = root[n & 31];
+        const double scale = __builtin_bit_cast(double, (uint64_t)((uint32_t)(root_bits >> 32) + (n << 15)) << 32 | (uint32_t)root_bits);
+        return __builtin_bit_cast(uint64_t, fma(p, scale, 0x1p52)) - 0x4330000000000000ull;
+    }
+    // A logit that none of `orders` binary orders below the maximum, or fewer, is below: with room for the rounding of all that is compared.
+    __device__ __forceinline__ float lowest(double orders) const
+    {
+        const float x = (float)(max - (orders + 1e-6) / per_order);
+        return x - (fabsf(x) + fabsf((float)max)) * 0x1p-21f;
+    }
+    __device__ __forceinline__ float highest(double orders) const
+    {
+        const float x = (float)(max - (orders - 1e-6) / per_order);
+        return x + (fabsf(x) + fabsf((float)max)) * 0x1p-21f;
+    }
+};
+
+// The columns of a row, each one thread's.  With DEPTH, rows of no more than THREADS * DEPTH groups stay in registers; else every pass loads them.
+template <bool BF16, int THREADS, int DEPTH>
+struct Columns {
+    static constexpr int kPer = Row<BF16>::kPer, kAhead = 4;
+    const Row<BF16> &row;
+    Quad q[DEPTH ? DEPTH : 1];
+    float last;
+
+    __device__ __forceinline__ explicit Columns(const Row<BF16> &row) : row(row)
+    {
+        if (DEPTH && row.groups != 0) {
+#pragma unroll
+            for (int j = 0; j < DEPTH; ++j) q[j] = row.group(min(j * THREADS + threadIdx.x, row.groups - 1));
+        }
+        last = threadIdx.x < row.rest ? row.one(row.last_column(threadIdx.x)) : -INFINITY;
+    }
+    // use(x, n, column): the n logits x from column `column` on
+    template <typename Use>
+    __device__ __forceinline__ void each(Use &&use)
+    {
+        float x[kPer];
+        if (DEPTH) {
+            // (the compiler does not know the logits from here on either: it would unpack and convert them once, in front of all passes)
+            const uint32_t thread = this_thread();
+#pragma unroll
+            for (int j = 0; j < DEPTH; ++j)
+                if (j * THREADS + thread < row.groups) {
+                    Quad a = q[j];
+                    forget(a);
+                    Lane16<BF16>::unpack(a, x);
+                    use(x, std::integral_constant<int, kPer>(), (j * THREADS + thread) * kPer);
+                }
+        } else {
+            for (uint32_t g0 = this_thread(); g0 < row.groups; g0 += THREADS * kAhead) {
+                Quad a[kAhead];
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j) a[j] = row.group(min(g0 + j * THREADS, row.groups - 1));
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j)
+                    if (g0 + j * THREADS < row.groups) {
+                        Lane16<BF16>::unpack(a[j], x);
+                        use(x, std::integral_constant<int, kPer>(), (g0 + j * THREADS) * kPer);
+                    }
+            }
+        }
+        if (threadIdx.x < row.rest) {
+            x[0] = last;
+            use(x, std::integral_constant<int, 1>(), row.last_column(threadIdx.x));
+        }
+    }
+    // use(x, column) for the logits from `from` to `to`: few
+    template <typename Use>
+    __device__ __forceinline__ void between(float from, float to, Use &&use)
+    {
+        each([&](const float *x, auto n, uint32_t column) {
+            bool any = false;
+#pragma unroll
+            for (int e = 0; e < n; ++e) any |= __builtin_amdgcn_fmed3f(x[e], from, to) == x[e];
+            if (!any) return;
+            uint32_t hits = 0;
+#pragma unroll
+            for (int e = 0; e < n; ++e) hits |= (x[e] >= from && x[e] <= to ? 1u : 0u) << e;
+            while (hits != 0) {
+                const uint32_t e = __builtin_ctz(hits);
+                hits &= hits - 1;
+                float it = x[0];
+#pragma unroll
+                for (int o = 1; o < n; ++o) it = (int)e == o ? x[o] : it;
+                use(it, column + e);
+            }
+        });
+    }
+};
+
+// A running sum over the lanes of a wavefront.
+template <typename T, int CONTROL, int ROWS>
+__device__ __forceinline__ T from_lane(T x)
+{
+    if constexpr (sizeof(T) == 4) {
+        return (T)__builtin_amdgcn_update_dpp(0, (int)x, CONTROL, ROWS, 0xF, false);
+    } else {
+        const uint32_t low = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CONTROL, ROWS, 0xF, false);
+        const uint32_t high = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CONTROL, ROWS, 0xF, false);
+        return (uint64_t)high << 32 | low;
+    }
+}
+template <typename T>
+__device__ __forceinline__ T running_sum(T x)
+{
+    x += from_lane<T, 0x111, 0xF>(x);                      // 1, 2, 4 and 8 lanes before, in rows of 16; then the rows before
+    x += from_lane<T, 0x112, 0xF>(x);
+    x += from_lane<T, 0x114, 0xF>(x);
+    x += from_lane<T, 0x118, 0xF>(x);
+    x += from_lane<T, 0x142, 0xA>(x);
+    x += from_lane<T, 0x143, 0xC>(x);
+    return x;
 }
 
 template <int THREADS>
 __device__ __forceinline__ void clear_buckets(SampleLds<THREADS> &lds)
 {
-    for (uint32_t b = threadIdx.x; b <= kBuckets; b += THREADS) {
+    const uint32_t thread = this_thread();
+    for (uint32_t b = thread; b <= kBuckets; b += THREADS) {
         lds.mass[b] = 0;
         lds.count[b] = 0;
     }
@@ -110,247 +234,369 @@ __device__ __forceinline__ void clear_buckets(SampleLds<THREADS> &lds)
 }
 
 // Sums of the buckets to sums of all in front of a bucket.  The last entry has the sums of all.
-template <int THREADS>
+template <bool MASS, bool COUNT, int THREADS>
 __device__ __forceinline__ void add_up_buckets(SampleLds<THREADS> &lds)
 {
+    const uint32_t thread = this_thread();
     constexpr uint32_t kEach = kBuckets / THREADS;
-    const uint32_t lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes, first = threadIdx.x * kEach;
+    constexpr int kWaves = THREADS / kLanes;
+    const uint32_t lane = thread % kLanes, wave = thread / kLanes, first = thread * kEach;
     __syncthreads();
-    uint64_t mass = 0;
-    uint32_t count = 0;
+    uint64_t mass[kEach], mass_to = 0;
+    uint32_t count[kEach], count_to = 0;
+#pragma unroll
     for (uint32_t b = 0; b < kEach; ++b) {
-        mass += lds.mass[first + b];
-        count += lds.count[first + b];
+        if (MASS) mass_to += mass[b] = lds.mass[first + b];
+        if (COUNT) count_to += count[b] = lds.count[first + b];
     }
-    uint64_t mass_to = mass;
-    uint32_t count_to = count;
-    for (uint32_t d = 1; d < kLanes; d *= 2) {
-        const uint64_t m = __shfl_up(mass_to, d);
-        const uint32_t c = __shfl_up(count_to, d);
-        if (lane >= d) {
-            mass_to += m;
-            count_to += c;
+    const uint64_t own_mass = mass_to;
+    const uint32_t own_count = count_to;
+    if (MASS) mass_to = running_sum(mass_to);
+    if (COUNT) count_to = running_sum(count_to);
+    if (lane == kLanes - 1) {
+        if (MASS) lds.wave_mass[wave] = mass_to;
+        if (COUNT) lds.wave_count[wave] = count_to;
+    }
+    __syncthreads();
+    const uint32_t part = lane % kWaves;
+    if (MASS) mass_to += wave_sum<kWaves>(part < wave ? lds.wave_mass[part] : 0) - own_mass;
+    if (COUNT) count_to += wave_sum<kWaves>(part < wave ? lds.wave_count[part] : 0) - own_count;
+#pragma unroll
+    for (uint32_t b = 0; b < kEach; ++b) {
+        if (MASS) {
+            lds.mass[first + b] = mass_to;
+            mass_to += mass[b];
+        }
+        if (COUNT) {
+            lds.count[first + b] = count_to;
+            count_to += count[b];
         }
     }
-    if (lane == kLanes - 1) {
-        lds.wave_mass[wave] = mass_to;
-        lds.wave_count[wave] = count_to;
-    }
-    __syncthreads();
-    mass_to -= mass;
-    count_to -= count;
-    for (uint32_t w = 0; w < wave; ++w) {
-        mass_to += lds.wave_mass[w];
-        count_to += lds.wave_count[w];
-    }
-    for (uint32_t b = 0; b < kEach; ++b) {
-        const uint64_t m = lds.mass[first + b];
-        const uint32_t c = lds.count[first + b];
-        lds.mass[first + b] = mass_to;
-        lds.count[first + b] = count_to;
-        mass_to += m;
-        count_to += c;
-    }
-    if (threadIdx.x == THREADS - 1) {
-        lds.mass[kBuckets] = mass_to;
-        lds.count[kBuckets] = count_to;
+    if (thread == THREADS - 1) {
+        if (MASS) lds.mass[kBuckets] = mass_to;
+        if (COUNT) lds.count[kBuckets] = count_to;
     }
     __syncthreads();
 }
 
-// The column at which the running sum (BY_COUNT: of ones) reaches `goal`, 1 to the sum of all: its key and the sum of w up to and with
-// it, in lds.found_key and found_mass.  The buckets are those of the whole row when it begins; `spoilt` is set where they no longer are at the end.
-template <bool BF16, bool BY_COUNT, int THREADS>
-__device__ __forceinline__ void find_place(const Row<BF16> &row, const Weights &weights, uint64_t goal, SampleLds<THREADS> &lds, bool &spoilt)
+// The bucket in which the running sum reaches `goal`, for every thread.
+template <int THREADS, typename Sum>
+__device__ __forceinline__ uint32_t bucket_of(SampleLds<THREADS> &lds, const Sum *before, uint64_t goal)
 {
-    uint64_t from = 0, to = ~0ull, mass_before = 0;        // keys of the columns that can be it; of those in front of them, the sum of w
-    uint64_t count_before = 0;
-    uint32_t only = kBuckets, narrowed = 0;                // the bucket they are in
-    for (;;) {
-        for (uint32_t b = threadIdx.x; b < kBuckets; b += THREADS) {
-            const uint64_t before = BY_COUNT ? count_before + lds.count[b] : mass_before + lds.mass[b];
-            const uint64_t upto = BY_COUNT ? count_before + lds.count[b + 1] : mass_before + lds.mass[b + 1];
-            if (before < goal && goal <= upto) lds.bucket = b;
+    const uint32_t thread = this_thread();
+    for (uint32_t b = thread; b < kBuckets; b += THREADS)
+        if (before[b] < goal && goal <= before[b + 1]) lds.bucket = b;
+    __syncthreads();
+    return lds.bucket;
+}
+
+// The place in the order: the goal that a running sum, of ones (`by_count`) or of w, reaches there, and what stands in front of the listed columns.
+struct Goal {
+    uint64_t sum, mass_before, count_before;
+    bool by_count;
+};
+
+// Puts n columns, no more than kSorted, in order: lds.ordered says which stands at a place, lds.running has the sums of w up to and with it.
+// lds.place is 0 before.  A thread compares one column with a part of the others.
+template <int THREADS>
+__device__ __forceinline__ void put_in_order(SampleLds<THREADS> &lds, const uint64_t *keys, const uint64_t *weights, uint32_t n)
+{
+    const uint32_t thread = this_thread();
+    const uint32_t across = min((n + kLanes - 1) / kLanes * kLanes, (uint32_t)THREADS), parts = THREADS / across, part = thread / across;
+    for (uint32_t i = part < parts ? thread - part * across : n; i < n; i += across) {
+        const uint64_t key = keys[i];
+        uint32_t place = 0;
+#pragma unroll 8
+        for (uint32_t j = part; j < n; j += parts) place += keys[j] > key;
+        if (parts == 1) lds.place[i] = place;
+        else if (place) atomicAdd(&lds.place[i], place);
+    }
+    __syncthreads();
+    for (uint32_t i = thread; i < n; i += THREADS) {
+        const uint32_t place = lds.place[i];
+        lds.ordered[place] = i;
+        lds.running[place] = weights[i];
+    }
+    __syncthreads();
+    if (thread < kLanes) {
+        constexpr uint32_t kEach = kSorted / kLanes;
+        const uint32_t each = (n + kLanes - 1) / kLanes;
+        uint64_t own = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < kEach; ++k)
+            if (k < each && thread * each + k < n) own += lds.running[thread * each + k];
+        uint64_t sum = running_sum(own) - own;
+#pragma unroll
+        for (uint32_t k = 0; k < kEach; ++k)
+            if (k < each && thread * each + k < n) {
+                sum += lds.running[thread * each + k];
+                lds.running[thread * each + k] = sum;
+            }
+    }
+    __syncthreads();
+}
+
+// The column at the goal among those in order: its key in lds.found_key, the sum of w up to and with it in lds.found_mass.
+template <int THREADS>
+__device__ __forceinline__ void pick(SampleLds<THREADS> &lds, const uint64_t *keys, uint32_t n, const Goal &goal)
+{
+    for (uint32_t i = this_thread(); i < n; i += THREADS) {
+        const uint64_t upto = lds.running[i], before = i == 0 ? 0 : lds.running[i - 1];
+        if (goal.by_count ? goal.count_before + i + 1 == goal.sum : goal.mass_before + before < goal.sum && goal.sum <= goal.mass_before + upto) {
+            lds.found_key = keys[lds.ordered[i]];
+            lds.found_mass = goal.mass_before + upto;
         }
-        if (threadIdx.x == 0) lds.listed = 0;
-        __syncthreads();
-        const uint32_t b = lds.bucket;
-        mass_before += lds.mass[b];
-        count_before += lds.count[b];
-        if (only == kBuckets) {
-            only = b;
-        } else {                                           // (bucket b of the keys: narrowed is their shift)
-            const uint64_t last = to - ((uint64_t)b << narrowed);
-            const uint64_t width = (1ull << narrowed) - 1;
-            from = last - from > width ? last - width : from;
-            to = last;
-        }
-        auto in_bucket = [&](float x, uint32_t column, auto &&use) {
-            const float place = weights.place(x);
-            if (!Weights::counts(place) || Weights::bucket(place) != only) return;
-            const uint64_t key = key_of(order_of(x), column);
-            if (key < from || key > to) return;
-            const uint64_t w = weights(x);
-            if (w != 0) use(key, w);
-        };
-        for_columns<BF16, THREADS>(row, [&](float x, uint32_t column) {
-            in_bucket(x, column, [&](uint64_t key, uint64_t w) {
-                const uint32_t i = atomicAdd(&lds.listed, 1u);
-                if (i < kListed) {
-                    lds.key[i] = key;
-                    lds.weight[i] = w;
-                    lds.before[i] = 0;
-                    lds.places[i] = 0;
-                }
-            });
+    }
+    __syncthreads();
+}
+
+template <int THREADS>
+__device__ __forceinline__ void list_in_bucket(SampleLds<THREADS> &lds, uint64_t key, uint64_t w)
+{
+    const uint32_t i = atomicAdd(&lds.listed, 1u);
+    if (i < kSorted) {
+        lds.sub_key[i] = key;
+        lds.sub_weight[i] = w;
+        lds.place[i] = 0;
+    }
+}
+
+// Of a bucket with too many columns: cuts it by their keys until the part that holds the goal has few, and lists these; returns how many.
+// The row's buckets are lost.  (Seldom: the row is read again.)
+template <bool BF16, int THREADS>
+__device__ __forceinline__ uint32_t narrow(const Row<BF16> &row, const Weights &weights, uint32_t only, Goal &goal, SampleLds<THREADS> &lds)
+{
+    Columns<BF16, THREADS, 0> columns(row);
+    const float lowest = weights.lowest((only + 0.5) / 32), highest = weights.highest((only - 0.5) / 32);
+    uint64_t from = 0, to = ~0ull;
+    auto candidates = [&](auto &&use) {
+        columns.between(lowest, highest, [&](float x, uint32_t column) {
+            uint32_t bucket;
+            const uint64_t w = weights(x, bucket), key = key_of(order_of(x), column);
+            if (bucket == only && w >= weights.least && key >= from && key <= to) use(key, w);
         });
         __syncthreads();
-        const uint32_t n = lds.listed;
-        if (n <= kListed) {
-            // a thread compares one column with a part of the others
-            const uint32_t across = min((n + kLanes - 1) / kLanes * kLanes, (uint32_t)THREADS), parts = THREADS / across, part = threadIdx.x / across;
-            for (uint32_t i = part < parts ? threadIdx.x % across : n; i < n; i += across) {
-                const uint64_t key = lds.key[i];
-                uint64_t before = 0;
-                uint32_t places = 0;
-                for (uint32_t j = part; j < n; j += parts)
-                    if (lds.key[j] > key) {
-                        before += lds.weight[j];
-                        ++places;
-                    }
-                if (places) {
-                    atomicAdd((unsigned long long *)&lds.before[i], (unsigned long long)before);
-                    atomicAdd(&lds.places[i], places);
-                }
-            }
-            __syncthreads();
-            for (uint32_t i = threadIdx.x; i < n; i += THREADS) {
-                const uint64_t before = BY_COUNT ? count_before + lds.places[i] : mass_before + lds.before[i];
-                if (before < goal && goal <= before + (BY_COUNT ? 1 : lds.weight[i])) {
-                    lds.found_key = lds.key[i];
-                    lds.found_mass = mass_before + lds.before[i] + lds.weight[i];
-                }
-            }
-            __syncthreads();
-            return;
-        }
-        // too many: their keys, cut into buckets
+    };
+    for (;;) {
         if (threadIdx.x == 0) {
             lds.lowest = ~0ull;
             lds.highest = 0;
         }
-        spoilt = true;
         clear_buckets<THREADS>(lds);
-        for_columns<BF16, THREADS>(row, [&](float x, uint32_t column) {
-            in_bucket(x, column, [&](uint64_t key, uint64_t) {
-                atomicMin((unsigned long long *)&lds.lowest, (unsigned long long)key);
-                atomicMax((unsigned long long *)&lds.highest, (unsigned long long)key);
-            });
+        candidates([&](uint64_t key, uint64_t) {
+            atomicMin((unsigned long long *)&lds.lowest, (unsigned long long)key);
+            atomicMax((unsigned long long *)&lds.highest, (unsigned long long)key);
         });
-        __syncthreads();
         from = lds.lowest;
         to = lds.highest;
-        narrowed = 0;
-        while ((to - from) >> narrowed >= kBuckets) ++narrowed;
-        for_columns<BF16, THREADS>(row, [&](float x, uint32_t column) {
-            in_bucket(x, column, [&](uint64_t key, uint64_t w) {
-                const uint32_t at = (uint32_t)((to - key) >> narrowed);
-                atomicAdd((unsigned long long *)&lds.mass[at], (unsigned long long)w);
-                atomicAdd(&lds.count[at], 1u);
-            });
+        uint32_t shift = 0;
+        while ((to - from) >> shift >= kBuckets) ++shift;
+        candidates([&](uint64_t key, uint64_t w) {
+            const uint32_t b = (uint32_t)((to - key) >> shift);
+            atomicAdd((unsigned long long *)&lds.mass[b], (unsigned long long)w);
+            atomicAdd(&lds.count[b], 1u);
         });
-        add_up_buckets<THREADS>(lds);
+        add_up_buckets<true, true, THREADS>(lds);
+        if (threadIdx.x == 0) lds.listed = 0;
+        const uint32_t b = goal.by_count ? bucket_of<THREADS>(lds, lds.count, goal.sum - goal.count_before)
+                                         : bucket_of<THREADS>(lds, lds.mass, goal.sum - goal.mass_before);
+        goal.mass_before += lds.mass[b];
+        goal.count_before += lds.count[b];
+        to -= (uint64_t)b << shift;
+        const uint64_t width = (1ull << shift) - 1;
+        from = to - from > width ? to - width : from;
+        candidates([&](uint64_t key, uint64_t w) { list_in_bucket<THREADS>(lds, key, w); });
+        const uint32_t n = lds.listed;
+        if (n <= kSorted) return n;
+        __syncthreads();                                   // (the buckets and the number, before they are cleared again)
     }
 }
 
-template <bool BF16, int THREADS>
+template <int THREADS>
+__device__ __forceinline__ uint64_t goal_of(const SampleLds<THREADS> &lds, int step, uint32_t top_k, uint64_t mass)
+{
+    return step == 0   ? (uint64_t)top_k
+           : step == 1 ? min(max((uint64_t)ceil(lds.nucleus * (double)mass), (uint64_t)1), mass)
+                       : min((uint64_t)(lds.below * (double)mass), mass - 1) + 1;
+}
+
+// One place after the other: that of top_k (0), of top_p (1), of the token (2), whose key is lds.found_key then, `mass` the sum of what is kept.
+// Of the `kept` columns in the list, or, where that is 0, of the row.  Without NARROW a bucket with too many columns ends it: false.
+template <bool NARROW, bool BF16, int THREADS, int DEPTH>
+__device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH> &columns, const Weights &weights, uint32_t top_k, bool nucleus, uint32_t kept,
+                                            SampleLds<THREADS> &lds, uint64_t &mass)
+{
+    const bool counted = top_k < (kept ? kept : columns.row.groups * Row<BF16>::kPer + columns.row.rest), picky = counted || weights.least > 1;      // (else a weight of 0 may be added)
+    bool filled = false;
+#pragma unroll 1
+    for (int step = 0; step < 3; ++step) {
+        if (step == 1 && !nucleus) continue;
+        if (!filled) {
+            clear_buckets<THREADS>(lds);
+            auto add = [&](float x) {
+                uint32_t bucket;
+                const uint64_t w = weights(x, bucket);
+                if (picky && w < weights.least) return;
+                atomicAdd((unsigned long long *)&lds.mass[bucket], (unsigned long long)w);
+                if (counted) atomicAdd(&lds.count[bucket], 1u);
+            };
+            if (kept)
+                for (uint32_t i = this_thread(); i < kept; i += THREADS) add(value_of(lds.key[i]));
+            else
+                columns.each([&](const float *x, auto n, uint32_t) {
+#pragma unroll
+                    for (int e = 0; e < n; ++e) add(x[e]);
+                });
+            add_up_buckets<true, true, THREADS>(lds);
+            filled = true;
+            if (step == 0) mass = scalar(lds.mass[kBuckets]);
+        }
+        if (step == 0 && (!counted || lds.count[kBuckets] <= top_k)) continue;
+        Goal goal = {goal_of(lds, step, top_k, mass), 0, 0, step == 0};
+        if (threadIdx.x == 0) lds.listed = 0;
+        const uint32_t only = goal.by_count ? bucket_of<THREADS>(lds, lds.count, goal.sum) : bucket_of<THREADS>(lds, lds.mass, goal.sum);
+        goal.mass_before = lds.mass[only];
+        goal.count_before = goal.by_count ? lds.count[only] : 0;
+        auto list = [&](float x, uint64_t key) {
+            uint32_t bucket;
+            const uint64_t w = weights(x, bucket);
+            if (bucket == only && w >= weights.least) list_in_bucket<THREADS>(lds, key, w);
+        };
+        if (kept)
+            for (uint32_t i = this_thread(); i < kept; i += THREADS) list(value_of(lds.key[i]), lds.key[i]);
+        else
+            columns.between(weights.lowest((only + 0.5) / 32), weights.highest((only - 0.5) / 32),
+                            [&](float x, uint32_t column) { list(x, key_of(order_of(x), column)); });
+        __syncthreads();
+        uint32_t n = lds.listed;
+        if (n > kSorted) {
+            if constexpr (!NARROW) return false;
+            __syncthreads();                               // (lds.listed)
+            n = narrow<BF16, THREADS>(columns.row, weights, only, goal, lds);
+            filled = false;
+        }
+        put_in_order<THREADS>(lds, lds.sub_key, lds.sub_weight, n);
+        pick<THREADS>(lds, lds.sub_key, n, goal);
+        if (step < 2) mass = scalar(lds.found_mass);
+        if (NARROW) __syncthreads();                       // (the buckets may be cleared next)
+    }
+    return true;
+}
+
+template <bool BF16, int THREADS, int DEPTH>
 __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleArgs a)
 {
     __shared__ SampleLds<THREADS> lds;
     constexpr int kWaves = THREADS / kLanes;
-    for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const Row<BF16> row(a, r);
-        const float temperature = a.temperature ? a.temperature[r] : a.one_temperature, top_p = a.top_p ? a.top_p[r] : a.one_top_p;
-        const float min_p = a.min_p ? a.min_p[r] : a.one_min_p, uniform = a.uniform[r];
-        const int32_t top_k = a.top_k ? a.top_k[r] : a.one_top_k;
-        auto put = [&](int64_t token, float logprob) {
-            if (threadIdx.x != 0) return;
-            if (a.wide) static_cast<int64_t *>(a.token)[r] = token;
-            else static_cast<int32_t *>(a.token)[r] = (int32_t)token;
-            if (a.logprob) a.logprob[r] = logprob;
-        };
-        float most = -INFINITY;
-        for_columns<BF16, THREADS>(row, [&](float x, uint32_t) { most = __builtin_elementwise_maximum(most, x); });
-        most = wave_reduce(most, [](float p, float q) { return __builtin_elementwise_maximum(p, q); });
-        if (threadIdx.x % kLanes == 0) lds.at[threadIdx.x / kLanes] = most;
-        if (threadIdx.x == 0) lds.column = 0xFFFFFFFFu;
-        __syncthreads();
-        most = wave_reduce<kWaves>(lds.at[threadIdx.x % kWaves], [](float p, float q) { return __builtin_elementwise_maximum(p, q); });
-        if (!(most < INFINITY) || !(temperature >= 0.0f) || top_p != top_p || min_p != min_p || uniform != uniform) {
-            put(-1, NAN);
-        } else if (most == -INFINITY) {
-            put(-1, -INFINITY);
-        } else if (temperature == 0.0f || top_k == 1) {
-            for_columns<BF16, THREADS>(row, [&](float x, uint32_t column) {
-                if (x == most) atomicMin(&lds.column, column);
-            });
-            __syncthreads();
-            put(lds.column, 0.0f);
-        } else {
-            Weights weights;
-            const double inverse = 1.0 / (double)temperature;
-            weights.max = most;
-            weights.shift = a.shift;
-            weights.per_order = inverse * 1.4426950408889634;
-            const float least = fminf(min_p, 1.0f);
-            weights.least = least > 0.0f ? __builtin_amdgcn_ldexp((double)least, (int)a.shift) : 0.0;
-            // w is half of 2^-shift behind the last bucket, or below min_p
-            const float orders = fminf(least > 0.0f ? 0.01f - 1.001f * __builtin_amdgcn_logf(fmaxf(least, FLT_MIN)) : FLT_MAX, (float)(a.shift + 1));
-            weights.per_bucket = fminf((float)weights.per_order * (kBuckets / orders), 1e30f);
-            const bool cut = top_k > 1 && (uint32_t)top_k < a.cols;
-            auto fill = [&] {
-                clear_buckets<THREADS>(lds);
-                for_columns<BF16, THREADS>(row, [&](float x, uint32_t) {
-                    const float place = weights.place(x);
-                    if (!Weights::counts(place)) return;
-                    const uint64_t w = weights(x);
-                    if (w == 0) return;
-                    atomicAdd((unsigned long long *)&lds.mass[Weights::bucket(place)], (unsigned long long)w);
-                    if (cut) atomicAdd(&lds.count[Weights::bucket(place)], 1u);
-                });
-                add_up_buckets<THREADS>(lds);
-            };
-            bool spoilt = false;
-            fill();
-            uint64_t mass = lds.mass[kBuckets];
-            if (cut && lds.count[kBuckets] > (uint32_t)top_k) {
-                find_place<BF16, true, THREADS>(row, weights, (uint64_t)top_k, lds, spoilt);
-                mass = lds.found_mass;
-            }
-            if (top_p < 1.0f) {
-                if (spoilt) fill();
-                spoilt = false;
-                const uint64_t goal = (uint64_t)ceil(fmax((double)top_p, 0.0) * (double)mass);
-                find_place<BF16, false, THREADS>(row, weights, min(max(goal, (uint64_t)1), mass), lds, spoilt);
-                mass = lds.found_mass;
-            }
-            if (spoilt) fill();
-            const uint64_t goal = (uint64_t)(fmax((double)uniform, 0.0) * (double)mass);
-            find_place<BF16, false, THREADS>(row, weights, min(goal, mass - 1) + 1, lds, spoilt);
-            const uint64_t key = lds.found_key;
-            put(column_of(key), (float)(((double)value_of(key) - (double)most) * inverse - log(__builtin_amdgcn_ldexp((double)mass, -(int)a.shift))));
-        }
-        __syncthreads();                                   // (what the next row writes to lds)
+    const uint64_t r = (uint64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (r >= a.rows) return;
+    const Row<BF16> row(a, r);
+    Columns<BF16, THREADS, DEPTH> columns(row);
+    const float own_temperature = a.temperature ? a.temperature[r] : a.one_temperature, top_p = a.top_p ? a.top_p[r] : a.one_top_p;
+    const float min_p = a.min_p ? a.min_p[r] : a.one_min_p, uniform = a.uniform[r];
+    const int32_t own_top_k = a.top_k ? a.top_k[r] : a.one_top_k;
+    auto put = [&](int64_t token, float logprob) {
+        if (threadIdx.x != 0) return;
+        if (a.wide) static_cast<int64_t *>(a.token)[r] = token;
+        else static_cast<int32_t *>(a.token)[r] = (int32_t)token;
+        if (a.logprob) a.logprob[r] = logprob;
+    };
+    if (threadIdx.x < 32)
+        lds.root[threadIdx.x] = __builtin_bit_cast(uint64_t, __builtin_amdgcn_ldexp(kRoots[threadIdx.x], (int)a.shift)) - ((uint64_t)threadIdx.x << 47);
+    float own_most = -INFINITY;
+    columns.each([&](const float *x, auto n, uint32_t) {
+#pragma unroll
+        for (int e = 0; e < n; ++e) own_most = __builtin_elementwise_maximum(own_most, x[e]);
+    });
+    float most = wave_reduce(own_most, [](float p, float q) { return __builtin_elementwise_maximum(p, q); });
+    if (threadIdx.x % kLanes == 0) lds.at[threadIdx.x / kLanes] = most;
+    if (threadIdx.x == 0) {
+        lds.listed = 0;
+        // (temperature 0: the first of the largest)
+        lds.inverse = own_temperature == 0.0f ? 1.0 : 1.0 / (double)own_temperature;
+        lds.below = uniform > 0.0f ? fmin((double)uniform, 2.0) : 0.0;
+        lds.nucleus = fmax((double)top_p, 0.0);
     }
+    clear_buckets<THREADS>(lds);
+    most = scalar(wave_reduce<kWaves>(lds.at[threadIdx.x % kWaves], [](float p, float q) { return __builtin_elementwise_maximum(p, q); }));
+    if (!(most < INFINITY) || !(own_temperature >= 0.0f) || top_p != top_p || min_p != min_p || uniform != uniform) return put(-1, NAN);
+    if (most == -INFINITY) return put(-1, -INFINITY);
+
+    const uint32_t top_k = own_temperature == 0.0f ? 1 : own_top_k > 0 ? (uint32_t)own_top_k : a.cols;
+    const float least = fminf(min_p, 1.0f);
+    Weights weights;
+    weights.max = scalar((double)most);
+    weights.per_order = scalar(lds.inverse * 1.4426950408889634);
+    weights.root = lds.root;
+    weights.least = scalar(least > 0.0f ? max((uint64_t)ceil(__builtin_amdgcn_ldexp((double)least, (int)a.shift)), (uint64_t)1) : 1);
+
+    // a logit that no kept column is below, where min_p or few columns give one
+    float bound = -INFINITY;
+    if (least > 0.0f) bound = weights.lowest(0.001 - (double)__builtin_amdgcn_logf(fmaxf(least, FLT_MIN)));
+    if (top_k == 1) {
+        bound = most;
+    } else if (top_k <= THREADS / 2 && top_k < a.cols) {   // the top_k-th of the threads' largest, by its bucket
+        if (own_most > -INFINITY) {
+            uint32_t bucket;
+            (void)weights(own_most, bucket);
+            atomicAdd(&lds.count[min(bucket, kBuckets - 1)], 1u);
+        }
+        add_up_buckets<false, true, THREADS>(lds);
+        if (lds.count[kBuckets] >= top_k) {
+            const uint32_t b = bucket_of<THREADS>(lds, lds.count, (uint64_t)top_k);
+            if (b < kBuckets - 1) bound = fmaxf(bound, weights.lowest((b + 0.5) / 32));
+        }
+    }
+    // The columns that are not below the bound, if they are few: kListed are kept instead of the row, kSorted are put in order at once.
+    uint32_t kept = 0;
+    if (bound > -INFINITY) {
+        columns.between(bound, INFINITY, [&](float x, uint32_t column) {
+            uint32_t bucket;
+            const uint64_t w = weights(x, bucket);
+            if (w < weights.least) return;
+            const uint32_t i = atomicAdd(&lds.listed, 1u);
+            if (i < kListed) {
+                lds.key[i] = key_of(order_of(x), column);
+                lds.weight[i] = w;
+                if (i < kSorted) lds.place[i] = 0;
+            }
+        });
+        __syncthreads();
+        kept = lds.listed;
+    }
+    const bool listed = kept != 0 && kept <= kListed;
+    uint64_t mass = 0;
+    if (listed && kept <= kSorted) {
+        put_in_order<THREADS>(lds, lds.key, lds.weight, kept);
+        mass = scalar(lds.running[min(top_k, kept) - 1]);
+        if (top_p < 1.0f) {
+            pick<THREADS>(lds, lds.key, kept, Goal{goal_of(lds, 1, top_k, mass), 0, 0, false});
+            mass = scalar(lds.found_mass);
+            __syncthreads();
+        }
+        pick<THREADS>(lds, lds.key, kept, Goal{goal_of(lds, 2, top_k, mass), 0, 0, false});
+    } else if (!find_places<false, BF16>(columns, weights, top_k, top_p < 1.0f, listed ? kept : 0, lds, mass)) {
+        // (seldom; the row does not stay in registers meanwhile)
+        Columns<BF16, THREADS, 0> again(row);
+        __syncthreads();
+        find_places<true, BF16>(again, weights, top_k, top_p < 1.0f, 0, lds, mass);
+    }
+    const uint64_t key = lds.found_key;
+    put(column_of(key), (float)(((double)value_of(key) - weights.max) * lds.inverse - log(__builtin_amdgcn_ldexp((double)mass, -(int)a.shift))));
 }
 
 // ---- host ------------------------------------------------------------------------------------
 template <bool BF16>
 static int sample_launch(const SampleArgs &a, hipStream_t stream)
 {
-    const dim3 grid((uint32_t)(a.rows < (1u << 20) ? a.rows : 1u << 20));
-    if (a.cols <= 8192) return launch(sample_kernel<BF16, 256>, grid, 256, stream, a);
-    return launch(sample_kernel<BF16, 1024>, grid, 1024, stream, a);
+    const uint32_t across = (uint32_t)(a.rows < (1u << 20) ? a.rows : 1u << 20);
+    const dim3 grid(across, (uint32_t)((a.rows + across - 1) / across));
+    const uint32_t quads = (a.cols + (BF16 ? 7 : 3)) / (BF16 ? 8 : 4);
+    if (quads <= 256 * 8) return launch(sample_kernel<BF16, 256, 8>, grid, 256, stream, a);
+    if (a.rows > 256 && quads <= 512 * 16) return launch(sample_kernel<BF16, 512, 16>, grid, 512, stream, a);
+    if (quads <= 1024 * 8) return launch(sample_kernel<BF16, 1024, 8>, grid, 1024, stream, a);
+    if (quads <= 1024 * 16) return launch(sample_kernel<BF16, 1024, 16>, grid, 1024, stream, a);
+    return launch(sample_kernel<BF16, 1024, 0>, grid, 1024, stream, a);
 }
 
 static bool optional_at(const void *p, uintptr_t size) { return !p || at_multiple(p, size); }
@@ -368,7 +614,7 @@ extern "C" int solo_sample(const void *logits, const float *uniform, const float
                          !optional_at(top_k, 4) || !optional_at(top_p, 4) || !optional_at(min_p, 4) || !at_multiple(token, s->token_bits / 8) ||
                          !optional_at(logprob, 4)))
         return SOLO_E_INVALID;
-    if (s->cols >= (1ull << 29) || s->rows >= (1ull << 40) || s->stride >= (1ull << 40)) return SOLO_E_UNSUPPORTED;
+    if (s->cols >= (1ull << 29) || s->rows >= (1ull << 35) || s->stride >= (1ull << 40)) return SOLO_E_UNSUPPORTED;
     if (s->rows == 0) return SOLO_OK;
     SampleArgs a = {};
     a.logits = logits; a.uniform = uniform; a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p;

@@ -172,7 +172,7 @@ def test_sampling_shapes_that_are_refused(changes):
     assert solo.solo_sample(*[16] * 8, sample(**changes), stream=0, check=False) == BAD
 
 
-@pytest.mark.parametrize("changes", [dict(cols=1 << 29, stride=1 << 29), dict(rows=1 << 40), dict(stride=1 << 40)])
+@pytest.mark.parametrize("changes", [dict(cols=1 << 29, stride=1 << 29), dict(rows=1 << 35), dict(stride=1 << 40)])
 def test_sampling_shapes_that_are_too_large(changes):
     assert solo.solo_sample(*[16] * 8, sample(**changes), stream=0, check=False) == TOO_LARGE
 
