@@ -48,15 +48,20 @@ struct SampleArgs {
     uint32_t shift;
 };
 
+typedef uint32_t Words __attribute__((ext_vector_type(2)));
+
 template <int THREADS>
 struct SampleLds {
     uint64_t mass[kBuckets + 1];       // sums of the buckets, then of all in front of a bucket
     uint32_t count[kBuckets + 1];
-    uint64_t key[kListed], weight[kListed];            // of the columns above a bound
-    uint64_t sub_key[kSorted], sub_weight[kSorted];        // of those in a bucket
+    float x[kListed];                  // of the columns above a bound
+    uint32_t column[kListed];
+    float sub_x[kSorted];              // of those in a bucket
+    uint32_t sub_column[kSorted];
+    uint64_t key[kSorted], weight[kSorted];
     uint64_t running[kSorted];         // in order: the sum of w up to and with each
     uint32_t place[kSorted], ordered[kSorted];
-    uint64_t root[32];                 // 2^(i / 32) times 2^shift, as bits, less what i adds to the exponent below
+    Words root[32];                    // 2^(i / 32) times 2^shift, less what i adds to the exponent below
     uint64_t wave_mass[THREADS / kLanes], lowest, highest;
     uint32_t wave_count[THREADS / kLanes];
     float at[THREADS / kLanes];
@@ -87,19 +92,25 @@ __device__ __forceinline__ T scalar(T x)
     }
 }
 
-// The weights of a row, as whole numbers of 2^-shift.
+// w as a whole number of 2^-shift, its logarithm, and the bytes from the first bucket's 64-bit sum to its own (that of w = 2^-64 for all below).
+struct Weight {
+    uint64_t w;
+    double order;
+    uint32_t bytes;
+    __device__ __forceinline__ uint32_t bucket() const { return bytes / 8; }
+};
+
+// The weights of a row.
 struct Weights {
     double max, per_order;             // (x - max) * per_order is log2 w
-    uint64_t least;                    // what counts: min_p, or 1
-    const uint64_t *root;
+    double least;                      // of what counts: log2 min_p, or that of half a whole number
+    const Words *root;
 
-    // w, and its bucket (that of w = 2^-64 for all below)
-    __device__ __forceinline__ uint64_t operator()(float x, uint32_t &bucket) const
+    __device__ __forceinline__ Weight operator()(float x) const
     {
         const double t = fmax(((double)x - max) * per_order, -64.0);
         const double z = t + 0x1.8p47, r = t - (z - 0x1.8p47);     // (to 32nds)
-        const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, z);
-        bucket = 0 - n;
+        const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, z), bytes = n * 8;
         // (2^r - 1) / r, interpolated at Chebyshev's nodes of [-1/64, 1/64]
         double p = 0.009618166713972776;
         p = fma(p, r, 0.055504434191939005);
@@ -107,10 +118,13 @@ struct Weights {
         p = fma(p, r, 0.693147180550011);
         p = fma(p, r, 1.0);
         // n / 32 whole orders are added to the exponent: n << 47, and what n % 32 adds there has been taken from the root
-        const uint64_t root_bits = root[n & 31];
-        const double scale = __builtin_bit_cast(double, (uint64_t)((uint32_t)(root_bits >> 32) + (n << 15)) << 32 | (uint32_t)root_bits);
-        return __builtin_bit_cast(uint64_t, fma(p, scale, 0x1p52)) - 0x4330000000000000ull;
+        Words scale = *reinterpret_cast<const Words *>(reinterpret_cast<const char *>(root) + (bytes & 0xF8));
+        scale[1] += n << 15;
+        Words whole = __builtin_bit_cast(Words, fma(p, __builtin_bit_cast(double, scale), 0x1p52));
+        whole[1] -= 0x43300000u;
+        return Weight{__builtin_bit_cast(uint64_t, whole), t, 0 - bytes};
     }
+    __device__ __forceinline__ bool counts(const Weight &w) const { return w.order >= least; }
     // A logit that none of `orders` binary orders below the maximum, or fewer, is below: with room for the rounding of all that is compared.
     __device__ __forceinline__ float lowest(double orders) const
     {
@@ -183,17 +197,9 @@ struct Columns {
 #pragma unroll
             for (int e = 0; e < n; ++e) any |= __builtin_amdgcn_fmed3f(x[e], from, to) == x[e];
             if (!any) return;
-            uint32_t hits = 0;
 #pragma unroll
-            for (int e = 0; e < n; ++e) hits |= (x[e] >= from && x[e] <= to ? 1u : 0u) << e;
-            while (hits != 0) {
-                const uint32_t e = __builtin_ctz(hits);
-                hits &= hits - 1;
-                float it = x[0];
-#pragma unroll
-                for (int o = 1; o < n; ++o) it = (int)e == o ? x[o] : it;
-                use(it, column + e);
-            }
+            for (int e = 0; e < n; ++e)
+                if (x[e] >= from && x[e] <= to) use(x[e], column + e);
         });
     }
 };
@@ -296,18 +302,55 @@ struct Goal {
     bool by_count;
 };
 
-// Puts n columns, no more than kSorted, in order: lds.ordered says which stands at a place, lds.running has the sums of w up to and with it.
-// lds.place is 0 before.  A thread compares one column with a part of the others.
+// One of a wavefront's columns: its key, and the sum of w before it and up to and with it.
+struct InOrder { uint64_t key, before, upto; uint32_t place; };
+
+__device__ __forceinline__ void lds_in_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
+
+// By one wavefront: n <= 64 columns, one a lane.
 template <int THREADS>
-__device__ __forceinline__ void put_in_order(SampleLds<THREADS> &lds, const uint64_t *keys, const uint64_t *weights, uint32_t n)
+__device__ __forceinline__ InOrder order_by_wave(SampleLds<THREADS> &lds, uint64_t key, uint64_t w, uint32_t n)
+{
+    const uint32_t lane = this_thread() % kLanes;
+    lds.key[lane] = key;
+    lds.weight[lane] = w;
+    lds_in_order();
+    InOrder it = {key, 0, 0, 0};
+#pragma unroll 4
+    for (uint32_t j = 0; j < n; ++j) {
+        const bool first = lds.key[j] > key;
+        it.before += first ? lds.weight[j] : 0;
+        it.place += first;
+    }
+    it.upto = it.before + w;
+    return it;
+}
+
+// The key of the one at the goal, and the sum of w up to and with it.
+__device__ __forceinline__ uint64_t pick_by_wave(const InOrder &it, uint32_t n, const Goal &goal, uint64_t &mass)
+{
+    const bool at = goal.by_count ? goal.count_before + it.place + 1 == goal.sum
+                                  : goal.mass_before + it.before < goal.sum && goal.sum <= goal.mass_before + it.upto;
+    const uint32_t lane = __builtin_ctzll(__ballot(at && threadIdx.x % kLanes < n) | 1ull << 63);
+    auto of = [&](uint64_t x) {
+        return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane);
+    };
+    mass = goal.mass_before + of(it.upto);
+    return of(it.key);
+}
+
+// Puts n columns, no more than kSorted, in order: lds.ordered says which stands at a place, lds.running has the sums of w up to and with it.
+// lds.key and lds.weight have them, and lds.place is 0.  A thread compares one column with a part of the others.
+template <int THREADS>
+__device__ __forceinline__ void put_in_order(SampleLds<THREADS> &lds, uint32_t n)
 {
     const uint32_t thread = this_thread();
     const uint32_t across = min((n + kLanes - 1) / kLanes * kLanes, (uint32_t)THREADS), parts = THREADS / across, part = thread / across;
     for (uint32_t i = part < parts ? thread - part * across : n; i < n; i += across) {
-        const uint64_t key = keys[i];
+        const uint64_t key = lds.key[i];
         uint32_t place = 0;
 #pragma unroll 8
-        for (uint32_t j = part; j < n; j += parts) place += keys[j] > key;
+        for (uint32_t j = part; j < n; j += parts) place += lds.key[j] > key;
         if (parts == 1) lds.place[i] = place;
         else if (place) atomicAdd(&lds.place[i], place);
     }
@@ -315,7 +358,7 @@ __device__ __forceinline__ void put_in_order(SampleLds<THREADS> &lds, const uint
     for (uint32_t i = thread; i < n; i += THREADS) {
         const uint32_t place = lds.place[i];
         lds.ordered[place] = i;
-        lds.running[place] = weights[i];
+        lds.running[place] = lds.weight[i];
     }
     __syncthreads();
     if (thread < kLanes) {
@@ -338,12 +381,12 @@ __device__ __forceinline__ void put_in_order(SampleLds<THREADS> &lds, const uint
 
 // The column at the goal among those in order: its key in lds.found_key, the sum of w up to and with it in lds.found_mass.
 template <int THREADS>
-__device__ __forceinline__ void pick(SampleLds<THREADS> &lds, const uint64_t *keys, uint32_t n, const Goal &goal)
+__device__ __forceinline__ void pick(SampleLds<THREADS> &lds, uint32_t n, const Goal &goal)
 {
     for (uint32_t i = this_thread(); i < n; i += THREADS) {
         const uint64_t upto = lds.running[i], before = i == 0 ? 0 : lds.running[i - 1];
         if (goal.by_count ? goal.count_before + i + 1 == goal.sum : goal.mass_before + before < goal.sum && goal.sum <= goal.mass_before + upto) {
-            lds.found_key = keys[lds.ordered[i]];
+            lds.found_key = lds.key[lds.ordered[i]];
             lds.found_mass = goal.mass_before + upto;
         }
     }
@@ -351,14 +394,63 @@ __device__ __forceinline__ void pick(SampleLds<THREADS> &lds, const uint64_t *ke
 }
 
 template <int THREADS>
-__device__ __forceinline__ void list_in_bucket(SampleLds<THREADS> &lds, uint64_t key, uint64_t w)
+__device__ __forceinline__ void list_in_bucket(SampleLds<THREADS> &lds, float x, uint32_t column)
 {
     const uint32_t i = atomicAdd(&lds.listed, 1u);
     if (i < kSorted) {
-        lds.sub_key[i] = key;
-        lds.sub_weight[i] = w;
+        lds.sub_x[i] = x;
+        lds.sub_column[i] = column;
+    }
+}
+
+// The key and w of the i-th listed column; for one that does not count or is of another bucket than `only`, 0 and a key behind those of all others.
+constexpr uint32_t kAnyBucket = 0xFFFFFFFFu;
+__device__ __forceinline__ uint64_t listed_key(const Weights &weights, float x, uint32_t column, uint32_t only, uint32_t i, uint64_t &w)
+{
+    const Weight it = weights(x);
+    const bool counts = weights.counts(it) && (only == kAnyBucket || it.bucket() == only);
+    w = counts ? it.w : 0;
+    return counts ? key_of(order_of(x), column) : i;
+}
+
+// picks(at) among n listed columns, no more than kSorted, of bucket `only`: at(goal) finds the column there, whose key is lds.found_key when it is the
+// last, and returns the sum of w up to and with it.  Returns what picks() does, in every thread.
+template <int THREADS, typename Picks>
+__device__ __forceinline__ uint64_t among(SampleLds<THREADS> &lds, const Weights &weights, const float *x, const uint32_t *column, uint32_t n, uint32_t only,
+                                          Picks &&picks)
+{
+    if (n <= kLanes) {                                     // a wavefront by itself: no barriers
+        if (threadIdx.x < kLanes) {
+            const uint32_t lane = this_thread();
+            uint64_t w = 0, key = lane < n ? listed_key(weights, x[lane], column[lane], only, lane, w) : 0;
+            const InOrder it = order_by_wave<THREADS>(lds, key, w, n);
+            const uint64_t mass = picks([&](const Goal &goal) {
+                uint64_t upto;
+                key = pick_by_wave(it, n, goal, upto);
+                return upto;
+            });
+            if (lane == 0) {
+                lds.found_key = key;
+                lds.found_mass = mass;
+            }
+        }
+        __syncthreads();
+        return scalar(lds.found_mass);
+    }
+    for (uint32_t i = this_thread(); i < n; i += THREADS) {
+        uint64_t w;
+        lds.key[i] = listed_key(weights, x[i], column[i], only, i, w);
+        lds.weight[i] = w;
         lds.place[i] = 0;
     }
+    __syncthreads();
+    put_in_order<THREADS>(lds, n);
+    return picks([&](const Goal &goal) {
+        pick<THREADS>(lds, n, goal);
+        const uint64_t upto = scalar(lds.found_mass);
+        __syncthreads();
+        return upto;
+    });
 }
 
 // Of a bucket with too many columns: cuts it by their keys until the part that holds the goal has few, and lists these; returns how many.
@@ -371,9 +463,9 @@ __device__ __forceinline__ uint32_t narrow(const Row<BF16> &row, const Weights &
     uint64_t from = 0, to = ~0ull;
     auto candidates = [&](auto &&use) {
         columns.between(lowest, highest, [&](float x, uint32_t column) {
-            uint32_t bucket;
-            const uint64_t w = weights(x, bucket), key = key_of(order_of(x), column);
-            if (bucket == only && w >= weights.least && key >= from && key <= to) use(key, w);
+            const Weight it = weights(x);
+            const uint64_t key = key_of(order_of(x), column);
+            if (it.bucket() == only && weights.counts(it) && key >= from && key <= to) use(key, it.w, x, column);
         });
         __syncthreads();
     };
@@ -383,7 +475,7 @@ __device__ __forceinline__ uint32_t narrow(const Row<BF16> &row, const Weights &
             lds.highest = 0;
         }
         clear_buckets<THREADS>(lds);
-        candidates([&](uint64_t key, uint64_t) {
+        candidates([&](uint64_t key, uint64_t, float, uint32_t) {
             atomicMin((unsigned long long *)&lds.lowest, (unsigned long long)key);
             atomicMax((unsigned long long *)&lds.highest, (unsigned long long)key);
         });
@@ -391,7 +483,7 @@ __device__ __forceinline__ uint32_t narrow(const Row<BF16> &row, const Weights &
         to = lds.highest;
         uint32_t shift = 0;
         while ((to - from) >> shift >= kBuckets) ++shift;
-        candidates([&](uint64_t key, uint64_t w) {
+        candidates([&](uint64_t key, uint64_t w, float, uint32_t) {
             const uint32_t b = (uint32_t)((to - key) >> shift);
             atomicAdd((unsigned long long *)&lds.mass[b], (unsigned long long)w);
             atomicAdd(&lds.count[b], 1u);
@@ -405,7 +497,7 @@ __device__ __forceinline__ uint32_t narrow(const Row<BF16> &row, const Weights &
         to -= (uint64_t)b << shift;
         const uint64_t width = (1ull << shift) - 1;
         from = to - from > width ? to - width : from;
-        candidates([&](uint64_t key, uint64_t w) { list_in_bucket<THREADS>(lds, key, w); });
+        candidates([&](uint64_t, uint64_t, float x, uint32_t column) { list_in_bucket<THREADS>(lds, x, column); });
         const uint32_t n = lds.listed;
         if (n <= kSorted) return n;
         __syncthreads();                                   // (the buckets and the number, before they are cleared again)
@@ -421,31 +513,41 @@ __device__ __forceinline__ uint64_t goal_of(const SampleLds<THREADS> &lds, int s
 }
 
 // One place after the other: that of top_k (0), of top_p (1), of the token (2), whose key is lds.found_key then, `mass` the sum of what is kept.
-// Of the `kept` columns in the list, or, where that is 0, of the row.  Without NARROW a bucket with too many columns ends it: false.
+// Of the `kept` columns in the list, or, where that is 0, of the row.  `clear`: the buckets are.  `all`: every column counts (or has a w of 0, which
+// may be added).  Without NARROW a bucket with too many columns ends it: false.
 template <bool NARROW, bool BF16, int THREADS, int DEPTH>
-__device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH> &columns, const Weights &weights, uint32_t top_k, bool nucleus, uint32_t kept,
-                                            SampleLds<THREADS> &lds, uint64_t &mass)
+__device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH> &columns, const Weights &weights, uint32_t top_k, bool nucleus, bool all, uint32_t kept,
+                                            bool clear, SampleLds<THREADS> &lds, uint64_t &mass)
 {
-    const bool counted = top_k < (kept ? kept : columns.row.groups * Row<BF16>::kPer + columns.row.rest), picky = counted || weights.least > 1;      // (else a weight of 0 may be added)
+    const bool counted = top_k < (kept ? kept : columns.row.groups * Row<BF16>::kPer + columns.row.rest);
     bool filled = false;
 #pragma unroll 1
     for (int step = 0; step < 3; ++step) {
         if (step == 1 && !nucleus) continue;
         if (!filled) {
-            clear_buckets<THREADS>(lds);
-            auto add = [&](float x) {
-                uint32_t bucket;
-                const uint64_t w = weights(x, bucket);
-                if (picky && w < weights.least) return;
-                atomicAdd((unsigned long long *)&lds.mass[bucket], (unsigned long long)w);
-                if (counted) atomicAdd(&lds.count[bucket], 1u);
+            if (!clear) clear_buckets<THREADS>(lds);
+            clear = false;
+            // (the weights of a few columns side by side: one is a chain of twenty instructions that wait for each other)
+            auto add = [&](const float *x, auto n) {
+                Weight it[n];
+#pragma unroll
+                for (int e = 0; e < n; ++e) it[e] = weights(x[e]);
+#pragma unroll
+                for (int e = 0; e < n; ++e) asm volatile("" : "+v"(it[e].w));      // (all of them here, not each in front of its use)
+#pragma unroll
+                for (int e = 0; e < n; ++e) {
+                    if (!all && !weights.counts(it[e])) continue;
+                    atomicAdd(reinterpret_cast<unsigned long long *>(reinterpret_cast<char *>(lds.mass) + it[e].bytes), (unsigned long long)it[e].w);
+                    if (counted) atomicAdd(&lds.count[it[e].bucket()], 1u);
+                }
             };
             if (kept)
-                for (uint32_t i = this_thread(); i < kept; i += THREADS) add(value_of(lds.key[i]));
+                for (uint32_t i = this_thread(); i < kept; i += THREADS) add(&lds.x[i], std::integral_constant<int, 1>());
             else
                 columns.each([&](const float *x, auto n, uint32_t) {
+                    constexpr int kSide = n < 4 ? n : 4;
 #pragma unroll
-                    for (int e = 0; e < n; ++e) add(x[e]);
+                    for (int e = 0; e < n; e += kSide) add(x + e, std::integral_constant<int, kSide>());
                 });
             add_up_buckets<true, true, THREADS>(lds);
             filled = true;
@@ -457,16 +559,13 @@ __device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH> &colum
         const uint32_t only = goal.by_count ? bucket_of<THREADS>(lds, lds.count, goal.sum) : bucket_of<THREADS>(lds, lds.mass, goal.sum);
         goal.mass_before = lds.mass[only];
         goal.count_before = goal.by_count ? lds.count[only] : 0;
-        auto list = [&](float x, uint64_t key) {
-            uint32_t bucket;
-            const uint64_t w = weights(x, bucket);
-            if (bucket == only && w >= weights.least) list_in_bucket<THREADS>(lds, key, w);
-        };
-        if (kept)
-            for (uint32_t i = this_thread(); i < kept; i += THREADS) list(value_of(lds.key[i]), lds.key[i]);
-        else
-            columns.between(weights.lowest((only + 0.5) / 32), weights.highest((only - 0.5) / 32),
-                            [&](float x, uint32_t column) { list(x, key_of(order_of(x), column)); });
+        const float lowest = weights.lowest((only + 0.5) / 32), highest = weights.highest((only - 0.5) / 32);
+        if (kept) {
+            for (uint32_t i = this_thread(); i < kept; i += THREADS)
+                if (lds.x[i] >= lowest && lds.x[i] <= highest) list_in_bucket<THREADS>(lds, lds.x[i], lds.column[i]);
+        } else {
+            columns.between(lowest, highest, [&](float x, uint32_t column) { list_in_bucket<THREADS>(lds, x, column); });
+        }
         __syncthreads();
         uint32_t n = lds.listed;
         if (n > kSorted) {
@@ -475,16 +574,17 @@ __device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH> &colum
             n = narrow<BF16, THREADS>(columns.row, weights, only, goal, lds);
             filled = false;
         }
-        put_in_order<THREADS>(lds, lds.sub_key, lds.sub_weight, n);
-        pick<THREADS>(lds, lds.sub_key, n, goal);
-        if (step < 2) mass = scalar(lds.found_mass);
+        mass = among<THREADS>(lds, weights, lds.sub_x, lds.sub_column, n, only, [&](auto &&at) {
+            const uint64_t upto = at(goal);
+            return step == 2 ? mass : upto;
+        });
         if (NARROW) __syncthreads();                       // (the buckets may be cleared next)
     }
     return true;
 }
 
 template <bool BF16, int THREADS, int DEPTH>
-__global__ __launch_bounds__(THREADS) void sample_kernel(const SampleArgs a)
+__global__ __launch_bounds__(THREADS, 4) void sample_kernel(const SampleArgs a)
 {
     __shared__ SampleLds<THREADS> lds;
     constexpr int kWaves = THREADS / kLanes;
@@ -502,7 +602,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleArgs a)
         if (a.logprob) a.logprob[r] = logprob;
     };
     if (threadIdx.x < 32)
-        lds.root[threadIdx.x] = __builtin_bit_cast(uint64_t, __builtin_amdgcn_ldexp(kRoots[threadIdx.x], (int)a.shift)) - ((uint64_t)threadIdx.x << 47);
+        lds.root[threadIdx.x] = __builtin_bit_cast(Words, __builtin_bit_cast(uint64_t, __builtin_amdgcn_ldexp(kRoots[threadIdx.x], (int)a.shift)) - ((uint64_t)threadIdx.x << 47));
     float own_most = -INFINITY;
     columns.each([&](const float *x, auto n, uint32_t) {
 #pragma unroll
@@ -523,63 +623,61 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(const SampleArgs a)
     if (most == -INFINITY) return put(-1, -INFINITY);
 
     const uint32_t top_k = own_temperature == 0.0f ? 1 : own_top_k > 0 ? (uint32_t)own_top_k : a.cols;
-    const float least = fminf(min_p, 1.0f);
     Weights weights;
     weights.max = scalar((double)most);
     weights.per_order = scalar(lds.inverse * 1.4426950408889634);
     weights.root = lds.root;
-    weights.least = scalar(least > 0.0f ? max((uint64_t)ceil(__builtin_amdgcn_ldexp((double)least, (int)a.shift)), (uint64_t)1) : 1);
-
+    weights.least = -1.0 - (double)a.shift;
     // a logit that no kept column is below, where min_p or few columns give one
     float bound = -INFINITY;
-    if (least > 0.0f) bound = weights.lowest(0.001 - (double)__builtin_amdgcn_logf(fmaxf(least, FLT_MIN)));
+    bool spoilt = false;               // the buckets
+    if (min_p > 0.0f) {
+        weights.least = scalar(fmax(log2((double)fminf(min_p, 1.0f)), weights.least));
+        bound = weights.lowest(-weights.least);
+    }
     if (top_k == 1) {
         bound = most;
     } else if (top_k <= THREADS / 2 && top_k < a.cols) {   // the top_k-th of the threads' largest, by its bucket
-        if (own_most > -INFINITY) {
-            uint32_t bucket;
-            (void)weights(own_most, bucket);
-            atomicAdd(&lds.count[min(bucket, kBuckets - 1)], 1u);
-        }
+        if (own_most > -INFINITY) atomicAdd(&lds.count[min(weights(own_most).bucket(), kBuckets - 1)], 1u);
         add_up_buckets<false, true, THREADS>(lds);
+        spoilt = true;
         if (lds.count[kBuckets] >= top_k) {
             const uint32_t b = bucket_of<THREADS>(lds, lds.count, (uint64_t)top_k);
             if (b < kBuckets - 1) bound = fmaxf(bound, weights.lowest((b + 0.5) / 32));
+        } else {
+            __syncthreads();                               // (the buckets, before they are cleared)
         }
     }
     // The columns that are not below the bound, if they are few: kListed are kept instead of the row, kSorted are put in order at once.
     uint32_t kept = 0;
     if (bound > -INFINITY) {
         columns.between(bound, INFINITY, [&](float x, uint32_t column) {
-            uint32_t bucket;
-            const uint64_t w = weights(x, bucket);
-            if (w < weights.least) return;
             const uint32_t i = atomicAdd(&lds.listed, 1u);
             if (i < kListed) {
-                lds.key[i] = key_of(order_of(x), column);
-                lds.weight[i] = w;
-                if (i < kSorted) lds.place[i] = 0;
+                lds.x[i] = x;
+                lds.column[i] = column;
             }
         });
         __syncthreads();
         kept = lds.listed;
     }
-    const bool listed = kept != 0 && kept <= kListed;
     uint64_t mass = 0;
-    if (listed && kept <= kSorted) {
-        put_in_order<THREADS>(lds, lds.key, lds.weight, kept);
-        mass = scalar(lds.running[min(top_k, kept) - 1]);
-        if (top_p < 1.0f) {
-            pick<THREADS>(lds, lds.key, kept, Goal{goal_of(lds, 1, top_k, mass), 0, 0, false});
-            mass = scalar(lds.found_mass);
+    if (kept != 0 && kept <= kSorted) {
+        mass = among<THREADS>(lds, weights, lds.x, lds.column, kept, kAnyBucket, [&](auto &&at) {
+            uint64_t sum = at(Goal{top_k < kept ? top_k : kept, 0, 0, true});
+            if (top_p < 1.0f) sum = at(Goal{goal_of(lds, 1, top_k, sum), 0, 0, false});
+            at(Goal{goal_of(lds, 2, top_k, sum), 0, 0, false});
+            return sum;
+        });
+    } else {
+        if (kept > kListed) kept = 0;
+        const bool all = min_p <= 0.0f && top_k >= a.cols;
+        if (!find_places<false, BF16>(columns, weights, top_k, top_p < 1.0f, all, kept, !spoilt, lds, mass)) {
+            // (seldom; the row does not stay in registers meanwhile)
+            Columns<BF16, THREADS, 0> again(row);
             __syncthreads();
+            find_places<true, BF16>(again, weights, top_k, top_p < 1.0f, all, 0, false, lds, mass);
         }
-        pick<THREADS>(lds, lds.key, kept, Goal{goal_of(lds, 2, top_k, mass), 0, 0, false});
-    } else if (!find_places<false, BF16>(columns, weights, top_k, top_p < 1.0f, listed ? kept : 0, lds, mass)) {
-        // (seldom; the row does not stay in registers meanwhile)
-        Columns<BF16, THREADS, 0> again(row);
-        __syncthreads();
-        find_places<true, BF16>(again, weights, top_k, top_p < 1.0f, 0, lds, mass);
     }
     const uint64_t key = lds.found_key;
     put(column_of(key), (float)(((double)value_of(key) - weights.max) * lds.inverse - log(__builtin_amdgcn_ldexp((double)mass, -(int)a.shift))));
