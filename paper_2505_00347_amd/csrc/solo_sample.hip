@@ -21,7 +21,7 @@ namespace solo {
 
 constexpr uint32_t kBuckets = 2048;    // of a 32nd of a binary order of w each
 constexpr uint32_t kListed = 1024;     // columns that are kept as a list
-constexpr uint32_t kSorted = 512;      // columns that are put in order by comparing each with all others
+constexpr uint32_t kSub = 512;         // parts that a list is cut into
 
 // 2^(i / 32)
 __constant__ const double kRoots[32] = {
@@ -56,11 +56,11 @@ struct SampleLds {
     uint32_t count[kBuckets + 1];
     float x[kListed];                  // of the columns above a bound
     uint32_t column[kListed];
-    float sub_x[kSorted];              // of those in a bucket
-    uint32_t sub_column[kSorted];
-    uint64_t key[kSorted], weight[kSorted];
-    uint64_t running[kSorted];         // in order: the sum of w up to and with each
-    uint32_t place[kSorted], ordered[kSorted];
+    float sub_x[kListed];              // of those in a bucket
+    uint32_t sub_column[kListed];
+    uint64_t sub_mass[kSub];
+    uint32_t sub_count[kSub];
+    uint64_t key[kLanes], weight[kLanes];
     Words root[32];                    // 2^(i / 32) times 2^shift, less what i adds to the exponent below
     uint64_t wave_mass[THREADS / kLanes], lowest, highest;
     uint32_t wave_count[THREADS / kLanes];
@@ -339,65 +339,11 @@ __device__ __forceinline__ uint64_t pick_by_wave(const InOrder &it, uint32_t n, 
     return of(it.key);
 }
 
-// Puts n columns, no more than kSorted, in order: lds.ordered says which stands at a place, lds.running has the sums of w up to and with it.
-// lds.key and lds.weight have them, and lds.place is 0.  A thread compares one column with a part of the others.
-template <int THREADS>
-__device__ __forceinline__ void put_in_order(SampleLds<THREADS> &lds, uint32_t n)
-{
-    const uint32_t thread = this_thread();
-    const uint32_t across = min((n + kLanes - 1) / kLanes * kLanes, (uint32_t)THREADS), parts = THREADS / across, part = thread / across;
-    for (uint32_t i = part < parts ? thread - part * across : n; i < n; i += across) {
-        const uint64_t key = lds.key[i];
-        uint32_t place = 0;
-#pragma unroll 8
-        for (uint32_t j = part; j < n; j += parts) place += lds.key[j] > key;
-        if (parts == 1) lds.place[i] = place;
-        else if (place) atomicAdd(&lds.place[i], place);
-    }
-    __syncthreads();
-    for (uint32_t i = thread; i < n; i += THREADS) {
-        const uint32_t place = lds.place[i];
-        lds.ordered[place] = i;
-        lds.running[place] = lds.weight[i];
-    }
-    __syncthreads();
-    if (thread < kLanes) {
-        constexpr uint32_t kEach = kSorted / kLanes;
-        const uint32_t each = (n + kLanes - 1) / kLanes;
-        uint64_t own = 0;
-#pragma unroll
-        for (uint32_t k = 0; k < kEach; ++k)
-            if (k < each && thread * each + k < n) own += lds.running[thread * each + k];
-        uint64_t sum = running_sum(own) - own;
-#pragma unroll
-        for (uint32_t k = 0; k < kEach; ++k)
-            if (k < each && thread * each + k < n) {
-                sum += lds.running[thread * each + k];
-                lds.running[thread * each + k] = sum;
-            }
-    }
-    __syncthreads();
-}
-
-// The column at the goal among those in order: its key in lds.found_key, the sum of w up to and with it in lds.found_mass.
-template <int THREADS>
-__device__ __forceinline__ void pick(SampleLds<THREADS> &lds, uint32_t n, const Goal &goal)
-{
-    for (uint32_t i = this_thread(); i < n; i += THREADS) {
-        const uint64_t upto = lds.running[i], before = i == 0 ? 0 : lds.running[i - 1];
-        if (goal.by_count ? goal.count_before + i + 1 == goal.sum : goal.mass_before + before < goal.sum && goal.sum <= goal.mass_before + upto) {
-            lds.found_key = lds.key[lds.ordered[i]];
-            lds.found_mass = goal.mass_before + upto;
-        }
-    }
-    __syncthreads();
-}
-
 template <int THREADS>
 __device__ __forceinline__ void list_in_bucket(SampleLds<THREADS> &lds, float x, uint32_t column)
 {
     const uint32_t i = atomicAdd(&lds.listed, 1u);
-    if (i < kSorted) {
+    if (i < kListed) {
         lds.sub_x[i] = x;
         lds.sub_column[i] = column;
     }
@@ -413,44 +359,120 @@ __device__ __forceinline__ uint64_t listed_key(const Weights &weights, float x, 
     return counts ? key_of(order_of(x), column) : i;
 }
 
-// picks(at) among n listed columns, no more than kSorted, of bucket `only`: at(goal) finds the column there, whose key is lds.found_key when it is the
-// last, and returns the sum of w up to and with it.  Returns what picks() does, in every thread.
+// picks(at) by one wavefront among n listed columns, no more than 64, of bucket `only`: at(goal) finds the column there, whose key is lds.found_key when
+// it is the last, and returns the sum of w up to and with it.  Returns what picks() does, in every thread.
 template <int THREADS, typename Picks>
 __device__ __forceinline__ uint64_t among(SampleLds<THREADS> &lds, const Weights &weights, const float *x, const uint32_t *column, uint32_t n, uint32_t only,
                                           Picks &&picks)
 {
-    if (n <= kLanes) {                                     // a wavefront by itself: no barriers
-        if (threadIdx.x < kLanes) {
-            const uint32_t lane = this_thread();
-            uint64_t w = 0, key = lane < n ? listed_key(weights, x[lane], column[lane], only, lane, w) : 0;
-            const InOrder it = order_by_wave<THREADS>(lds, key, w, n);
-            const uint64_t mass = picks([&](const Goal &goal) {
-                uint64_t upto;
-                key = pick_by_wave(it, n, goal, upto);
-                return upto;
-            });
-            if (lane == 0) {
-                lds.found_key = key;
-                lds.found_mass = mass;
+    if (threadIdx.x < kLanes) {
+        const uint32_t lane = this_thread();
+        uint64_t w = 0, key = lane < n ? listed_key(weights, x[lane], column[lane], only, lane, w) : 0;
+        const InOrder it = order_by_wave<THREADS>(lds, key, w, n);
+        const uint64_t mass = picks([&](const Goal &goal) {
+            uint64_t upto;
+            key = pick_by_wave(it, n, goal, upto);
+            return upto;
+        });
+        if (lane == 0) {
+            lds.found_key = key;
+            lds.found_mass = mass;
+        }
+    }
+    __syncthreads();
+    return scalar(lds.found_mass);
+}
+
+// Of the n columns listed as those of bucket `only`, no more than kListed, keeps the part that holds the goal, cut by keys until it has no more than 64;
+// returns how many.
+template <int THREADS>
+__device__ __forceinline__ uint32_t refine(SampleLds<THREADS> &lds, const Weights &weights, uint32_t n, uint32_t only, Goal &goal)
+{
+    constexpr uint32_t kEach = kListed / THREADS, kPart = kSub / kLanes;
+    const uint32_t thread = this_thread();
+    uint64_t key[kEach], w[kEach], low = 1ull << 32, high = ~0ull;         // (keys that count are not below 2^32)
+#pragma unroll
+    for (uint32_t k = 0; k < kEach; ++k) {
+        const uint32_t i = thread + k * THREADS;
+        key[k] = w[k] = 0;
+        if (i < n) key[k] = listed_key(weights, lds.sub_x[i], lds.sub_column[i], only, i, w[k]);
+    }
+    for (;;) {
+        uint64_t least = ~0ull, most = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < kEach; ++k)
+            if (key[k] >= low && key[k] <= high) {
+                least = min(least, key[k]);
+                most = max(most, key[k]);
+            }
+        least = wave_reduce(least, [](uint64_t p, uint64_t q) { return p < q ? p : q; });
+        most = wave_max(most);
+        if (thread == 0) {
+            lds.lowest = ~0ull;
+            lds.highest = 0;
+        }
+        for (uint32_t b = thread; b < kSub; b += THREADS) {
+            lds.sub_mass[b] = 0;
+            lds.sub_count[b] = 0;
+        }
+        __syncthreads();
+        if (thread == 0) lds.listed = 0;                   // (read in front of the barrier)
+        if (thread % kLanes == 0 && most != 0) {
+            atomicMin((unsigned long long *)&lds.lowest, (unsigned long long)least);
+            atomicMax((unsigned long long *)&lds.highest, (unsigned long long)most);
+        }
+        __syncthreads();
+        least = scalar(lds.lowest);
+        most = scalar(lds.highest);
+        const int bits = 64 - __builtin_clzll((most - least) | 1), shift = bits > 9 ? bits - 9 : 0;
+#pragma unroll
+        for (uint32_t k = 0; k < kEach; ++k)
+            if (key[k] >= low && key[k] <= high) {
+                const uint32_t b = (uint32_t)((most - key[k]) >> shift);
+                atomicAdd((unsigned long long *)&lds.sub_mass[b], (unsigned long long)w[k]);
+                atomicAdd(&lds.sub_count[b], 1u);
+            }
+        __syncthreads();
+        if (thread < kLanes) {                             // which part has the goal
+            uint64_t mass = 0, count = 0;
+#pragma unroll
+            for (uint32_t k = 0; k < kPart; ++k) {
+                mass += lds.sub_mass[thread * kPart + k];
+                count += lds.sub_count[thread * kPart + k];
+            }
+            uint64_t mass_to = goal.mass_before + running_sum(mass) - mass, count_to = goal.count_before + running_sum(count) - count;
+#pragma unroll
+            for (uint32_t k = 0; k < kPart; ++k) {
+                const uint64_t m = lds.sub_mass[thread * kPart + k], c = lds.sub_count[thread * kPart + k];
+                const uint64_t to = goal.by_count ? count_to : mass_to, upto = goal.by_count ? count_to + c : mass_to + m;
+                if (to < goal.sum && goal.sum <= upto) {
+                    lds.bucket = thread * kPart + k;
+                    lds.wave_mass[0] = mass_to;
+                    lds.found_mass = count_to;
+                }
+                mass_to += m;
+                count_to += c;
             }
         }
         __syncthreads();
-        return scalar(lds.found_mass);
-    }
-    for (uint32_t i = this_thread(); i < n; i += THREADS) {
-        uint64_t w;
-        lds.key[i] = listed_key(weights, x[i], column[i], only, i, w);
-        lds.weight[i] = w;
-        lds.place[i] = 0;
-    }
-    __syncthreads();
-    put_in_order<THREADS>(lds, n);
-    return picks([&](const Goal &goal) {
-        pick<THREADS>(lds, n, goal);
-        const uint64_t upto = scalar(lds.found_mass);
+        goal.mass_before = scalar(lds.wave_mass[0]);
+        goal.count_before = scalar(lds.found_mass);
+        high = most - ((uint64_t)scalar(lds.bucket) << shift);
+        const uint64_t width = (1ull << shift) - 1;
+        low = high - least > width ? high - width : least;
+#pragma unroll
+        for (uint32_t k = 0; k < kEach; ++k)
+            if (key[k] >= low && key[k] <= high) {
+                const uint32_t i = atomicAdd(&lds.listed, 1u);
+                if (i < kLanes) {
+                    lds.sub_x[i] = value_of(key[k]);
+                    lds.sub_column[i] = column_of(key[k]);
+                }
+            }
         __syncthreads();
-        return upto;
-    });
+        n = lds.listed;
+        if (n <= kLanes) return n;
+    }
 }
 
 // Of a bucket with too many columns: cuts it by their keys until the part that holds the goal has few, and lists these; returns how many.
@@ -499,7 +521,7 @@ __device__ __forceinline__ uint32_t narrow(const Row<BF16> &row, const Weights &
         from = to - from > width ? to - width : from;
         candidates([&](uint64_t, uint64_t, float x, uint32_t column) { list_in_bucket<THREADS>(lds, x, column); });
         const uint32_t n = lds.listed;
-        if (n <= kSorted) return n;
+        if (n <= kListed) return n;
         __syncthreads();                                   // (the buckets and the number, before they are cleared again)
     }
 }
@@ -568,12 +590,13 @@ __device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH> &colum
         }
         __syncthreads();
         uint32_t n = lds.listed;
-        if (n > kSorted) {
+        if (n > kListed) {
             if constexpr (!NARROW) return false;
             __syncthreads();                               // (lds.listed)
             n = narrow<BF16, THREADS>(columns.row, weights, only, goal, lds);
             filled = false;
         }
+        if (n > kLanes) n = refine<THREADS>(lds, weights, n, only, goal);
         mass = among<THREADS>(lds, weights, lds.sub_x, lds.sub_column, n, only, [&](auto &&at) {
             const uint64_t upto = at(goal);
             return step == 2 ? mass : upto;
@@ -584,7 +607,7 @@ __device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH> &colum
 }
 
 template <bool BF16, int THREADS, int DEPTH>
-__global__ __launch_bounds__(THREADS, 4) void sample_kernel(const SampleArgs a)
+__global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(const SampleArgs a)
 {
     __shared__ SampleLds<THREADS> lds;
     constexpr int kWaves = THREADS / kLanes;
@@ -648,7 +671,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(const SampleArgs a)
             __syncthreads();                               // (the buckets, before they are cleared)
         }
     }
-    // The columns that are not below the bound, if they are few: kListed are kept instead of the row, kSorted are put in order at once.
+    // The columns that are not below the bound, if they are few: kListed are kept instead of the row, 64 are put in order at once.
     uint32_t kept = 0;
     if (bound > -INFINITY) {
         columns.between(bound, INFINITY, [&](float x, uint32_t column) {
@@ -662,7 +685,7 @@ __global__ __launch_bounds__(THREADS, 4) void sample_kernel(const SampleArgs a)
         kept = lds.listed;
     }
     uint64_t mass = 0;
-    if (kept != 0 && kept <= kSorted) {
+    if (kept != 0 && kept <= kLanes) {
         mass = among<THREADS>(lds, weights, lds.x, lds.column, kept, kAnyBucket, [&](auto &&at) {
             uint64_t sum = at(Goal{top_k < kept ? top_k : kept, 0, 0, true});
             if (top_p < 1.0f) sum = at(Goal{goal_of(lds, 1, top_k, sum), 0, 0, false});
