@@ -193,13 +193,13 @@ struct Columns {
     __device__ __forceinline__ void between(float from, float to, Use &&use)
     {
         each([&](const float *x, auto n, uint32_t column) {
-            bool any = false;
+            bool hit[n], any = false;
 #pragma unroll
-            for (int e = 0; e < n; ++e) any |= __builtin_amdgcn_fmed3f(x[e], from, to) == x[e];
-            if (!any) return;
+            for (int e = 0; e < n; ++e) any |= hit[e] = __builtin_amdgcn_fmed3f(x[e], from, to) == x[e];
+            if (__ballot(any) == 0) return;
 #pragma unroll
             for (int e = 0; e < n; ++e)
-                if (x[e] >= from && x[e] <= to) use(x[e], column + e);
+                if (hit[e]) use(x[e], column + e);
         });
     }
 };
