@@ -6,10 +6,9 @@
 //   dx_j = s a (e_j T / S - sum over k with c_k = j of p_k)  among the c_k,   s a e_j (T / S - r / R)  elsewhere,   T = sum_k p_k + r
 //
 // (r is 0 where the p_k are brought to a sum of 1.)  R is summed by itself: as 1 minus the rest of the q it would have no digits left in a
-// student that is sure of an alternative.  So the columns c_k have to be told apart in the sums already.  One wavefront reads the
-// teacher's row while the logits are on their way and hangs every alternative into a list of the thread that has its column; a thread
-// knows by one bit for each of its groups whether to look at its list.  It takes the alternatives' logits out of the sums and leaves
-// them in LDS, where the loss finds them.
+// student that is sure of an alternative.  So the columns c_k are taken out in front of the sums.  One wavefront reads the teacher's row while
+// the logits are on their way and hangs every alternative into a list of the thread that has its column; a thread knows by one bit for each of its
+// groups whether it has any there.  The gradient is written as if there were none; then the threads write those of their alternatives over it.
 //
 // Otherwise as the log probabilities: a workgroup takes a row, one pass for the sums, the row stays in registers for the gradient.
 #include "solo_rows.h"
@@ -38,35 +37,26 @@ template <int THREADS>
 struct TeacherLds {
     uint32_t head[THREADS];            // a thread's first alternative; kNone: it has none
     uint32_t column[kMostTop];         // of an alternative; kNone: none, or an earlier one has the same
-    uint32_t next[kMostTop];
-    float p[kMostTop];                 // of all alternatives of the column
+    uint32_t next[kMostTop], same[kMostTop];       // same: the first alternative with its column
+    float p[kMostTop], log_p[kMostTop];
+    float all_p[kMostTop];             // of all alternatives of the column
     float logit[kMostTop];
     float total, left;                 // T and r
     uint32_t any;
     float at[THREADS / kLanes], s[THREADS / kLanes];
 };
 
-// What a lane of the first wavefront keeps of its alternatives (lane, lane + 64).
-struct Alternatives {
-    static constexpr int kPer = kMostTop / kLanes;
-    float p[kPer], log_p[kPer];
-    uint32_t same[kPer];               // the first alternative with the column
-};
-
 __device__ __forceinline__ void lds_in_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
 
 // By the first wavefront: the teacher's row, and the lists.  A barrier has to follow.
 template <bool BF16, int THREADS>
-__device__ __forceinline__ void read_teacher(const DistillArgs &a, const Row<BF16> &row, uint64_t r, TeacherLds<THREADS> &lds, Alternatives &own)
+__device__ __forceinline__ void read_teacher(const DistillArgs &a, const Row<BF16> &row, uint64_t r, TeacherLds<THREADS> &lds)
 {
-    constexpr int kPer = Alternatives::kPer;
+    constexpr int kPer = kMostTop / kLanes;                // a lane has alternatives `lane` and `lane` + 64
     const uint32_t lane = threadIdx.x;
     uint32_t column[kPer];
-    float value[kPer];
+    float value[kPer], p[kPer], log_p[kPer];
     bool live[kPer];
-    for (uint32_t t = lane; t < THREADS; t += kLanes) lds.head[t] = kNone;
-    float most = -INFINITY;
-    bool some = false;
 #pragma unroll
     for (int h = 0; h < kPer; ++h) {
         const uint32_t i = lane + h * kLanes;
@@ -78,6 +68,12 @@ __device__ __forceinline__ void read_teacher(const DistillArgs &a, const Row<BF1
         }
         live[h] = id >= 0 && id < (int64_t)a.cols && value[h] != -INFINITY;      // (a NaN counts, and shows)
         column[h] = live[h] ? (uint32_t)id : kNone;
+    }
+    for (uint32_t t = lane; t < THREADS; t += kLanes) lds.head[t] = kNone;
+    float most = -INFINITY;
+    bool some = false;
+#pragma unroll
+    for (int h = 0; h < kPer; ++h) {
         some = some || live[h];
         if (live[h]) most = fmaxf(most, value[h]);
     }
@@ -87,10 +83,10 @@ __device__ __forceinline__ void read_teacher(const DistillArgs &a, const Row<BF1
         double sum = 0.0;
 #pragma unroll
         for (int h = 0; h < kPer; ++h) {
-            const double p = live[h] ? exp((double)value[h]) : 0.0;
-            own.p[h] = (float)p;
-            own.log_p[h] = value[h];
-            sum += p;
+            const double exact = live[h] ? exp((double)value[h]) : 0.0;
+            p[h] = (float)exact;
+            log_p[h] = value[h];
+            sum += exact;
         }
         sum = wave_sum(sum);
         if (!(1.0 - sum < kNoRest)) left = (float)(1.0 - sum);
@@ -100,24 +96,24 @@ __device__ __forceinline__ void read_teacher(const DistillArgs &a, const Row<BF1
         float sum = 0.0f;
 #pragma unroll
         for (int h = 0; h < kPer; ++h) {
-            own.log_p[h] = (value[h] - most) * a.teacher_scale;
-            own.p[h] = live[h] ? __builtin_amdgcn_exp2f(own.log_p[h] * kLog2E) : 0.0f;
-            sum += own.p[h];
+            log_p[h] = (value[h] - most) * a.teacher_scale;
+            p[h] = live[h] ? __builtin_amdgcn_exp2f(log_p[h] * kLog2E) : 0.0f;
+            sum += p[h];
         }
         sum = wave_sum(sum);
         const float log_sum = __builtin_amdgcn_logf(sum) * kLn2;
 #pragma unroll
         for (int h = 0; h < kPer; ++h) {
-            own.p[h] /= any ? sum : 1.0f;
-            own.log_p[h] -= log_sum;
+            p[h] /= any ? sum : 1.0f;
+            log_p[h] -= log_sum;
         }
         total = any ? 1.0f : 0.0f;
     }
 #pragma unroll
     for (int h = 0; h < kPer; ++h) {
         lds.column[lane + h * kLanes] = column[h];
-        lds.p[lane + h * kLanes] = own.p[h];
-        own.same[h] = lane + h * kLanes;
+        lds.p[lane + h * kLanes] = p[h];
+        lds.log_p[lane + h * kLanes] = log_p[h];
     }
     if (lane == 0) {
         lds.total = total;
@@ -125,7 +121,13 @@ __device__ __forceinline__ void read_teacher(const DistillArgs &a, const Row<BF1
         lds.any = any;
     }
     lds_in_order();
-    float p[kPer] = {};
+    uint32_t same[kPer];
+#pragma unroll
+    for (int h = 0; h < kPer; ++h) {
+        p[h] = 0.0f;
+        same[h] = lane + h * kLanes;
+    }
+#pragma unroll 4
     for (uint32_t i = 0; i < a.top; ++i) {                 // (the alternatives of one column in their order)
         const uint32_t c = lds.column[i];
         const float pi = lds.p[i];
@@ -133,15 +135,16 @@ __device__ __forceinline__ void read_teacher(const DistillArgs &a, const Row<BF1
         for (int h = 0; h < kPer; ++h)
             if (c == column[h]) {
                 p[h] += pi;
-                own.same[h] = min(own.same[h], i);
+                same[h] = min(same[h], i);
             }
     }
     lds_in_order();
 #pragma unroll
     for (int h = 0; h < kPer; ++h) {
         const uint32_t i = lane + h * kLanes;
-        lds.p[i] = p[h];
-        if (own.same[h] != i || !live[h]) {
+        lds.all_p[i] = p[h];
+        lds.same[i] = same[h];
+        if (same[h] != i || !live[h]) {
             lds.column[i] = kNone;
         } else {
             const uint32_t g = column[h] / Row<BF16>::kPer;
@@ -164,13 +167,24 @@ __device__ __forceinline__ uint32_t own_alternatives(const Row<BF16> &row, const
     return mask;
 }
 
-// use(k, element) for the alternatives in group g.
-template <bool BF16, int THREADS, typename Use>
-__device__ __forceinline__ void for_alternatives(const TeacherLds<THREADS> &lds, uint32_t g, Use &&use)
+// The logits of group g without those of the alternatives, which go to lds; `most` is no less than any of them.
+template <bool BF16, int THREADS>
+__device__ __forceinline__ void take_out(Quad &quad, uint32_t g, TeacherLds<THREADS> &lds, float &most)
 {
     for (uint32_t k = lds.head[threadIdx.x]; k != kNone; k = lds.next[k]) {
-        const uint32_t c = lds.column[k];
-        if (c / Row<BF16>::kPer == g) use(k, c % Row<BF16>::kPer);
+        const uint32_t c = lds.column[k], e = c % Row<BF16>::kPer;
+        if (c / Row<BF16>::kPer != g) continue;
+        const uint32_t at = BF16 ? e / 2 : e;
+        uint32_t word = quad[0];
+#pragma unroll
+        for (uint32_t o = 1; o < 4; ++o) word = at == o ? quad[o] : word;
+        const float x = __uint_as_float(!BF16 ? word : e % 2 ? word & 0xFFFF0000u : word << 16);
+        const uint32_t without = !BF16 ? 0xFF800000u : e % 2 ? (word & 0xFFFFu) | 0xFF800000u : (word & 0xFFFF0000u) | 0xFF80u;
+#pragma unroll
+        for (uint32_t o = 0; o < 4; ++o)
+            if (at == o) quad[o] = without;
+        lds.logit[k] = x;
+        most = __builtin_elementwise_maximum(most, x);
     }
 }
 
@@ -187,21 +201,10 @@ __device__ __forceinline__ RowSums student_sums(const Row<BF16> &row, float k, T
         s *= __builtin_amdgcn_exp2f((at - to) * k);        // (0 where nothing has been added)
         at = to;
     };
-    auto add = [&](const Quad &quad, uint32_t g) {
+    auto add = [&](Quad &quad, uint32_t g) {
+        if (mask >> (g / THREADS % 32) & 1) take_out<BF16, THREADS>(quad, g, lds, most);
         float x[kPer];
         Lane16<BF16>::unpack(quad, x);
-        if (mask >> (g / THREADS % 32) & 1)
-            for_alternatives<BF16, THREADS>(lds, g, [&](uint32_t i, uint32_t e) {
-                float it = x[0];
-#pragma unroll
-                for (int o = 0; o < kPer; ++o)
-                    if (o == (int)e) {
-                        it = x[o];
-                        x[o] = -INFINITY;
-                    }
-                lds.logit[i] = it;
-                most = __builtin_elementwise_maximum(most, it);
-            });
         const float m = max_of<kPer>(x);
         if (m > at) rebase(m);
 #pragma unroll
@@ -257,14 +260,14 @@ __device__ __forceinline__ RowSums student_sums(const Row<BF16> &row, float k, T
 
 // By the first wavefront, behind the sums: the row's loss, for each of its lanes.
 template <int THREADS>
-__device__ __forceinline__ float row_loss(const RowSums &sums, const Alternatives &own, const TeacherLds<THREADS> &lds, uint32_t top, float scale)
+__device__ __forceinline__ float row_loss(const RowSums &sums, const TeacherLds<THREADS> &lds, uint32_t top, float scale)
 {
     const float log_s = __builtin_amdgcn_logf(sums.all) * kLn2;
     float loss = 0.0f;
-#pragma unroll
-    for (int h = 0; h < Alternatives::kPer; ++h)
-        if (threadIdx.x + h * kLanes < top && !(own.p[h] <= 0.0f))
-            loss = fmaf(own.p[h], own.log_p[h] - fmaf(lds.logit[own.same[h]] - sums.at, scale, -log_s), loss);
+    for (uint32_t i = threadIdx.x; i < top; i += kLanes) {
+        const float p = lds.p[i];
+        if (!(p <= 0.0f)) loss = fmaf(p, lds.log_p[i] - fmaf(lds.logit[lds.same[i]] - sums.at, scale, -log_s), loss);
+    }
     loss = wave_sum(loss);
     if (lds.left > 0.0f) loss = fmaf(lds.left, (__builtin_amdgcn_logf(lds.left) - __builtin_amdgcn_logf(sums.rest)) * kLn2 + log_s, loss);
     return sums.all == 0.0f ? INFINITY : loss;
@@ -280,96 +283,85 @@ __device__ __forceinline__ DistillSlope distill_slope(const RowSums &sums, float
     return DistillSlope{sums.at, all, rest, sums.all == 0.0f ? 0.0f : factor};
 }
 
-template <bool BF16, bool PAST, int THREADS>
-__device__ __forceinline__ void put_distilled(const Quad &q, void *out, uint32_t g, uint32_t mask, const TeacherLds<THREADS> &lds, const DistillSlope &s, float k)
+// Wavefronts per SIMD that the registers have to leave room for: two workgroups of 1024 threads, so that one loads while the other computes, where 64
+// registers are enough.
+constexpr int distill_waves(bool forward, bool grad, bool resident, int depth)
 {
-    constexpr int kPer = Row<BF16>::kPer;
-    float x[kPer];
-    Lane16<BF16>::unpack(q, x);
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) x[e] = __builtin_amdgcn_exp2f((x[e] - s.at) * k);
-    float among[kPer];
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) among[e] = x[e] * s.rest * s.factor;
-    if (mask >> (g / THREADS % 32) & 1)
-        for_alternatives<BF16, THREADS>(lds, g, [&](uint32_t i, uint32_t e) {
-            const float p = lds.p[i];
-#pragma unroll
-            for (int o = 0; o < kPer; ++o)
-                if (o == (int)e) among[o] = fmaf(x[o], s.all, -p) * s.factor;
-        });
-    Lane16<BF16>::template store_near<PAST>(out, g * kPer, among);
+    return forward && grad && resident && depth > 8 ? 4 : 8;
 }
 
 // FORWARD: the sums and the loss; GRAD: the gradient, from the sums or, without FORWARD, from those that are given.  RESIDENT: the row has no more
 // than THREADS * DEPTH groups, which stay in registers between the two.  PAST: 1 stores past the caches, 2 loads as well.
 template <bool BF16, bool FORWARD, bool GRAD, bool RESIDENT, int PAST, int THREADS, int DEPTH>
-__global__ __launch_bounds__(THREADS) void distill_kernel(const DistillArgs a)
+__global__ __launch_bounds__(THREADS, distill_waves(FORWARD, GRAD, RESIDENT, DEPTH)) void distill_kernel(const DistillArgs a)
 {
     __shared__ TeacherLds<THREADS> lds;
+    constexpr int kPer = Row<BF16>::kPer;
     const float k = a.scale * kLog2E;
-    for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const Row<BF16> row(a, r);
-        Quad raw[DEPTH];
-        if (FORWARD) first_groups<BF16, (PAST > 1), THREADS, DEPTH>(row, raw);
-        const float last = threadIdx.x < row.rest ? row.one(row.last_column(threadIdx.x)) : -INFINITY;
-        Alternatives own;
-        if (threadIdx.x < kLanes) read_teacher<BF16, THREADS>(a, row, r, lds, own);
-        __syncthreads();
-        char *out = static_cast<char *>(a.grad) + r * a.grad_stride * Elements<BF16>::kBytes;
-        if (!lds.any) {                                    // no teacher
-            if (GRAD) {
-                const float none[Row<BF16>::kPer] = {};
-                for (uint32_t g = threadIdx.x; g < row.groups; g += THREADS) Lane16<BF16>::template store_near<(PAST > 0)>(out, g * Row<BF16>::kPer, none);
-                if (threadIdx.x < row.rest) Elements<BF16>::store1(out, row.last_column(threadIdx.x), 0.0f);
-            }
-            if (FORWARD && threadIdx.x == 0) {
-                if (a.loss) a.loss[r] = 0.0f;
-                if (a.stats) { a.stats[3 * r] = 0.0f; a.stats[3 * r + 1] = 0.0f; a.stats[3 * r + 2] = 0.0f; }
-            }
-            __syncthreads();                               // (lds.any)
-            continue;
+    const uint64_t r = (uint64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (r >= a.rows) return;
+    const Row<BF16> row(a, r);
+    Quad raw[DEPTH];
+    if (FORWARD) first_groups<BF16, (PAST > 1), THREADS, DEPTH>(row, raw);
+    const float last = threadIdx.x < row.rest ? row.one(row.last_column(threadIdx.x)) : -INFINITY;
+    if (threadIdx.x < kLanes) read_teacher<BF16, THREADS>(a, row, r, lds);
+    __syncthreads();
+    char *out = static_cast<char *>(a.grad) + r * a.grad_stride * Elements<BF16>::kBytes;
+    if (!lds.any) {                                        // no teacher
+        if (GRAD) {
+            const float none[kPer] = {};
+            for (uint32_t g = threadIdx.x; g < row.groups; g += THREADS) Lane16<BF16>::template store_near<(PAST > 0)>(out, g * kPer, none);
+            if (threadIdx.x < row.rest) Elements<BF16>::store1(out, row.last_column(threadIdx.x), 0.0f);
         }
+        if (FORWARD && threadIdx.x == 0) {
+            if (a.loss) a.loss[r] = 0.0f;
+            if (a.stats) { a.stats[3 * r] = 0.0f; a.stats[3 * r + 1] = 0.0f; a.stats[3 * r + 2] = 0.0f; }
+        }
+        return;
+    }
+    RowSums sums;
+    if (FORWARD) {
         uint32_t at_last;
         const uint32_t mask = own_alternatives<BF16, THREADS>(row, lds, at_last);
-        RowSums sums;
-        if (FORWARD) {
-            sums = student_sums<BF16, RESIDENT, (PAST > 1), THREADS, DEPTH>(row, k, lds, raw, last, a.top, mask, at_last);
-            if (threadIdx.x < kLanes) {
-                const float loss = row_loss<THREADS>(sums, own, lds, a.top, a.scale);
-                if (threadIdx.x == 0) {
-                    if (a.loss) a.loss[r] = loss;
-                    if (a.stats) { a.stats[3 * r] = sums.at; a.stats[3 * r + 1] = sums.all; a.stats[3 * r + 2] = sums.rest; }
-                }
-            }
-        } else {
-            sums = RowSums{a.stats[3 * r], a.stats[3 * r + 1], a.stats[3 * r + 2]};
-        }
-        if (GRAD) {
-            const DistillSlope slope = distill_slope(sums, lds.total, lds.left, a.scale * a.grad_loss[r]);
-            for (uint32_t g0 = threadIdx.x; g0 < row.groups; g0 += THREADS * DEPTH) {
-                if (!(FORWARD && RESIDENT)) {
-#pragma unroll
-                    for (int j = 0; j < DEPTH; ++j)
-                        if (g0 + j * THREADS < row.groups) raw[j] = row.template group<(PAST > 1)>(g0 + j * THREADS);
-                }
-#pragma unroll
-                for (int j = 0; j < DEPTH; ++j)
-                    if (g0 + j * THREADS < row.groups) {
-                        // (what has been unpacked for the sums is not kept: it would take twice the registers)
-                        if (FORWARD && RESIDENT) forget(raw[j]);
-                        put_distilled<BF16, (PAST > 0), THREADS>(raw[j], out, g0 + j * THREADS, mask, lds, slope, k);
-                    }
-                if (FORWARD && RESIDENT) break;
-            }
-            if (threadIdx.x < row.rest) {
-                const float e = __builtin_amdgcn_exp2f((last - slope.at) * k);
-                const float dx = at_last != kNone ? fmaf(e, slope.all, -lds.p[at_last]) * slope.factor : e * slope.rest * slope.factor;
-                Elements<BF16>::store1(out, row.last_column(threadIdx.x), dx);
+        sums = student_sums<BF16, RESIDENT, (PAST > 1), THREADS, DEPTH>(row, k, lds, raw, last, a.top, mask, at_last);
+        if (threadIdx.x < kLanes) {
+            const float loss = row_loss<THREADS>(sums, lds, a.top, a.scale);
+            if (threadIdx.x == 0) {
+                if (a.loss) a.loss[r] = loss;
+                if (a.stats) { a.stats[3 * r] = sums.at; a.stats[3 * r + 1] = sums.all; a.stats[3 * r + 2] = sums.rest; }
             }
         }
-        __syncthreads();                                   // (the lists and sums in lds)
+    } else {
+        sums = RowSums{a.stats[3 * r], a.stats[3 * r + 1], a.stats[3 * r + 2]};
+        // (the gradient may be written over them)
+        for (uint32_t i = lds.head[threadIdx.x]; i != kNone; i = lds.next[i]) lds.logit[i] = row.one(lds.column[i]);
     }
+    if (!GRAD) return;
+    const DistillSlope slope = distill_slope(sums, lds.total, lds.left, a.scale * a.grad_loss[r]);
+    for (uint32_t g0 = threadIdx.x; g0 < row.groups; g0 += THREADS * DEPTH) {
+        if (!(FORWARD && RESIDENT)) {
+#pragma unroll
+            for (int j = 0; j < DEPTH; ++j)
+                if (g0 + j * THREADS < row.groups) raw[j] = row.template group<(PAST > 1)>(g0 + j * THREADS);
+        }
+#pragma unroll
+        for (int j = 0; j < DEPTH; ++j)
+            if (g0 + j * THREADS < row.groups) {
+                // (what has been unpacked for the sums is not kept: it would take twice the registers)
+                if (FORWARD && RESIDENT) forget(raw[j]);
+                float x[kPer];
+                Lane16<BF16>::unpack(raw[j], x);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) x[e] = __builtin_amdgcn_exp2f((x[e] - slope.at) * k) * slope.rest * slope.factor;
+                Lane16<BF16>::template store_near<(PAST > 0)>(out, (g0 + j * THREADS) * kPer, x);
+            }
+        if (FORWARD && RESIDENT) break;
+    }
+    if (threadIdx.x < row.rest)
+        Elements<BF16>::store1(out, row.last_column(threadIdx.x), __builtin_amdgcn_exp2f((last - slope.at) * k) * slope.rest * slope.factor);
+    // over what the same thread has just written
+    for (uint32_t i = lds.head[threadIdx.x]; i != kNone; i = lds.next[i])
+        Elements<BF16>::store1(out, lds.column[i], fmaf(__builtin_amdgcn_exp2f((lds.logit[i] - slope.at) * k), slope.all, -lds.all_p[i]) * slope.factor);
 }
 
 // ---- host ------------------------------------------------------------------------------------
@@ -383,7 +375,7 @@ static int distill_args(DistillArgs &a, const void *logits, const void *value, c
     if (s->rows != 0 && ((s->cols != 0 && !at_multiple(logits, element_bytes(s->dtype))) || !at_multiple(value, element_bytes(s->value_dtype)) ||
                          !at_multiple(token, s->token_bits / 8)))
         return SOLO_E_INVALID;
-    if (s->cols >= (1ull << 29) || s->rows >= (1ull << 40) || s->stride >= (1ull << 40) || s->grad_stride >= (1ull << 40) || s->value_stride >= (1ull << 40) ||
+    if (s->cols >= (1ull << 29) || s->rows >= (1ull << 35) || s->stride >= (1ull << 40) || s->grad_stride >= (1ull << 40) || s->value_stride >= (1ull << 40) ||
         s->token_stride >= (1ull << 40))
         return SOLO_E_UNSUPPORTED;
     a = DistillArgs{};
@@ -405,7 +397,8 @@ static int distill_launch(const DistillArgs &a, hipStream_t stream)
 {
     constexpr int kDepth = BF16 ? DEPTH : 2 * DEPTH;
     const uint64_t bytes = a.rows * a.cols * (BF16 ? 2 : 4);
-    const dim3 grid((uint32_t)(a.rows < (1u << 20) ? a.rows : 1u << 20));
+    const uint32_t across = (uint32_t)(a.rows < (1u << 20) ? a.rows : 1u << 20);
+    const dim3 grid(across, (uint32_t)((a.rows + across - 1) / across));
     if constexpr (GRAD) {
         constexpr int kBoth = FORWARD && !RESIDENT ? 1 : 2;        // (a row that is read twice stays in the caches)
         return launch(bytes > kDistillPastLoads    ? distill_kernel<BF16, FORWARD, GRAD, RESIDENT, kBoth, THREADS, kDepth>
