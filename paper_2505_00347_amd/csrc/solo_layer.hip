@@ -392,10 +392,10 @@ struct LayerSumArgs {
     uint32_t cols, parts, bf16, accumulate;
 };
 
-// The parts' sums, 64 columns a workgroup: 16 threads have four columns each, 16 of those every sixteenth part.
-__global__ __launch_bounds__(256) void layer_parts_kernel(const LayerSumArgs a)
+// The parts' sums, 64 columns a workgroup: 16 threads have four columns each, 64 of those every 64th part.
+__global__ __launch_bounds__(1024) void layer_parts_kernel(const LayerSumArgs a)
 {
-    __shared__ float lds[16][64];
+    __shared__ float lds[64][64];
     void *const out = blockIdx.y ? a.db : a.dw;
     if (!out) return;
     const float *const part = a.part + (blockIdx.y ? (uint64_t)a.parts * a.cols : 0);
@@ -403,7 +403,7 @@ __global__ __launch_bounds__(256) void layer_parts_kernel(const LayerSumArgs a)
     float sum[4] = {};
     if (n == 4) {
 #pragma unroll 8
-        for (uint32_t p = threadIdx.x / 16; p < a.parts; p += 16) {
+        for (uint32_t p = threadIdx.x / 16; p < a.parts; p += 64) {
             float x[4];
             Raw<false, 4> q;
             q.load(part, (uint64_t)p * a.cols + c);
@@ -412,17 +412,21 @@ __global__ __launch_bounds__(256) void layer_parts_kernel(const LayerSumArgs a)
             for (int e = 0; e < 4; ++e) sum[e] += x[e];
         }
     } else if (n != 0) {
-        for (uint32_t p = threadIdx.x / 16; p < a.parts; p += 16)
+        for (uint32_t p = threadIdx.x / 16; p < a.parts; p += 64)
             for (uint32_t e = 0; e < 4; ++e)
                 if (e < n) sum[e] += part[(uint64_t)p * a.cols + c + e];
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) lds[threadIdx.x / 16][threadIdx.x % 16 * 4 + e] = sum[e];
     __syncthreads();
+    const uint32_t own = threadIdx.x % 64, rows = threadIdx.x / 64 * 4;    // a wavefront adds four rows, then the first one the wavefronts' sums
+    lds[rows][own] = (lds[rows][own] + lds[rows + 1][own]) + (lds[rows + 2][own] + lds[rows + 3][own]);
+    __syncthreads();
     const uint32_t column = blockIdx.x * 64 + threadIdx.x;
     if (threadIdx.x >= 64 || column >= a.cols) return;
-    float total = lds[0][threadIdx.x];
-    for (int k = 1; k < 16; ++k) total += lds[k][threadIdx.x];
+    float total = lds[0][own];
+#pragma unroll
+    for (int k = 4; k < 64; k += 4) total += lds[k][own];
     if (a.bf16) Elements<true>::store1(out, column, a.accumulate ? Elements<true>::load1(out, column) + total : total);
     else Elements<false>::store1(out, column, a.accumulate ? Elements<false>::load1(out, column) + total : total);
 }
@@ -449,7 +453,10 @@ static LayerArgs layer_args(const solo_layernorm_shape *s)
 
 constexpr uint32_t kLongCols = 16384;      // rows of more do not stay in registers
 
-// Threads and rows of a workgroup that takes rows of `cols` elements.
+// Threads of a row and elements of a thread.  More threads with fewer elements leave registers for more rows under way, and take more barriers and idle lanes:
+// forward and gradient of 8192 x 2048 fp32 (bf16 out) with 256 x 8 17 and 34 us, 256 x 16 20 and 43, 512 x 8 21 and 41; of 16384 x 4096 bf16 with 256 x 16
+// 45 and 79, 512 x 8 49 and 80; of 8192 x 8192 bf16 with 1024 x 8 51 and 84, 512 x 16 45 and 90, 256 x 32 46 and 88; of 20000 x 1024 fp32 with
+// 64 x 16 21 and 38, 256 x 8 25 and 49; of 100000 x 256 bf16 with 32 x 8 18 and 32, 64 x 8 29 and 57.
 struct LayerForm { uint32_t lanes, elements; };
 static LayerForm layer_form(uint32_t cols)
 {
@@ -457,13 +464,15 @@ static LayerForm layer_form(uint32_t cols)
     if (cols <= 256) return {32, 8};
     if (cols <= 512) return {64, 8};
     if (cols <= 1024) return {64, 16};
+    if (cols <= 2048) return {256, 8};
     if (cols <= 4096) return {256, 16};
-    if (cols <= 8192) return {512, 16};
+    if (cols <= 8192) return {1024, 8};
     return {1024, 16};
 }
 static uint32_t layer_rows_of(uint32_t lanes) { return lanes < 256 ? 256 / lanes : 1; }
 
-// Workgroups of the gradient, each of which leaves sums of its own: never fewer for more rows.
+// Workgroups of the gradient, each of which leaves sums of its own: never fewer for more rows.  Two of 256 threads a compute unit: more have more rows under
+// way, but write more sums (16384 x 4096 bf16: 256 workgroups 108 us, 512 79, 768 83, 1024 93).
 static uint32_t layer_parts(uint64_t rows, uint32_t cols)
 {
     if (cols > kLongCols) {
@@ -471,7 +480,15 @@ static uint32_t layer_parts(uint64_t rows, uint32_t cols)
         return (uint32_t)(rows < most ? rows : most);
     }
     const LayerForm f = layer_form(cols);
-    const uint64_t groups = (rows + layer_rows_of(f.lanes) - 1) / layer_rows_of(f.lanes), most = f.lanes <= 256 ? 1024 : 131072 / f.lanes;
+    const uint64_t groups = (rows + layer_rows_of(f.lanes) - 1) / layer_rows_of(f.lanes), most = f.lanes <= 256 ? 512 : 256;
+    return (uint32_t)(groups < most ? groups : most);
+}
+
+// Workgroups of the forward pass: each reads the weights once.  (16384 x 4096 bf16: 1024 workgroups 45 us, 2048 51, one for each row 61; 100000 x 256
+// bf16: 1024 18.7, 2048 18.3)
+static uint32_t layer_groups(uint64_t rows, uint32_t lanes)
+{
+    const uint64_t groups = (rows + layer_rows_of(lanes) - 1) / layer_rows_of(lanes), most = lanes < 256 ? 2048 : lanes == 256 ? 1024 : 512;
     return (uint32_t)(groups < most ? groups : most);
 }
 
@@ -480,15 +497,15 @@ static int layer_forward_launch(const LayerArgs &a, hipStream_t stream)
 {
     if (a.cols > kLongCols) return launch(layer_forward_long_kernel<XB, YB>, dim3((uint32_t)(a.rows < (1u << 20) ? a.rows : 1u << 20)), 1024, stream, a);
     const LayerForm f = layer_form(a.cols);
-    const uint64_t groups = (a.rows + layer_rows_of(f.lanes) - 1) / layer_rows_of(f.lanes), most = f.lanes <= 256 ? 2048 : 524288 / f.lanes;
-    const dim3 grid((uint32_t)(groups < most ? groups : most));
+    const dim3 grid(layer_groups(a.rows, f.lanes));
     const uint32_t threads = f.lanes < 256 ? 256 : f.lanes;
     if (f.lanes == 8) return launch(layer_forward_kernel<XB, YB, 8, 8>, grid, threads, stream, a);
     if (f.lanes == 32) return launch(layer_forward_kernel<XB, YB, 32, 8>, grid, threads, stream, a);
     if (f.lanes == 64 && f.elements == 8) return launch(layer_forward_kernel<XB, YB, 64, 8>, grid, threads, stream, a);
     if (f.lanes == 64) return launch(layer_forward_kernel<XB, YB, 64, 16>, grid, threads, stream, a);
+    if (f.lanes == 256 && f.elements == 8) return launch(layer_forward_kernel<XB, YB, 256, 8>, grid, threads, stream, a);
     if (f.lanes == 256) return launch(layer_forward_kernel<XB, YB, 256, 16>, grid, threads, stream, a);
-    if (f.lanes == 512) return launch(layer_forward_kernel<XB, YB, 512, 16>, grid, threads, stream, a);
+    if (f.elements == 8) return launch(layer_forward_kernel<XB, YB, 1024, 8>, grid, threads, stream, a);
     return launch(layer_forward_kernel<XB, YB, 1024, 16>, grid, threads, stream, a);
 }
 
@@ -508,8 +525,9 @@ static int layer_backward_launch(const LayerArgs &a, uint32_t parts, hipStream_t
     if (f.lanes == 32) return launch(layer_backward_kernel<XB, YB, 32, 8>, grid, threads, stream, a);
     if (f.lanes == 64 && f.elements == 8) return launch(layer_backward_kernel<XB, YB, 64, 8>, grid, threads, stream, a);
     if (f.lanes == 64) return launch(layer_backward_kernel<XB, YB, 64, 16>, grid, threads, stream, a);
+    if (f.lanes == 256 && f.elements == 8) return launch(layer_backward_kernel<XB, YB, 256, 8>, grid, threads, stream, a);
     if (f.lanes == 256) return launch(layer_backward_kernel<XB, YB, 256, 16>, grid, threads, stream, a);
-    if (f.lanes == 512) return launch(layer_backward_kernel<XB, YB, 512, 16>, grid, threads, stream, a);
+    if (f.elements == 8) return launch(layer_backward_kernel<XB, YB, 1024, 8>, grid, threads, stream, a);
     return launch(layer_backward_kernel<XB, YB, 1024, 16>, grid, threads, stream, a);
 }
 
@@ -576,7 +594,7 @@ int solo_layernorm_grad(const void *grad_y, const void *x, const void *weight, c
     LayerSumArgs t = {};
     t.part = static_cast<const float *>(workspace); t.dw = grad_weight; t.db = grad_bias;
     t.cols = cols; t.parts = parts; t.bf16 = shape->weight_dtype == SOLO_BF16; t.accumulate = accumulate;
-    return launch(layer_parts_kernel, dim3((cols + 63) / 64, 2), 256, s, t);
+    return launch(layer_parts_kernel, dim3((cols + 63) / 64, 2), 1024, s, t);
 }
 
 }  // extern "C"
