@@ -116,7 +116,10 @@ def test_loss_and_gradient(dtype, rows, cols, extra, top, rest):
     check(strided(rows, cols, dtype, 1, extra, 3.0), value, token, rest, scale=(1.0, 0.5)[kind], teacher_scale=1.0 if rest else 1.7, extra=extra)
 
 
-@pytest.mark.parametrize("rows,cols", [(40_000, 300), (200, 40_000)])
+MANY = [(40_000, 300), (70_000, 1100), (200, 40_000), (2000, 70_000), (30_000, 5000), (9000, 15_000), (5000, 30_000), (2500, 65_000)]
+
+
+@pytest.mark.parametrize("rows,cols", MANY[:1] + MANY[2:3])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_many_rows(dtype, rows, cols):
     """Gradients that are written past the caches."""
@@ -124,6 +127,32 @@ def test_many_rows(dtype, rows, cols):
     token = torch.randint(0, cols, (rows, 9), generator=gen, device="cuda")
     value = torch.log_softmax(randn((rows, 9), torch.float32, 4), 1) - 0.1
     check(randn((rows, cols), dtype, 1, 2.0), value, token, True)
+
+
+@pytest.mark.parametrize("rows,cols", MANY)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_sets_that_are_larger_than_the_caches(dtype, rows, cols):
+    """Past the caches, whole sets against the same rows in parts that are not."""
+    gen = generator(3)
+    x = torch.randn((rows, cols), generator=gen, device="cuda", dtype=dtype)
+    token = torch.randint(0, cols, (rows, 5), generator=gen, device="cuda")
+    value, weight = torch.log_softmax(randn((rows, 5), torch.float32, 4), 1) - 0.1, torch.rand(rows, generator=gen, device="cuda")
+    plan, part = solo.SoloDistill(rows, cols, 5, rest=True), solo.SoloDistill(100, cols, 5, rest=True)
+    loss, one = plan.forward(x, value, token).clone(), torch.empty_like(x)
+    two = plan.grad(x, value, token, weight, torch.empty_like(x))
+    again, _ = plan.forward_grad(x, value, token, weight, one)
+    for a in (0, rows // 2, rows - 100):
+        rows_ = slice(a, a + 100)
+        some = x[rows_], value[rows_], token[rows_]
+        # (another number of threads may take a row: sums in another order)
+        within(loss[rows_], part.forward(*some), 1e-5 * loss[rows_].abs())
+        within(again[rows_], part.loss, 1e-5 * loss[rows_].abs())
+        small = part.forward_grad(*some, weight[rows_], torch.empty_like(x[rows_]))[1].double()
+        for whole in (one, two):
+            within(whole[rows_], small, (2 * ROUND[dtype] + 1e-5) * small.abs() + 1e-7)
+    for whole in (one, two):                               # the gradient of the shares sums to nothing: every element of every row has been written
+        total = whole.double().sum(1)
+        within(total, 0 * total, (ROUND[dtype] + 1e-5) * whole.double().abs().sum(1) + 1e-7)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
