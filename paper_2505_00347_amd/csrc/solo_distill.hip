@@ -48,17 +48,16 @@ struct TeacherLds {
 
 __device__ __forceinline__ void lds_in_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
 
-// By the first wavefront: the teacher's row, and the lists.  A barrier has to follow.
-template <bool BF16, int THREADS>
-__device__ __forceinline__ void read_teacher(const DistillArgs &a, const Row<BF16> &row, uint64_t r, TeacherLds<THREADS> &lds)
+// By the first wavefront: the teacher's row, and the lists.  A lane has alternatives `lane`, `lane` + 64, ... of PER * 64.  A barrier has to follow.
+template <int PER, bool BF16, int THREADS>
+__device__ __forceinline__ void read_alternatives(const DistillArgs &a, const Row<BF16> &row, uint64_t r, TeacherLds<THREADS> &lds)
 {
-    constexpr int kPer = kMostTop / kLanes;                // a lane has alternatives `lane` and `lane` + 64
     const uint32_t lane = threadIdx.x;
-    uint32_t column[kPer];
-    float value[kPer], p[kPer], log_p[kPer];
-    bool live[kPer];
+    uint32_t column[PER];
+    float value[PER], p[PER], log_p[PER];
+    bool live[PER];
 #pragma unroll
-    for (int h = 0; h < kPer; ++h) {
+    for (int h = 0; h < PER; ++h) {
         const uint32_t i = lane + h * kLanes;
         int64_t id = -1;
         value[h] = -INFINITY;
@@ -69,11 +68,10 @@ __device__ __forceinline__ void read_teacher(const DistillArgs &a, const Row<BF1
         live[h] = id >= 0 && id < (int64_t)a.cols && value[h] != -INFINITY;      // (a NaN counts, and shows)
         column[h] = live[h] ? (uint32_t)id : kNone;
     }
-    for (uint32_t t = lane; t < THREADS; t += kLanes) lds.head[t] = kNone;
     float most = -INFINITY;
     bool some = false;
 #pragma unroll
-    for (int h = 0; h < kPer; ++h) {
+    for (int h = 0; h < PER; ++h) {
         some = some || live[h];
         if (live[h]) most = fmaxf(most, value[h]);
     }
@@ -82,7 +80,7 @@ __device__ __forceinline__ void read_teacher(const DistillArgs &a, const Row<BF1
     if (a.rest) {
         double sum = 0.0;
 #pragma unroll
-        for (int h = 0; h < kPer; ++h) {
+        for (int h = 0; h < PER; ++h) {
             const double exact = live[h] ? exp((double)value[h]) : 0.0;
             p[h] = (float)exact;
             log_p[h] = value[h];
@@ -95,7 +93,7 @@ __device__ __forceinline__ void read_teacher(const DistillArgs &a, const Row<BF1
         most = wave_max(most);
         float sum = 0.0f;
 #pragma unroll
-        for (int h = 0; h < kPer; ++h) {
+        for (int h = 0; h < PER; ++h) {
             log_p[h] = (value[h] - most) * a.teacher_scale;
             p[h] = live[h] ? __builtin_amdgcn_exp2f(log_p[h] * kLog2E) : 0.0f;
             sum += p[h];
@@ -103,17 +101,27 @@ __device__ __forceinline__ void read_teacher(const DistillArgs &a, const Row<BF1
         sum = wave_sum(sum);
         const float log_sum = __builtin_amdgcn_logf(sum) * kLn2;
 #pragma unroll
-        for (int h = 0; h < kPer; ++h) {
+        for (int h = 0; h < PER; ++h) {
             p[h] /= any ? sum : 1.0f;
             log_p[h] -= log_sum;
         }
         total = any ? 1.0f : 0.0f;
     }
+    // every alternative into the list of the thread that has its column
+    auto hang = [&](int h) {
+        const uint32_t i = lane + h * kLanes, g = column[h] / Row<BF16>::kPer;
+        lds.next[i] = atomicExch(&lds.head[g < row.groups ? g % THREADS : column[h] - row.groups * Row<BF16>::kPer], i);
+    };
+    for (uint32_t t = lane; t < THREADS; t += kLanes) lds.head[t] = kNone;
+    lds_in_order();
 #pragma unroll
-    for (int h = 0; h < kPer; ++h) {
-        lds.column[lane + h * kLanes] = column[h];
-        lds.p[lane + h * kLanes] = p[h];
-        lds.log_p[lane + h * kLanes] = log_p[h];
+    for (int h = 0; h < PER; ++h) {
+        const uint32_t i = lane + h * kLanes;
+        lds.column[i] = column[h];
+        lds.p[i] = lds.all_p[i] = p[h];
+        lds.log_p[i] = log_p[h];
+        lds.same[i] = i;
+        if (live[h]) hang(h);
     }
     if (lane == 0) {
         lds.total = total;
@@ -121,36 +129,47 @@ __device__ __forceinline__ void read_teacher(const DistillArgs &a, const Row<BF1
         lds.any = any;
     }
     lds_in_order();
-    uint32_t same[kPer];
+    bool twice = false;                                    // (of two with one column the one that came later sees the other)
 #pragma unroll
-    for (int h = 0; h < kPer; ++h) {
+    for (int h = 0; h < PER; ++h)
+        if (live[h])
+            for (uint32_t k = lds.next[lane + h * kLanes]; k != kNone; k = lds.next[k]) twice = twice || lds.column[k] == column[h];
+    if (__ballot(twice) == 0) return;
+    // Seldom: the first of each column stays in the lists, with the probabilities of all of them, added in their order.
+    uint32_t same[PER];
+#pragma unroll
+    for (int h = 0; h < PER; ++h) {
         p[h] = 0.0f;
         same[h] = lane + h * kLanes;
     }
-#pragma unroll 4
-    for (uint32_t i = 0; i < a.top; ++i) {                 // (the alternatives of one column in their order)
+    for (uint32_t i = 0; i < a.top; ++i) {
         const uint32_t c = lds.column[i];
         const float pi = lds.p[i];
 #pragma unroll
-        for (int h = 0; h < kPer; ++h)
+        for (int h = 0; h < PER; ++h)
             if (c == column[h]) {
                 p[h] += pi;
                 same[h] = min(same[h], i);
             }
     }
     lds_in_order();
+    for (uint32_t t = lane; t < THREADS; t += kLanes) lds.head[t] = kNone;
+    lds_in_order();
 #pragma unroll
-    for (int h = 0; h < kPer; ++h) {
+    for (int h = 0; h < PER; ++h) {
         const uint32_t i = lane + h * kLanes;
         lds.all_p[i] = p[h];
         lds.same[i] = same[h];
-        if (same[h] != i || !live[h]) {
-            lds.column[i] = kNone;
-        } else {
-            const uint32_t g = column[h] / Row<BF16>::kPer;
-            lds.next[i] = atomicExch(&lds.head[g < row.groups ? g % THREADS : column[h] - row.groups * Row<BF16>::kPer], i);
-        }
+        if (same[h] != i) lds.column[i] = kNone;
+        else if (live[h]) hang(h);
     }
+}
+
+template <bool BF16, int THREADS>
+__device__ __forceinline__ void read_teacher(const DistillArgs &a, const Row<BF16> &row, uint64_t r, TeacherLds<THREADS> &lds)
+{
+    if (a.top <= kLanes) read_alternatives<1, BF16, THREADS>(a, row, r, lds);
+    else read_alternatives<kMostTop / kLanes, BF16, THREADS>(a, row, r, lds);
 }
 
 // The bits of a thread's groups that hold an alternative (group g has bit g / THREADS, of 32), and the one of its last column.
