@@ -19,9 +19,14 @@
 
 namespace solo {
 
-constexpr uint32_t kBuckets = 2048;    // of a 32nd of a binary order of w each
-constexpr uint32_t kListed = 1024;     // columns that are kept as a list
-constexpr uint32_t kSub = 512;         // parts that a list is cut into
+// Buckets of the distance from the maximum, 64 binary orders of w in all; columns that are kept as a list; parts that a list is cut into.  A row of one
+// wavefront has an eighth of each: what it clears and adds up is most of its work, and what it has in LDS says how many rows a compute unit has
+// under way (100000 rows of 300 fp32: 145 us, with the others' sizes and 256 threads 1107).
+template <int THREADS>
+struct Sizes {
+    static constexpr bool kShort = THREADS == kLanes;
+    static constexpr uint32_t kBuckets = kShort ? 256 : 2048, kListed = kShort ? 128 : 1024, kSub = kShort ? 64 : 512;
+};
 
 // 2^(i / 32)
 __constant__ const double kRoots[32] = {
@@ -52,6 +57,7 @@ typedef uint32_t Words __attribute__((ext_vector_type(2)));
 
 template <int THREADS>
 struct SampleLds {
+    static constexpr uint32_t kBuckets = Sizes<THREADS>::kBuckets, kListed = Sizes<THREADS>::kListed, kSub = Sizes<THREADS>::kSub;
     uint64_t mass[kBuckets + 1];       // sums of the buckets, then of all in front of a bucket
     uint32_t count[kBuckets + 1];
     float x[kListed];                  // of the columns above a bound
@@ -92,12 +98,13 @@ __device__ __forceinline__ T scalar(T x)
     }
 }
 
-// w as a whole number of 2^-shift, its logarithm, and the bytes from the first bucket's 64-bit sum to its own (that of w = 2^-64 for all below).
+// w as a whole number of 2^-shift, its logarithm, and how far that lies below 0, in eighths of a 32nd (64 orders for all below).
 struct Weight {
     uint64_t w;
     double order;
-    uint32_t bytes;
-    __device__ __forceinline__ uint32_t bucket() const { return bytes / 8; }
+    uint32_t below;
+    template <int THREADS>
+    __device__ __forceinline__ uint32_t bucket() const { return below / (16384 / Sizes<THREADS>::kBuckets); }
 };
 
 // The weights of a row.
@@ -138,10 +145,16 @@ struct Weights {
     }
 };
 
-// The columns of a row, each one thread's.  With DEPTH, rows of no more than THREADS * DEPTH groups stay in registers; else every pass loads them.
-template <bool BF16, int THREADS, int DEPTH>
+// The binary orders below the maximum between which a bucket lies (a logarithm is rounded to a 32nd before it is cut into buckets).
+template <int THREADS>
+__device__ __forceinline__ double bucket_begin(uint32_t b) { return b * (64.0 / Sizes<THREADS>::kBuckets) - 1.0 / 64; }
+template <int THREADS>
+__device__ __forceinline__ double bucket_end(uint32_t b) { return (b + 1) * (64.0 / Sizes<THREADS>::kBuckets) - 1.0 / 64; }
+
+// The columns of a row, each one thread's.  The first DEPTH groups of a thread stay in registers, the others (LONG: if there may be any) are loaded in every pass.
+template <bool BF16, int THREADS, int DEPTH, bool LONG>
 struct Columns {
-    static constexpr int kPer = Row<BF16>::kPer, kAhead = 4;
+    static constexpr int kPer = Row<BF16>::kPer, kAhead = DEPTH ? 2 : 4;
     const Row<BF16> &row;
     Quad q[DEPTH ? DEPTH : 1];
     float last;
@@ -159,19 +172,18 @@ struct Columns {
     __device__ __forceinline__ void each(Use &&use)
     {
         float x[kPer];
-        if (DEPTH) {
-            // (the compiler does not know the logits from here on either: it would unpack and convert them once, in front of all passes)
-            const uint32_t thread = this_thread();
+        // (the compiler does not know the logits from here on either: it would unpack and convert them once, in front of all passes)
+        const uint32_t thread = this_thread();
 #pragma unroll
-            for (int j = 0; j < DEPTH; ++j)
-                if (j * THREADS + thread < row.groups) {
-                    Quad a = q[j];
-                    forget(a);
-                    Lane16<BF16>::unpack(a, x);
-                    use(x, std::integral_constant<int, kPer>(), (j * THREADS + thread) * kPer);
-                }
-        } else {
-            for (uint32_t g0 = this_thread(); g0 < row.groups; g0 += THREADS * kAhead) {
+        for (int j = 0; j < DEPTH; ++j)
+            if (j * THREADS + thread < row.groups) {
+                Quad a = q[j];
+                forget(a);
+                Lane16<BF16>::unpack(a, x);
+                use(x, std::integral_constant<int, kPer>(), (j * THREADS + thread) * kPer);
+            }
+        if (LONG) {
+            for (uint32_t g0 = DEPTH * THREADS + this_thread(); g0 < row.groups; g0 += THREADS * kAhead) {
                 Quad a[kAhead];
 #pragma unroll
                 for (int j = 0; j < kAhead; ++j) a[j] = row.group(min(g0 + j * THREADS, row.groups - 1));
@@ -232,7 +244,7 @@ template <int THREADS>
 __device__ __forceinline__ void clear_buckets(SampleLds<THREADS> &lds)
 {
     const uint32_t thread = this_thread();
-    for (uint32_t b = thread; b <= kBuckets; b += THREADS) {
+    for (uint32_t b = thread; b <= SampleLds<THREADS>::kBuckets; b += THREADS) {
         lds.mass[b] = 0;
         lds.count[b] = 0;
     }
@@ -244,7 +256,7 @@ template <bool MASS, bool COUNT, int THREADS>
 __device__ __forceinline__ void add_up_buckets(SampleLds<THREADS> &lds)
 {
     const uint32_t thread = this_thread();
-    constexpr uint32_t kEach = kBuckets / THREADS;
+    constexpr uint32_t kEach = SampleLds<THREADS>::kBuckets / THREADS;
     constexpr int kWaves = THREADS / kLanes;
     const uint32_t lane = thread % kLanes, wave = thread / kLanes, first = thread * kEach;
     __syncthreads();
@@ -279,8 +291,8 @@ __device__ __forceinline__ void add_up_buckets(SampleLds<THREADS> &lds)
         }
     }
     if (thread == THREADS - 1) {
-        if (MASS) lds.mass[kBuckets] = mass_to;
-        if (COUNT) lds.count[kBuckets] = count_to;
+        if (MASS) lds.mass[SampleLds<THREADS>::kBuckets] = mass_to;
+        if (COUNT) lds.count[SampleLds<THREADS>::kBuckets] = count_to;
     }
     __syncthreads();
 }
@@ -290,7 +302,7 @@ template <int THREADS, typename Sum>
 __device__ __forceinline__ uint32_t bucket_of(SampleLds<THREADS> &lds, const Sum *before, uint64_t goal)
 {
     const uint32_t thread = this_thread();
-    for (uint32_t b = thread; b < kBuckets; b += THREADS)
+    for (uint32_t b = thread; b < SampleLds<THREADS>::kBuckets; b += THREADS)
         if (before[b] < goal && goal <= before[b + 1]) lds.bucket = b;
     __syncthreads();
     return lds.bucket;
@@ -343,7 +355,7 @@ template <int THREADS>
 __device__ __forceinline__ void list_in_bucket(SampleLds<THREADS> &lds, float x, uint32_t column)
 {
     const uint32_t i = atomicAdd(&lds.listed, 1u);
-    if (i < kListed) {
+    if (i < SampleLds<THREADS>::kListed) {
         lds.sub_x[i] = x;
         lds.sub_column[i] = column;
     }
@@ -351,10 +363,11 @@ __device__ __forceinline__ void list_in_bucket(SampleLds<THREADS> &lds, float x,
 
 // The key and w of the i-th listed column; for one that does not count or is of another bucket than `only`, 0 and a key behind those of all others.
 constexpr uint32_t kAnyBucket = 0xFFFFFFFFu;
+template <int THREADS>
 __device__ __forceinline__ uint64_t listed_key(const Weights &weights, float x, uint32_t column, uint32_t only, uint32_t i, uint64_t &w)
 {
     const Weight it = weights(x);
-    const bool counts = weights.counts(it) && (only == kAnyBucket || it.bucket() == only);
+    const bool counts = weights.counts(it) && (only == kAnyBucket || it.template bucket<THREADS>() == only);
     w = counts ? it.w : 0;
     return counts ? key_of(order_of(x), column) : i;
 }
@@ -367,7 +380,7 @@ __device__ __forceinline__ uint64_t among(SampleLds<THREADS> &lds, const Weights
 {
     if (threadIdx.x < kLanes) {
         const uint32_t lane = this_thread();
-        uint64_t w = 0, key = lane < n ? listed_key(weights, x[lane], column[lane], only, lane, w) : 0;
+        uint64_t w = 0, key = lane < n ? listed_key<THREADS>(weights, x[lane], column[lane], only, lane, w) : 0;
         const InOrder it = order_by_wave<THREADS>(lds, key, w, n);
         const uint64_t mass = picks([&](const Goal &goal) {
             uint64_t upto;
@@ -383,19 +396,20 @@ __device__ __forceinline__ uint64_t among(SampleLds<THREADS> &lds, const Weights
     return scalar(lds.found_mass);
 }
 
-// Of the n columns listed as those of bucket `only`, no more than kListed, keeps the part that holds the goal, cut by keys until it has no more than 64;
+// Of the n columns listed as those of bucket `only`, no more than SampleLds<THREADS>::kListed, keeps the part that holds the goal, cut by keys until it has no more than 64;
 // returns how many.
 template <int THREADS>
 __device__ __forceinline__ uint32_t refine(SampleLds<THREADS> &lds, const Weights &weights, uint32_t n, uint32_t only, Goal &goal)
 {
-    constexpr uint32_t kEach = kListed / THREADS, kPart = kSub / kLanes;
+    constexpr uint32_t kEach = SampleLds<THREADS>::kListed / THREADS, kPart = SampleLds<THREADS>::kSub / kLanes;
+    constexpr int kCut = SampleLds<THREADS>::kSub == 512 ? 9 : 6;
     const uint32_t thread = this_thread();
     uint64_t key[kEach], w[kEach], low = 1ull << 32, high = ~0ull;         // (keys that count are not below 2^32)
 #pragma unroll
     for (uint32_t k = 0; k < kEach; ++k) {
         const uint32_t i = thread + k * THREADS;
         key[k] = w[k] = 0;
-        if (i < n) key[k] = listed_key(weights, lds.sub_x[i], lds.sub_column[i], only, i, w[k]);
+        if (i < n) key[k] = listed_key<THREADS>(weights, lds.sub_x[i], lds.sub_column[i], only, i, w[k]);
     }
     for (;;) {
         uint64_t least = ~0ull, most = 0;
@@ -411,7 +425,7 @@ __device__ __forceinline__ uint32_t refine(SampleLds<THREADS> &lds, const Weight
             lds.lowest = ~0ull;
             lds.highest = 0;
         }
-        for (uint32_t b = thread; b < kSub; b += THREADS) {
+        for (uint32_t b = thread; b < SampleLds<THREADS>::kSub; b += THREADS) {
             lds.sub_mass[b] = 0;
             lds.sub_count[b] = 0;
         }
@@ -424,7 +438,7 @@ __device__ __forceinline__ uint32_t refine(SampleLds<THREADS> &lds, const Weight
         __syncthreads();
         least = scalar(lds.lowest);
         most = scalar(lds.highest);
-        const int bits = 64 - __builtin_clzll((most - least) | 1), shift = bits > 9 ? bits - 9 : 0;
+        const int bits = 64 - __builtin_clzll((most - least) | 1), shift = bits > kCut ? bits - kCut : 0;
 #pragma unroll
         for (uint32_t k = 0; k < kEach; ++k)
             if (key[k] >= low && key[k] <= high) {
@@ -480,14 +494,14 @@ __device__ __forceinline__ uint32_t refine(SampleLds<THREADS> &lds, const Weight
 template <bool BF16, int THREADS>
 __device__ __forceinline__ uint32_t narrow(const Row<BF16> &row, const Weights &weights, uint32_t only, Goal &goal, SampleLds<THREADS> &lds)
 {
-    Columns<BF16, THREADS, 0> columns(row);
-    const float lowest = weights.lowest((only + 0.5) / 32), highest = weights.highest((only - 0.5) / 32);
+    Columns<BF16, THREADS, 0, true> columns(row);
+    const float lowest = weights.lowest(bucket_end<THREADS>(only)), highest = weights.highest(bucket_begin<THREADS>(only));
     uint64_t from = 0, to = ~0ull;
     auto candidates = [&](auto &&use) {
         columns.between(lowest, highest, [&](float x, uint32_t column) {
             const Weight it = weights(x);
             const uint64_t key = key_of(order_of(x), column);
-            if (it.bucket() == only && weights.counts(it) && key >= from && key <= to) use(key, it.w, x, column);
+            if (it.template bucket<THREADS>() == only && weights.counts(it) && key >= from && key <= to) use(key, it.w, x, column);
         });
         __syncthreads();
     };
@@ -504,7 +518,7 @@ __device__ __forceinline__ uint32_t narrow(const Row<BF16> &row, const Weights &
         from = lds.lowest;
         to = lds.highest;
         uint32_t shift = 0;
-        while ((to - from) >> shift >= kBuckets) ++shift;
+        while ((to - from) >> shift >= SampleLds<THREADS>::kBuckets) ++shift;
         candidates([&](uint64_t key, uint64_t w, float, uint32_t) {
             const uint32_t b = (uint32_t)((to - key) >> shift);
             atomicAdd((unsigned long long *)&lds.mass[b], (unsigned long long)w);
@@ -521,7 +535,7 @@ __device__ __forceinline__ uint32_t narrow(const Row<BF16> &row, const Weights &
         from = to - from > width ? to - width : from;
         candidates([&](uint64_t, uint64_t, float x, uint32_t column) { list_in_bucket<THREADS>(lds, x, column); });
         const uint32_t n = lds.listed;
-        if (n <= kListed) return n;
+        if (n <= SampleLds<THREADS>::kListed) return n;
         __syncthreads();                                   // (the buckets and the number, before they are cleared again)
     }
 }
@@ -537,8 +551,8 @@ __device__ __forceinline__ uint64_t goal_of(const SampleLds<THREADS> &lds, int s
 // One place after the other: that of top_k (0), of top_p (1), of the token (2), whose key is lds.found_key then, `mass` the sum of what is kept.
 // Of the `kept` columns in the list, or, where that is 0, of the row.  `clear`: the buckets are.  `all`: every column counts (or has a w of 0, which
 // may be added).  Without NARROW a bucket with too many columns ends it: false.
-template <bool NARROW, bool BF16, int THREADS, int DEPTH>
-__device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH> &columns, const Weights &weights, uint32_t top_k, bool nucleus, bool all, uint32_t kept,
+template <bool NARROW, bool BF16, int THREADS, int DEPTH, bool LONG>
+__device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH, LONG> &columns, const Weights &weights, uint32_t top_k, bool nucleus, bool all, uint32_t kept,
                                             bool clear, SampleLds<THREADS> &lds, uint64_t &mass)
 {
     const bool counted = top_k < (kept ? kept : columns.row.groups * Row<BF16>::kPer + columns.row.rest);
@@ -559,8 +573,9 @@ __device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH> &colum
 #pragma unroll
                 for (int e = 0; e < n; ++e) {
                     if (!all && !weights.counts(it[e])) continue;
-                    atomicAdd(reinterpret_cast<unsigned long long *>(reinterpret_cast<char *>(lds.mass) + it[e].bytes), (unsigned long long)it[e].w);
-                    if (counted) atomicAdd(&lds.count[it[e].bucket()], 1u);
+                    const uint32_t b = it[e].template bucket<THREADS>();
+                    atomicAdd((unsigned long long *)&lds.mass[b], (unsigned long long)it[e].w);
+                    if (counted) atomicAdd(&lds.count[b], 1u);
                 }
             };
             if (kept)
@@ -573,15 +588,15 @@ __device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH> &colum
                 });
             add_up_buckets<true, true, THREADS>(lds);
             filled = true;
-            if (step == 0) mass = scalar(lds.mass[kBuckets]);
+            if (step == 0) mass = scalar(lds.mass[SampleLds<THREADS>::kBuckets]);
         }
-        if (step == 0 && (!counted || lds.count[kBuckets] <= top_k)) continue;
+        if (step == 0 && (!counted || lds.count[SampleLds<THREADS>::kBuckets] <= top_k)) continue;
         Goal goal = {goal_of(lds, step, top_k, mass), 0, 0, step == 0};
         if (threadIdx.x == 0) lds.listed = 0;
         const uint32_t only = goal.by_count ? bucket_of<THREADS>(lds, lds.count, goal.sum) : bucket_of<THREADS>(lds, lds.mass, goal.sum);
         goal.mass_before = lds.mass[only];
         goal.count_before = goal.by_count ? lds.count[only] : 0;
-        const float lowest = weights.lowest((only + 0.5) / 32), highest = weights.highest((only - 0.5) / 32);
+        const float lowest = weights.lowest(bucket_end<THREADS>(only)), highest = weights.highest(bucket_begin<THREADS>(only));
         if (kept) {
             for (uint32_t i = this_thread(); i < kept; i += THREADS)
                 if (lds.x[i] >= lowest && lds.x[i] <= highest) list_in_bucket<THREADS>(lds, lds.x[i], lds.column[i]);
@@ -590,7 +605,7 @@ __device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH> &colum
         }
         __syncthreads();
         uint32_t n = lds.listed;
-        if (n > kListed) {
+        if (n > SampleLds<THREADS>::kListed) {
             if constexpr (!NARROW) return false;
             __syncthreads();                               // (lds.listed)
             n = narrow<BF16, THREADS>(columns.row, weights, only, goal, lds);
@@ -606,7 +621,7 @@ __device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH> &colum
     return true;
 }
 
-template <bool BF16, int THREADS, int DEPTH>
+template <bool BF16, int THREADS, int DEPTH, bool LONG>
 __global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(const SampleArgs a)
 {
     __shared__ SampleLds<THREADS> lds;
@@ -614,7 +629,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(
     const uint64_t r = (uint64_t)blockIdx.y * gridDim.x + blockIdx.x;
     if (r >= a.rows) return;
     const Row<BF16> row(a, r);
-    Columns<BF16, THREADS, DEPTH> columns(row);
+    Columns<BF16, THREADS, DEPTH, LONG> columns(row);
     const float own_temperature = a.temperature ? a.temperature[r] : a.one_temperature, top_p = a.top_p ? a.top_p[r] : a.one_top_p;
     const float min_p = a.min_p ? a.min_p[r] : a.one_min_p, uniform = a.uniform[r];
     const int32_t own_top_k = a.top_k ? a.top_k[r] : a.one_top_k;
@@ -661,22 +676,22 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(
     if (top_k == 1) {
         bound = most;
     } else if (top_k <= THREADS / 2 && top_k < a.cols) {   // the top_k-th of the threads' largest, by its bucket
-        if (own_most > -INFINITY) atomicAdd(&lds.count[min(weights(own_most).bucket(), kBuckets - 1)], 1u);
+        if (own_most > -INFINITY) atomicAdd(&lds.count[min(weights(own_most).template bucket<THREADS>(), SampleLds<THREADS>::kBuckets - 1)], 1u);
         add_up_buckets<false, true, THREADS>(lds);
         spoilt = true;
-        if (lds.count[kBuckets] >= top_k) {
+        if (lds.count[SampleLds<THREADS>::kBuckets] >= top_k) {
             const uint32_t b = bucket_of<THREADS>(lds, lds.count, (uint64_t)top_k);
-            if (b < kBuckets - 1) bound = fmaxf(bound, weights.lowest((b + 0.5) / 32));
+            if (b < SampleLds<THREADS>::kBuckets - 1) bound = fmaxf(bound, weights.lowest(bucket_end<THREADS>(b)));
         } else {
             __syncthreads();                               // (the buckets, before they are cleared)
         }
     }
-    // The columns that are not below the bound, if they are few: kListed are kept instead of the row, 64 are put in order at once.
+    // The columns that are not below the bound, if they are few: SampleLds<THREADS>::kListed are kept instead of the row, 64 are put in order at once.
     uint32_t kept = 0;
     if (bound > -INFINITY) {
         columns.between(bound, INFINITY, [&](float x, uint32_t column) {
             const uint32_t i = atomicAdd(&lds.listed, 1u);
-            if (i < kListed) {
+            if (i < SampleLds<THREADS>::kListed) {
                 lds.x[i] = x;
                 lds.column[i] = column;
             }
@@ -693,11 +708,11 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(
             return sum;
         });
     } else {
-        if (kept > kListed) kept = 0;
+        if (kept > SampleLds<THREADS>::kListed) kept = 0;
         const bool all = min_p <= 0.0f && top_k >= a.cols;
         if (!find_places<false, BF16>(columns, weights, top_k, top_p < 1.0f, all, kept, !spoilt, lds, mass)) {
             // (seldom; the row does not stay in registers meanwhile)
-            Columns<BF16, THREADS, 0> again(row);
+            Columns<BF16, THREADS, 0, true> again(row);
             __syncthreads();
             find_places<true, BF16>(again, weights, top_k, top_p < 1.0f, all, 0, false, lds, mass);
         }
@@ -713,11 +728,12 @@ static int sample_launch(const SampleArgs &a, hipStream_t stream)
     const uint32_t across = (uint32_t)(a.rows < (1u << 20) ? a.rows : 1u << 20);
     const dim3 grid(across, (uint32_t)((a.rows + across - 1) / across));
     const uint32_t quads = (a.cols + (BF16 ? 7 : 3)) / (BF16 ? 8 : 4);
-    if (quads <= 256 * 8) return launch(sample_kernel<BF16, 256, 8>, grid, 256, stream, a);
-    if (a.rows > 256 && quads <= 512 * 16) return launch(sample_kernel<BF16, 512, 16>, grid, 512, stream, a);
-    if (quads <= 1024 * 8) return launch(sample_kernel<BF16, 1024, 8>, grid, 1024, stream, a);
-    if (quads <= 1024 * 16) return launch(sample_kernel<BF16, 1024, 16>, grid, 1024, stream, a);
-    return launch(sample_kernel<BF16, 1024, 0>, grid, 1024, stream, a);
+    if (quads <= 64 * 4) return launch(sample_kernel<BF16, 64, 4, false>, grid, 64, stream, a);
+    if (quads <= 256 * 8) return launch(sample_kernel<BF16, 256, 8, false>, grid, 256, stream, a);
+    if (a.rows > 256 && quads <= 512 * 16) return launch(sample_kernel<BF16, 512, 16, false>, grid, 512, stream, a);
+    if (quads <= 1024 * 8) return launch(sample_kernel<BF16, 1024, 8, false>, grid, 1024, stream, a);
+    if (quads <= 1024 * 16) return launch(sample_kernel<BF16, 1024, 16, false>, grid, 1024, stream, a);
+    return launch(sample_kernel<BF16, 1024, 16, true>, grid, 1024, stream, a);
 }
 
 static bool optional_at(const void *p, uintptr_t size) { return !p || at_multiple(p, size); }

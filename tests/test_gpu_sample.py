@@ -95,11 +95,12 @@ def test_rows_with_parameters_of_their_own(dtype, cols):
     check(randn((rows, cols), dtype, 3, 2.5), uniform(rows, 4), temperature=0.8, top_p=choose([1.0, 0.5], 1), top_k=30)
 
 
+@pytest.mark.parametrize("cols", [900, 6000, 30_000])
 @pytest.mark.parametrize("spread", [0.0, 0.01, 0.5, 30.0])
 @pytest.mark.parametrize("dtype", TYPES)
-def test_flat_and_peaked_rows(dtype, spread):
+def test_flat_and_peaked_rows(dtype, spread, cols):
     """Thousands of equal logits (bfloat16 has few values near each other), a nucleus of most of the row, one of a single column."""
-    x = randn((12, 30_000), dtype, 1, spread) + 5
+    x = randn((12, cols), dtype, 1, spread) + 5
     for parameters in (dict(), dict(top_p=0.95), dict(top_k=2000), dict(top_k=5000, top_p=0.7, temperature=2.0), dict(min_p=0.5), dict(temperature=0.05, top_p=0.99)):
         if spread:
             check(x, uniform(12, 2), least_clear=0.5, **parameters)
@@ -119,9 +120,10 @@ def test_equal_logits_go_by_the_column():
             within(logprob, torch.full((5,), -math.log(kept), dtype=torch.float64, device="cuda"), 2 * U * math.log(kept))
 
 
-def test_few_values_in_a_long_row():
-    x = torch.randint(0, 4, (16, 90_000), generator=generator(1), device="cuda").float() * 0.5
-    for parameters in (dict(), dict(top_p=0.6), dict(top_k=30_000), dict(top_k=100, top_p=0.5), dict(min_p=0.5, top_p=0.9)):
+@pytest.mark.parametrize("cols", [1000, 8000, 90_000])
+def test_few_values_in_a_row(cols):
+    x = torch.randint(0, 4, (16, cols), generator=generator(1), device="cuda").float() * 0.5
+    for parameters in (dict(), dict(top_p=0.6), dict(top_k=cols // 3), dict(top_k=100, top_p=0.5), dict(min_p=0.5, top_p=0.9)):
         ones = parameters.get("top_k") == 100              # (more than 100 columns have the largest value)
         check(x, uniform(16, 2), least_clear=0.8, exact_sums=ones, **parameters)
         check(x.bfloat16(), uniform(16, 3), least_clear=0.8, exact_sums=ones, **parameters)
