@@ -20,12 +20,12 @@
 namespace solo {
 
 // Buckets of the distance from the maximum, 64 binary orders of w in all; columns that are kept as a list; parts that a list is cut into.  A row of one
-// wavefront has an eighth of each: what it clears and adds up is most of its work, and what it has in LDS says how many rows a compute unit has
-// under way (100000 rows of 300 fp32: 145 us, with the others' sizes and 256 threads 1107).
+// wavefront has an eighth or a quarter of each: what it clears and adds up is most of its work, and what it has in LDS says how many rows a compute unit has
+// under way (100000 rows of 300 fp32: 163 us, with the others' sizes and 256 threads 1107).
 template <int THREADS>
 struct Sizes {
     static constexpr bool kShort = THREADS == kLanes;
-    static constexpr uint32_t kBuckets = kShort ? 256 : 2048, kListed = kShort ? 128 : 1024, kSub = kShort ? 64 : 512;
+    static constexpr uint32_t kBuckets = kShort ? 256 : 2048, kListed = kShort ? 256 : 1024, kSub = kShort ? 64 : 512;
 };
 
 // 2^(i / 32)
@@ -722,6 +722,9 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(
 }
 
 // ---- host ------------------------------------------------------------------------------------
+// The fewest threads that hold the row, by groups of 16 bytes, without many a thread; more where there are fewer rows than compute units and it is one row's time
+// that counts.  (One row of 4000 bf16: 256 threads 11 us, 64 21; 5000 rows of 1900 fp32: 256 threads 79, 64 38, and 300 of them 13 and 21; 1024 rows of 16000
+// fp32: 512 threads with eight groups 33, with sixteen 36, 1024 threads 46; 1024 of 50257 bf16: 512 threads 102, 1024 128.)
 template <bool BF16>
 static int sample_launch(const SampleArgs &a, hipStream_t stream)
 {
@@ -729,8 +732,11 @@ static int sample_launch(const SampleArgs &a, hipStream_t stream)
     const dim3 grid(across, (uint32_t)((a.rows + across - 1) / across));
     const uint32_t quads = (a.cols + (BF16 ? 7 : 3)) / (BF16 ? 8 : 4);
     if (quads <= 64 * 4) return launch(sample_kernel<BF16, 64, 4, false>, grid, 64, stream, a);
+    if (!BF16 && quads <= 64 * 8 && a.rows > 1024) return launch(sample_kernel<false, 64, 8, false>, grid, 64, stream, a);
+    if (quads <= 256 * 4) return launch(sample_kernel<BF16, 256, 4, false>, grid, 256, stream, a);
     if (quads <= 256 * 8) return launch(sample_kernel<BF16, 256, 8, false>, grid, 256, stream, a);
-    if (a.rows > 256 && quads <= 512 * 16) return launch(sample_kernel<BF16, 512, 16, false>, grid, 512, stream, a);
+    if (quads <= 512 * 8 && a.rows > 256) return launch(sample_kernel<BF16, 512, 8, false>, grid, 512, stream, a);
+    if (quads <= 512 * 16 && a.rows > 256) return launch(sample_kernel<BF16, 512, 16, false>, grid, 512, stream, a);
     if (quads <= 1024 * 8) return launch(sample_kernel<BF16, 1024, 8, false>, grid, 1024, stream, a);
     if (quads <= 1024 * 16) return launch(sample_kernel<BF16, 1024, 16, false>, grid, 1024, stream, a);
     return launch(sample_kernel<BF16, 1024, 16, true>, grid, 1024, stream, a);

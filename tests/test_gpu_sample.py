@@ -70,7 +70,8 @@ def uniform(rows, seed):
     return torch.rand(rows, generator=generator(seed), device="cuda")
 
 
-SHAPES = [(1, 1, 0), (9, 2, 0), (50, 7, 1), (300, 100, 0), (64, 1000, 3), (20, 4096, 0), (9, 8192, 0), (9, 8193, 1), (9, 16_390, 0), (300, 20_000, 0), (6, 32_000, 0), (5, 50_257, 47),
+SHAPES = [(1, 1, 0), (9, 2, 0), (50, 7, 1), (300, 100, 0), (64, 1000, 3), (1100, 1500, 0), (20, 4096, 0), (9, 8192, 0), (9, 8193, 1), (9, 16_390, 0), (300, 15_000, 0),
+          (300, 20_000, 0), (270, 33_000, 0), (20, 15_000, 0), (3, 25_000, 0), (6, 32_000, 0), (5, 50_257, 47),
           (3, 65_540, 0), (2, 150_001, 0)]
 
 PARAMETERS = [dict(), dict(temperature=0.0), dict(temperature=0.7, top_p=0.9), dict(top_k=1), dict(top_k=40), dict(top_k=1500, temperature=1.5), dict(min_p=0.05),
