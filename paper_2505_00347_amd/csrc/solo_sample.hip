@@ -19,13 +19,14 @@
 
 namespace solo {
 
-// Buckets of the distance from the maximum, 64 binary orders of w in all; columns that are kept as a list; parts that a list is cut into.  A row of one
+// Buckets of the distance from the maximum, 64 binary orders of w in all; columns above a bound that are kept instead of the row; columns of a bucket that are
+// listed; parts that a list is cut into.  A row of one
 // wavefront has an eighth or a quarter of each: what it clears and adds up is most of its work, and what it has in LDS says how many rows a compute unit has
 // under way (100000 rows of 300 fp32: 163 us, with the others' sizes and 256 threads 1107).
 template <int THREADS>
 struct Sizes {
     static constexpr bool kShort = THREADS == kLanes;
-    static constexpr uint32_t kBuckets = kShort ? 256 : 2048, kListed = kShort ? 256 : 1024, kSub = kShort ? 64 : 512;
+    static constexpr uint32_t kBuckets = kShort ? 256 : 2048, kKept = kShort ? 256 : 2048, kListed = kShort ? 256 : 1024, kSub = kShort ? 64 : 512;
 };
 
 // 2^(i / 32)
@@ -57,11 +58,12 @@ typedef uint32_t Words __attribute__((ext_vector_type(2)));
 
 template <int THREADS>
 struct SampleLds {
-    static constexpr uint32_t kBuckets = Sizes<THREADS>::kBuckets, kListed = Sizes<THREADS>::kListed, kSub = Sizes<THREADS>::kSub;
+    static constexpr uint32_t kBuckets = Sizes<THREADS>::kBuckets, kKept = Sizes<THREADS>::kKept, kListed = Sizes<THREADS>::kListed,
+                              kSub = Sizes<THREADS>::kSub;
     uint64_t mass[kBuckets + 1];       // sums of the buckets, then of all in front of a bucket
     uint32_t count[kBuckets + 1];
-    float x[kListed];                  // of the columns above a bound
-    uint32_t column[kListed];
+    float x[kKept];                    // of the columns above a bound
+    uint32_t column[kKept];
     float sub_x[kListed];              // of those in a bucket
     uint32_t sub_column[kListed];
     uint64_t sub_mass[kSub];
@@ -199,6 +201,19 @@ struct Columns {
             x[0] = last;
             use(x, std::integral_constant<int, 1>(), row.last_column(threadIdx.x));
         }
+    }
+    // use(x, column) for the logits from `from` on: few
+    template <typename Use>
+    __device__ __forceinline__ void not_below(float from, Use &&use)
+    {
+        each([&](const float *x, auto n, uint32_t column) {
+            float most = x[0];
+            if constexpr (n > 1) most = max_of<n>(x);
+            if (__ballot(most >= from) == 0) return;
+#pragma unroll
+            for (int e = 0; e < n; ++e)
+                if (x[e] >= from) use(x[e], column + e);
+        });
     }
     // use(x, column) for the logits from `from` to `to`: few
     template <typename Use>
@@ -396,7 +411,7 @@ __device__ __forceinline__ uint64_t among(SampleLds<THREADS> &lds, const Weights
     return scalar(lds.found_mass);
 }
 
-// Of the n columns listed as those of bucket `only`, no more than SampleLds<THREADS>::kListed, keeps the part that holds the goal, cut by keys until it has no more than 64;
+// Of the n columns listed as those of bucket `only`, no more than kListed, keeps the part that holds the goal, cut by keys until it has no more than 64;
 // returns how many.
 template <int THREADS>
 __device__ __forceinline__ uint32_t refine(SampleLds<THREADS> &lds, const Weights &weights, uint32_t n, uint32_t only, Goal &goal)
@@ -686,12 +701,12 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(
             __syncthreads();                               // (the buckets, before they are cleared)
         }
     }
-    // The columns that are not below the bound, if they are few: SampleLds<THREADS>::kListed are kept instead of the row, 64 are put in order at once.
+    // The columns that are not below the bound, if they are few: kKept are kept instead of the row, 64 are put in order at once.
     uint32_t kept = 0;
     if (bound > -INFINITY) {
-        columns.between(bound, INFINITY, [&](float x, uint32_t column) {
+        columns.not_below(bound, [&](float x, uint32_t column) {
             const uint32_t i = atomicAdd(&lds.listed, 1u);
-            if (i < SampleLds<THREADS>::kListed) {
+            if (i < SampleLds<THREADS>::kKept) {
                 lds.x[i] = x;
                 lds.column[i] = column;
             }
@@ -708,7 +723,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(
             return sum;
         });
     } else {
-        if (kept > SampleLds<THREADS>::kListed) kept = 0;
+        if (kept > SampleLds<THREADS>::kKept) kept = 0;
         const bool all = min_p <= 0.0f && top_k >= a.cols;
         if (!find_places<false, BF16>(columns, weights, top_k, top_p < 1.0f, all, kept, !spoilt, lds, mass)) {
             // (seldom; the row does not stay in registers meanwhile)
