@@ -9,6 +9,11 @@
 // as well, so a row far from zero loses no digits.  The gradient's threads keep
 // their columns: each adds dy h and dy of all its rows in registers, the workgroups' sums go to the workspace, and a second launch
 // adds those in the order of the workgroups.
+//
+// Bound by memory where rows are wide: 16384 x 4096 bf16 forward 50 us (5.4 TB/s), gradient 80 us (5.0), sums of the parts 4 us.  Loads of the next row in
+// front of the work on this one gain nothing (80 us with them, 41 instead of 36 for 8192 x 2048 fp32): the other wavefronts have theirs under way.  Accesses past the
+// caches take 3 to 8 % off calls of more than 256 MiB (32768 x 4096 bf16, both, 247 and 227 us), which the product that reads the output next would lose.  Rows
+// that do not fill their threads (560 bf16: 70 of 128 groups) are bound by instructions, 2.9 TB/s.
 #include "solo_ops.h"
 
 #include <math.h>

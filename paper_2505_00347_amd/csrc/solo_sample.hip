@@ -12,6 +12,11 @@
 // Which column it is hangs on comparisons of sums, so these are exact: w is computed in binary64 (the rate of its instructions is that of
 // binary32), to 2e-13, and rounded to a whole multiple of 2^-shift; sums of such are whole numbers below 2^63, the same in every order, and atomic
 // additions in LDS make them.
+//
+// A workgroup takes a row.  One row of 50257 fp32, nucleus of 0.95, 22 us: 3 until the maximum is known, 9.5 for weights and buckets (28 cycles for 64 of them: twenty
+// vector instructions on each of four SIMDs, and the additions in LDS), 1 to add up, 3.5 for each of two places, most of it the pass over the row.  One after
+// the other, without the next one's chain of instructions beside its own, the weights took 13.  1024 x 32000 fp32, the whole distribution, 55 us (2.4 TB/s, and two
+// thirds of the vector issue); 1024 x 50257 bf16 with min_p and nucleus 71 us, where the rows with many columns above the bound come last.
 #include "solo_rows.h"
 
 #include <float.h>
@@ -66,13 +71,15 @@ struct SampleLds {
     uint32_t column[kKept];
     float sub_x[kListed];              // of those in a bucket
     uint32_t sub_column[kListed];
+    float few_x[kLanes];               // of a part of those
+    uint32_t few_column[kLanes];
     uint64_t sub_mass[kSub];
     uint32_t sub_count[kSub];
     uint64_t key[kLanes], weight[kLanes];
     Words root[32];                    // 2^(i / 32) times 2^shift, less what i adds to the exponent below
     uint64_t wave_mass[THREADS / kLanes], lowest, highest;
     uint32_t wave_count[THREADS / kLanes];
-    float at[THREADS / kLanes];
+    float at[THREADS / kLanes], last[8];
     uint32_t listed, bucket;
     uint64_t found_key, found_mass;
     double inverse, below, nucleus;    // of temperature; uniform and top_p, within their ends
@@ -159,15 +166,15 @@ struct Columns {
     static constexpr int kPer = Row<BF16>::kPer, kAhead = DEPTH ? 2 : 4;
     const Row<BF16> &row;
     Quad q[DEPTH ? DEPTH : 1];
-    float last;
+    float *last;                       // of LDS: the threads' columns behind the groups
 
-    __device__ __forceinline__ explicit Columns(const Row<BF16> &row) : row(row)
+    __device__ __forceinline__ Columns(const Row<BF16> &row, float *last) : row(row), last(last)
     {
         if (DEPTH && row.groups != 0) {
 #pragma unroll
             for (int j = 0; j < DEPTH; ++j) q[j] = row.group(min(j * THREADS + threadIdx.x, row.groups - 1));
         }
-        last = threadIdx.x < row.rest ? row.one(row.last_column(threadIdx.x)) : -INFINITY;
+        if (threadIdx.x < row.rest) last[threadIdx.x] = row.one(row.last_column(threadIdx.x));
     }
     // use(x, n, column): the n logits x from column `column` on
     template <typename Use>
@@ -198,7 +205,7 @@ struct Columns {
             }
         }
         if (threadIdx.x < row.rest) {
-            x[0] = last;
+            x[0] = last[threadIdx.x];
             use(x, std::integral_constant<int, 1>(), row.last_column(threadIdx.x));
         }
     }
@@ -411,42 +418,41 @@ __device__ __forceinline__ uint64_t among(SampleLds<THREADS> &lds, const Weights
     return scalar(lds.found_mass);
 }
 
-// Of the n columns listed as those of bucket `only`, no more than kListed, keeps the part that holds the goal, cut by keys until it has no more than 64;
-// returns how many.
+// Of the n columns listed as those of bucket `only`, no more than kListed, lists the part that holds the goal as lds.few_x and few_column: cut by keys until it
+// has no more than 64; returns how many.  (The keys are made again where they are used: kept in registers, beside those of a long row, they would be spilled.)
 template <int THREADS>
 __device__ __forceinline__ uint32_t refine(SampleLds<THREADS> &lds, const Weights &weights, uint32_t n, uint32_t only, Goal &goal)
 {
-    constexpr uint32_t kEach = SampleLds<THREADS>::kListed / THREADS, kPart = SampleLds<THREADS>::kSub / kLanes;
+    constexpr uint32_t kPart = SampleLds<THREADS>::kSub / kLanes;
     constexpr int kCut = SampleLds<THREADS>::kSub == 512 ? 9 : 6;
-    const uint32_t thread = this_thread();
-    uint64_t key[kEach], w[kEach], low = 1ull << 32, high = ~0ull;         // (keys that count are not below 2^32)
-#pragma unroll
-    for (uint32_t k = 0; k < kEach; ++k) {
-        const uint32_t i = thread + k * THREADS;
-        key[k] = w[k] = 0;
-        if (i < n) key[k] = listed_key<THREADS>(weights, lds.sub_x[i], lds.sub_column[i], only, i, w[k]);
-    }
+    uint64_t low = 1ull << 32, high = ~0ull;               // (keys that count are not below 2^32)
+    auto candidates = [&](auto &&use) {
+#pragma unroll 1
+        for (uint32_t i = this_thread(); i < n; i += THREADS) {
+            uint64_t w;
+            const uint64_t key = listed_key<THREADS>(weights, lds.sub_x[i], lds.sub_column[i], only, i, w);
+            if (key >= low && key <= high) use(key, w, i);
+        }
+    };
     for (;;) {
-        uint64_t least = ~0ull, most = 0;
-#pragma unroll
-        for (uint32_t k = 0; k < kEach; ++k)
-            if (key[k] >= low && key[k] <= high) {
-                least = min(least, key[k]);
-                most = max(most, key[k]);
-            }
-        least = wave_reduce(least, [](uint64_t p, uint64_t q) { return p < q ? p : q; });
-        most = wave_max(most);
-        if (thread == 0) {
+        if (this_thread() == 0) {
             lds.lowest = ~0ull;
             lds.highest = 0;
         }
-        for (uint32_t b = thread; b < SampleLds<THREADS>::kSub; b += THREADS) {
+        for (uint32_t b = this_thread(); b < SampleLds<THREADS>::kSub; b += THREADS) {
             lds.sub_mass[b] = 0;
             lds.sub_count[b] = 0;
         }
         __syncthreads();
-        if (thread == 0) lds.listed = 0;                   // (read in front of the barrier)
-        if (thread % kLanes == 0 && most != 0) {
+        if (this_thread() == 0) lds.listed = 0;            // (read in front of the barrier)
+        uint64_t least = ~0ull, most = 0;
+        candidates([&](uint64_t key, uint64_t, uint32_t) {
+            least = min(least, key);
+            most = max(most, key);
+        });
+        least = wave_reduce(least, [](uint64_t p, uint64_t q) { return p < q ? p : q; });
+        most = wave_max(most);
+        if (this_thread() % kLanes == 0 && most != 0) {
             atomicMin((unsigned long long *)&lds.lowest, (unsigned long long)least);
             atomicMax((unsigned long long *)&lds.highest, (unsigned long long)most);
         }
@@ -454,14 +460,13 @@ __device__ __forceinline__ uint32_t refine(SampleLds<THREADS> &lds, const Weight
         least = scalar(lds.lowest);
         most = scalar(lds.highest);
         const int bits = 64 - __builtin_clzll((most - least) | 1), shift = bits > kCut ? bits - kCut : 0;
-#pragma unroll
-        for (uint32_t k = 0; k < kEach; ++k)
-            if (key[k] >= low && key[k] <= high) {
-                const uint32_t b = (uint32_t)((most - key[k]) >> shift);
-                atomicAdd((unsigned long long *)&lds.sub_mass[b], (unsigned long long)w[k]);
-                atomicAdd(&lds.sub_count[b], 1u);
-            }
+        candidates([&](uint64_t key, uint64_t w, uint32_t) {
+            const uint32_t b = (uint32_t)((most - key) >> shift);
+            atomicAdd((unsigned long long *)&lds.sub_mass[b], (unsigned long long)w);
+            atomicAdd(&lds.sub_count[b], 1u);
+        });
         __syncthreads();
+        const uint32_t thread = this_thread();
         if (thread < kLanes) {                             // which part has the goal
             uint64_t mass = 0, count = 0;
 #pragma unroll
@@ -489,18 +494,16 @@ __device__ __forceinline__ uint32_t refine(SampleLds<THREADS> &lds, const Weight
         high = most - ((uint64_t)scalar(lds.bucket) << shift);
         const uint64_t width = (1ull << shift) - 1;
         low = high - least > width ? high - width : least;
-#pragma unroll
-        for (uint32_t k = 0; k < kEach; ++k)
-            if (key[k] >= low && key[k] <= high) {
-                const uint32_t i = atomicAdd(&lds.listed, 1u);
-                if (i < kLanes) {
-                    lds.sub_x[i] = value_of(key[k]);
-                    lds.sub_column[i] = column_of(key[k]);
-                }
+        candidates([&](uint64_t, uint64_t, uint32_t i) {
+            const uint32_t at = atomicAdd(&lds.listed, 1u);
+            if (at < kLanes) {
+                lds.few_x[at] = lds.sub_x[i];
+                lds.few_column[at] = lds.sub_column[i];
             }
+        });
         __syncthreads();
-        n = lds.listed;
-        if (n <= kLanes) return n;
+        const uint32_t few = scalar(lds.listed);
+        if (few <= kLanes) return few;
     }
 }
 
@@ -509,7 +512,7 @@ __device__ __forceinline__ uint32_t refine(SampleLds<THREADS> &lds, const Weight
 template <bool BF16, int THREADS>
 __device__ __forceinline__ uint32_t narrow(const Row<BF16> &row, const Weights &weights, uint32_t only, Goal &goal, SampleLds<THREADS> &lds)
 {
-    Columns<BF16, THREADS, 0, true> columns(row);
+    Columns<BF16, THREADS, 0, true> columns(row, lds.last);
     const float lowest = weights.lowest(bucket_end<THREADS>(only)), highest = weights.highest(bucket_begin<THREADS>(only));
     uint64_t from = 0, to = ~0ull;
     auto candidates = [&](auto &&use) {
@@ -597,7 +600,7 @@ __device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH, LONG> 
                 for (uint32_t i = this_thread(); i < kept; i += THREADS) add(&lds.x[i], std::integral_constant<int, 1>());
             else
                 columns.each([&](const float *x, auto n, uint32_t) {
-                    constexpr int kSide = n < 4 ? n : 4;
+                    constexpr int kMost = DEPTH > 8 ? 2 : 4, kSide = n < kMost ? n : kMost;       // (beside a long row there are registers for two)
 #pragma unroll
                     for (int e = 0; e < n; e += kSide) add(x + e, std::integral_constant<int, kSide>());
                 });
@@ -606,12 +609,12 @@ __device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH, LONG> 
             if (step == 0) mass = scalar(lds.mass[SampleLds<THREADS>::kBuckets]);
         }
         if (step == 0 && (!counted || lds.count[SampleLds<THREADS>::kBuckets] <= top_k)) continue;
-        Goal goal = {goal_of(lds, step, top_k, mass), 0, 0, step == 0};
+        Goal goal = {scalar(goal_of(lds, step, top_k, mass)), 0, 0, step == 0};
         if (threadIdx.x == 0) lds.listed = 0;
-        const uint32_t only = goal.by_count ? bucket_of<THREADS>(lds, lds.count, goal.sum) : bucket_of<THREADS>(lds, lds.mass, goal.sum);
-        goal.mass_before = lds.mass[only];
-        goal.count_before = goal.by_count ? lds.count[only] : 0;
-        const float lowest = weights.lowest(bucket_end<THREADS>(only)), highest = weights.highest(bucket_begin<THREADS>(only));
+        const uint32_t only = scalar(goal.by_count ? bucket_of<THREADS>(lds, lds.count, goal.sum) : bucket_of<THREADS>(lds, lds.mass, goal.sum));
+        goal.mass_before = scalar(lds.mass[only]);
+        goal.count_before = goal.by_count ? scalar(lds.count[only]) : 0;
+        const float lowest = scalar(weights.lowest(bucket_end<THREADS>(only))), highest = scalar(weights.highest(bucket_begin<THREADS>(only)));
         if (kept) {
             for (uint32_t i = this_thread(); i < kept; i += THREADS)
                 if (lds.x[i] >= lowest && lds.x[i] <= highest) list_in_bucket<THREADS>(lds, lds.x[i], lds.column[i]);
@@ -619,15 +622,16 @@ __device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH, LONG> 
             columns.between(lowest, highest, [&](float x, uint32_t column) { list_in_bucket<THREADS>(lds, x, column); });
         }
         __syncthreads();
-        uint32_t n = lds.listed;
+        uint32_t n = scalar(lds.listed);
         if (n > SampleLds<THREADS>::kListed) {
             if constexpr (!NARROW) return false;
             __syncthreads();                               // (lds.listed)
             n = narrow<BF16, THREADS>(columns.row, weights, only, goal, lds);
             filled = false;
         }
-        if (n > kLanes) n = refine<THREADS>(lds, weights, n, only, goal);
-        mass = among<THREADS>(lds, weights, lds.sub_x, lds.sub_column, n, only, [&](auto &&at) {
+        const bool many = n > kLanes;
+        if (many) n = refine<THREADS>(lds, weights, n, only, goal);
+        mass = among<THREADS>(lds, weights, many ? lds.few_x : lds.sub_x, many ? lds.few_column : lds.sub_column, n, only, [&](auto &&at) {
             const uint64_t upto = at(goal);
             return step == 2 ? mass : upto;
         });
@@ -644,7 +648,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(
     const uint64_t r = (uint64_t)blockIdx.y * gridDim.x + blockIdx.x;
     if (r >= a.rows) return;
     const Row<BF16> row(a, r);
-    Columns<BF16, THREADS, DEPTH, LONG> columns(row);
+    Columns<BF16, THREADS, DEPTH, LONG> columns(row, lds.last);
     const float own_temperature = a.temperature ? a.temperature[r] : a.one_temperature, top_p = a.top_p ? a.top_p[r] : a.one_top_p;
     const float min_p = a.min_p ? a.min_p[r] : a.one_min_p, uniform = a.uniform[r];
     const int32_t own_top_k = a.top_k ? a.top_k[r] : a.one_top_k;
@@ -727,7 +731,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(
         const bool all = min_p <= 0.0f && top_k >= a.cols;
         if (!find_places<false, BF16>(columns, weights, top_k, top_p < 1.0f, all, kept, !spoilt, lds, mass)) {
             // (seldom; the row does not stay in registers meanwhile)
-            Columns<BF16, THREADS, 0, true> again(row);
+            Columns<BF16, THREADS, 0, true> again(row, lds.last);
             __syncthreads();
             find_places<true, BF16>(again, weights, top_k, top_p < 1.0f, all, 0, false, lds, mass);
         }
