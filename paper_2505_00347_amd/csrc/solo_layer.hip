@@ -285,31 +285,33 @@ __global__ __launch_bounds__((Deal<XB, YB, LANES, E>::kThreads)) void layer_back
             }
         }
     } else {
-        // the sums of a wavefront's rows, then one wavefront after the other
-        __shared__ float all[2][LANES * E];
+        // the sums of a wavefront's rows, then those of the wavefronts in their order
+        constexpr int kWaves = D::kThreads / kLanes;
+        __shared__ float all[2][kWaves][LANES * E];
+        const uint32_t wave = threadIdx.x / kLanes;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             if constexpr (LANES < kLanes) {
                 dw[e] = wave_reduce<kLanes, LANES>(dw[e], [](float p, float q) { return p + q; });
                 db[e] = wave_reduce<kLanes, LANES>(db[e], [](float p, float q) { return p + q; });
             }
-        }
-        for (uint32_t wave = 0; wave < D::kThreads / kLanes; ++wave) {
-            if (threadIdx.x / kLanes == wave && threadIdx.x % kLanes < LANES) {
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    // (element e of each lane side by side: no two lanes in one bank)
-                    const uint32_t at = e * LANES + deal.lane;
-                    all[0][at] = wave == 0 ? dw[e] : all[0][at] + dw[e];
-                    all[1][at] = wave == 0 ? db[e] : all[1][at] + db[e];
-                }
+            if (threadIdx.x % kLanes < LANES) {
+                // (element e of each lane side by side: no two lanes in one bank)
+                all[0][wave][e * LANES + deal.lane] = dw[e];
+                all[1][wave][e * LANES + deal.lane] = db[e];
             }
-            __syncthreads();
         }
+        __syncthreads();
         for (uint32_t c = threadIdx.x; c < a.cols; c += D::kThreads) {
-            const uint32_t group = c / kPer, lane = group % LANES, e = group / LANES * kPer + c % kPer;
-            part_w[c] = all[0][e * LANES + lane];
-            part_b[c] = all[1][e * LANES + lane];
+            const uint32_t group = c / kPer, at = (group / LANES * kPer + c % kPer) * LANES + group % LANES;
+            float sum_w = all[0][0][at], sum_b = all[1][0][at];
+#pragma unroll
+            for (int k = 1; k < kWaves; ++k) {
+                sum_w += all[0][k][at];
+                sum_b += all[1][k][at];
+            }
+            part_w[c] = sum_w;
+            part_b[c] = sum_b;
         }
     }
 }
