@@ -245,8 +245,8 @@ int solo_adamw_step_multi(const void *table_device, uint32_t count, uint64_t uni
  * negative code with nothing enqueued (but SOLO_E_HIP of a call of several launches: those before the
  * one that the runtime refused are enqueued, and the outputs are then not specified).  A workspace needs no initialisation, holds nothing between
  * calls and serves one call at a time (calls on one stream follow each other).  Tensors need the
- * alignment of their elements only.  Every call gives the same bits for the same inputs: no sum is
- * made by atomic additions.  All calls can be captured into a HIP graph. */
+ * alignment of their elements only.  Every call gives the same bits for the same inputs: no sum of
+ * floating-point numbers is made by atomic additions.  All calls can be captured into a HIP graph. */
 
 /* ---- global norm and clipping ---------------------------------------------------------------
  * Over the tensors g_k of a table, with u = *unscale (the reciprocal of a loss scale; NULL: 1):
@@ -374,7 +374,7 @@ int solo_logprob_with_grad(const void *logits, const void *targets, const float 
  * grad_weight and grad_bias have the weights' type; with SOLO_LAYERNORM_ACCUMULATE the sums are added to what is there (a second
  * micro-batch).  Sums are binary32, over the rows in an order that the shape alone determines; one rounding at the end.  The squares
  * are those of the differences from the mean.  A row with a NaN or an infinity, or whose squares overflow binary32, has unspecified
- * results in that row (and in the sums over the rows), no others.  y may be x, grad_x may be x or grad_y, where types and
+ * results in that row (NaN behind a NaN) and in the sums over the rows, no others.  y may be x, grad_x may be x or grad_y, where types and
  * strides are the same; otherwise outputs must not overlap inputs. */
 #define SOLO_LAYERNORM_RMS 1u
 #define SOLO_LAYERNORM_ACCUMULATE 2u
@@ -424,7 +424,7 @@ int solo_layernorm_grad(const void *grad_y, const void *x, const void *weight, c
 #define SOLO_DISTILL_REST 1u
 #define SOLO_DISTILL_MAX 128
 typedef struct solo_distill_shape {
-    uint64_t rows, cols;        /* cols below 2^29                                               */
+    uint64_t rows, cols;        /* below 2^35 and 2^29                                           */
     uint64_t stride;            /* elements from row to row of logits, >= cols                   */
     uint64_t grad_stride;       /* the same of grad_logits                                       */
     uint64_t value_stride;      /* the same of teacher_value, >= top                             */
@@ -463,7 +463,7 @@ int solo_distill_with_grad(const void *logits, const void *teacher_value, const 
  * Weights are computed in binary64 and summed exactly as whole multiples of 2^-(62 - log2 cols) (2^-51 at most) of the largest, so the token is
  * that of exact arithmetic unless u or a limit lies within some 1e-11 of a border; columns below half such a multiple are never chosen. */
 typedef struct solo_sample_shape {
-    uint64_t rows, cols;        /* cols below 2^29                                               */
+    uint64_t rows, cols;        /* below 2^35 and 2^29                                           */
     uint64_t stride;            /* elements from row to row of logits, >= cols                   */
     uint32_t dtype;             /* of logits                                                     */
     uint32_t token_bits;        /* of token, 32 or 64                                            */

@@ -200,7 +200,8 @@ __global__ __launch_bounds__((Deal<XB, YB, LANES, E>::kThreads)) void layer_forw
         row_total<LANES, 2>(left, lds, turn);
         // what the mean's rounding has left of it: of rows far from zero more than the spread
         const float shift = a.rms ? 0.0f : left[0] * inverse;
-        const float rstd = 1.0f / sqrtf(fmaxf(fmaf(-shift, shift, left[1] * inverse), 0.0f) + a.eps);
+        const float variance = fmaf(-shift, shift, left[1] * inverse);
+        const float rstd = 1.0f / sqrtf((variance < 0.0f ? 0.0f : variance) + a.eps);        // (NaN stays)
         mean += shift;
 #pragma unroll
         for (int j = 0; j < kDepth; ++j) {
@@ -337,7 +338,8 @@ __global__ __launch_bounds__(1024) void layer_forward_long_kernel(const LayerArg
         }
         row_total<1024, 2>(left, lds, turn);
         const float shift = a.rms ? 0.0f : left[0] / (float)a.cols;
-        const float rstd = 1.0f / sqrtf(fmaxf(fmaf(-shift, shift, left[1] / (float)a.cols), 0.0f) + a.eps);
+        const float variance = fmaf(-shift, shift, left[1] / (float)a.cols);
+        const float rstd = 1.0f / sqrtf((variance < 0.0f ? 0.0f : variance) + a.eps);
         for (uint32_t c = threadIdx.x; c < a.cols; c += 1024) {
             const float w = !a.w ? 1.0f : a.w_bf16 ? Elements<true>::load1(a.w, c) : Elements<false>::load1(a.w, c);
             const float b = !a.b ? 0.0f : a.w_bf16 ? Elements<true>::load1(a.b, c) : Elements<false>::load1(a.b, c);

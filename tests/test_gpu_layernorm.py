@@ -152,6 +152,7 @@ def test_a_row_that_is_not_finite_stays_by_itself(cols):
     assert torch.equal(plan.forward(bad, None, None, torch.empty_like(x))[others], y[others])
     assert torch.equal(plan.grad(dy, bad, None, torch.empty_like(x), None, None)[0][others], dx[others])
     assert bool(plan.forward(bad, None, None, torch.empty_like(x))[4].isnan().all())
+    assert bool(solo.SoloLayerNorm(21, cols, rms=True).forward(bad, None, None, torch.empty_like(x))[4].isnan().all())
 
 
 def test_fewer_rows_than_the_handle_has_room_for_and_none():

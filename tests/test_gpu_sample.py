@@ -113,7 +113,8 @@ def test_equal_logits_go_by_the_column():
     """n equal columns: the token is column floor(u n) of those that are kept, exactly."""
     for cols in (8, 1024, 1025, 4096, 65_536, 100_000):
         # (half of an odd number: the sum of (cols + 1) / 2 ones is the first that reaches it)
-        for kept, parameters in ((cols, {}), ((cols + 1) // 2, dict(top_p=0.5)), (cols // 4, dict(top_k=cols // 4)), (cols // 8, dict(top_k=cols // 4, top_p=0.5)), (1, dict(top_p=0.0))):
+        for kept, parameters in ((cols, {}), ((cols + 1) // 2, dict(top_p=0.5)), (cols // 4, dict(top_k=cols // 4)), (cols // 8, dict(top_k=cols // 4, top_p=0.5)), (1, dict(top_p=0.0)), (1, dict(top_k=1)), (1, dict(temperature=0.0)),
+                                 (cols, dict(min_p=1.0)), (cols // 2, dict(min_p=0.5, top_k=cols // 2))):
             u = torch.tensor([0.0, 0.25, 0.5, 0.75, 1 - 2.0 ** -24], device="cuda")
             x = torch.full((5, cols), -3.0, device="cuda")
             token, logprob = solo.SoloSampler(5, cols, **parameters).sample(x, u)
