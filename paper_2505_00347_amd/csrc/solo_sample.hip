@@ -588,9 +588,14 @@ __device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH, LONG> 
                 for (int e = 0; e < n; ++e) it[e] = weights(x[e]);
 #pragma unroll
                 for (int e = 0; e < n; ++e) asm volatile("" : "+v"(it[e].w));      // (all of them here, not each in front of its use)
+                if (all) {
+#pragma unroll
+                    for (int e = 0; e < n; ++e) atomicAdd((unsigned long long *)&lds.mass[it[e].template bucket<THREADS>()], (unsigned long long)it[e].w);
+                    return;
+                }
 #pragma unroll
                 for (int e = 0; e < n; ++e) {
-                    if (!all && !weights.counts(it[e])) continue;
+                    if (!weights.counts(it[e])) continue;
                     const uint32_t b = it[e].template bucket<THREADS>();
                     atomicAdd((unsigned long long *)&lds.mass[b], (unsigned long long)it[e].w);
                     if (counted) atomicAdd(&lds.count[b], 1u);
