@@ -31,7 +31,7 @@ namespace solo {
 template <int THREADS>
 struct Sizes {
     static constexpr bool kShort = THREADS == kLanes;
-    static constexpr uint32_t kBuckets = kShort ? 256 : 2048, kKept = kShort ? 256 : 2048, kListed = kShort ? 256 : 1024, kSub = kShort ? 64 : 512;
+    static constexpr uint32_t kBuckets = kShort ? 256 : THREADS == 256 ? 1024 : 2048, kKept = kShort ? 256 : THREADS == 256 ? 1024 : 2048, kListed = kShort ? 256 : 1024, kSub = kShort ? 64 : 512;
 };
 
 // 2^(i / 32)
