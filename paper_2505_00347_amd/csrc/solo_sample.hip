@@ -25,13 +25,15 @@
 namespace solo {
 
 // Buckets of the distance from the maximum, 64 binary orders of w in all; columns above a bound that are kept instead of the row; columns of a bucket that are
-// listed; parts that a list is cut into.  A row of one
-// wavefront has an eighth or a quarter of each: what it clears and adds up is most of its work, and what it has in LDS says how many rows a compute unit has
-// under way (100000 rows of 300 fp32: 163 us, with the others' sizes and 256 threads 1107).
+// listed; parts that a list is cut into.  What a row has in LDS says how many rows a compute unit has under way, and what it clears and adds up is much of a
+// short row's work: two workgroups of 512 threads, whose registers allow no more, five of 256 (5000 rows of 4000 bf16, nucleus: 56 us, with the long rows' sizes
+// 118) and twenty of one wavefront (100000 rows of 300 fp32: 150, with lists twice as long 160).  With half the buckets a long row's places take 4 to 7 % longer;
+// with half the list 1024 rows of 50257 bf16 of which min_p leaves up to 4000 columns take 75 us instead of 66.
 template <int THREADS>
 struct Sizes {
-    static constexpr bool kShort = THREADS == kLanes;
-    static constexpr uint32_t kBuckets = kShort ? 256 : THREADS == 256 ? 1024 : 2048, kKept = kShort ? 256 : THREADS == 256 ? 1024 : 2048, kListed = kShort ? 256 : 1024, kSub = kShort ? 64 : 512;
+    static constexpr bool kShort = THREADS == kLanes, kMiddle = THREADS == 256;
+    static constexpr uint32_t kBuckets = kShort ? 256 : kMiddle ? 512 : 2048, kKept = kShort ? 128 : kMiddle ? 1024 : 4096, kListed = kShort ? 128 : 1024,
+                              kSub = kShort ? 64 : 512;
 };
 
 // 2^(i / 32)
@@ -67,8 +69,6 @@ struct SampleLds {
                               kSub = Sizes<THREADS>::kSub;
     uint64_t mass[kBuckets + 1];       // sums of the buckets, then of all in front of a bucket
     uint32_t count[kBuckets + 1];
-    float x[kKept];                    // of the columns above a bound
-    uint32_t column[kKept];
     float sub_x[kListed];              // of those in a bucket
     uint32_t sub_column[kListed];
     float few_x[kLanes];               // of a part of those
@@ -83,6 +83,8 @@ struct SampleLds {
     uint32_t listed, bucket;
     uint64_t found_key, found_mass;
     double inverse, below, nucleus;    // of temperature; uniform and top_p, within their ends
+    float x[kKept];                    // of the columns above a bound (last: what lies beyond 64 KB costs address registers)
+    uint32_t column[kKept];
 };
 
 // threadIdx.x, as something that the compiler does not know: addresses made of it are made where they are used.  Made in front of the loop
@@ -713,12 +715,22 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(
     // The columns that are not below the bound, if they are few: kKept are kept instead of the row, 64 are put in order at once.
     uint32_t kept = 0;
     if (bound > -INFINITY) {
+        // (counted first: an atomic addition for each is waited for, and these may be many)
+        uint32_t own = 0;
+        columns.each([&](const float *x, auto n, uint32_t) {
+#pragma unroll
+            for (int e = 0; e < n; ++e) own += x[e] >= bound;
+        });
+        const uint32_t upto = running_sum(own);
+        uint32_t i = 0;
+        if (threadIdx.x % kLanes == kLanes - 1) i = atomicAdd(&lds.listed, upto);
+        i = (uint32_t)__builtin_amdgcn_readlane((int)i, kLanes - 1) + upto - own;
         columns.not_below(bound, [&](float x, uint32_t column) {
-            const uint32_t i = atomicAdd(&lds.listed, 1u);
             if (i < SampleLds<THREADS>::kKept) {
                 lds.x[i] = x;
                 lds.column[i] = column;
             }
+            ++i;
         });
         __syncthreads();
         kept = lds.listed;

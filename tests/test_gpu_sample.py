@@ -109,6 +109,18 @@ def test_flat_and_peaked_rows(dtype, spread, cols):
             check(x, uniform(12, 2), exact_sums=True, **{**parameters, "top_p": 0.5 if "top_p" in parameters else 1.0})
 
 
+@pytest.mark.parametrize("parameters", [{}, dict(top_p=0.9), dict(top_p=0.7, top_k=37), dict(top_k=3000)], ids=lambda p: "-".join("%s%g" % i for i in p.items()) or "min_p")
+@pytest.mark.parametrize("cols", [900, 6000, 30_000, 60_000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_numbers_of_columns_above_a_bound(dtype, cols, parameters):
+    """min_p keeps n columns of a row exactly, for n on both sides of what is put in order at once and of what a list holds."""
+    counts = torch.tensor([n for n in (1, 2, 63, 64, 65, 127, 128, 129, 512, 513, 1023, 1024, 1025, 2048, 2049, 4095, 4096, 4097, 20_000) if n <= cols], device="cuda")
+    place = torch.rand(len(counts), cols, generator=generator(70), device="cuda").argsort(1)
+    x = 2 * torch.rand(len(counts), cols, generator=generator(71), device="cuda") - 1      # (no w of these is below e^-2)
+    x = torch.where(place < counts[:, None], x, x - 20).to(dtype)
+    check(x, uniform(len(counts), 72), min_p=0.1, least_clear=0.9, **parameters)
+
+
 def test_equal_logits_go_by_the_column():
     """n equal columns: the token is column floor(u n) of those that are kept, exactly."""
     for cols in (8, 1024, 1025, 4096, 65_536, 100_000):
