@@ -758,19 +758,22 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(
 }
 
 // ---- host ------------------------------------------------------------------------------------
-// The fewest threads that hold the row, by groups of 16 bytes, without many a thread; more where there are fewer rows than compute units and it is one row's time
-// that counts.  (One row of 4000 bf16: 256 threads 11 us, 64 21; 5000 rows of 1900 fp32: 256 threads 79, 64 38, and 300 of them 13 and 21; 1024 rows of 16000
-// fp32: 512 threads with eight groups 33, with sixteen 36, 1024 threads 46; 1024 of 50257 bf16: 512 threads 102, 1024 128.)
+// The fewest threads that hold the row, by groups of 16 bytes, without many a thread; more where there are fewer rows than the card takes side by side and it is one
+// row's time that counts.  (Nucleus: 20000 rows of 1000 fp32, 256 threads 123 us, 64 61, and 1000 of them 11 and 14; 5000 of 1900 fp32 43 and 36, 1200 of them 14
+// and 21.  4000 rows of 16000 fp32: 512 threads 129, 256 with sixteen groups 110, 1200 of 12000 42 and 42; of bf16, twice the columns a group, 2000 of 32000 111 and 114.
+// 1024 rows of 50257 bf16: 512 threads 102, 1024 128.)
 template <bool BF16>
 static int sample_launch(const SampleArgs &a, hipStream_t stream)
 {
     const uint32_t across = (uint32_t)(a.rows < (1u << 20) ? a.rows : 1u << 20);
     const dim3 grid(across, (uint32_t)((a.rows + across - 1) / across));
     const uint32_t quads = (a.cols + (BF16 ? 7 : 3)) / (BF16 ? 8 : 4);
-    if (quads <= 64 * 4) return launch(sample_kernel<BF16, 64, 4, false>, grid, 64, stream, a);
-    if (!BF16 && quads <= 64 * 8 && a.rows > 1024) return launch(sample_kernel<false, 64, 8, false>, grid, 64, stream, a);
+    const bool many = a.rows > 2048;
+    if (quads <= 64 * 2 || (quads <= 64 * 4 && many)) return launch(sample_kernel<BF16, 64, 4, false>, grid, 64, stream, a);
+    if (!BF16 && quads <= 64 * 8 && many) return launch(sample_kernel<false, 64, 8, false>, grid, 64, stream, a);
     if (quads <= 256 * 4) return launch(sample_kernel<BF16, 256, 4, false>, grid, 256, stream, a);
     if (quads <= 256 * 8) return launch(sample_kernel<BF16, 256, 8, false>, grid, 256, stream, a);
+    if (!BF16 && quads <= 256 * 16 && a.rows >= 1024) return launch(sample_kernel<false, 256, 16, false>, grid, 256, stream, a);
     if (quads <= 512 * 8 && a.rows > 256) return launch(sample_kernel<BF16, 512, 8, false>, grid, 512, stream, a);
     if (quads <= 512 * 16 && a.rows > 256) return launch(sample_kernel<BF16, 512, 16, false>, grid, 512, stream, a);
     if (quads <= 1024 * 8) return launch(sample_kernel<BF16, 1024, 8, false>, grid, 1024, stream, a);

@@ -72,7 +72,7 @@ def uniform(rows, seed):
 
 SHAPES = [(1, 1, 0), (9, 2, 0), (50, 7, 1), (300, 100, 0), (64, 1000, 3), (1100, 1500, 0), (20, 4096, 0), (9, 8192, 0), (9, 8193, 1), (9, 16_390, 0), (300, 15_000, 0),
           (300, 20_000, 0), (270, 33_000, 0), (20, 15_000, 0), (3, 25_000, 0), (6, 32_000, 0), (5, 50_257, 47),
-          (3, 65_540, 0), (2, 150_001, 0)]
+          (3, 65_540, 0), (2, 150_001, 0), (2100, 700, 0), (2100, 1500, 1), (1030, 13_000, 0)]
 
 PARAMETERS = [dict(), dict(temperature=0.0), dict(temperature=0.7, top_p=0.9), dict(top_k=1), dict(top_k=40), dict(top_k=1500, temperature=1.5), dict(min_p=0.05),
               dict(top_k=50, top_p=0.8, min_p=0.01, temperature=1.3), dict(top_p=0.3, min_p=0.2), dict(top_k=7, min_p=1.0)]
