@@ -6,17 +6,17 @@
 //
 // Each of the three is a place in the order at which a running sum (of ones or of w) reaches a goal, and none needs the order itself: a
 // histogram over the distance from the maximum gives the bucket that holds the place, and only that bucket's columns are looked at
-// again, each against all others of them.  A bucket with too many (equal logits, mostly) is cut further by whole keys, value and column, until
-// it has few.  Where top_k or min_p leave few columns, which a bound on their logits shows beforehand, only these are weighed and put in order.
+// again: up to 64 by one wavefront, each against all others; more are listed and cut by whole keys, value and column, until the part that holds the place
+// has no more than 64; more than the list holds (equal logits, mostly) are cut that way from the row itself.  Where top_k or min_p leave few columns, which a bound on their logits shows beforehand, only these are weighed and put in order.
 //
 // Which column it is hangs on comparisons of sums, so these are exact: w is computed in binary64 (the rate of its instructions is that of
 // binary32), to 2e-13, and rounded to a whole multiple of 2^-shift; sums of such are whole numbers below 2^63, the same in every order, and atomic
 // additions in LDS make them.
 //
-// A workgroup takes a row.  One row of 50257 fp32, nucleus of 0.95, 22 us: 3 until the maximum is known, 9.5 for weights and buckets (28 cycles for 64 of them: twenty
-// vector instructions on each of four SIMDs, and the additions in LDS), 1 to add up, 3.5 for each of two places, most of it the pass over the row.  One after
-// the other, without the next one's chain of instructions beside its own, the weights took 13.  1024 x 32000 fp32, the whole distribution, 55 us (2.4 TB/s, and two
-// thirds of the vector issue); 1024 x 50257 bf16 with min_p and nucleus 71 us, where the rows with many columns above the bound come last.
+// A workgroup takes a row.  One row of 50257 fp32, nucleus of 0.95, 20 us: 3 until the maximum is known, 8.5 for weights and buckets (25 vector instructions for 64
+// columns on each of four SIMDs), 1 to add up, 3.5 for each of two places, most of it the pass over the row.  One after the other, without the next one's chain of
+// instructions beside its own, the weights took 13.  1024 x 32000 fp32, the whole distribution, 50 us: 2.6 TB/s, vector instructions and loads about half of it each,
+// side by side only where two rows of a compute unit are at different stages.  1024 x 50257 bf16 with min_p and nucleus 66 us.
 #include "solo_rows.h"
 
 #include <float.h>
