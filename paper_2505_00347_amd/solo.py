@@ -472,13 +472,13 @@ def _on(device, *tensors):
 class _Handle:
     """Device and streams of a handle.  A call takes tensors of the handle's device, which has to be torch's current one.
 
-    Its buffers are made on torch's current stream, and a call may run on another one (`stream`, or what is
+    Its buffers are made on torch's current stream (a workspace in the first call that needs it), and a call may run on another one (`stream`, or what is
     current then).  The first call on such a stream waits for what was enqueued on the current stream when the buffers were made (a
     new buffer may be memory that earlier work still uses), and the allocator learns that this stream uses them.  The calls of
     a handle follow each other, each with the buffers that the one before has left: on several streams the caller orders them, and of
     calls on a stream that is not torch's (a bare number, another library's object) it keeps the handle until they are done."""
 
-    _buffers, _home = (), None
+    _held = None, (), None
 
     def __init__(self, device):
         lib()
@@ -488,21 +488,33 @@ class _Handle:
         self._index = self.device.index if self.device.type == "cuda" else None
 
     def _hold(self, *buffers):
-        self._others, self._home, self._ready = {}, None, None
+        """Buffers that have just been made, in the place of those before."""
+        self._held = self._made(*buffers)
+
+    def _hold_more(self, *buffers):
+        """The same beside those before, which may be another stream's."""
+        self._held = self._made(*buffers, before=self._held[1])
+
+    def _made(self, *buffers, before=()):
+        home = ready = None
         if self._index is not None:
             stream = _torch.cuda.current_stream(self.device)
-            self._home = stream.cuda_stream
+            home = stream.cuda_stream
             if not _torch.cuda.is_current_stream_capturing():
-                self._ready = stream.record_event()
-        self._buffers = [b for b in buffers if b is not None]          # (last: a lookup of another thread finds all of it or none)
+                ready = stream.record_event()
+        made = *before, (home, ready, [b for b in buffers if b is not None])
+        # the stream that is home to all, the buffers by the stream that made them, and the streams that have been told of them (as one: a lookup
+        # of another thread finds all of it or none)
+        return home if all(h == home for h, _, _ in made) else None, made, {}
 
     def _on_stream(self, stream):
         """The number of the stream that a call runs on, ready for the buffers."""
         if self._index is None or _device_now() != self._index:
             raise ValueError(f"a call runs on the GPU that is torch's current device, this handle is on {self.device}")
         number = _stream_now(self._index) if stream is None else stream if isinstance(stream, int) else self._number_of(stream)
-        if number != self._home and self._buffers and number not in self._others:
-            self._visit(stream, number)
+        home, made, others = self._held
+        if number != home and made and number not in others:
+            self._visit(stream, number, made, others)
         return number
 
     def _number_of(self, stream):
@@ -511,7 +523,7 @@ class _Handle:
         number = stream.cuda_stream
         return getattr(number, "value", number) or 0       # (one of ctypes; None: the default stream)
 
-    def _visit(self, stream, number):
+    def _visit(self, stream, number, made, others):
         foreign = not (stream is None or isinstance(stream, _torch.cuda.Stream))
         if foreign:
             stream = _torch.cuda.ExternalStream(number)
@@ -520,13 +532,16 @@ class _Handle:
         with _torch.cuda.stream(stream):
             if _torch.cuda.is_current_stream_capturing():  # (a graph's nodes wait for nothing outside; capturing begins on an idle GPU)
                 return
-        if self._ready is not None:
-            stream.wait_event(self._ready)
-        if foreign:                                        # (there may be another stream of this number later, or none)
-            return
-        for b in self._buffers:
-            b.record_stream(stream)
-        self._others[number] = stream
+        for home, ready, buffers in made:
+            if home == number:
+                continue
+            if ready is not None:
+                stream.wait_event(ready)
+            if not foreign:                                # (there may be another stream of this number later, or none)
+                for b in buffers:
+                    b.record_stream(stream)
+        if not foreign:
+            others[number] = stream
 
 
 class SoloGradNorm(_Handle):
@@ -789,7 +804,7 @@ class SoloLayerNorm(_Handle):
             raise ValueError(f"grad() takes what forward() left on the same rows: {shape.rows} expected, got {rows}")
         if self.workspace is None:
             self.workspace = _torch.empty(self.workspace_bytes, dtype=_torch.uint8, device=self.device)
-            self._hold(self.stats, self.workspace)
+            self._hold_more(self.workspace)
         _operation("solo_layernorm_grad", True, grad_out, x, weight, self.stats, grad_x, grad_weight, grad_bias, self.workspace, self.workspace_bytes,
                    C.addressof(shape), self._on_stream(stream))
         return grad_x, grad_weight, grad_bias
