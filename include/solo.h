@@ -408,7 +408,8 @@ int solo_layernorm_grad(const void *grad_y, const void *x, const void *weight, c
  *
  *   loss = sum p_k (ln p_k - ln q_(t_k)) + r (ln r - ln q_r)            (terms with p_k = 0 or r = 0 are 0)
  *   stats [rows, 3]: what solo_distill_grad takes: the row's largest logit, and the sums of e^z relative to it, of all columns and of
- *            those that are not among the t_k
+ *            those that are not among the t_k.  Where the latter is below 2^-64 and r > 0, another three: the largest logit of those columns,
+ *            the sum of all columns negated, and that of those columns relative to their own largest logit
  *
  * and with d loss / d z times scale, for a = grad_loss of the row and T = sum p_k + r:
  *
@@ -419,7 +420,7 @@ int solo_layernorm_grad(const void *grad_y, const void *x, const void *weight, c
  * column may occur more than once.  A row without alternatives is not read (a padding position): loss and gradient are 0.  Where the student
  * gives no probability to an alternative that has some (-inf), the loss is +inf and the gradient the formula's; in a row of -inf alone the loss is +inf, the gradient 0.  A NaN or
  * +inf among the logits or values of a row makes its results NaN or unspecified, no other row's.  q_r is summed by itself, not taken from 1.  Sums
- * are binary32 and relative to the row's largest logit (1 - sum p_k: binary64).  solo_distill_with_grad does both for weights that are known beforehand,
+ * are binary32 and relative to the row's largest logit, q_r's to that of its columns where the two lie far apart (1 - sum p_k: binary64).  solo_distill_with_grad does both for weights that are known beforehand,
  * reading the logits from HBM once. */
 #define SOLO_DISTILL_REST 1u
 #define SOLO_DISTILL_MAX 128

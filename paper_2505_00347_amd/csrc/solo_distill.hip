@@ -1,12 +1,13 @@
 // Distillation: the divergence of every row of a student's logits from a teacher of which a few alternatives are known, and the gradient.
 //
-//   e_j = e^(s (x_j - max x)),  S = sum_j e_j,  q_j = e_j / S;   the teacher's p_k at columns c_k, and what they leave of 1, r
-//   R = sum of e_j over the columns that are not among the c_k
-//   loss = sum_k p_k (ln p_k - ln q_(c_k)) + r (ln r - ln (R / S))
-//   dx_j = s a (e_j T / S - sum over k with c_k = j of p_k)  among the c_k,   s a e_j (T / S - r / R)  elsewhere,   T = sum_k p_k + r
+//   e_j = e^(s (x_j - m)),  m = max x,  S = sum_j e_j,  q_j = e_j / S;   the teacher's p_k at columns c_k, and what they leave of 1, r
+//   of the columns that are not among the c_k:  f_j = e^(s (x_j - o)),  R = sum of f_j;   g = e^(s (o - m)), so that e_j = g f_j
+//   loss = sum_k p_k (ln p_k - ln q_(c_k)) + r (ln r - (s (o - m) + ln R - ln S))
+//   dx_j = s a (e_j T / S - sum over k with c_k = j of p_k)  among the c_k,   s a f_j (g T / S - r / R)  elsewhere,   T = sum_k p_k + r
 //
 // (r is 0 where the p_k are brought to a sum of 1.)  R is summed by itself: as 1 minus the rest of the q it would have no digits left in a
-// student that is sure of an alternative.  So the columns c_k are taken out in front of the sums.  One wavefront reads the teacher's row while
+// student that is sure of an alternative.  So the columns c_k are taken out in front of the sums.  o is m, or, where R would be below 2^-64, the largest logit
+// of those columns: beside an alternative that leads by 88 / s their e_j are 0 in binary32, their shares f_j / R of what the teacher leaves are not.  One wavefront reads the teacher's row while
 // the logits are on their way and hangs every alternative into a list of the thread that has its column; a thread knows by one bit for each of its
 // groups whether it has any there.  The gradient is written as if there were none; then the threads write those of their alternatives over it.
 //
@@ -26,6 +27,7 @@ namespace solo {
 constexpr int kMostTop = SOLO_DISTILL_MAX;
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 constexpr double kNoRest = 1.0 / (1 << 20);    // what is left of 1 below this is the probabilities' rounding
+constexpr float kSmallRest = 0x1p-64f;         // R below this, relative to the row's largest: its smallest terms may be 0, and so may soon all of it
 
 struct DistillArgs {
     const void *logits, *value, *token;
@@ -212,12 +214,33 @@ __device__ __forceinline__ void take_out(Quad &quad, uint32_t g, TeacherLds<THRE
     }
 }
 
-struct RowSums { float at, all, rest; };       // the largest logit, S and R
+struct RowSums { float at, rest_at, all, rest; };          // m, o, S and R
+struct OwnSum { float at, s; };                            // a thread's largest logit of the rest and its sum relative to it
+
+// The sum of all threads' relative to the largest of all, from wavefronts' sums relative to theirs.
+template <int THREADS>
+__device__ __forceinline__ float join_waves(float wave_at, float wave_s, float k, TeacherLds<THREADS> &lds, float &all_at)
+{
+    constexpr int kWaves = THREADS / kLanes;
+    if (threadIdx.x % kLanes == 0) {
+        lds.at[threadIdx.x / kLanes] = wave_at;
+        lds.s[threadIdx.x / kLanes] = wave_s;
+    }
+    __syncthreads();
+    all_at = wave_at;
+    if (kWaves > 1) {
+        const int part = threadIdx.x % kWaves;
+        const float part_at = lds.at[part];
+        all_at = wave_max<kWaves>(part_at);
+        wave_s = wave_sum<kWaves>(lds.s[part] * __builtin_amdgcn_exp2f((part_at - all_at) * k));
+    }
+    return wave_s;
+}
 
 // The sums of a row, for every thread; the alternatives' logits go to lds.  `q`, `last`: as for the sums of the log probabilities.
 template <bool BF16, bool RESIDENT, bool PAST, int THREADS, int DEPTH>
 __device__ __forceinline__ RowSums student_sums(const Row<BF16> &row, float k, TeacherLds<THREADS> &lds, Quad q[DEPTH], float last, uint32_t top,
-                                                uint32_t mask, uint32_t at_last)
+                                                uint32_t mask, uint32_t at_last, OwnSum &own)
 {
     constexpr int kPer = Row<BF16>::kPer;
     float at = -FLT_MAX, s = 0.0f, most = -FLT_MAX;        // the largest logit of the rest and its sum relative to it; the alternatives' largest
@@ -258,23 +281,13 @@ __device__ __forceinline__ RowSums student_sums(const Row<BF16> &row, float k, T
             s += __builtin_amdgcn_exp2f((last - at) * k);
         }
     }
+    own = OwnSum{at, s};
     // (an alternative that is NaN shows in its own term below)
     const float wave_at = wave_max(fmaxf(at, most));
     rebase(wave_at);
-    s = wave_sum(s);
-    constexpr int kWaves = THREADS / kLanes;
-    RowSums sums = {wave_at, 0.0f, s};
-    if (threadIdx.x % kLanes == 0) {
-        lds.at[threadIdx.x / kLanes] = wave_at;
-        lds.s[threadIdx.x / kLanes] = s;
-    }
-    __syncthreads();
-    if (kWaves > 1) {
-        const int part = threadIdx.x % kWaves;
-        const float part_at = lds.at[part];
-        sums.at = wave_max<kWaves>(part_at);
-        sums.rest = wave_sum<kWaves>(lds.s[part] * __builtin_amdgcn_exp2f((part_at - sums.at) * k));
-    }
+    RowSums sums;
+    sums.rest = join_waves<THREADS>(wave_at, wave_sum(s), k, lds, sums.at);
+    sums.rest_at = sums.at;
     float among = 0.0f;
     for (uint32_t i = threadIdx.x % kLanes; i < top; i += kLanes)
         if (lds.column[i] != kNone) among += __builtin_amdgcn_exp2f((lds.logit[i] - sums.at) * k);
@@ -282,29 +295,44 @@ __device__ __forceinline__ RowSums student_sums(const Row<BF16> &row, float k, T
     return sums;
 }
 
-// By the first wavefront, behind the sums: the row's loss, for each of its lanes.
+// The rest once more, relative to its own largest.
 template <int THREADS>
-__device__ __forceinline__ float row_loss(const RowSums &sums, const TeacherLds<THREADS> &lds, uint32_t top, float scale)
+__device__ __forceinline__ void rest_by_itself(RowSums &sums, const OwnSum &own, float k, TeacherLds<THREADS> &lds)
+{
+    const float rest_at = wave_max(own.at);
+    __syncthreads();                                       // (lds.at and lds.s have been read)
+    sums.rest = join_waves<THREADS>(rest_at, wave_sum(own.s * __builtin_amdgcn_exp2f((own.at - rest_at) * k)), k, lds, sums.rest_at);
+}
+
+// By the first wavefront, behind the sums: the row's loss and, if asked for, stats.  APART: o is not m.
+template <bool APART, int THREADS>
+__device__ __forceinline__ void put_loss(const DistillArgs &a, uint64_t r, const RowSums &sums, const TeacherLds<THREADS> &lds)
 {
     const float log_s = __builtin_amdgcn_logf(sums.all) * kLn2;
     float loss = 0.0f;
-    for (uint32_t i = threadIdx.x; i < top; i += kLanes) {
+    for (uint32_t i = threadIdx.x; i < a.top; i += kLanes) {
         const float p = lds.p[i];
-        if (!(p <= 0.0f)) loss = fmaf(p, lds.log_p[i] - fmaf(lds.logit[lds.same[i]] - sums.at, scale, -log_s), loss);
+        if (!(p <= 0.0f)) loss = fmaf(p, lds.log_p[i] - fmaf(lds.logit[lds.same[i]] - sums.at, a.scale, -log_s), loss);
     }
     loss = wave_sum(loss);
-    if (lds.left > 0.0f) loss = fmaf(lds.left, (__builtin_amdgcn_logf(lds.left) - __builtin_amdgcn_logf(sums.rest)) * kLn2 + log_s, loss);
-    return sums.all == 0.0f ? INFINITY : loss;
+    if (lds.left > 0.0f)
+        loss = fmaf(lds.left, (__builtin_amdgcn_logf(lds.left) - __builtin_amdgcn_logf(sums.rest)) * kLn2 + (APART ? fmaf(sums.at - sums.rest_at, a.scale, log_s) : log_s),
+                    loss);
+    if (threadIdx.x == 0) {
+        if (a.loss) a.loss[r] = sums.all == 0.0f ? INFINITY : loss;
+        if (a.stats) { a.stats[3 * r] = sums.rest_at; a.stats[3 * r + 1] = APART ? -sums.all : sums.all; a.stats[3 * r + 2] = sums.rest; }
+    }
 }
 
-// What the gradient of a row needs: dx_j = (e_j rest) factor, or (e_j all - p) factor at an alternative.
-struct DistillSlope { float at, all, rest, factor; };
+// What the gradient of a row needs: dx_j = (f_j rest) factor, or (e_j all - p) factor at an alternative.
+struct DistillSlope { float at, rest_at, all, rest, factor; };
 
-__device__ __forceinline__ DistillSlope distill_slope(const RowSums &sums, float total, float left, float factor)
+// `lowered`: g.
+__device__ __forceinline__ DistillSlope distill_slope(const RowSums &sums, float lowered, float total, float left, float factor)
 {
     // (no column of a student's row without probabilities has a gradient)
-    const float all = sums.all == 0.0f ? 0.0f : total / sums.all, rest = sums.rest == 0.0f ? 0.0f : all - left / sums.rest;
-    return DistillSlope{sums.at, all, rest, sums.all == 0.0f ? 0.0f : factor};
+    const float all = sums.all == 0.0f ? 0.0f : total / sums.all, rest = sums.rest == 0.0f ? 0.0f : fmaf(all, lowered, -(left / sums.rest));
+    return DistillSlope{sums.at, sums.rest_at, all, rest, sums.all == 0.0f ? 0.0f : factor};
 }
 
 // Wavefronts per SIMD that the registers have to leave room for: two workgroups of 1024 threads, so that one loads while the other computes, where 64
@@ -344,24 +372,35 @@ __global__ __launch_bounds__(THREADS, distill_waves(FORWARD, GRAD, RESIDENT, DEP
         return;
     }
     RowSums sums;
+    float lowered = 1.0f;
     if (FORWARD) {
         uint32_t at_last;
+        OwnSum own;
         const uint32_t mask = own_alternatives<BF16, THREADS>(row, lds, at_last);
-        sums = student_sums<BF16, RESIDENT, (PAST > 1), THREADS, DEPTH>(row, k, lds, raw, last, a.top, mask, at_last);
-        if (threadIdx.x < kLanes) {
-            const float loss = row_loss<THREADS>(sums, lds, a.top, a.scale);
-            if (threadIdx.x == 0) {
-                if (a.loss) a.loss[r] = loss;
-                if (a.stats) { a.stats[3 * r] = sums.at; a.stats[3 * r + 1] = sums.all; a.stats[3 * r + 2] = sums.rest; }
-            }
+        sums = student_sums<BF16, RESIDENT, (PAST > 1), THREADS, DEPTH>(row, k, lds, raw, last, a.top, mask, at_last, own);
+        if (threadIdx.x < kLanes) put_loss<false, THREADS>(a, r, sums, lds);
+        // Seldom.  (The sum is bit by bit the same in all threads, so all of them come here or none; it is not below +0, and its bits are in the order of its value.)
+        if (scalar(__float_as_uint(sums.rest)) < __float_as_uint(kSmallRest) && scalar(lds.left) > 0.0f) {
+            rest_by_itself<THREADS>(sums, own, k, lds);
+            if (threadIdx.x < kLanes && sums.rest != 0.0f) put_loss<true, THREADS>(a, r, sums, lds);
+            lowered = scalar(__builtin_amdgcn_exp2f((sums.rest_at - sums.at) * k));
         }
     } else {
-        sums = RowSums{a.stats[3 * r], a.stats[3 * r + 1], a.stats[3 * r + 2]};
+        sums = RowSums{a.stats[3 * r], a.stats[3 * r], a.stats[3 * r + 1], a.stats[3 * r + 2]};
         // (the gradient may be written over them)
         for (uint32_t i = lds.head[threadIdx.x]; i != kNone; i = lds.next[i]) lds.logit[i] = row.one(lds.column[i]);
+        if (scalar(sums.all) < 0.0f) {                     // (an alternative is the row's largest)
+            __syncthreads();
+            float at = -FLT_MAX;
+            for (uint32_t i = threadIdx.x % kLanes; i < a.top; i += kLanes)
+                if (lds.column[i] != kNone) at = fmaxf(at, lds.logit[i]);
+            sums.at = wave_max(at);
+            sums.all = -sums.all;
+            lowered = scalar(__builtin_amdgcn_exp2f((sums.rest_at - sums.at) * k));
+        }
     }
     if (!GRAD) return;
-    const DistillSlope slope = distill_slope(sums, lds.total, lds.left, a.scale * a.grad_loss[r]);
+    const DistillSlope slope = distill_slope(sums, lowered, lds.total, lds.left, a.scale * a.grad_loss[r]);
     for (uint32_t g0 = threadIdx.x; g0 < row.groups; g0 += THREADS * DEPTH) {
         if (!(FORWARD && RESIDENT)) {
 #pragma unroll
@@ -376,14 +415,14 @@ __global__ __launch_bounds__(THREADS, distill_waves(FORWARD, GRAD, RESIDENT, DEP
                 float x[kPer];
                 Lane16<BF16>::unpack(raw[j], x);
 #pragma unroll
-                for (int e = 0; e < kPer; ++e) x[e] = __builtin_amdgcn_exp2f((x[e] - slope.at) * k) * slope.rest * slope.factor;
+                for (int e = 0; e < kPer; ++e) x[e] = __builtin_amdgcn_exp2f((x[e] - slope.rest_at) * k) * slope.rest * slope.factor;
                 Lane16<BF16>::template store_near<(PAST > 0)>(out, (g0 + j * THREADS) * kPer, x);
             }
         if (FORWARD && RESIDENT) break;
     }
     if (threadIdx.x < row.rest)
-        Elements<BF16>::store1(out, row.last_column(threadIdx.x), __builtin_amdgcn_exp2f((last - slope.at) * k) * slope.rest * slope.factor);
-    // over what the same thread has just written
+        Elements<BF16>::store1(out, row.last_column(threadIdx.x), __builtin_amdgcn_exp2f((last - slope.rest_at) * k) * slope.rest * slope.factor);
+    // over what the same thread has just written (of an alternative's logit, where the row has been read again, anything)
     for (uint32_t i = lds.head[threadIdx.x]; i != kNone; i = lds.next[i])
         Elements<BF16>::store1(out, lds.column[i], fmaf(__builtin_amdgcn_exp2f((lds.logit[i] - slope.at) * k), slope.all, -lds.all_p[i]) * slope.factor);
 }

@@ -128,6 +128,19 @@ struct Lane16 {
 // From here on the compiler does not know what `q` holds.
 __device__ __forceinline__ void forget(Quad &q) { asm volatile("" : "+v"(q)); }
 
+// A value that is the same in all lanes, in scalar registers.
+template <typename T>
+__device__ __forceinline__ T scalar(T x)
+{
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+    } else {
+        const uint64_t bits = __builtin_bit_cast(uint64_t, x);
+        const uint32_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)bits), high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(bits >> 32));
+        return __builtin_bit_cast(T, (uint64_t)high << 32 | low);
+    }
+}
+
 // One step of a reduction: the values of the lanes of groups of D, which are all alike in a group, and of the neighbouring
 // groups of D.  By the data paths of the vector unit: through LDS a step takes several times as long.
 template <int D>

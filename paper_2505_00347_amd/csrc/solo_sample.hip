@@ -96,19 +96,6 @@ __device__ __forceinline__ uint32_t this_thread()
     return thread;
 }
 
-// A value that is the same in all lanes, in scalar registers.
-template <typename T>
-__device__ __forceinline__ T scalar(T x)
-{
-    if constexpr (sizeof(T) == 4) {
-        return __builtin_bit_cast(T, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
-    } else {
-        const uint64_t bits = __builtin_bit_cast(uint64_t, x);
-        const uint32_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)bits), high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(bits >> 32));
-        return __builtin_bit_cast(T, (uint64_t)high << 32 | low);
-    }
-}
-
 // w as a whole number of 2^-shift, its logarithm, and how far that lies below 0, in eighths of a 32nd (64 orders for all below).
 struct Weight {
     uint64_t w;
