@@ -458,7 +458,7 @@ int solo_distill_with_grad(const void *logits, const void *teacher_value, const 
  *   token = the first column, in that order, at which the running sum of the kept w exceeds u times their sum
  *   logprob = ln of the token's share of the kept w
  *
- * temperature 0: the largest logit's column (lowest of several), logprob 0.  top_k <= 0, top_p >= 1, min_p <= 0: no limit by it.  A
+ * temperature 0, or min_p above 1: the largest logit's column (lowest of several), logprob 0.  top_k <= 0, top_p >= 1, min_p <= 0: no limit by it.  A
  * logit of -inf is never chosen; in a row that has no other the token is -1 and logprob -inf.  A row with a NaN or +inf among its
  * logits, or with a NaN or a negative temperature among its parameters, gives -1 and NaN.
  * Weights are computed in binary64 and summed exactly as whole multiples of 2^-(62 - log2 cols) (2^-51 at most) of the largest, so the token is

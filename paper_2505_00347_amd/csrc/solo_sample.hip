@@ -673,7 +673,8 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(
     if (!(most < INFINITY) || !(own_temperature >= 0.0f) || top_p != top_p || min_p != min_p || uniform != uniform) return put(-1, NAN);
     if (most == -INFINITY) return put(-1, -INFINITY);
 
-    const uint32_t top_k = own_temperature == 0.0f ? 1 : own_top_k > 0 ? (uint32_t)own_top_k : a.cols;
+    // (a min_p above every w leaves the one column that is kept at least)
+    const uint32_t top_k = own_temperature == 0.0f || min_p > 1.0f ? 1 : own_top_k > 0 ? (uint32_t)own_top_k : a.cols;
     Weights weights;
     weights.max = scalar((double)most);
     weights.per_order = scalar(lds.inverse * 1.4426950408889634);

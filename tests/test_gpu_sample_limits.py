@@ -1,0 +1,34 @@
+"""Sampling at the ends of what its parameters and shapes allow."""
+import math
+
+import pytest
+import torch
+
+from paper_2505_00347_amd import solo
+from test_gpu_operators import TYPES, generator, randn
+
+pytestmark = pytest.mark.gpu
+
+
+def uniform(rows, seed):
+    return torch.rand(rows, generator=generator(seed), device="cuda")
+
+
+@pytest.mark.parametrize("min_p", [1.0 + 2.0 ** -23, 1.5, 3e38, math.inf])
+@pytest.mark.parametrize("rows,cols", [(9, 2), (40, 300), (9, 4000), (9, 9000), (300, 20_000), (9, 50_257), (3, 150_000)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_floor_above_every_weight_keeps_the_first_column(dtype, rows, cols, min_p):
+    """No column has a weight of more than 1, and one is kept at least: of several largest logits the lowest column, whatever the other parameters say."""
+    x = randn((rows, cols), dtype, 1)
+    x[::2] = x[::2].clamp(max=0.0)                         # (half of such a row is its largest)
+    x[1] = 2.0
+    want = x.double().eq(x.double().amax(1, keepdim=True)).int().argmax(1)
+    for other in (dict(), dict(top_p=0.9), dict(top_k=5), dict(temperature=2.0, top_p=0.5, top_k=100), dict(temperature=0.0)):
+        token, logprob = solo.SoloSampler(rows, cols, min_p=min_p, **other).sample(x, uniform(rows, 2))
+        assert torch.equal(token, want) and not bool(logprob.any()), other
+    floors = torch.where(torch.arange(rows, device="cuda") % 3 == 0, min_p, 1.0)
+    token, logprob = solo.SoloSampler(rows, cols).sample(x, uniform(rows, 2), min_p=floors)
+    assert torch.equal(token[::3], want[::3]) and not bool(logprob[::3].any())
+    # a floor of 1 keeps all of the largest
+    ties = x.double().eq(x.double().amax(1, keepdim=True)).sum(1)
+    assert torch.allclose(logprob.double(), torch.where(floors > 1, 0.0, -ties.double().log()), atol=0, rtol=2.0 ** -23)
