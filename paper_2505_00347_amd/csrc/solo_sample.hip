@@ -665,7 +665,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(
         lds.listed = 0;
         // (temperature 0: the first of the largest)
         lds.inverse = own_temperature == 0.0f ? 1.0 : 1.0 / (double)own_temperature;
-        lds.below = uniform > 0.0f ? fmin((double)uniform, 2.0) : 0.0;
+        lds.below = uniform > 0.0f ? fmin((double)uniform, 0x1.fffffep-1) : 0.0;       // (the number next to 1)
         lds.nucleus = fmax((double)top_p, 0.0);
     }
     clear_buckets<THREADS>(lds);

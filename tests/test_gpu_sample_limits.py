@@ -32,3 +32,20 @@ def test_a_floor_above_every_weight_keeps_the_first_column(dtype, rows, cols, mi
     # a floor of 1 keeps all of the largest
     ties = x.double().eq(x.double().amax(1, keepdim=True)).sum(1)
     assert torch.allclose(logprob.double(), torch.where(floors > 1, 0.0, -ties.double().log()), atol=0, rtol=2.0 ** -23)
+
+
+@pytest.mark.parametrize("rows,cols", [(9, 2), (40, 300), (9, 4000), (9, 9000), (300, 20_000), (9, 50_257), (3, 150_000)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_numbers_from_1_on_count_as_the_one_next_to_1(dtype, rows, cols):
+    """Not as a way to the least likely column of all: its share may be far below 2^-24."""
+    x = randn((rows, cols), dtype, 1, 3.0) - 40.0
+    x[:, cols // 2] = 2.0
+    x[1] = 1.0
+    last = torch.full((rows,), 1 - 2.0 ** -24, device="cuda")
+    for parameters in (dict(), dict(top_p=0.9), dict(top_k=40), dict(top_k=2000), dict(min_p=1e-30), dict(temperature=0.3)):
+        plan = solo.SoloSampler(rows, cols, **parameters)
+        token, logprob = (t.clone() for t in plan.sample(x, last))
+        for beyond in (1.0, 1.5, 2.0, 1e30, math.inf):
+            got = plan.sample(x, torch.full_like(last, beyond))
+            assert torch.equal(got[0], token) and torch.equal(got[1], logprob), (parameters, beyond)
+        assert token[0].item() == cols // 2
