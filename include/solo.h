@@ -461,8 +461,11 @@ int solo_distill_with_grad(const void *logits, const void *teacher_value, const 
  * temperature 0, or min_p above 1: the largest logit's column (lowest of several), logprob 0.  top_k <= 0, top_p >= 1, min_p <= 0: no limit by it.  A
  * logit of -inf is never chosen; in a row that has no other the token is -1 and logprob -inf.  A row with a NaN or +inf among its
  * logits, or with a NaN or a negative temperature among its parameters, gives -1 and NaN.
- * Weights are computed in binary64 and summed exactly as whole multiples of 2^-(62 - log2 cols) (2^-51 at most) of the largest, so the token is
- * that of exact arithmetic unless u or a limit lies within some 1e-11 of a border; columns below half such a multiple are never chosen. */
+ * Weights are computed in binary64 (off by 2e-13 of themselves) and rounded to whole multiples of 2^-k of the largest, whose sums are exact in any order.  Up to 2^19
+ * columns k is 62 - log2 cols (rounded up), 51 at most: a sum is off by no more than cols 2^-(k + 1) of the largest weight, 3.6e-10 for 50257 columns and 2^-25 for
+ * 2^19.  In longer rows k follows the sum of the row's weights: off by no more than cols 2^-52 of the largest weight or cols 2^-61 of the sum, whichever is more
+ * (2^-23 for 2^29 columns).  The token is that of exact arithmetic unless u times the kept sum, or a limit, lies nearer than that to a border; columns below half
+ * a multiple are never chosen. */
 typedef struct solo_sample_shape {
     uint64_t rows, cols;        /* below 2^35 and 2^29                                           */
     uint64_t stride;            /* elements from row to row of logits, >= cols                   */

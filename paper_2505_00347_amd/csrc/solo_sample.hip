@@ -10,7 +10,7 @@
 // has no more than 64; more than the list holds (equal logits, mostly) are cut that way from the row itself.  Where top_k or min_p leave few columns, which a bound on their logits shows beforehand, only these are weighed and put in order.
 //
 // Which column it is hangs on comparisons of sums, so these are exact: w is computed in binary64 (the rate of its instructions is that of
-// binary32), to 2e-13, and rounded to a whole multiple of 2^-shift; sums of such are whole numbers below 2^63, the same in every order, and atomic
+// binary32), to 2e-13, and rounded to a whole multiple of 2^-shift of the largest; sums of such are whole numbers below 2^63, the same in every order, and atomic
 // additions in LDS make them.
 //
 // A workgroup takes a row.  One row of 50257 fp32, nucleus of 0.95, 20 us: 3 until the maximum is known, 8.5 for weights and buckets (25 vector instructions for 64
@@ -35,6 +35,10 @@ struct Sizes {
     static constexpr uint32_t kBuckets = kShort ? 256 : kMiddle ? 512 : 2048, kKept = kShort ? 128 : kMiddle ? 1024 : 4096, kListed = kShort ? 128 : 1024,
                               kSub = kShort ? 64 : 512;
 };
+
+// Up to this many columns their number says how fine weights can be, and a sum is off by 2^-25 of the largest weight at most: half of what a number of 24 bits
+// tells apart.  In longer rows it would be 2^-23, 2^-21 and so on; there their sum says it, which takes a pass more (four rows of 1000000 fp32, nucleus: 973 us, 897 without).
+constexpr uint32_t kCountedCols = 1u << 19;
 
 // 2^(i / 32)
 __constant__ const double kRoots[32] = {
@@ -634,6 +638,30 @@ __device__ __forceinline__ bool find_places(Columns<BF16, THREADS, DEPTH, LONG> 
     return true;
 }
 
+__device__ __forceinline__ void put_roots(Words *root, uint32_t shift)
+{
+    if (threadIdx.x < 32)
+        root[threadIdx.x] = __builtin_bit_cast(Words, __builtin_bit_cast(uint64_t, __builtin_amdgcn_ldexp(kRoots[threadIdx.x], (int)shift)) - ((uint64_t)threadIdx.x << 47));
+}
+
+// For a row whose sum of weights is far below the number of its columns: multiples of 2^-shift that are as fine as the sum allows.  The sum, of exponentials in
+// binary32, is off by less than a thousandth; with a sixteenth more it is below 2^bits, and so the sum of the whole numbers, each half of one more, below 2^62.
+template <int THREADS, typename Of>
+__device__ __forceinline__ uint32_t shift_of_sum(Of &columns, const Weights &weights, SampleLds<THREADS> &lds)
+{
+    double sum = 0.0;
+    columns.each([&](const float *x, auto n, uint32_t) {
+#pragma unroll
+        for (int e = 0; e < n; ++e) sum += (double)__builtin_amdgcn_exp2f((float)fmax(((double)x[e] - weights.max) * weights.per_order, -200.0));
+    });
+    sum = wave_sum(sum);
+    if (threadIdx.x % kLanes == 0) lds.wave_mass[threadIdx.x / kLanes] = __builtin_bit_cast(uint64_t, sum);
+    __syncthreads();
+    sum = wave_sum<THREADS / kLanes>(__builtin_bit_cast(double, lds.wave_mass[threadIdx.x % (THREADS / kLanes)]));
+    const uint32_t bits = scalar((uint32_t)__builtin_amdgcn_frexp_exp(sum * 1.0625));
+    return bits < 11 ? 51 : 62 - bits;
+}
+
 template <bool BF16, int THREADS, int DEPTH, bool LONG>
 __global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(const SampleArgs a)
 {
@@ -652,8 +680,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(
         else static_cast<int32_t *>(a.token)[r] = (int32_t)token;
         if (a.logprob) a.logprob[r] = logprob;
     };
-    if (threadIdx.x < 32)
-        lds.root[threadIdx.x] = __builtin_bit_cast(Words, __builtin_bit_cast(uint64_t, __builtin_amdgcn_ldexp(kRoots[threadIdx.x], (int)a.shift)) - ((uint64_t)threadIdx.x << 47));
+    put_roots(lds.root, a.shift);
     float own_most = -INFINITY;
     columns.each([&](const float *x, auto n, uint32_t) {
 #pragma unroll
@@ -679,7 +706,15 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(
     weights.max = scalar((double)most);
     weights.per_order = scalar(lds.inverse * 1.4426950408889634);
     weights.root = lds.root;
-    weights.least = -1.0 - (double)a.shift;
+    uint32_t shift = a.shift;
+    if constexpr (LONG)
+        if (a.cols > kCountedCols && top_k != 1) {
+            shift = shift_of_sum<THREADS>(columns, weights, lds);
+            __syncthreads();                               // (nothing of the roots has been read)
+            put_roots(lds.root, shift);
+            __syncthreads();
+        }
+    weights.least = -1.0 - (double)shift;
     // a logit that no kept column is below, where min_p or few columns give one
     float bound = -INFINITY;
     bool spoilt = false;               // the buckets
@@ -742,7 +777,7 @@ __global__ __launch_bounds__(THREADS, THREADS < 512 ? 1 : 4) void sample_kernel(
         }
     }
     const uint64_t key = lds.found_key;
-    put(column_of(key), (float)(((double)value_of(key) - weights.max) * lds.inverse - log(__builtin_amdgcn_ldexp((double)mass, -(int)a.shift))));
+    put(column_of(key), (float)(((double)value_of(key) - weights.max) * lds.inverse - log(__builtin_amdgcn_ldexp((double)mass, -(int)shift))));
 }
 
 // ---- host ------------------------------------------------------------------------------------
