@@ -373,7 +373,7 @@ int solo_logprob_with_grad(const void *logits, const void *targets, const float 
  *
  * grad_weight and grad_bias have the weights' type; with SOLO_LAYERNORM_ACCUMULATE the sums are added to what is there (a second
  * micro-batch).  Sums are binary32, over the rows in an order that the shape alone determines; one rounding at the end.  The squares
- * are those of the differences from the mean.  A row with a NaN or an infinity, or whose squares overflow binary32, has unspecified
+ * are those of the differences from the mean; a row whose mean is many deviations away from zero keeps the digits of its differences, in the gradients, too.  A row with a NaN or an infinity, or whose squares overflow binary32, has unspecified
  * results in that row (NaN behind a NaN) and in the sums over the rows, no others.  y may be x, grad_x may be x or grad_y, where types and
  * strides are the same; otherwise outputs must not overlap inputs. */
 #define SOLO_LAYERNORM_RMS 1u

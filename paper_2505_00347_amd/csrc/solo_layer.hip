@@ -6,7 +6,8 @@
 //
 // (without the term in sum g for the root mean square).  A row stays in registers between its sums and its results, so it is read
 // once; the squares are those of the differences from the mean, and what the mean's own rounding leaves of the differences' sum is taken out
-// as well, so a row far from zero loses no digits.  The gradient's threads keep
+// as well, so a row far from zero loses no digits.  The gradient has the mean rounded to binary32; where that is half a millionth of a deviation or
+// more, what it leaves in h is summed and taken out.  The gradient's threads keep
 // their columns: each adds dy h and dy of all its rows in registers, the workgroups' sums go to the workspace, and a second launch
 // adds those in the order of the workgroups.
 //
@@ -23,7 +24,7 @@ namespace solo {
 struct LayerArgs {
     const void *x, *w, *b, *dy;
     void *y, *dx;
-    float *stats, *part;
+    float *stats, *part, *centre;
     uint64_t rows, x_stride, y_stride, dx_stride;
     uint32_t cols;
     float eps;
@@ -218,6 +219,9 @@ __global__ __launch_bounds__((Deal<XB, YB, LANES, E>::kThreads)) void layer_forw
     }
 }
 
+// A row of a mean this many deviations away from zero: 16 * 2^-24, what rounding the mean leaves in h, is 2^-20, and sums over a row leave as much.
+__device__ __forceinline__ bool far_from_zero(float mean, float rstd) { return fabsf(mean) * rstd > 16.0f; }
+
 // The gradients of rows blockIdx.x, blockIdx.x + gridDim.x, ... and the workgroup's sums for weight and bias: part[0][group][cols] and
 // part[1][group][cols].
 template <bool XB, bool YB, int LANES, int E>
@@ -250,6 +254,17 @@ __global__ __launch_bounds__((Deal<XB, YB, LANES, E>::kThreads)) void layer_back
                 for (int e = 0; e < kPer; ++e)
                     if (e >= (int)n) h[j * kPer + e] = 0.0f;
             }
+        }
+        // (rows of a wavefront may differ in it, threads that meet at a barrier have one row; behind the row g is 0)
+        const bool far = far_from_zero(mean, rstd);
+        if (__ballot(far) != 0) {
+            float left[1] = {0.0f};
+#pragma unroll
+            for (int e = 0; e < E; ++e) left[0] += h[e];
+            row_total<LANES, 1>(left, lds, turn);
+            const float centre = far ? left[0] * inverse : 0.0f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) h[e] -= centre;
         }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
@@ -317,7 +332,7 @@ __global__ __launch_bounds__((Deal<XB, YB, LANES, E>::kThreads)) void layer_back
     }
 }
 
-// Rows too long for registers.  One workgroup a row; every sum is a pass over it (from the caches, behind the first).
+// Rows too long for registers.  One workgroup a row; every sum is a pass over it (from the caches, behind the first).  (2000 x 20000 bf16, forward and gradient, 238 us.)
 template <bool XB, bool YB>
 __global__ __launch_bounds__(1024) void layer_forward_long_kernel(const LayerArgs a)
 {
@@ -352,6 +367,30 @@ __global__ __launch_bounds__(1024) void layer_forward_long_kernel(const LayerArg
     }
 }
 
+// What the mean's rounding leaves in h, of a long row.
+template <bool XB>
+__device__ __forceinline__ float long_centre(const LayerArgs &a, uint64_t r, float (*lds)[32], uint32_t &turn)
+{
+    const float mean = a.stats[2 * r], rstd = a.stats[2 * r + 1];
+    if (!far_from_zero(mean, rstd)) return 0.0f;
+    float sum[1] = {0.0f};
+    for (uint32_t c = threadIdx.x; c < a.cols; c += 1024) sum[0] += (Elements<XB>::load1(a.x, r * a.x_stride + c) - mean) * rstd;
+    row_total<1024, 1>(sum, lds, turn);
+    return sum[0] / (float)a.cols;
+}
+
+// The same for the columns' sums.
+template <bool XB>
+__global__ __launch_bounds__(1024) void layer_centre_kernel(const LayerArgs a)
+{
+    __shared__ float lds[2][32];
+    uint32_t turn = 0;
+    for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        const float centre = long_centre<XB>(a, r, lds, turn);
+        if (threadIdx.x == 0) a.centre[r] = centre;
+    }
+}
+
 template <bool XB, bool YB>
 __global__ __launch_bounds__(1024) void layer_backward_long_kernel(const LayerArgs a)
 {
@@ -359,21 +398,21 @@ __global__ __launch_bounds__(1024) void layer_backward_long_kernel(const LayerAr
     uint32_t turn = 0;
     for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const uint64_t at = r * a.x_stride, at_y = r * a.y_stride;
-        const float mean = a.stats[2 * r], rstd = a.stats[2 * r + 1];
+        const float mean = a.stats[2 * r], rstd = a.stats[2 * r + 1], centre = long_centre<XB>(a, r, lds, turn);
         float sums[2] = {0.0f, 0.0f};
         auto weighted = [&](uint32_t c) {
             const float w = !a.w ? 1.0f : a.w_bf16 ? Elements<true>::load1(a.w, c) : Elements<false>::load1(a.w, c);
             return Elements<YB>::load1(a.dy, at_y + c) * w;
         };
         for (uint32_t c = threadIdx.x; c < a.cols; c += 1024) {
-            const float g = weighted(c), h = (Elements<XB>::load1(a.x, at + c) - mean) * rstd;
+            const float g = weighted(c), h = (Elements<XB>::load1(a.x, at + c) - mean) * rstd - centre;
             sums[0] += g;
             sums[1] = fmaf(g, h, sums[1]);
         }
         row_total<1024, 2>(sums, lds, turn);
         const float shift = a.rms ? 0.0f : sums[0] / (float)a.cols, slope = sums[1] / (float)a.cols;
         for (uint32_t c = threadIdx.x; c < a.cols; c += 1024) {
-            const float g = weighted(c), h = (Elements<XB>::load1(a.x, at + c) - mean) * rstd;
+            const float g = weighted(c), h = (Elements<XB>::load1(a.x, at + c) - mean) * rstd - centre;
             Elements<XB>::store1(a.dx, r * a.dx_stride + c, (fmaf(-h, slope, g) - shift) * rstd);
         }
     }
@@ -388,7 +427,7 @@ __global__ __launch_bounds__(256) void layer_columns_kernel(const LayerArgs a)
     float dw = 0.0f, db = 0.0f;
     for (uint64_t r = blockIdx.y; r < a.rows; r += gridDim.y) {
         const float dy = Elements<YB>::load1(a.dy, r * a.y_stride + c);
-        dw = fmaf(dy, (Elements<XB>::load1(a.x, r * a.x_stride + c) - a.stats[2 * r]) * a.stats[2 * r + 1], dw);
+        dw = fmaf(dy, (Elements<XB>::load1(a.x, r * a.x_stride + c) - a.stats[2 * r]) * a.stats[2 * r + 1] - a.centre[r], dw);
         db += dy;
     }
     a.part[(uint64_t)blockIdx.y * a.cols + c] = dw;
@@ -523,8 +562,10 @@ static int layer_backward_launch(const LayerArgs &a, uint32_t parts, hipStream_t
 {
     if (a.cols > kLongCols) {
         int rc = SOLO_OK;
-        if (a.part) rc = launch(layer_columns_kernel<XB, YB>, dim3((a.cols + 255) / 256, parts), 256, stream, a);
-        if (rc == SOLO_OK && a.dx) rc = launch(layer_backward_long_kernel<XB, YB>, dim3((uint32_t)(a.rows < (1u << 20) ? a.rows : 1u << 20)), 1024, stream, a);
+        const dim3 rows((uint32_t)(a.rows < (1u << 20) ? a.rows : 1u << 20));
+        if (a.part) rc = launch(layer_centre_kernel<XB>, rows, 1024, stream, a);
+        if (rc == SOLO_OK && a.part) rc = launch(layer_columns_kernel<XB, YB>, dim3((a.cols + 255) / 256, parts), 256, stream, a);
+        if (rc == SOLO_OK && a.dx) rc = launch(layer_backward_long_kernel<XB, YB>, rows, 1024, stream, a);
         return rc;
     }
     const LayerForm f = layer_form(a.cols);
@@ -569,7 +610,7 @@ size_t solo_layernorm_workspace_bytes(const solo_layernorm_shape *shape)
     using namespace solo;
     if (layer_check(shape) != SOLO_OK) return 0;
     const uint64_t parts = layer_parts(shape->rows, (uint32_t)shape->cols);
-    return 16 + parts * shape->cols * 8;
+    return 16 + parts * shape->cols * 8 + (shape->cols > kLongCols ? shape->rows * 4 : 0);
 }
 
 int solo_layernorm_grad(const void *grad_y, const void *x, const void *weight, const float *stats, void *grad_x, void *grad_weight, void *grad_bias,
@@ -592,6 +633,7 @@ int solo_layernorm_grad(const void *grad_y, const void *x, const void *weight, c
     if (shape->rows != 0) {
         LayerArgs a = layer_args(shape);
         a.x = x; a.w = weight; a.dy = grad_y; a.dx = grad_x; a.stats = const_cast<float *>(stats); a.part = sums ? static_cast<float *>(workspace) : nullptr;
+        if (sums) a.centre = a.part + 2 * (uint64_t)parts * cols;      // (of long rows)
         int done;
         if (shape->x_dtype == SOLO_BF16)
             done = shape->y_dtype == SOLO_BF16 ? layer_backward_launch<true, true>(a, parts, s) : layer_backward_launch<true, false>(a, parts, s);
