@@ -512,9 +512,9 @@ class _Handle:
         if self._index is None or _device_now() != self._index:
             raise ValueError(f"a call runs on the GPU that is torch's current device, this handle is on {self.device}")
         number = _stream_now(self._index) if stream is None else stream if isinstance(stream, int) else self._number_of(stream)
-        home, made, others = self._held
-        if number != home and made and number not in others:
-            self._visit(stream, number, made, others)
+        held = self._held
+        if number != held[0] and held[1] and number not in held[2]:
+            self._visit(stream, number, *held[1:])
         return number
 
     def _number_of(self, stream):
