@@ -417,7 +417,8 @@ int solo_layernorm_grad(const void *grad_y, const void *x, const void *weight, c
  *   grad_logits_j = scale * a * q_j (T - r / q_r)                                   elsewhere (0 where q_r is)
  *
  * A place whose token lies outside [0, cols) or whose value is -inf is none (solo_logprob writes -1 and -inf behind the last column); a
- * column may occur more than once.  A row without alternatives is not read (a padding position): loss and gradient are 0.  Where the student
+ * column may occur more than once.  What a row without alternatives holds is of no account (a padding position): loss and gradient are 0; its memory
+ * has to be readable, like any row's, since logits are read before the alternatives are known.  Where the student
  * gives no probability to an alternative that has some (-inf), the loss is +inf and the gradient the formula's; in a row of -inf alone the loss is +inf, the gradient 0.  A NaN or
  * +inf among the logits or values of a row makes its results NaN or unspecified, no other row's.  q_r is summed by itself, not taken from 1.  Sums
  * are binary32 and relative to the row's largest logit, q_r's to that of its columns where the two lie far apart (1 - sum p_k: binary64).  solo_distill_with_grad does both for weights that are known beforehand,
