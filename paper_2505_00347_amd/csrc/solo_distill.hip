@@ -14,9 +14,9 @@
 // Otherwise as the log probabilities: a workgroup takes a row, one pass for the sums, the row stays in registers for the gradient.
 //
 // Bound by memory: loss and gradient of 8192 x 32000 bf16, a tenth without a teacher, 181 us (5.5 TB/s of what it needs; rows without a teacher are
-// read, too, since the logits are under way before the teacher is known); loss of 512 x 50304 bf16 12.6 us; 1000 x 50257 fp32 in
-// two calls 103 us.  The alternatives' logits as they come by in both passes, inside the loops, took 313 us of the first: four times the registers, one workgroup a
-// compute unit instead of two.  Short rows, one a wavefront, are bound by vector instructions: 608462 x 154 fp32 with 32 alternatives 330 us, 370 a row.
+// read, too, since the logits are under way before the teacher is known); loss of 512 x 50304 bf16 12.7 us; 1000 x 50257 fp32 in
+// two calls 104 us.  The alternatives' logits as they come by in both passes, inside the loops, took 313 us of the first: four times the registers, one workgroup a
+// compute unit instead of two.  Short rows, one a wavefront, are bound by vector instructions: 608462 x 154 fp32 with 32 alternatives 328 us, 372 a row.
 #include "solo_rows.h"
 
 #include <float.h>
