@@ -373,6 +373,7 @@ __global__ __launch_bounds__(THREADS, distill_waves(FORWARD, GRAD, RESIDENT, DEP
     }
     RowSums sums;
     float lowered = 1.0f;
+    const uint32_t head = FORWARD ? kNone : lds.head[threadIdx.x];        // (once, not again behind a barrier that few rows come to)
     if (FORWARD) {
         uint32_t at_last;
         OwnSum own;
@@ -388,7 +389,7 @@ __global__ __launch_bounds__(THREADS, distill_waves(FORWARD, GRAD, RESIDENT, DEP
     } else {
         sums = RowSums{a.stats[3 * r], a.stats[3 * r], a.stats[3 * r + 1], a.stats[3 * r + 2]};
         // (the gradient may be written over them)
-        for (uint32_t i = lds.head[threadIdx.x]; i != kNone; i = lds.next[i]) lds.logit[i] = row.one(lds.column[i]);
+        for (uint32_t i = head; i != kNone; i = lds.next[i]) lds.logit[i] = row.one(lds.column[i]);
         if (scalar(sums.all) < 0.0f) {                     // (an alternative is the row's largest)
             __syncthreads();
             float at = -FLT_MAX;
@@ -423,7 +424,7 @@ __global__ __launch_bounds__(THREADS, distill_waves(FORWARD, GRAD, RESIDENT, DEP
     if (threadIdx.x < row.rest)
         Elements<BF16>::store1(out, row.last_column(threadIdx.x), __builtin_amdgcn_exp2f((last - slope.rest_at) * k) * slope.rest * slope.factor);
     // over what the same thread has just written (of an alternative's logit, where the row has been read again, anything)
-    for (uint32_t i = lds.head[threadIdx.x]; i != kNone; i = lds.next[i])
+    for (uint32_t i = FORWARD ? lds.head[threadIdx.x] : head; i != kNone; i = lds.next[i])
         Elements<BF16>::store1(out, lds.column[i], fmaf(__builtin_amdgcn_exp2f((lds.logit[i] - slope.at) * k), slope.all, -lds.all_p[i]) * slope.factor);
 }
 
