@@ -16,7 +16,7 @@
 // A workgroup takes a row.  One row of 50257 fp32, nucleus of 0.95, 20 us: 3 until the maximum is known, 8.5 for weights and buckets (25 vector instructions for 64
 // columns on each of four SIMDs), 1 to add up, 3.5 for each of two places, most of it the pass over the row.  One after the other, without the next one's chain of
 // instructions beside its own, the weights took 13.  1024 x 32000 fp32, the whole distribution, 50 us: 2.6 TB/s, vector instructions and loads about half of it each,
-// side by side only where two rows of a compute unit are at different stages.  1024 x 50257 bf16 with min_p and nucleus 57 to 67 us, by the box.
+// side by side only where two rows of a compute unit are at different stages.  1024 x 50257 bf16 with min_p and nucleus 57 to 67 us, from card to card.
 #include "solo_rows.h"
 
 #include <float.h>
@@ -28,7 +28,7 @@ namespace solo {
 // listed; parts that a list is cut into.  What a row has in LDS says how many rows a compute unit has under way, and what it clears and adds up is much of a
 // short row's work: two workgroups of 512 threads, whose registers allow no more, five of 256 (5000 rows of 4000 bf16, nucleus: 56 us, with the long rows' sizes
 // 118) and twenty of one wavefront (100000 rows of 300 fp32: 150, with lists twice as long 160).  With half the buckets a long row's places take 4 to 7 % longer;
-// with half the list 1024 rows of 50257 bf16 of which min_p leaves up to 4000 columns take 75 us instead of 66 on the same box.
+// with half the list 1024 rows of 50257 bf16 of which min_p leaves up to 4000 columns take 75 us instead of 66 on the same card.
 template <int THREADS>
 struct Sizes {
     static constexpr bool kShort = THREADS == kLanes, kMiddle = THREADS == 256;
